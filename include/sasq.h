@@ -11,6 +11,9 @@
  *   inference:  Y = s * (q(X) . Wq^T) * s_w (+ bias)     sasq_static_linear
  *   set-up:     Wq, s_w from frozen fp32 weights         sasq_quantize_weight
  *               s0 = max|X| / (2^(bits-1) - 1)           sasq_absmax_scale
+ *   serving:    between the linears q/k/v and o of an attention block, on a paged key/value cache:
+ *               rotate by position, append           sasq_kv_append
+ *               out = softmax(scale q k^T) v             sasq_paged_attention
  *
  * Conventions shared by every entry point
  *   - Every data pointer is DEVICE memory owned by the caller (the library never allocates,
@@ -411,6 +414,90 @@ size_t sasq_absmax_scale_workspace(int64_t rows, int64_t cols);
  */
 int sasq_absmax_scale(const void* x, float* s, int64_t rows, int64_t cols, int bits,
                       sasq_dtype dt, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Paged key/value cache of one attention block.  The cache is `pages` pages of `page_size` places; a place holds, for each of `heads`
+ * kv heads, `dim` channels of a key in `k` and of a value in `v`.  Element (page, place, head, channel) lies at
+ *     page * page_stride + place * token_stride + head * head_stride + channel                (elements; k and v alike),
+ * so a cache may be stored [pages, heads, page_size, dim] or [pages, page_size, heads, dim], or be a part of a larger tensor.
+ *   SASQ_KV_16    elements in the activations' 16-bit type
+ *   SASQ_KV_INT8  int8 codes with a fixed factor for each kv head (static quantization, Sec. 3, applied to what is kept):
+ *                 value = code * k_scale[head], code = clamp(round(x / k_scale[head]), -128, 127) of the 16-bit x (any finite
+ *                 non-zero factor, negative allowed).
+ *   page_size     a power of two, 16 to 65536;  dim: 64 or 128;  pages * page_size may pass 2^31 (all offsets are 64 bits)
+ *   strides       at least dim, multiples of 16 bytes; k and v 16-byte aligned
+ */
+typedef enum { SASQ_KV_16 = 0, SASQ_KV_INT8 = 1 } sasq_kvfmt;
+typedef struct {
+    void* k;                /* device */
+    void* v;                /* device */
+    const float* k_scale;   /* [heads] device fp32; SASQ_KV_INT8 only */
+    const float* v_scale;   /* [heads] device fp32; SASQ_KV_INT8 only */
+    int64_t pages, page_size, heads, dim;
+    int64_t page_stride, token_stride, head_stride;
+    sasq_kvfmt fmt;
+} sasq_kv_cache;
+
+/*
+ * The sequences of one step, shared by the calls of all layers.  Rows cu_q[b] .. cu_q[b+1]-1 of the `tokens` rows are the new tokens
+ * of sequence b; kv_len[b] is the length of its cache with the new tokens in it, so new token i is at position
+ * kv_len[b] - (cu_q[b+1] - cu_q[b]) + i.  Position j lies on page block_table[b][j / page_size], at place j % page_size.
+ *   cu_q          [batch + 1] device int32, ascending from 0;  a sequence may have no new token
+ *   kv_len        [batch] device int32;  block_table  [batch, max_pages] device int32
+ *   tokens        rows of q, k, v and the outputs; rows from cu_q[batch] on belong to no sequence and are not touched
+ *   max_q         at least the most new tokens that a sequence has (tokens will do)
+ *   max_kv        at least the longest kv_len (max_pages * page_size will do): how far the work is split, not which keys count
+ *   max_pages * page_size at most 2^30
+ * What lies on the device is not validated but bounded: an entry of block_table outside [0, pages) is a page that is not there (its
+ * keys do not count, tokens on it are not stored), as are positions past the table.
+ */
+typedef struct {
+    const int32_t* cu_q;
+    const int32_t* kv_len;
+    const int32_t* block_table;
+    int64_t batch, max_pages, tokens, max_q, max_kv;
+} sasq_kv_batch;
+
+/*
+ * Append: rotate the new tokens' queries and keys by their positions and store keys and values in the cache.
+ * With r = rot_dim, c = cos[row][j], s = sin[row][j], j < r/2, each head of q and k becomes (fp32, every product and sum rounded,
+ * then one rounding to 16 bits; channels from r on unchanged)
+ *     SASQ_ROPE_HALVES:  y[j]  = x[j] c - x[j + r/2] s      y[j + r/2] = x[j + r/2] c + x[j] s
+ *     SASQ_ROPE_PAIRS:   y[2j] = x[2j] c - x[2j + 1] s      y[2j + 1]  = x[2j + 1] c + x[2j] s
+ * and y of k, and v as it is, go to their place in the cache (SASQ_KV_INT8: their codes).
+ *   q        [tokens, q_heads, dim] 16-bit `dt`, rows q_stride elements apart, or NULL with q_out: keys and values only
+ *   k, v     [tokens, heads, dim] 16-bit `dt`, rows k_stride and v_stride apart (columns of one fused projection, for instance)
+ *   q_out    [tokens, q_heads, dim] 16-bit `dt`, rows q_out_stride apart, written; may be q itself
+ *   cos, sin [table_rows, rot_dim/2] device fp32, or both NULL: no rotation (rot_dim is then not read)
+ *   positions  [tokens] device int32: the row of the table for each token, or NULL: the token's position in its cache.  A token
+ *            whose row is not in the table is not stored, and its row of q_out is 0.
+ *   rot_dim  a multiple of 16, at most dim;  q_heads a multiple of heads;  row strides: multiples of 8, at least a row's length
+ *   k and v must not overlap the cache; the order in which tokens are stored does not matter (no two share a place).
+ */
+typedef enum { SASQ_ROPE_HALVES = 0, SASQ_ROPE_PAIRS = 1 } sasq_rope;
+int sasq_kv_append(const void* q, const void* k, const void* v, void* q_out,
+                   int64_t q_stride, int64_t k_stride, int64_t v_stride, int64_t q_out_stride, int64_t q_heads,
+                   const float* cos, const float* sin, const int32_t* positions, int64_t table_rows, int64_t rot_dim, sasq_rope style,
+                   const sasq_kv_cache* cache, const sasq_kv_batch* batch, sasq_dtype dt, void* stream);
+
+/*
+ * Causal attention of the new tokens over the paged cache, which holds their own keys and values already.  For the new token i of
+ * sequence b at position p, head h, and the positions j <= p that are there:
+ *     S[j] = scale * sum_d q[i,h,d] k[j,h',d]      P = softmax over j of S      out[i,h,d] = sum_j P[j] v[j,h',d]
+ * with h' = h / (q_heads / heads).  Keys that are masked (later ones, places past kv_len, pages that are not there) do not count
+ * whatever their places hold, infinities and NaN included.  A row without any key: out = 0, lse = -inf.
+ *   q        [tokens, q_heads, dim] 16-bit `dt`, rows q_stride elements apart;  out: the same, rows out_stride apart, written;
+ *            must not overlap q
+ *   lse      [tokens, q_heads] device fp32 or NULL, written: ln sum_j exp S[j], with which results over parts of the keys are joined
+ *   scale    finite, above 0
+ * Sums, maxima and the softmax are fp32; probabilities are rounded to 16 bits before they multiply the values (with an int8 cache:
+ * to fp16, which holds every code exactly), and the output is rounded once.  Results do not change from run to run.
+ *   workspace  >= sasq_paged_attention_workspace(...) bytes, 16-byte aligned (NULL allowed when that is 0), holds partial results of split sequences
+ */
+size_t sasq_paged_attention_workspace(const sasq_kv_cache* cache, const sasq_kv_batch* batch, int64_t q_heads);
+int sasq_paged_attention(const void* q, void* out, float* lse, int64_t q_stride, int64_t out_stride, int64_t q_heads, float scale,
+                         const sasq_kv_cache* cache, const sasq_kv_batch* batch, sasq_dtype dt,
+                         void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -27,6 +27,9 @@ MARSHAL_PATH = os.path.join(_PKG, "_marshal.so")
 SASQ_F16, SASQ_BF16 = 0, 1
 SASQ_W_INT8, SASQ_W_INT4_PACKED, SASQ_W_INT8_BLOCKED, SASQ_W_INT4_BLOCKED = 0, 1, 2, 3
 
+SASQ_KV_16, SASQ_KV_INT8 = 0, 1
+SASQ_ROPE_HALVES, SASQ_ROPE_PAIRS = 0, 1
+
 SASQ_MAX_BATCH = 8
 
 _DT = {torch.float16: SASQ_F16, torch.bfloat16: SASQ_BF16}
@@ -43,6 +46,17 @@ class _FqItem(ctypes.Structure):
                 ("ds", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64)]
 
 
+class _KvCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("pages", ctypes.c_int64), ("page_size", ctypes.c_int64), ("heads", ctypes.c_int64), ("dim", ctypes.c_int64),
+                ("page_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("fmt", ctypes.c_int)]
+
+
+class _KvBatch(ctypes.Structure):
+    _fields_ = [("cu_q", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("block_table", ctypes.c_void_p), ("batch", ctypes.c_int64),
+                ("max_pages", ctypes.c_int64), ("tokens", ctypes.c_int64), ("max_q", ctypes.c_int64), ("max_kv", ctypes.c_int64)]
+
+
 class SasqError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -57,6 +71,9 @@ _NATIVE = ("sasq_fakequant_fwd", "sasq_fakequant_bwd", "sasq_fakequant_fwd_batch
            "sasq_fakequant_fwd_pc_batch", "sasq_fakequant_bwd_pc_batch", "sasq_scale_sgd", "sasq_scale_sgd_vec", "sasq_scale_adamw",
            "sasq_static_linear", "sasq_static_linear_batch", "sasq_static_linear_grouped", "sasq_linear_bwd_input",
            "sasq_absmax_scale", "sasq_quantize_weight", "sasq_pack_weight", "sasq_prepare_bwd_weight")
+
+# The same for serving: what it takes and refuses is in tests of its own.
+_NATIVE_SERVING = ("sasq_kv_append", "sasq_paged_attention")
 
 
 class _Unbound:
@@ -83,7 +100,7 @@ def _load_native(lib: ctypes.CDLL):
         if module.ABI != marshal_abi():
             raise ImportError(f"built for {module.ABI}, this is {marshal_abi()}")
         module.bind({name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value
-                     for name in _NATIVE + ("sasq_packed_weight_bytes", "sasq_bwd_weight_bytes")})
+                     for name in _NATIVE + _NATIVE_SERVING + ("sasq_packed_weight_bytes", "sasq_bwd_weight_bytes")})
     except (ImportError, OSError, AttributeError) as e:
         warnings.warn(f"{MARSHAL_PATH} is not used, calls go through ctypes ({e}); "
                       "build it with `python -m paper_2512_14481_amd.build`", RuntimeWarning, stacklevel=3)
@@ -146,6 +163,10 @@ def _lib() -> ctypes.CDLL:
         L.sasq_absmax_scale_workspace.restype = sz
         L.sasq_absmax_scale_workspace.argtypes = [i64, i64]
         L.sasq_absmax_scale.argtypes = [vp, vp, i64, i64, i32, i32, vp, sz, vp]
+        L.sasq_kv_append.argtypes = [vp] * 4 + [i64] * 5 + [vp] * 3 + [i64, i64, i32, ctypes.POINTER(_KvCache), ctypes.POINTER(_KvBatch), i32, vp]
+        L.sasq_paged_attention_workspace.restype = sz
+        L.sasq_paged_attention_workspace.argtypes = [ctypes.POINTER(_KvCache), ctypes.POINTER(_KvBatch), i64]
+        L.sasq_paged_attention.argtypes = [vp] * 3 + [i64] * 3 + [f32, ctypes.POINTER(_KvCache), ctypes.POINTER(_KvBatch), i32, vp, sz, vp]
         _native = _load_native(L)
         _LIB = L
     return _LIB
@@ -595,3 +616,111 @@ def sasq_absmax_scale(x: torch.Tensor, s: torch.Tensor, workspace: torch.Tensor,
     rows, cols = x.shape[0], x.numel() // max(x.shape[0], 1)
     _check(_lib().sasq_absmax_scale(_ptr(x), _ptr(s), rows, cols, bits, _dt(x), _ptr(workspace),
                                     workspace.numel() * workspace.element_size(), _stream()), "sasq_absmax_scale")
+
+
+class KVCache:
+    """A paged key/value cache: k and v are [pages, page_size, heads, dim] tensors of the same strides, with the channels of a head
+    next to each other (a cache stored [pages, heads, page_size, dim] is passed as its transpose(1, 2)).  int8 tensors hold codes and
+    need k_scale and v_scale, one float32 factor for each head.  Keeps its tensors; made once for a layer."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None):
+        if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype or v.stride() != k.stride():
+            raise ValueError("k and v must be [pages, page_size, heads, dim] of one type and layout")
+        if k.dtype != torch.int8 and k.dtype not in _DT:
+            raise TypeError(f"a cache holds float16, bfloat16 or int8, got {k.dtype}")
+        if (k.dtype == torch.int8) != (k_scale is not None) or (k_scale is None) != (v_scale is None):
+            raise ValueError("an int8 cache takes k_scale and v_scale, another takes none")
+        pages, page_size, heads, dim = k.shape
+        for scale in (k_scale, v_scale):
+            _want(scale, torch.float32, "k_scale and v_scale")
+            if scale is not None and scale.numel() != heads:
+                raise ValueError("k_scale and v_scale must have one element per head")
+        if not (k.is_cuda and v.is_cuda):
+            raise ValueError("SASQ entry points take device tensors")
+        if k.stride(3) != 1:
+            raise ValueError("the channels of a head must be next to each other")
+        strides = [k.stride(i) if k.shape[i] > 1 else max(dim, 16) for i in range(3)]      # of a single page, place or head: any
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.heads, self.dim, self.dtype = heads, dim, k.dtype
+        self._dt = _DT.get(k.dtype, -1)
+        at = lambda t: None if t is None else _ptr(t).value
+        self._c = _KvCache(k.data_ptr(), v.data_ptr(), at(k_scale), at(v_scale), pages, page_size, heads, dim,
+                           strides[0], strides[1], strides[2], SASQ_KV_INT8 if k.dtype == torch.int8 else SASQ_KV_16)
+        self._at = ctypes.addressof(self._c)
+
+
+class KVBatch:
+    """The sequences of one step, for the calls of all layers: cu_q [batch + 1], kv_len [batch] and block_table [batch, max_pages],
+    int32 on the device, and how many rows the step has.  max_q and max_kv: the most new tokens and the longest cache of a sequence,
+    where the program knows them (otherwise what the shapes allow).  Keeps its tensors; they may be written anew for the next step."""
+
+    def __init__(self, cu_q: torch.Tensor, kv_len: torch.Tensor, block_table: torch.Tensor, tokens: int,
+                 max_q: Optional[int] = None, max_kv: Optional[int] = None):
+        for t, name in ((cu_q, "cu_q"), (kv_len, "kv_len"), (block_table, "block_table")):
+            _want(t, torch.int32, name)
+        if kv_len.dim() != 1 or cu_q.dim() != 1 or cu_q.numel() != kv_len.numel() + 1 or block_table.dim() != 2 or block_table.shape[0] != kv_len.numel():
+            raise ValueError("cu_q must be [batch + 1], kv_len [batch] and block_table [batch, max_pages]")
+        self.cu_q, self.kv_len, self.block_table, self.tokens = cu_q, kv_len, block_table, int(tokens)
+        self._c = _KvBatch(_ptr(cu_q).value, _ptr(kv_len).value, _ptr(block_table).value, kv_len.numel(), block_table.shape[1], int(tokens),
+                           int(tokens if max_q is None else max_q), int(1 << 30 if max_kv is None else max_kv))
+        self._at = ctypes.addressof(self._c)
+
+
+def _rows(t: torch.Tensor, heads: int, like: Optional[torch.Tensor], cache: KVCache, batch: KVBatch, name: str) -> int:
+    """Checks one [tokens, heads, dim] operand; the distance of its rows in elements."""
+    if t.dim() != 3 or t.shape[0] != batch.tokens or t.shape[1] != heads or t.shape[2] != cache.dim:
+        raise ValueError(f"{name} must be [tokens, heads, dim] = {(batch.tokens, heads, cache.dim)}, got {tuple(t.shape)}")
+    if not t.is_cuda:
+        raise ValueError("SASQ entry points take device tensors")
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != cache.dim):
+        raise ValueError(f"the heads of a row of {name} must follow each other without gaps")
+    if _dt(t) != (_dt(t) if like is None else _dt(like)) or (cache._dt >= 0 and _dt(t) != cache._dt):
+        raise TypeError(f"{name} must have the type of the other operands and of a 16-bit cache")
+    return t.stride(0) if t.shape[0] > 1 else heads * cache.dim
+
+
+def _at(t: Optional[torch.Tensor]):
+    return None if t is None else ctypes.c_void_p(t.data_ptr())
+
+
+def sasq_kv_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, q_out: Optional[torch.Tensor], cache: KVCache, batch: KVBatch,
+                   cos: Optional[torch.Tensor] = None, sin: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                   style: int = SASQ_ROPE_HALVES) -> None:
+    """q, q_out: [tokens, q_heads, dim] or both None; k, v: [tokens, heads, dim]; rows may be apart.  cos, sin: [table_rows, rot_dim/2]."""
+    rc = _native.sasq_kv_append(q, k, v, q_out, cache._at, cache._dt, batch._at, cos, sin, positions, style)
+    if rc is not None:
+        return _check(rc, "sasq_kv_append")
+    if (q is None) != (q_out is None) or (cos is None) != (sin is None):
+        raise ValueError("q goes with q_out, and cos with sin")
+    heads = cache.heads if q is None else q.shape[1] if q.dim() == 3 else 0
+    k_stride, v_stride = _rows(k, cache.heads, None, cache, batch, "k"), _rows(v, cache.heads, k, cache, batch, "v")
+    q_stride = 0 if q is None else _rows(q, heads, k, cache, batch, "q")
+    q_out_stride = 0 if q is None else _rows(q_out, heads, k, cache, batch, "q_out")
+    _want(cos, torch.float32, "cos"); _want(sin, torch.float32, "sin"); _want(positions, torch.int32, "positions")
+    if cos is not None and (cos.dim() != 2 or sin.shape != cos.shape):
+        raise ValueError("cos and sin must be [table_rows, rot_dim / 2]")
+    if positions is not None and positions.numel() != batch.tokens:
+        raise ValueError("positions must have one element per token")
+    rows, half = (0, 0) if cos is None else cos.shape
+    _check(_lib().sasq_kv_append(_at(q), _at(k), _at(v), _at(q_out), q_stride, k_stride, v_stride, q_out_stride, heads, _ptr(cos), _ptr(sin),
+                                 _ptr(positions), rows, 2 * half, style, cache._c, batch._c, _dt(k), _stream()), "sasq_kv_append")
+
+
+def sasq_paged_attention_workspace(cache: KVCache, batch: KVBatch, q_heads: int) -> int:
+    return int(_lib().sasq_paged_attention_workspace(cache._c, batch._c, q_heads))
+
+
+def sasq_paged_attention(q: torch.Tensor, out: torch.Tensor, cache: KVCache, batch: KVBatch, workspace: Optional[torch.Tensor], scale: float,
+                         lse: Optional[torch.Tensor] = None) -> None:
+    """q, out: [tokens, q_heads, dim], rows may be apart; lse: [tokens, q_heads] float32."""
+    rc = _native.sasq_paged_attention(q, out, lse, cache._at, cache._dt, batch._at, workspace, scale)
+    if rc is not None:
+        return _check(rc, "sasq_paged_attention")
+    heads = q.shape[1] if q.dim() == 3 else 0
+    q_stride, out_stride = _rows(q, heads, None, cache, batch, "q"), _rows(out, heads, q, cache, batch, "out")
+    _want(lse, torch.float32, "lse")
+    if lse is not None and tuple(lse.shape) != (batch.tokens, heads):
+        raise ValueError("lse must be [tokens, q_heads]")
+    wsb = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(_lib().sasq_paged_attention(_at(q), _at(out), _ptr(lse), q_stride, out_stride, heads, ctypes.c_float(scale), cache._c, batch._c, _dt(q),
+                                       _ptr(workspace), wsb, _stream()), "sasq_paged_attention")

@@ -35,6 +35,8 @@ struct Entry {
     decltype(&sasq_quantize_weight) quantize_weight;
     decltype(&sasq_pack_weight) pack_weight;
     decltype(&sasq_prepare_bwd_weight) prepare_bwd_weight;
+    decltype(&sasq_kv_append) kv_append;
+    decltype(&sasq_paged_attention) paged_attention;
 };
 Entry entry{};
 
@@ -410,6 +412,80 @@ PyObject* method(PyObject*, PyObject* const* args, Py_ssize_t nargs)
     Py_RETURN_NONE;
 }
 
+// The C structures that a KVCache and a KVBatch of the binding keep, by address; cache_type: the cache's sasq_dtype, -1 for codes.
+template <typename T>
+const T* kept(PyObject* o)
+{
+    const int64_t at = integer(o);
+    want(at != 0);
+    return reinterpret_cast<const T*>(at);
+}
+
+// One [tokens, heads, dim] operand whose rows may be apart.
+struct Rows {
+    void* at;
+    int64_t heads, stride;
+    sasq_dtype dt;
+};
+Rows rows(PyObject* o, const sasq_kv_cache* c, const sasq_kv_batch* b, int cache_type)
+{
+    want(THPVariable_CheckExact(o));
+    const at::Tensor& t = THPVariable_Unpack(o);
+    want(t.is_cuda() && t.dim() == 3 && t.size(0) == b->tokens && t.size(2) == c->dim && t.stride(2) == 1);
+    want(t.size(1) == 1 || t.stride(1) == c->dim);
+    const sasq_dtype dt = dtype_of(t);
+    want(cache_type < 0 || cache_type == dt);
+    return {t.data_ptr(), t.size(1), t.size(0) > 1 ? t.stride(0) : t.size(1) * c->dim, dt};
+}
+
+// (q_or_None, k, v, q_out_or_None, cache, cache_type, batch, cos_or_None, sin_or_None, positions_or_None, style)
+int kv_append(PyObject* const* a)
+{
+    const auto* c = kept<sasq_kv_cache>(a[4]);
+    const int type = small(a[5]);
+    const auto* b = kept<sasq_kv_batch>(a[6]);
+    const Rows k = rows(a[1], c, b, type), v = rows(a[2], c, b, type);
+    want(k.heads == c->heads && v.heads == c->heads && v.dt == k.dt && (a[0] == Py_None) == (a[3] == Py_None));
+    Rows q{nullptr, c->heads, 0, k.dt}, to{nullptr, c->heads, 0, k.dt};
+    if (a[0] != Py_None) {
+        q = rows(a[0], c, b, type);
+        to = rows(a[3], c, b, type);
+        want(q.dt == k.dt && to.dt == k.dt && to.heads == q.heads);
+    }
+    const at::Tensor *cos = optional_tensor(a[7]), *sin = optional_tensor(a[8]), *positions = optional_tensor(a[9]);
+    want(!cos == !sin);
+    if (cos) want(cos->scalar_type() == at::kFloat && sin->scalar_type() == at::kFloat && cos->dim() == 2 && sin->sizes() == cos->sizes());
+    if (positions) want(positions->scalar_type() == at::kInt && positions->numel() == b->tokens);
+    const int style = small(a[10]);
+    const float *cp = pointer<float>(cos), *sp = pointer<float>(sin);
+    const int32_t* pp = pointer<int32_t>(positions);
+    const int64_t table_rows = cos ? cos->size(0) : 0, rot = cos ? 2 * cos->size(1) : 0;
+    return unlocked([&](void* st) {
+        return entry.kv_append(q.at, k.at, v.at, to.at, q.stride, k.stride, v.stride, to.stride, q.heads, cp, sp, pp, table_rows, rot,
+                               static_cast<sasq_rope>(style), c, b, k.dt, st);
+    });
+}
+
+// (q, out, lse_or_None, cache, cache_type, batch, workspace_or_None, scale)
+int paged_attention(PyObject* const* a)
+{
+    const auto* c = kept<sasq_kv_cache>(a[3]);
+    const int type = small(a[4]);
+    const auto* b = kept<sasq_kv_batch>(a[5]);
+    const Rows q = rows(a[0], c, b, type), out = rows(a[1], c, b, type);
+    want(out.dt == q.dt && out.heads == q.heads);
+    const at::Tensor* lse = optional_tensor(a[2]);
+    if (lse) want(lse->scalar_type() == at::kFloat && lse->dim() == 2 && lse->size(0) == b->tokens && lse->size(1) == q.heads);
+    const at::Tensor* ws = optional_tensor(a[6]);
+    const float scale = static_cast<float>(real(a[7]));
+    auto* lp = pointer<float>(lse);
+    void* wp = pointer<void>(ws);
+    const size_t wb = bytes(ws);
+    return unlocked([&](void* st) {
+        return entry.paged_attention(q.at, out.at, lp, q.stride, out.stride, q.heads, scale, c, b, q.dt, wp, wb, st);
+    });
+}
+
 // bind({"sasq_...": address, ...}): the entry points of the library that the binding has loaded
 PyObject* bind(PyObject*, PyObject* table)
 {
@@ -429,7 +505,8 @@ PyObject* bind(PyObject*, PyObject* table)
         set("sasq_static_linear_grouped", e.static_linear_grouped) && set("sasq_packed_weight_bytes", e.packed_weight_bytes) &&
         set("sasq_bwd_weight_bytes", e.bwd_weight_bytes) && set("sasq_linear_bwd_input", e.linear_bwd_input) &&
         set("sasq_absmax_scale", e.absmax_scale) && set("sasq_quantize_weight", e.quantize_weight) &&
-        set("sasq_pack_weight", e.pack_weight) && set("sasq_prepare_bwd_weight", e.prepare_bwd_weight);
+        set("sasq_pack_weight", e.pack_weight) && set("sasq_prepare_bwd_weight", e.prepare_bwd_weight) &&
+        set("sasq_kv_append", e.kv_append) && set("sasq_paged_attention", e.paged_attention);
     if (!ok) return nullptr;
     entry = e;
     Py_RETURN_NONE;
@@ -456,6 +533,8 @@ PyMethodDef methods[] = {
     SASQ_METHOD("sasq_quantize_weight", quantize_weight, 4),
     SASQ_METHOD("sasq_pack_weight", pack_weight, 5),
     SASQ_METHOD("sasq_prepare_bwd_weight", prepare_bwd_weight, 7),
+    SASQ_METHOD("sasq_kv_append", kv_append, 11),
+    SASQ_METHOD("sasq_paged_attention", paged_attention, 8),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
