@@ -53,6 +53,7 @@ inline int kv_check(const sasq_kv_cache* c, const sasq_kv_batch* b, int64_t q_he
     const int64_t e = c->fmt == SASQ_KV_16 ? 2 : 1, most = INT64_C(1) << 60;
     for (int64_t stride : {c->page_stride, c->token_stride, c->head_stride})
         if (stride < c->dim || stride > most / (2 * c->pages) || (stride * e) % 16) return SASQ_ERR_SHAPE;
+    if (c->token_stride > INT64_C(1) << 26) return SASQ_ERR_SHAPE;          // sixteen places in a 32-bit offset
     if (b->batch <= 0 || b->batch >= kKvMost || b->tokens <= 0 || b->tokens > kKvMost || b->max_q <= 0 || b->max_kv <= 0) return SASQ_ERR_SHAPE;
     if (b->max_pages <= 0 || b->max_pages > kKvMost / c->page_size) return SASQ_ERR_SHAPE;
     if (q_heads <= 0 || q_heads > 65535 || q_heads % c->heads) return SASQ_ERR_SHAPE;
