@@ -31,10 +31,12 @@ struct AttnSplit {
     float2* ml;                                           // running maximum (of log2-scaled scores) and sum
     float* o;                                             // unnormalized sums of values
 };
-__device__ __forceinline__ int64_t attn_slot(const AttnSplit& s, int batch, int heads, int split, int b, int hk, int r)
+// Places of the partial results of row r of a sequence (rows kernel), and of token t and a head (tiles kernel).
+__device__ __forceinline__ int64_t rows_slot(const AttnSplit& s, int batch, int heads, int run, int b, int hk, int r)
 {
-    return (((int64_t)split * batch + b) * heads + hk) * ((int64_t)s.tiles * s.tile_rows) + r;
+    return (((int64_t)run * batch + b) * heads + hk) * ((int64_t)s.tiles * s.tile_rows) + r;
 }
+__device__ __forceinline__ int64_t tiles_slot(int tokens, int q_heads, int run, int t, int head) { return ((int64_t)run * tokens + t) * q_heads + head; }
 // Keys that a tile's last row sees, and how many runs they make.
 __device__ __forceinline__ int attn_end(const KvSeq& seq, int group, const AttnSplit& s, int tile)
 {
@@ -76,22 +78,135 @@ __device__ __forceinline__ bool any_special(uint32_t w)
     constexpr uint32_t e = DT == SASQ_F16 ? 0x7C00u : 0x7F80u;
     return (w & e) == e || (w >> 16 & e) == e;
 }
-// The dword with 1 where a value is of the kind asked for (0: +inf, 1: -inf, 2: NaN) and 0 elsewhere; kind 3: the finite values.
+// The dword with its infinite and NaN values at 0.
 template <int DT>
-__device__ __forceinline__ uint32_t special_mask(uint32_t w, int kind)
+__device__ __forceinline__ uint32_t finite_of(uint32_t w)
 {
-    constexpr uint32_t e = DT == SASQ_F16 ? 0x7C00u : 0x7F80u, one = DT == SASQ_F16 ? 0x3C00u : 0x3F80u;
-    uint32_t r = 0;
+    constexpr uint32_t e = DT == SASQ_F16 ? 0x7C00u : 0x7F80u;
+    return ((w & e) == e ? 0u : w & 0xFFFFu) | ((w >> 16 & e) == e ? 0u : w & 0xFFFF0000u);
+}
+// Adds +inf, or -inf, to the output of the rows that see an infinite value of that sign, and both for a NaN: as a product of the largest
+// bf16 value by itself, which overflows, so that the rows that do not see it (a factor of 0) stay as they are.  v: eight values of the
+// first operand, seen: kSeen (else 0) for the eight keys of the second.
+constexpr uint32_t kSeen = 0x7F7Fu;
+template <int DT>
+__device__ __forceinline__ f32x4 add_specials(const u32x4& v, const u32x4& seen, f32x4 o)
+{
+    constexpr uint32_t e = DT == SASQ_F16 ? 0x7C00u : 0x7F80u;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint32_t h = w >> (16 * i) & 0xFFFFu;
-        const bool special = (h & e) == e, nan = (h & 0x7FFFu) > e;
-        const int is = !special ? 3 : nan ? 2 : (int)(h >> 15);
-        r |= (is != kind ? 0u : kind == 3 ? h : one) << (16 * i);
+    for (int sign = 0; sign < 2; ++sign) {
+        u32x4 w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            w[j] = 0;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t h = v[j] >> (16 * i) & 0xFFFFu;
+                const bool mine = (h & 0x7FFFu) > e || h == (e | (uint32_t)sign << 15);
+                w[j] |= (mine ? kSeen | (uint32_t)sign << 15 : 0u) << (16 * i);
+            }
+        }
+        o = mfma16<SASQ_BF16>(w, seen, o);
     }
-    return r;
+    return o;
 }
 
-int attention_rows_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& split, int dim, bool int8, sasq_dtype dt, hipStream_t st);
+template <int N>
+__device__ __forceinline__ void wait_loads()
+{
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(N));
+    asm volatile("" ::: "memory");
+}
+
+// A score may pass the running maximum by so much (in powers of two) before the maximum is moved: probabilities then reach 2^8 at most,
+// their rounding is relative all the same, and the common step needs no reduction over lanes and no rescaling of the output.
+constexpr float kLazy = 8.0f;
+
+// Keys or values of one head in LDS.  A wave-wide load brings whole rows, 1 KB of them, and puts them down as a block in which the rows'
+// 16-byte chunks of one place follow each other; blocks are 64 bytes apart.  The eight rows that a wave reads at a time at one chunk then
+// lie in different banks, and so does what a transposing read of 16 lanes takes (16 bits: two chunks of four rows; codes: a chunk of four
+// rows of both halves of 32), and every place is a lane's own plus a constant.
+template <int D, bool I8>
+struct KvRow {
+    static constexpr int kRow = D * (I8 ? 1 : 2);         // bytes of a key
+    static constexpr int kPerLoad = 1024 / kRow;          // rows of a block
+    static constexpr int kLoads = 16 / kPerLoad;          // blocks of 16 rows
+    static constexpr int kBlock = 1024 + 64;
+    static constexpr int k16 = kLoads * kBlock;           // bytes of 16 rows
+    static __device__ __forceinline__ int place(int row, int chunk) { return row / kPerLoad * kBlock + (chunk * kPerLoad + row % kPerLoad) * 16; }
+    // Where lane's 16 bytes of block j of 16 rows come from.
+    static __device__ __forceinline__ uint32_t source(int j, int lane, int64_t token_stride)
+    {
+        return (uint32_t)((j * kPerLoad + lane % kPerLoad) * token_stride) + 16 * (lane / kPerLoad);
+    }
+    // First operand of K Q^T: lane (l16, g) has 16 bytes of row l16 of 16, from chunk 4 t + g on.  at: the 16 rows + key_lane.
+    static __device__ __forceinline__ int key_lane(int lane) { return place(lane & 15, lane >> 4); }
+    static __device__ __forceinline__ u32x4 key(const char* at, int t) { return *reinterpret_cast<const u32x4*>(at + 4 * t * kPerLoad * 16); }
+    // First operand of V^T P^T: lane (l16, g) has channel 16 n + l16 of rows 4g..4g+3 and 16+4g..16+4g+3 of 32, in 16 bits.  at: the 32 rows
+    // + value_lane.
+    static __device__ __forceinline__ int value_lane(int lane)
+    {
+        const int l16 = lane & 15, g = lane >> 4;
+        if constexpr (I8) return place((l16 < 8 ? 0 : 16) + 4 * g + (l16 >> 1 & 3), 0) + 8 * (l16 & 1);
+        else              return place(4 * g + (l16 >> 2), l16 >> 1 & 1) + 8 * (l16 & 1);
+    }
+    static __device__ __forceinline__ u32x4 value(const char* at, int n)
+    {
+        if constexpr (I8) {
+            const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2)(at + n * kPerLoad * 16));
+            const u32x2 x = codes_to_f16((uint32_t)w[0]), y = codes_to_f16((uint32_t)w[1]);
+            return u32x4{x[0], x[1], y[0], y[1]};
+        } else {
+            const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(at + 2 * n * kPerLoad * 16)));
+            const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(at + k16 + 2 * n * kPerLoad * 16)));
+            return u32x4{x[0], x[1], y[0], y[1]};
+        }
+    }
+};
+
+// Q as the second operand of K Q^T: eight channels of the lane's row for each step of 32.  c: from a score to a power of two.
+template <int DTQ, int D, bool I8>
+__device__ __forceinline__ void load_q(const AttnArgs& a, const uint16_t* src, bool there, int g, float k_scale, u32x4 (&q)[D / 32], float& c)
+{
+    constexpr int DS = D / 32;
+#pragma unroll
+    for (int t = 0; t < DS; ++t) {
+        const int d = I8 ? 64 * (t >> 1) + 16 * g + 8 * (t & 1) : 32 * t + 8 * g;          // sixteen codes of one load serve two steps
+        q[t] = *reinterpret_cast<const u32x4*>(src + d);
+        if (!there) q[t] = u32x4{0, 0, 0, 0};
+    }
+    c = a.scale * 1.44269504088896f;
+    if constexpr (I8) {
+        // fp16 products: a bf16 row is brought to at most 2 by a power of two (exact but for values 2^-14 and more below its largest),
+        // and the sign of the factor goes into Q, so that larger products stay larger scores.
+        c *= fabsf(k_scale);
+        const uint32_t flip = k_scale < 0.0f ? 0x80008000u : 0u;
+        if constexpr (DTQ == SASQ_BF16) {
+            float top = 0.0f;
+#pragma unroll
+            for (int t = 0; t < DS; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(Store16<DTQ>::lo(q[t][i])), fabsf(Store16<DTQ>::hi(q[t][i]))));
+            top = fmaxf(top, __shfl_xor(top, 16, kWave));
+            top = fmaxf(top, __shfl_xor(top, 32, kWave));
+            const int e = top > 0.0f && top < INFINITY ? min(max(((int)(__float_as_uint(top) >> 23)) - 127, -100), 100) : 0;
+            const float down = __uint_as_float((uint32_t)(127 - e) << 23);
+            c *= __uint_as_float((uint32_t)(127 + e) << 23);
+#pragma unroll
+            for (int t = 0; t < DS; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) q[t][i] = Store16<SASQ_F16>::pack(Store16<DTQ>::lo(q[t][i]) * down, Store16<DTQ>::hi(q[t][i]) * down);
+        }
+#pragma unroll
+        for (int t = 0; t < DS; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q[t][i] ^= flip;
+    }
+}
+
+// Sequences of at most `few` rows of a kv head are the rows kernel's, the others the tiles kernel's.
+int attention_rows_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& split, int few, int dim, bool int8, sasq_dtype dt, hipStream_t st);
+int attention_tiles_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& split, int few, int dim, bool int8, sasq_dtype dt, hipStream_t st);
+int attention_join_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& rows, const AttnSplit& tiles, int few, int dim, sasq_dtype dt, hipStream_t st);
 
 }  // namespace sasq

@@ -17,38 +17,20 @@ namespace sasq {
 
 constexpr int kSlab = 32, kRing = 2, kRowWaves = 4;
 constexpr int kSegment = 2048;                            // keys whose pages are listed in LDS at a time
-constexpr float kLazy = 8.0f;
 
 template <int D, bool I8>
-struct RowsGeo {
-    static constexpr int kRow = D * (I8 ? 1 : 2);         // bytes of a key
-    static constexpr int kChunks = kRow / 16;
-    static constexpr int kPart = kSlab * kRow;            // a slab's keys, or its values
+struct RowsGeo : KvRow<D, I8> {
+    using K = KvRow<D, I8>;
+    static constexpr int kPart = 2 * K::k16;              // a slab's keys, or its values
     static constexpr int kStage = 2 * kPart;
-    static constexpr int kPerLoad = 1024 / kRow;          // rows that one wave-wide load brings
-    static constexpr int kLoads = 16 / kPerLoad;          // loads for 16 rows
     static constexpr int kRingBytes = kRowWaves * kRing * kStage;
     static constexpr int kJoin = kRowWaves * 16 * (D + 4) * 4;
     static constexpr int kBody = kRingBytes > kJoin ? kRingBytes : kJoin;
     static constexpr int kLds = kBody + kRowWaves * 16 * 8 + kSegment / 16 * 4;
-    // Place of 16-byte chunk c of row r (of 32): the eight rows that a wave reads at a time at one c lie in different banks, and so do
-    // the rows that one transposing read takes (16 bits: rows 4g..4g+3, two chunks each; codes: 4g..4g+3 of both halves).
-    static __device__ __forceinline__ int swizzle(int r)
-    {
-        if constexpr (!I8) return kChunks == 16 ? ((r & 7) << 1) | ((r >> 3) & 1) : ((r & 3) << 1) | ((r >> 2) & 1);
-        else return kChunks == 8 ? (r & 3) | ((((r >> 4) ^ (r >> 2)) & 1) << 2) : ((r >> 4) ^ (r >> 2)) & 1;
-    }
 };
 
-template <int N>
-__device__ __forceinline__ void wait_loads()
-{
-    __builtin_amdgcn_s_waitcnt(waitcnt_vm(N));
-    asm volatile("" ::: "memory");
-}
-
 template <int DTQ, int D, bool I8, int RB>
-__global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnArgs a, KvPages cache, KvSteps steps, AttnSplit split, int first)
+__global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnArgs a, KvPages cache, KvSteps steps, AttnSplit split, int few, int first)
 {
     using G = RowsGeo<D, I8>;
     constexpr int DT = I8 ? SASQ_F16 : DTQ;               // of the products
@@ -63,7 +45,7 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
     const int b = rest % steps.batch, run = rest / steps.batch;
     const KvSeq seq = kv_seq(steps, b, cache.page_shift);
     const int rows = seq.rows * a.group, row0 = tile * 16 * RB;
-    if (row0 >= rows) return;
+    if (rows > few || row0 >= rows) return;
     const int end = attn_end(seq, a.group, split, tile), runs = attn_runs(split, end);
     if (run >= runs) return;
     const int from = run * split.chunk, to = run == runs - 1 ? end : min(end, from + split.chunk);
@@ -80,51 +62,12 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
         const bool there = r < rows;
         const int token = (there ? r : row0) / a.group, head = (there ? r : row0) % a.group;
         sees[rb] = seq.keys - seq.rows + token;
-        const uint16_t* src = a.q + (int64_t)(seq.row0 + token) * a.q_stride + (int64_t)(hk * a.group + head) * D;
-#pragma unroll
-        for (int t = 0; t < DS; ++t) {
-            const int d = I8 ? 64 * (t >> 1) + 16 * g + 8 * (t & 1) : 32 * t + 8 * g;      // a code's load of 16 serves two steps
-            q[rb][t] = *reinterpret_cast<const u32x4*>(src + d);
-            if (!there) q[rb][t] = u32x4{0, 0, 0, 0};
-        }
-        c[rb] = a.scale * 1.44269504088896f;
-        if constexpr (I8) {
-            // fp16 products: a bf16 row is brought to at most 2 by a power of two (exact but for values 2^-14 and more below its largest),
-            // and the sign of the factor goes into Q, so that larger products stay larger scores.
-            c[rb] *= fabsf(k_scale);
-            const uint32_t flip = k_scale < 0.0f ? 0x80008000u : 0u;
-            if constexpr (DTQ == SASQ_BF16) {
-                float top = 0.0f;
-#pragma unroll
-                for (int t = 0; t < DS; ++t)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(Store16<DTQ>::lo(q[rb][t][i])), fabsf(Store16<DTQ>::hi(q[rb][t][i]))));
-                top = fmaxf(top, __shfl_xor(top, 16, kWave));
-                top = fmaxf(top, __shfl_xor(top, 32, kWave));
-                const int e = top > 0.0f && top < INFINITY ? min(max(((int)(__float_as_uint(top) >> 23)) - 127, -100), 100) : 0;
-                const float down = __uint_as_float((uint32_t)(127 - e) << 23);
-                c[rb] *= __uint_as_float((uint32_t)(127 + e) << 23);
-#pragma unroll
-                for (int t = 0; t < DS; ++t)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) q[rb][t][i] = Store16<SASQ_F16>::pack(Store16<DTQ>::lo(q[rb][t][i]) * down, Store16<DTQ>::hi(q[rb][t][i]) * down);
-            }
-#pragma unroll
-            for (int t = 0; t < DS; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) q[rb][t][i] ^= flip;
-        }
+        load_q<DTQ, D, I8>(a, a.q + (int64_t)(seq.row0 + token) * a.q_stride + (int64_t)(hk * a.group + head) * D, there, g, k_scale, q[rb], c[rb]);
     }
 
-    // Where the lane's 16 bytes of each load come from, for both halves of a slab.
-    uint32_t off[2][G::kLoads];
+    uint32_t off[G::kLoads];
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int j = 0; j < G::kLoads; ++j) {
-            const int r = j * G::kPerLoad + lane / G::kChunks;
-            off[h][j] = (uint32_t)(r * cache.token_stride) + 16 * ((lane % G::kChunks) ^ G::swizzle(16 * h + r));
-        }
+    for (int j = 0; j < G::kLoads; ++j) off[j] = G::source(j, lane, cache.token_stride);
     char* const ring = lds + wave * kRing * G::kStage;
     const uint32_t ring_at = (uint32_t)(uintptr_t)(lds_ptr_t)ring;
     int* const pages = reinterpret_cast<int*>(lds + G::kBody + kRowWaves * 16 * 8);
@@ -160,15 +103,16 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
                 const int page = page_of(i, h), place = (k0 + 16 * h) & ((1 << cache.page_shift) - 1);
                 const uint8_t* base = plane + (int64_t)hk * cache.head_stride + (page < 0 ? 0 : page * cache.page_stride + place * cache.token_stride);
 #pragma unroll
-                for (int j = 0; j < G::kLoads; ++j) load_to_lds(at + (h * G::kLoads + j) * 1024, base, off[h][j]);
+                for (int j = 0; j < G::kLoads; ++j) load_to_lds(at + (h * G::kLoads + j) * G::kBlock, base, off[j]);
             }
         };
         wait_loads<0>();                                                   // Q has landed: the loop's waits count the ring's loads alone
         constexpr int NL = 2 * G::kLoads;                                  // loads of a slab's keys, or of its values
         for (int i = 0; i < kRing && i < mine; ++i) { fetch(i, cache.k, 0); fetch(i, cache.v, 1); }
         for (int i = 0; i < mine; ++i) {
-            const char* kp = ring + (i % kRing) * G::kStage;
-            const char* vp = kp + G::kPart;
+            const char* stage = ring + (i % kRing) * G::kStage;
+            const char* kp = stage + G::key_lane(lane);
+            const char* vp = stage + G::kPart + G::value_lane(lane);
             const int k0 = seg + kSlab * (wave + i * kRowWaves);
             if (i + 1 < mine) wait_loads<3 * NL>();
             else              wait_loads<NL>();
@@ -179,8 +123,7 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
             for (int t = 0; t < (I8 ? DS / 2 : DS); ++t)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int r = 16 * h + l16;
-                    const u32x4 w = *reinterpret_cast<const u32x4*>(kp + r * G::kRow + 16 * ((4 * t + g) ^ G::swizzle(r)));
+                    const u32x4 w = G::key(kp + h * G::k16, t);
                     if constexpr (I8) {
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
@@ -246,26 +189,9 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
             if (i + kRing < mine)    wait_loads<3 * NL>();
             else if (i + 1 < mine)   wait_loads<2 * NL>();
             else                     wait_loads<0>();
-            auto value = [&](int n) -> u32x4 {                             // channels 16 n + l16, the eight keys of the lane's slots
-                if constexpr (I8) {
-                    const int e = l16 >> 1, r = (e < 4 ? 0 : 16) + 4 * g + (e & 3);
-                    const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2)(vp + r * G::kRow + 16 * (n ^ G::swizzle(r)) + 8 * (l16 & 1)));
-                    const u32x2 x = codes_to_f16((uint32_t)w[0]), y = codes_to_f16((uint32_t)w[1]);
-                    return u32x4{x[0], x[1], y[0], y[1]};
-                } else {
-                    u32x2 half[2];
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int r = 16 * h + 4 * g + (l16 >> 2), ch = 2 * n + ((l16 & 3) >> 1);
-                        half[h] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                            (lds_i16x4)(vp + r * G::kRow + 16 * (ch ^ G::swizzle(r)) + 8 * (l16 & 1))));
-                    }
-                    return u32x4{half[0][0], half[0][1], half[1][0], half[1][1]};
-                }
-            };
             u32x4 v[DO];
 #pragma unroll
-            for (int n = 0; n < DO; ++n) v[n] = value(n);
+            for (int n = 0; n < DO; ++n) v[n] = G::value(vp, n);
             if constexpr (!I8) {
                 // A masked place may hold anything, and 0 times infinity is not 0: infinities and NaN are taken out of the product and
                 // put in by hand for the rows that see them.
@@ -276,7 +202,6 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
 #pragma unroll
                         for (int j = 0; j < 4; ++j) special |= any_special<DT>(v[n][j]);
                     if (__any(special)) {
-                        const uint32_t one = DT == SASQ_F16 ? 0x3C00u : 0x3F80u;
 #pragma unroll
                         for (int rb = 0; rb < RB; ++rb) {
                             u32x4 seen;
@@ -284,26 +209,15 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
                             for (int j = 0; j < 4; ++j) {
                                 const int key = k0 + (j < 2 ? 0 : 16) + 4 * g + 2 * (j & 1);
                                 const bool there = (j < 2 ? page0 : page1) >= 0;
-                                seen[j] = (there && key <= sees[rb] ? one : 0u) | (there && key + 1 <= sees[rb] ? one << 16 : 0u);
+                                seen[j] = (there && key <= sees[rb] ? kSeen : 0u) | (there && key + 1 <= sees[rb] ? kSeen << 16 : 0u);
                             }
 #pragma unroll
-                            for (int n = 0; n < DO; ++n)
-#pragma unroll
-                                for (int kind = 0; kind < 3; ++kind) {
-                                    u32x4 w;
-#pragma unroll
-                                    for (int j = 0; j < 4; ++j) w[j] = special_mask<DT>(v[n][j], kind);
-                                    const f32x4 count = mfma16<DT>(w, seen, f32x4{0, 0, 0, 0});
-                                    const float add = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
-#pragma unroll
-                                    for (int j = 0; j < 4; ++j)
-                                        if (count[j] > 0.0f) o[rb][n][j] += add;
-                                }
+                            for (int n = 0; n < DO; ++n) o[rb][n] = add_specials<DT>(v[n], seen, o[rb][n]);
                         }
 #pragma unroll
                         for (int n = 0; n < DO; ++n)
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) v[n][j] = special_mask<DT>(v[n][j], 3);
+                            for (int j = 0; j < 4; ++j) v[n][j] = finite_of<DT>(v[n][j]);
                     }
                 }
             }
@@ -358,7 +272,7 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
             __builtin_memcpy(dst, w, sizeof(w));
             if (a.lse && d == 0) a.lse[(int64_t)(seq.row0 + token) * a.q_heads + head] = none ? -INFINITY : (top + log2f(sum)) * 0.693147180559945f;
         } else {
-            const int64_t slot = attn_slot(split, steps.batch, cache.heads, run, b, hk, r);
+            const int64_t slot = rows_slot(split, steps.batch, cache.heads, run, b, hk, r);
             float* dst = split.o + slot * D + d;
 #pragma unroll
             for (int e = 0; e < E; e += 4) *reinterpret_cast<f32x4*>(dst + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
@@ -367,63 +281,18 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
     }
 }
 
-// Joins the runs of one row: a wave for each, D / 64 channels a lane.
-template <int DTQ, int D>
-__global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, KvPages cache, KvSteps steps, AttnSplit split, int first)
+int attention_rows_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& split, int few, int dim, bool int8, sasq_dtype dt, hipStream_t st)
 {
-    constexpr int E = D / 64;
-    const int lane = (int)threadIdx.x & 63;
-    const int64_t row = ((int64_t)blockIdx.x + first) * 4 + ((int)threadIdx.x >> 6);
-    const int t = (int)(row / a.q_heads), head = (int)(row % a.q_heads);
-    if (t >= steps.tokens) return;
-    int before = 0;
-    for (int i = 0; i <= steps.batch; i += kWave)
-        before += __popcll(__ballot(i + lane <= steps.batch && steps.cu_q[min(i + lane, steps.batch)] <= t));
-    const int b = before - 1;
-    if (b < 0 || b >= steps.batch) return;
-    const KvSeq seq = kv_seq(steps, b, cache.page_shift);
-    const int token = t - seq.row0, hk = head / a.group, r = token * a.group + head % a.group;
-    if (token < 0 || token >= seq.rows || r >= split.tiles * split.tile_rows) return;
-    if (attn_runs(split, attn_end(seq, a.group, split, r / split.tile_rows)) == 1) return;      // written already
-    const int sees = seq.keys - seq.rows + token;
-    const int runs = sees < 0 ? 0 : min(split.splits, sees / split.chunk + 1);                    // later ones have no key of this row
-    float top = -INFINITY;
-    for (int i = lane; i < runs; i += kWave) top = fmaxf(top, split.ml[attn_slot(split, steps.batch, cache.heads, i, b, hk, r)].x);
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, kWave));
-    float sum = 0.0f, x[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = 0.0f;
-#pragma unroll 4
-    for (int i = 0; i < runs; ++i) {
-        const int64_t slot = attn_slot(split, steps.batch, cache.heads, i, b, hk, r);
-        const float2 f = split.ml[slot];
-        const float weight = f.x == -INFINITY && f.y == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(f.x == top ? 0.0f : f.x - top);
-        sum += f.y * weight;
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = __builtin_fmaf(split.o[slot * D + lane * E + e], weight, x[e]);
-    }
-    const bool none = sum == 0.0f;
-    const float f = none ? 0.0f : (cache.v_scale ? cache.v_scale[hk] : 1.0f) / sum;
-    uint16_t* dst = a.out + (int64_t)t * a.out_stride + (int64_t)head * D + lane * E;
-#pragma unroll
-    for (int e = 0; e < E; ++e) dst[e] = none ? (uint16_t)0 : Store16<DTQ>::enc(x[e] * f);
-    if (a.lse && lane == 0) a.lse[(int64_t)t * a.q_heads + head] = none ? -INFINITY : (top + log2f(sum)) * 0.693147180559945f;
-}
-
-int attention_rows_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& split, int dim, bool int8, sasq_dtype dt, hipStream_t st)
-{
-    auto go = [&](auto kernel, int64_t blocks) {
-        launch_in_parts(blocks, 256, [&](unsigned n, int first) { hipLaunchKernelGGL(kernel, dim3(n), dim3(256), 0, st, a, c, s, split, first); });
+    auto go = [&](auto kernel) {
+        launch_in_parts((int64_t)split.splits * s.batch * split.tiles * c.heads, 256,
+                        [&](unsigned n, int first) { hipLaunchKernelGGL(kernel, dim3(n), dim3(256), 0, st, a, c, s, split, few, first); });
     };
     auto with = [&](auto dtv, auto dimv, auto i8v) {
         constexpr int DT = decltype(dtv)::value, D = decltype(dimv)::value;
         constexpr bool I8 = decltype(i8v)::value;
-        const int64_t blocks = (int64_t)split.splits * s.batch * split.tiles * c.heads;
-        if (split.tile_rows == 16)      go(attention_rows_kernel<DT, D, I8, 1>, blocks);
-        else if (split.tile_rows == 32) go(attention_rows_kernel<DT, D, I8, 2>, blocks);
-        else                            go(attention_rows_kernel<DT, D, I8, 4>, blocks);
-        if (split.splits > 1) go(attention_join_kernel<DT, D>, ((int64_t)s.tokens * a.q_heads + 3) / 4);
+        if (split.tile_rows == 16)      go(attention_rows_kernel<DT, D, I8, 1>);
+        else if (split.tile_rows == 32) go(attention_rows_kernel<DT, D, I8, 2>);
+        else                            go(attention_rows_kernel<DT, D, I8, 4>);
     };
     auto by_format = [&](auto dtv, auto dimv) {
         if (int8) with(dtv, dimv, std::true_type{});
