@@ -121,6 +121,16 @@ __device__ __forceinline__ void wait_loads()
 // A score may pass the running maximum by so much (in powers of two) before the maximum is moved: probabilities then reach 2^8 at most,
 // their rounding is relative all the same, and the common step needs no reduction over lanes and no rescaling of the output.
 constexpr float kLazy = 8.0f;
+// The maximum before any score: finite, so that a row whose scores are all masked gets probabilities of 0 and any other score moves it.
+constexpr float kNoMax = -1e30f;
+// What sums over an older maximum are multiplied by.  Never 0, which would make NaN of an infinite sum.
+__device__ __forceinline__ float kept(float before, float now) { return fmaxf(__builtin_amdgcn_exp2f(before - now), 1e-37f); }
+// The same for a part of a row's keys, f = (maximum, sum), joined with others under `top`: a part without keys has nothing to add, one whose
+// maximum is infinite or whose sum is NaN hands that on.
+__device__ __forceinline__ float part_weight(const float2& f, float top)
+{
+    return f.x == -INFINITY && f.y == 0.0f ? 0.0f : f.x == top ? 1.0f : kept(f.x, top);
+}
 
 // Keys or values of one head in LDS.  A wave-wide load brings whole rows, 1 KB of them, and puts them down as a block in which the rows'
 // 16-byte chunks of one place follow each other; blocks are 64 bytes apart.  The eight rows that a wave reads at a time at one chunk then
@@ -207,6 +217,6 @@ __device__ __forceinline__ void load_q(const AttnArgs& a, const uint16_t* src, b
 // Sequences of at most `few` rows of a kv head are the rows kernel's, the others the tiles kernel's.
 int attention_rows_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& split, int few, int dim, bool int8, sasq_dtype dt, hipStream_t st);
 int attention_tiles_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& split, int few, int dim, bool int8, sasq_dtype dt, hipStream_t st);
-int attention_join_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& rows, const AttnSplit& tiles, int few, int dim, sasq_dtype dt, hipStream_t st);
+int attention_join_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& split, bool tiled, int few, int dim, sasq_dtype dt, hipStream_t st);
 
 }  // namespace sasq

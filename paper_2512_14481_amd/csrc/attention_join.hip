@@ -3,29 +3,39 @@
 
 namespace sasq {
 
-// A wave for each row, D / 64 channels a lane.
-template <int DTQ, int D>
-__global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, KvPages cache, KvSteps steps, AttnSplit by_rows, AttnSplit by_tiles, int few, int first)
+// A wave for each row, D / 64 channels a lane.  Of the rows kernel: row r of a sequence and kv head, of the places of all sequences; of the
+// tiles kernel: a token and a head.
+template <int DTQ, int D, bool TILED>
+__global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, KvPages cache, KvSteps steps, AttnSplit split, int few, int first)
 {
     constexpr int E = D / 64;
     const int lane = (int)threadIdx.x & 63;
-    const int64_t row = ((int64_t)blockIdx.x + first) * 4 + ((int)threadIdx.x >> 6);
-    const int t = (int)(row / a.q_heads), head = (int)(row % a.q_heads);
-    if (t >= steps.tokens) return;
-    int before = 0;
-    for (int i = 0; i <= steps.batch; i += kWave)
-        before += __popcll(__ballot(i + lane <= steps.batch && steps.cu_q[min(i + lane, steps.batch)] <= t));
-    const int b = before - 1;
-    if (b < 0 || b >= steps.batch) return;
+    const int64_t row = ((int64_t)blockIdx.x + first) * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    int b, hk, r;
+    if constexpr (TILED) {
+        const int t = (int)(row / a.q_heads), head = (int)(row % a.q_heads);
+        if (t >= steps.tokens) return;
+        int before = 0;
+        for (int i = 0; i <= steps.batch; i += kWave)
+            before += __popcll(__ballot(i + lane <= steps.batch && steps.cu_q[min(i + lane, steps.batch)] <= t));
+        b = before - 1;
+        if (b < 0 || b >= steps.batch) return;
+        hk = head / a.group;
+        r = (t - kv_seq(steps, b, cache.page_shift).row0) * a.group + head % a.group;
+    } else {
+        const int rows = split.tiles * split.tile_rows;
+        r = (int)(row % rows);
+        hk = (int)(row / rows % cache.heads);
+        if (row / rows / cache.heads >= steps.batch) return;
+        b = (int)(row / rows / cache.heads);
+    }
     const KvSeq seq = kv_seq(steps, b, cache.page_shift);
-    const int token = t - seq.row0, hk = head / a.group, r = token * a.group + head % a.group;
-    const bool tiled = seq.rows * a.group > few;
-    const AttnSplit& split = tiled ? by_tiles : by_rows;
-    if (token < 0 || token >= seq.rows || r >= split.tiles * split.tile_rows) return;
+    if (r < 0 || r >= seq.rows * a.group || r >= split.tiles * split.tile_rows || (seq.rows * a.group > few) != TILED) return;
     if (attn_runs(split, attn_end(seq, a.group, split, r / split.tile_rows)) == 1) return;      // written already
+    const int token = r / a.group, t = seq.row0 + token, head = hk * a.group + r % a.group;
     const int sees = seq.keys - seq.rows + token;
     const int runs = sees < 0 ? 0 : min(split.splits, sees / split.chunk + 1);                    // later ones have no key of this row
-    auto slot = [&](int i) -> int64_t { return tiled ? tiles_slot(steps.tokens, a.q_heads, i, t, head) : rows_slot(split, steps.batch, cache.heads, i, b, hk, r); };
+    auto slot = [&](int i) -> int64_t { return TILED ? tiles_slot(steps.tokens, a.q_heads, i, t, head) : rows_slot(split, steps.batch, cache.heads, i, b, hk, r); };
     float top = -INFINITY;
     for (int i = lane; i < runs; i += kWave) top = fmaxf(top, split.ml[slot(i)].x);
 #pragma unroll
@@ -37,7 +47,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, KvPages
     for (int i = 0; i < runs; ++i) {
         const int64_t at = slot(i);
         const float2 f = split.ml[at];
-        const float weight = f.x == -INFINITY && f.y == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(f.x == top ? 0.0f : f.x - top);
+        const float weight = part_weight(f, top);
         sum += f.y * weight;
 #pragma unroll
         for (int e = 0; e < E; ++e) x[e] = __builtin_fmaf(split.o[at * D + lane * E + e], weight, x[e]);
@@ -50,15 +60,23 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, KvPages
     if (a.lse && lane == 0) a.lse[(int64_t)t * a.q_heads + head] = none ? -INFINITY : (top + log2f(sum)) * 0.693147180559945f;
 }
 
-int attention_join_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& rows, const AttnSplit& tiles, int few, int dim, sasq_dtype dt, hipStream_t st)
+int attention_join_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& split, bool tiled, int few, int dim, sasq_dtype dt, hipStream_t st)
 {
+    const int64_t rows = tiled ? (int64_t)s.tokens * a.q_heads : (int64_t)s.batch * c.heads * split.tiles * split.tile_rows;
     auto go = [&](auto kernel) {
-        launch_in_parts(((int64_t)s.tokens * a.q_heads + 3) / 4, 256, [&](unsigned n, int first) {
-            hipLaunchKernelGGL(kernel, dim3(n), dim3(256), 0, st, a, c, s, rows, tiles, few, first);
-        });
+        launch_in_parts((rows + 3) / 4, 256, [&](unsigned n, int first) { hipLaunchKernelGGL(kernel, dim3(n), dim3(256), 0, st, a, c, s, split, few, first); });
     };
-    if (dt == SASQ_F16) dim == 64 ? go(attention_join_kernel<SASQ_F16, 64>) : go(attention_join_kernel<SASQ_F16, 128>);
-    else                dim == 64 ? go(attention_join_kernel<SASQ_BF16, 64>) : go(attention_join_kernel<SASQ_BF16, 128>);
+    auto with = [&](auto dtv, auto dimv) {
+        constexpr int DT = decltype(dtv)::value, D = decltype(dimv)::value;
+        if (tiled) go(attention_join_kernel<DT, D, true>);
+        else       go(attention_join_kernel<DT, D, false>);
+    };
+    auto by_dim = [&](auto dtv) {
+        if (dim == 64) with(dtv, std::integral_constant<int, 64>{});
+        else           with(dtv, std::integral_constant<int, 128>{});
+    };
+    if (dt == SASQ_F16) by_dim(std::integral_constant<int, SASQ_F16>{});
+    else                by_dim(std::integral_constant<int, SASQ_BF16>{});
     return hipGetLastError() == hipSuccess ? SASQ_OK : SASQ_ERR_LAUNCH;
 }
 

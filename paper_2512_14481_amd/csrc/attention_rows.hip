@@ -73,10 +73,10 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
     int* const pages = reinterpret_cast<int*>(lds + G::kBody + kRowWaves * 16 * 8);
 
     f32x4 o[RB][DO];
-    float m[RB], l[RB], lim[RB], mc[RB];                                   // maximum, sum; lim: scores up to it leave the maximum; mc: m c
+    float m[RB], l[RB];                                                    // maximum of the log2-scaled scores, sum
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-        m[rb] = -INFINITY; lim[rb] = -INFINITY; l[rb] = 0.0f; mc[rb] = 0.0f;
+        m[rb] = kNoMax; l[rb] = 0.0f;
 #pragma unroll
         for (int i = 0; i < DO; ++i) o[rb][i] = f32x4{0, 0, 0, 0};
     }
@@ -159,18 +159,16 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
             for (int rb = 0; rb < RB; ++rb) {
                 top[rb] = fmaxf(fmaxf(fmaxf(s[rb][0][0], s[rb][0][1]), fmaxf(s[rb][0][2], s[rb][0][3])),
                                 fmaxf(fmaxf(s[rb][1][0], s[rb][1][1]), fmaxf(s[rb][1][2], s[rb][1][3])));
-                above |= top[rb] > lim[rb];
+                above |= __builtin_fmaf(top[rb], c[rb], -m[rb]) > kLazy;
             }
             if (__any(above)) {
 #pragma unroll
                 for (int rb = 0; rb < RB; ++rb) {
                     float t = fmaxf(top[rb], __shfl_xor(top[rb], 16, kWave));
                     t = fmaxf(t, __shfl_xor(t, 32, kWave));
-                    t = fmaxf(t, m[rb]);
-                    const float keep = t == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m[rb] - t) * c[rb]);
+                    t = fmaxf(t * c[rb], m[rb]);
+                    const float keep = kept(m[rb], t);
                     m[rb] = t;
-                    mc[rb] = t == -INFINITY ? 0.0f : t * c[rb];
-                    lim[rb] = t + kLazy / c[rb];
                     l[rb] *= keep;
 #pragma unroll
                     for (int i2 = 0; i2 < DO; ++i2) o[rb][i2] *= keep;
@@ -180,7 +178,7 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
             for (int rb = 0; rb < RB; ++rb) {
                 float e[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][j >> 2][j & 3], c[rb], -mc[rb]));
+                for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][j >> 2][j & 3], c[rb], -m[rb]));
                 l[rb] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
 #pragma unroll
                 for (int j = 0; j < 4; ++j) p[rb][j] = Store16<DT>::pack(e[2 * j], e[2 * j + 1]);
@@ -241,7 +239,7 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
         __syncthreads();
         l[rb] += __shfl_xor(l[rb], 16, kWave);
         l[rb] += __shfl_xor(l[rb], 32, kWave);
-        if (g == 0) ml[wave * 16 + l16] = make_float2(m[rb] == -INFINITY ? -INFINITY : m[rb] * c[rb], l[rb]);
+        if (g == 0) ml[wave * 16 + l16] = make_float2(m[rb] == kNoMax ? -INFINITY : m[rb], l[rb]);
 #pragma unroll
         for (int n = 0; n < DO; ++n) *reinterpret_cast<f32x4*>(part + (wave * 16 + l16) * (D + 4) + 16 * n + 4 * g) = o[rb][n];
         __syncthreads();
@@ -254,8 +252,7 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
 #pragma unroll
         for (int w = 0; w < kRowWaves; ++w) {
             const float2 f = ml[w * 16 + rr];
-            // a wave without keys has nothing to add; one whose maximum is NaN or infinite hands that on
-            const float weight = f.x == -INFINITY && f.y == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(f.x == top ? 0.0f : f.x - top);
+            const float weight = part_weight(f, top);
             sum += f.y * weight;
 #pragma unroll
             for (int e = 0; e < E; ++e) x[e] = __builtin_fmaf(part[(w * 16 + rr) * (D + 4) + d + e], weight, x[e]);

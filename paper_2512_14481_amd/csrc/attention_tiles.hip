@@ -1,19 +1,22 @@
 // Attention of many rows over the paged cache (chunks and prompts): bound by the matrix units and the exponentials beside them.
 //
 // A workgroup has one kv head of one sequence, 64 RB rows of it (its four waves 16 RB each, the heads that share the kv head packed into
-// the rows) and one run of keys, which it takes in tiles of 64 through rings of three stages in LDS for K and for V.
+// the rows) and one run of keys, which it takes in tiles of 64 through rings of four stages in LDS for K and for V.
 //
 // Both products are taken transposed on 16x16x32 (see attention_rows.hip), a lane keeps one row of each block of 16 from the scores to the
 // output, and each fragment of K or V that a wave reads from LDS serves RB products.  The scores of the next tile take the registers of
 // this one's as these become probabilities, 16 keys after 16, so that products and exponentials stand side by side.
 #include "attention.h"
 
+#ifndef SCHED_A
+#define SCHED_A 4
+#endif
 #ifndef SASQ_RB
 #define SASQ_RB 2
 #endif
 namespace sasq {
 
-constexpr int kTileKeys = 64, kTileRing = 3;
+constexpr int kTileKeys = 64, kTileRing = 4;
 
 template <int D, bool I8, int W>
 struct TilesGeo : KvRow<D, I8> {
@@ -96,53 +99,59 @@ __global__ __launch_bounds__(W * 64, W / 4) void attention_tiles_kernel(AttnArgs
     uint32_t off[L];
 #pragma unroll
     for (int j = 0; j < L; ++j) off[j] = G::source(j, lane, cache.token_stride);
-    auto page_offset = [&](int i) -> int64_t {                             // where the wave's unit of tile i lies in either plane
-        const int page = __builtin_amdgcn_readfirstlane(list[i & 127]);
+    auto page_of = [&](int i) -> int { return list[i & 127]; };
+    auto fetch = [&](int i, int page, const uint8_t* plane, int at) {       // the wave's unit of tile i, which lies on `page`
+        page = __builtin_amdgcn_readfirstlane(page);
         const int place = (from + kTileKeys * i + 16 * unit) & ((1 << cache.page_shift) - 1);
-        return (int64_t)hk * cache.head_stride + (page < 0 || page >= cache.pages ? 0 : page * cache.page_stride + place * cache.token_stride);
-    };
-    auto fetch = [&](int i, const uint8_t* plane, int at) {
-        const uint8_t* base = plane + page_offset(i);
-        const uint32_t to_lds = lds_at + at + (i % kTileRing) * G::kTile + unit * G::k16;
+        const uint8_t* base = plane + (int64_t)hk * cache.head_stride + (page < 0 || page >= cache.pages ? 0 : page * cache.page_stride + place * cache.token_stride);
+        const uint32_t to_lds = lds_at + at + unit * G::k16;
 #pragma unroll
         for (int j = 0; j < L; ++j) load_to_lds(to_lds + G::kBlock * j, base, off[j]);
     };
-    auto keys_at = [&](int i) -> const char* { return lds + G::kKeysAt + (i % kTileRing) * G::kTile; };
-    auto values_at = [&](int i) -> char* { return lds + G::kValuesAt + (i % kTileRing) * G::kTile; };
+    auto fetch_keys = [&](int i, int page) { fetch(i, page, cache.k, G::kKeysAt + i % kTileRing * G::kTile); };
+    auto fetch_values = [&](int i, int page) { fetch(i, page, cache.v, G::kValuesAt + i % kTileRing * G::kTile); };
+    auto keys_at = [&](int i) -> const char* { return lds + G::kKeysAt + i % kTileRing * G::kTile; };
+    auto values_at = [&](int i) -> char* { return lds + G::kValuesAt + i % kTileRing * G::kTile; };
 
     f32x4 o[RB][DO];
-    float m[RB], l[RB], lim[RB], mc[RB];
+    float m[RB], l[RB];                                                    // maximum of the log2-scaled scores, sum
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-        m[rb] = -INFINITY; lim[rb] = -INFINITY; l[rb] = 0.0f; mc[rb] = 0.0f;
+        m[rb] = kNoMax; l[rb] = 0.0f;
 #pragma unroll
         for (int n = 0; n < DO; ++n) o[rb][n] = f32x4{0, 0, 0, 0};
     }
     f32x4 s[RB][KT];
     u32x4 p[RB][KT / 2];
-    auto scores = [&](int i, int k) {                                      // of keys 16 k .. of tile i
+    constexpr int KF = I8 ? DS / 2 : DS;                                   // fragments of 16 keys
+    typedef u32x4 KeyFrags[KF];
+    typedef u32x4 ValueFrags[4];
+    auto read_keys = [&](int i, int k, KeyFrags& w) {                      // keys 16 k .. of tile i
         const char* at = keys_at(i) + G::key_lane(lane) + k * G::k16;
+#pragma unroll
+        for (int t = 0; t < KF; ++t) w[t] = G::key(at, t);
+    };
+    auto scores = [&](int k, const KeyFrags& w) {
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) s[rb][k] = f32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int t = 0; t < (I8 ? DS / 2 : DS); ++t) {
-            const u32x4 w = G::key(at, t);
+        for (int t = 0; t < KF; ++t) {
             if constexpr (I8) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const u32x2 x = codes_to_f16(w[2 * e]), y = codes_to_f16(w[2 * e + 1]);
+                    const u32x2 x = codes_to_f16(w[t][2 * e]), y = codes_to_f16(w[t][2 * e + 1]);
 #pragma unroll
                     for (int rb = 0; rb < RB; ++rb) s[rb][k] = mfma16<DT>(u32x4{x[0], x[1], y[0], y[1]}, q[rb][2 * t + e], s[rb][k]);
                 }
             } else {
 #pragma unroll
-                for (int rb = 0; rb < RB; ++rb) s[rb][k] = mfma16<DT>(w, q[rb][t], s[rb][k]);
+                for (int rb = 0; rb < RB; ++rb) s[rb][k] = mfma16<DT>(w[t], q[rb][t], s[rb][k]);
             }
         }
     };
+    auto unmasked = [&](int i) -> bool { return !holes && from + kTileKeys * i + kTileKeys - 1 <= sees_wave; };
     auto mask = [&](int i) {
         const int k0 = from + kTileKeys * i;
-        if (!holes && k0 + kTileKeys - 1 <= sees_wave) return;
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
             const int last = sees[rb] - k0 - 4 * g;                        // of the lane's keys, 0 being its first
@@ -171,7 +180,7 @@ __global__ __launch_bounds__(W * 64, W / 4) void attention_tiles_kernel(AttnArgs
             for (int k = 0; k < KT; ++k)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) top[rb] = fmaxf(top[rb], s[rb][k][j]);
-            above |= top[rb] > lim[rb];
+            above |= __builtin_fmaf(top[rb], c[rb], -m[rb]) > kLazy;
         }
         return __any(above);
     };
@@ -180,11 +189,9 @@ __global__ __launch_bounds__(W * 64, W / 4) void attention_tiles_kernel(AttnArgs
         for (int rb = 0; rb < RB; ++rb) {
             float t = fmaxf(top[rb], __shfl_xor(top[rb], 16, kWave));
             t = fmaxf(t, __shfl_xor(t, 32, kWave));
-            t = fmaxf(t, m[rb]);
-            const float keep = t == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m[rb] - t) * c[rb]);
+            t = fmaxf(t * c[rb], m[rb]);
+            const float keep = kept(m[rb], t);
             m[rb] = t;
-            mc[rb] = t == -INFINITY ? 0.0f : t * c[rb];
-            lim[rb] = t + kLazy / c[rb];
             l[rb] *= keep;
 #pragma unroll
             for (int n = 0; n < DO; ++n) o[rb][n] *= keep;
@@ -195,20 +202,23 @@ __global__ __launch_bounds__(W * 64, W / 4) void attention_tiles_kernel(AttnArgs
         for (int rb = 0; rb < RB; ++rb) {
             float e[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][k][j], c[rb], -mc[rb]));
+            for (int j = 0; j < 4; ++j) e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][k][j], c[rb], -m[rb]));
             l[rb] += (e[0] + e[1]) + (e[2] + e[3]);
             p[rb][k / 2][2 * (k & 1)] = Store16<DT>::pack(e[0], e[1]);
             p[rb][k / 2][2 * (k & 1) + 1] = Store16<DT>::pack(e[2], e[3]);
         }
     };
-    auto add_values = [&](int i, int k) {                                  // of keys 32 k ..
-        const char* at = values_at(i) + G::value_lane(lane) + 2 * k * G::k16;
+    constexpr int VG = KT / 2 * DO / 4;                                    // groups of four fragments of a tile's values: 64 channels of 32 keys
+    auto read_values = [&](int i, int x, ValueFrags& w) {
+        const char* at = values_at(i) + G::value_lane(lane) + 2 * (x / (DO / 4)) * G::k16;
 #pragma unroll
-        for (int n = 0; n < DO; ++n) {
-            const u32x4 v = G::value(at, n);
+        for (int n = 0; n < 4; ++n) w[n] = G::value(at, 4 * (x % (DO / 4)) + n);
+    };
+    auto add_values = [&](int x, const ValueFrags& w) {
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb) o[rb][n] = mfma16<DT>(v, p[rb][k], o[rb][n]);
-        }
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) o[rb][4 * (x % (DO / 4)) + n] = mfma16<DT>(w[n], p[rb][x / (DO / 4)], o[rb][4 * (x % (DO / 4)) + n]);
     };
     // A masked place may hold anything, and 0 times infinity is not 0: in a masked tile with infinities or NaN among its values these are
     // put into the rows that see them by hand, and taken out of the tile.
@@ -266,42 +276,71 @@ __global__ __launch_bounds__(W * 64, W / 4) void attention_tiles_kernel(AttnArgs
         asm volatile("" ::: "memory");
     };
 
-    // Tile i.  Its first 16 keys' probabilities, and the maxima, are there already.
-    auto step = [&](int i) {
-        // In order: of four waves, K(i+1) V(i) have landed when at most K(i+2) and V(i+1) are still under way; of eight each has one of them.
-        if (i + 2 < tiles) wait_loads<(W == 4 ? 2 : 1) * L>();
+    int ahead_k = 0, ahead_v = 0;                                          // pages of tiles i + 4 (keys) and i + 3 (values), read a tile before
+    auto enter = [&](int i) {                                              // the workgroup goes on to tile i
+        // In order: of four waves, K(i+2) V(i+1) have landed when at most V(i+2) and K(i+3) are still under way; of eight each has one of them.
+        if (i + 3 < tiles) wait_loads<(W == 4 ? 2 : 1) * L>();
         else               wait_loads<0>();
-        const bool look = !I8 && masked_group(i);
-        if (look && brings_v) look_for_specials(i);
-        __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (i + 3 < tiles) {
-            if (((i + 3) & 63) == 0) fetch_list((i + 3) / 64 + 1);
-            if (brings_k) fetch(i + 3, cache.k, G::kKeysAt);
-        }
-        if (brings_v && i + 2 < tiles) fetch(i + 2, cache.v, G::kValuesAt);
-        if (look) {
+        if (i + 4 < tiles && ((i + 4) & 63) == 0) fetch_list((i + 4) / 64 + 1);
+        if (brings_k && i + 4 < tiles) fetch_keys(i + 4, ahead_k);
+        if (brings_v && i + 3 < tiles) fetch_values(i + 3, ahead_v);
+        ahead_v = W == 4 ? ahead_k : page_of(i + 4);
+        ahead_k = page_of(i + 5);
+        if (!I8 && masked_group(i)) {
+            if (brings_v) look_for_specials(i);
+            __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
             const int* f = flags + (i & 1) * 4;
             if (__builtin_amdgcn_readfirstlane(f[0] | f[1] | f[2] | f[3])) take_specials_out(i);
         }
+    };
+    constexpr int kMfma = 0x8, kValu = 0x2;
+    KeyFrags kf;                                                           // of the first 16 keys of the next tile, read ahead of the barrier
+    bool above = false;
+    auto work = [&](int i) {
+        if (above) raise();
+        probabilities(0);
+        ValueFrags vf;
         if (i + 1 < wave_tiles) {
 #pragma unroll
             for (int k = 0; k < KT; ++k) {
-                scores(i + 1, k);
-                if (k + 1 < KT) probabilities(k + 1);
+                KeyFrags next;
+                if (k + 1 < KT) read_keys(i + 1, k + 1, next);
+                else            read_values(i, 0, vf);
+                __builtin_amdgcn_sched_barrier(0);                         // the reads of the next products stand ahead of these
+                scores(k, kf);
+                if (k + 1 < KT) {
+                    probabilities(k + 1);
+#pragma unroll
+                    for (int x = 0; x < RB * DS; ++x) {
+                        __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+                        __builtin_amdgcn_sched_group_barrier(kValu, SCHED_A, 0);
+                    }
+#pragma unroll
+                    for (int t = 0; t < KF; ++t) kf[t] = next[t];
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
-            mask(i + 1);
-            add_values(i, 0);
-            const bool above = maxima();
-            add_values(i, 1);
-            if (above) raise();
-            probabilities(0);
-        } else if (i < wave_tiles) {
+            if (!unmasked(i + 1)) mask(i + 1);
+        } else {
 #pragma unroll
             for (int k = 1; k < KT; ++k) probabilities(k);
-            add_values(i, 0);
-            add_values(i, 1);
+            read_values(i, 0, vf);
+        }
+#pragma unroll
+        for (int x = 0; x < VG; ++x) {
+            ValueFrags next;
+            if (x + 1 < VG) read_values(i, x + 1, next);
+            else            read_keys(i + 2, 0, kf);
+            __builtin_amdgcn_sched_barrier(0);
+            add_values(x, vf);
+            if (x == 0) above = maxima();                                  // (of the last tile's scores again after the last tile: never above)
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int n = 0; n < 4; ++n) vf[n] = next[n];
         }
     };
 
@@ -309,29 +348,30 @@ __global__ __launch_bounds__(W * 64, W / 4) void attention_tiles_kernel(AttnArgs
         fetch_list(0);
         fetch_list(1);
         wait_loads<0>();                                                   // Q too: the loop's waits count the rings' loads alone
-        for (int i = 0; i < 3 && i < tiles; ++i) {
-            if (brings_k) fetch(i, cache.k, G::kKeysAt);
-            if (brings_v && i < 2) fetch(i, cache.v, G::kValuesAt);
+        for (int i = 0; i < 4 && i < tiles; ++i) {
+            if (brings_k) fetch_keys(i, page_of(i));
+            if (brings_v && i < 3) fetch_values(i, page_of(i));
         }
-        if (W == 4) {
-            if (tiles > 2)      wait_loads<4 * L>();
-            else if (tiles > 1) wait_loads<3 * L>();
-            else                wait_loads<L>();
-        } else {
-            if (tiles > 2)      wait_loads<2 * L>();
-            else if (tiles > 1) wait_loads<L>();
-            else                wait_loads<0>();
-        }
+        ahead_k = page_of(4);
+        ahead_v = page_of(3);
+        if (tiles > 3) wait_loads<(W == 4 ? 4 : 2) * L>();
+        else           wait_loads<0>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         if (wave_tiles > 0) {
 #pragma unroll
-            for (int k = 0; k < KT; ++k) scores(0, k);
-            mask(0);
+            for (int k = 0; k < KT; ++k) {
+                read_keys(0, k, kf);
+                scores(k, kf);
+            }
+            if (!unmasked(0)) mask(0);
             if (maxima()) raise();
-            probabilities(0);
+            read_keys(1, 0, kf);
         }
-        for (int i = 0; i < tiles; ++i) step(i);
+        for (int i = 0; i < tiles; ++i) {
+            enter(i);
+            if (i < wave_tiles) work(i);
+        }
     }
 
     const float v_scale = I8 ? cache.v_scale[hk] : 1.0f;
@@ -343,7 +383,7 @@ __global__ __launch_bounds__(W * 64, W / 4) void attention_tiles_kernel(AttnArgs
         const int r = wave_row + 16 * rb + l16;
         if (r >= rows) continue;
         const int64_t t = seq.row0 + r / a.group, head = hk * a.group + r % a.group;
-        const float top = m[rb] == -INFINITY ? -INFINITY : m[rb] * c[rb];
+        const float top = m[rb] == kNoMax ? -INFINITY : m[rb];
         if (runs == 1) {
             const bool none = sum == 0.0f;
             const float f = none ? 0.0f : v_scale / sum;

@@ -93,6 +93,7 @@ extern "C" int sasq_paged_attention(const void* q, void* out, float* lse, int64_
     int rc = SASQ_OK;
     if (plan.tiled) rc = attention_tiles_launch(a, pages, steps, plan.tiles, few, (int)dim, int8, dt, st);
     if (rc == SASQ_OK) rc = attention_rows_launch(a, pages, steps, plan.rows, few, (int)dim, int8, dt, st);
-    if (rc == SASQ_OK && plan.rows_slots + plan.tiles_slots) rc = attention_join_launch(a, pages, steps, plan.rows, plan.tiles, few, (int)dim, dt, st);
+    if (rc == SASQ_OK && plan.tiles_slots) rc = attention_join_launch(a, pages, steps, plan.tiles, true, few, (int)dim, dt, st);
+    if (rc == SASQ_OK && plan.rows_slots) rc = attention_join_launch(a, pages, steps, plan.rows, false, few, (int)dim, dt, st);
     return rc;
 }
