@@ -62,7 +62,7 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
         const bool there = r < rows;
         const int token = (there ? r : row0) / a.group, head = (there ? r : row0) % a.group;
         sees[rb] = seq.keys - seq.rows + token;
-        load_q<DTQ, D, I8>(a, a.q + (int64_t)(seq.row0 + token) * a.q_stride + (int64_t)(hk * a.group + head) * D, there, g, k_scale, q[rb], c[rb]);
+        load_q<DTQ, D, I8, 16>(a, a.q + (int64_t)(seq.row0 + token) * a.q_stride + (int64_t)(hk * a.group + head) * D, there, g, k_scale, q[rb], c[rb]);
     }
 
     uint32_t off[G::kLoads];
@@ -111,8 +111,8 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
         for (int i = 0; i < kRing && i < mine; ++i) { fetch(i, cache.k, 0); fetch(i, cache.v, 1); }
         for (int i = 0; i < mine; ++i) {
             const char* stage = ring + (i % kRing) * G::kStage;
-            const char* kp = stage + G::key_lane(lane);
-            const char* vp = stage + G::kPart + G::value_lane(lane);
+            const char* kp = stage + G::template key_lane<16>(lane);
+            const char* vp = stage + G::kPart + G::template value_lane<16>(lane);
             const int k0 = seg + kSlab * (wave + i * kRowWaves);
             if (i + 1 < mine) wait_loads<3 * NL>();
             else              wait_loads<NL>();
@@ -123,7 +123,7 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
             for (int t = 0; t < (I8 ? DS / 2 : DS); ++t)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const u32x4 w = G::key(kp + h * G::k16, t);
+                    const u32x4 w = G::template key<16>(kp + h * G::k16, t);
                     if constexpr (I8) {
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
@@ -189,7 +189,7 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
             else                     wait_loads<0>();
             u32x4 v[DO];
 #pragma unroll
-            for (int n = 0; n < DO; ++n) v[n] = G::value(vp, n);
+            for (int n = 0; n < DO; ++n) v[n] = G::template value<16>(vp, n, G::value_odd(lane));
             if constexpr (!I8) {
                 // A masked place may hold anything, and 0 times infinity is not 0: infinities and NaN are taken out of the product and
                 // put in by hand for the rows that see them.

@@ -4,6 +4,9 @@
 #include <algorithm>
 #include <cmath>
 
+#ifndef SASQ_HEIGHT
+#define SASQ_HEIGHT 128
+#endif
 namespace sasq {
 
 constexpr int kFew = 64;                                 // rows of a kv head up to which a sequence is the rows kernel's
@@ -40,7 +43,7 @@ static Plan plan_of(const sasq_kv_cache* c, const sasq_kv_batch* b, int64_t q_he
     p.most_blocks = p.rows.splits * b->batch * c->heads;
     if (p.tiled) {
         // Many rows: runs only where the tiles would leave the chip half empty.
-        const int64_t height = rows <= 128 ? 128 : 256, about = std::max<int64_t>(1, b->tokens * group / height) * c->heads;
+        const int64_t height = SASQ_HEIGHT, about = std::max<int64_t>(1, b->tokens * group / height) * c->heads;
         p.tiles.tile_rows = (int)height;
         p.tiles.tiles = (int)((rows + height - 1) / height);
         cut(p.tiles, keys, 512 / about, 1024, INT64_C(1) << 30);
