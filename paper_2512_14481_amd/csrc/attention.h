@@ -52,6 +52,14 @@ __device__ __forceinline__ void load_to_lds(uint32_t lds_addr, const void* base,
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(lds_addr), "v"(lane_off), "s"(base) : "memory");
 }
 
+// The same, or nothing where `on` is 0 (all ones otherwise): no branch, which would part the products that the load stands among.  For code that
+// every lane of the wave runs.
+__device__ __forceinline__ void load_to_lds_if(int on, uint32_t lds_addr, const void* base, uint32_t lane_off)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, -1"
+                 :: "s"(lds_addr), "v"(lane_off), "s"(base), "s"(__builtin_amdgcn_readfirstlane(on)) : "memory");
+}
+
 // Four int8 codes as fp16, exactly: a byte c + 128 in the low half of 0x6400 is 1152 + c.
 __device__ __forceinline__ u32x2 codes_to_f16(uint32_t c)
 {

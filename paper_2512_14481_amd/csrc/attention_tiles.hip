@@ -1,7 +1,8 @@
 // Attention of many rows over the paged cache (chunks and prompts): bound by the matrix units and the exponentials beside them.
 //
-// A workgroup has one kv head of one sequence, up to 256 rows of it (32 for each of four or eight waves, the heads that share the kv head packed
-// into the rows) and one run of keys, which it takes in tiles of 64 through rings of four stages in LDS for K and for V.
+// A workgroup has one kv head of one sequence, 128 rows of it (32 for each of its four waves, the heads that share the kv head packed into the
+// rows) and one run of keys, which it takes in tiles of 64 through two stages in LDS for K and two for V.  Two workgroups share a CU: one's
+// waves have products for the matrix units while the other's wait.
 //
 // Both products are taken transposed (see attention_rows.hip) on 32x32x16: a lane keeps one row from the scores to the output.  The scores of
 // the next tile take the registers of this one's as these become probabilities, and what a product reads from LDS is
@@ -10,22 +11,20 @@
 
 namespace sasq {
 
-constexpr int kTileKeys = 64;
+constexpr int kTileKeys = 64, kTileWaves = 4;
 
-template <int D, bool I8, int W>
+template <int D, bool I8>
 struct TilesGeo : KvRow<D, I8> {
     using K = KvRow<D, I8>;
-    static constexpr int kTileRing = W == 4 ? 2 : 4;
     static constexpr int kTile = 4 * K::k16;     // bytes of a tile's keys, or of its values
-    static constexpr int kKeysAt = 0, kValuesAt = kTileRing * kTile, kPagesAt = 2 * kTileRing * kTile;
-    static constexpr int kFlagsAt = kPagesAt + W * 2 * 64 * 4;
+    static constexpr int kKeysAt = 0, kValuesAt = 2 * kTile, kFlagsAt = 4 * kTile;
     static constexpr int kLds = kFlagsAt + 64;
 };
 
-template <int DTQ, int D, bool I8, int W>
-__global__ __launch_bounds__(W * 64, 2) void attention_tiles_kernel(AttnArgs a, KvPages cache, KvSteps steps, AttnSplit split, int few, int first)
+template <int DTQ, int D, bool I8>
+__global__ __launch_bounds__(kTileWaves * 64, 2) void attention_tiles_kernel(AttnArgs a, KvPages cache, KvSteps steps, AttnSplit split, int few, int first)
 {
-    using G = TilesGeo<D, I8, W>;
+    using G = TilesGeo<D, I8>;
     constexpr int DT = I8 ? SASQ_F16 : DTQ;
     constexpr int R = 32, DS = D / 16, DO = D / 32, KB = kTileKeys / 32;   // steps of the first product, blocks of 32 channels, of 32 keys
     constexpr int L = G::kLoads;
@@ -39,7 +38,7 @@ __global__ __launch_bounds__(W * 64, 2) void attention_tiles_kernel(AttnArgs a, 
     const int b = rest % steps.batch; rest /= steps.batch;
     const int run = rest % split.splits, tile = split.tiles - 1 - rest / split.splits;
     const KvSeq seq = kv_seq(steps, b, cache.page_shift);
-    const int rows = seq.rows * a.group, row0 = tile * R * W;
+    const int rows = seq.rows * a.group, row0 = tile * R * kTileWaves;
     if (rows <= few || row0 >= rows) return;
     const int end = attn_end(seq, a.group, split, tile), runs = attn_runs(split, end);
     if (run >= runs) return;
@@ -63,7 +62,7 @@ __global__ __launch_bounds__(W * 64, 2) void attention_tiles_kernel(AttnArgs a, 
     // A page that is not there makes every tile of the run a masked one (a rare thing: no list of which).
     const int* const table = steps.table + (int64_t)b * steps.max_pages;
     bool hole = false;
-    for (int u = (from >> cache.page_shift) + (int)threadIdx.x; u <= (to - 1) >> cache.page_shift; u += W * 64)
+    for (int u = (from >> cache.page_shift) + (int)threadIdx.x; u <= (to - 1) >> cache.page_shift; u += kTileWaves * 64)
         hole |= u >= steps.max_pages || kv_page(cache, steps, b, u) < 0;
     const bool holes = __builtin_amdgcn_readfirstlane(__syncthreads_or(hole));
     auto there_is = [&](int i, int unit) -> bool {                         // keys 16 unit .. of tile i
@@ -74,34 +73,34 @@ __global__ __launch_bounds__(W * 64, 2) void attention_tiles_kernel(AttnArgs a, 
         return index < steps.max_pages && kv_page(cache, steps, b, index) >= 0;
     };
 
-    // Wave w brings unit w % 4 (16 keys) of every tile, of eight waves the first four of K and the others of V.  The pages of its next 64 tiles lie in a list of its own, the ones after them in another;
-    // loads return in order, so a list has long landed when its first entry is read.
-    const int unit = wave & 3;
-    const bool brings_k = W == 4 || wave < 4, brings_v = W == 4 || wave >= 4;
-    int* const list = reinterpret_cast<int*>(lds + G::kPagesAt) + wave * 128;
+    // Wave w brings unit w (16 keys) of every tile.  Where the unit of tile 64 n + t lies in either plane is lane t's to know.
+    const int unit = wave;
     const uint32_t lds_at = (uint32_t)(uintptr_t)(lds_ptr_t)lds;
-    const uint32_t list_at = lds_at + G::kPagesAt + wave * 512;
-    auto fetch_list = [&](int n) {                                         // of tiles 64 n and on
-        const int64_t key = (int64_t)from + kTileKeys * (64 * (int64_t)n + lane) + 16 * unit;
-        const int64_t index = min(key >> cache.page_shift, (int64_t)steps.max_pages - 1);
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" :: "s"(list_at + (n & 1) * 256), "v"((uint32_t)(4 * index)), "s"(table) : "memory");
-    };
     uint32_t off[L];
 #pragma unroll
     for (int j = 0; j < L; ++j) off[j] = G::source(j, lane, cache.token_stride);
-    auto page_of = [&](int i) -> int { return list[i & 127]; };
-    auto fetch = [&](int i, int page, const uint8_t* plane, int at) {       // the wave's unit of tile i, which lies on `page`
-        page = __builtin_amdgcn_readfirstlane(page);
-        const int place = (from + kTileKeys * i + 16 * unit) & ((1 << cache.page_shift) - 1);
-        const uint8_t* base = plane + (int64_t)hk * cache.head_stride + (page < 0 || page >= cache.pages ? 0 : page * cache.page_stride + place * cache.token_stride);
-        const uint32_t to_lds = lds_at + at + unit * G::k16;
-#pragma unroll
-        for (int j = 0; j < L; ++j) load_to_lds(to_lds + G::kBlock * j, base, off[j]);
+    int64_t lies;
+    auto look_up = [&](int n) {
+        const int64_t key = (int64_t)from + kTileKeys * (64 * (int64_t)n + lane) + 16 * unit;
+        const int page = kv_page(cache, steps, b, (int)min(key >> cache.page_shift, (int64_t)steps.max_pages - 1));
+        const int place = (int)key & ((1 << cache.page_shift) - 1);
+        lies = hk * cache.head_stride + (page < 0 ? 0 : page * cache.page_stride + place * cache.token_stride);
     };
-    auto fetch_keys = [&](int i, int page) { fetch(i, page, cache.k, G::kKeysAt + i % G::kTileRing * G::kTile); };
-    auto fetch_values = [&](int i, int page) { fetch(i, page, cache.v, G::kValuesAt + i % G::kTileRing * G::kTile); };
-    auto keys_at = [&](int i) -> const char* { return lds + G::kKeysAt + i % G::kTileRing * G::kTile; };
-    auto values_at = [&](int i) -> char* { return lds + G::kValuesAt + i % G::kTileRing * G::kTile; };
+    auto lies_at = [&](int i) -> int64_t {
+        const uint32_t lo = __builtin_amdgcn_readlane((int)lies, i & 63), hi = __builtin_amdgcn_readlane((int)(lies >> 32), i & 63);
+        return (int64_t)((uint64_t)hi << 32 | lo);
+    };
+    struct Source {                                                        // the wave's unit of a tile: where it comes from and where it goes, if it is asked for
+        const uint8_t* base;
+        uint32_t to;
+        int on;
+    };
+    auto source = [&](int i, int64_t at, const uint8_t* plane, int to) -> Source {
+        return {plane + at, lds_at + to + (i & 1) * G::kTile + unit * G::k16, i < tiles ? -1 : 0};
+    };
+    auto fetch = [&](const Source& f, int j) { load_to_lds_if(f.on, f.to + G::kBlock * j, f.base, off[j]); };
+    auto keys_at = [&](int i) -> const char* { return lds + G::kKeysAt + (i & 1) * G::kTile; };
+    auto values_at = [&](int i) -> char* { return lds + G::kValuesAt + (i & 1) * G::kTile; };
 
     f32x16 o[DO], s[KB];
     float m = kNoMax, l = 0.0f;                                            // maximum of the log2-scaled scores, sum
@@ -167,7 +166,7 @@ __global__ __launch_bounds__(W * 64, 2) void attention_tiles_kernel(AttnArgs a, 
             for (int j = 0; j < 16; ++j) top = fmaxf(top, s[k][j]);
         return __any(__builtin_fmaf(top, c, -m) > kLazy);
     };
-    auto raise = [&]() {                                                   // moves the maxima, and the sums with them
+    auto raise = [&]() {                                                   // moves the maximum, and the sums with it
         const float t = fmaxf(fmaxf(top, __shfl_xor(top, 32, kWave)) * c, m);
         const float keep = kept(m, t);
         m = t;
@@ -175,16 +174,18 @@ __global__ __launch_bounds__(W * 64, 2) void attention_tiles_kernel(AttnArgs a, 
 #pragma unroll
         for (int n = 0; n < DO; ++n) o[n] *= keep;
     };
-    auto probabilities = [&](int k) {                                      // of block k
+    auto probabilities = [&](int k) -> float {                             // of block k, and their sum
+        float sum[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             float e[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k][8 * h + j], c, -m));
-            l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+            sum[h] = ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
 #pragma unroll
             for (int j = 0; j < 4; ++j) p[2 * k + h][j] = Store16<DT>::pack(e[2 * j], e[2 * j + 1]);
         }
+        return sum[0] + sum[1];
     };
     auto read_values = [&](int i, int x, ValueFrags& w) {
         const char* at = values_at(i) + G::template value_lane<R>(lane);
@@ -231,14 +232,12 @@ __global__ __launch_bounds__(W * 64, 2) void attention_tiles_kernel(AttnArgs a, 
         __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (brings_v) {
 #pragma unroll
-            for (int j = 0; j < L; ++j) {
-                u32x4 w = own_values(i)[G::kBlock / 16 * j + lane];
+        for (int j = 0; j < L; ++j) {
+            u32x4 w = own_values(i)[G::kBlock / 16 * j + lane];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) w[e] = finite_of<DT>(w[e]);
-                own_values(i)[G::kBlock / 16 * j + lane] = w;
-            }
+            for (int e = 0; e < 4; ++e) w[e] = finite_of<DT>(w[e]);
+            own_values(i)[G::kBlock / 16 * j + lane] = w;
         }
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
@@ -246,23 +245,18 @@ __global__ __launch_bounds__(W * 64, 2) void attention_tiles_kernel(AttnArgs a, 
         asm volatile("" ::: "memory");
     };
 
-    constexpr int LEAD = G::kTileRing;                                     // tile i + LEAD's keys are requested at tile i, and i + LEAD - 1's values
-    constexpr bool AHEAD = LEAD == 4;
-    int ahead_k = 0, ahead_v = 0;                                          // their pages, read a tile before
-    auto enter = [&](int i) {                                              // the workgroup goes on to tile i
-        // LEAD 2: K(i+1) and V(i) have to be there, all that is under way.  LEAD 4: K(i+2) V(i+1), of four waves all but V(i+2) and K(i+3), of
-        // eight all but one of these.
-        if (AHEAD && i + 3 < tiles) wait_loads<L>();
-        else                        wait_loads<0>();
+    Source next_keys, next_values;                                         // of tiles i + 2 and i + 1, requested while tile i is worked on
+    int64_t next_at;                                                       // where tile i + 1's unit lies
+    auto enter = [&](int i) {                                              // the workgroup goes on to tile i: K(i+1) and V(i), all that is under way, have to be there
+        wait_loads<0>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (i + LEAD < tiles && ((i + LEAD) & 63) == 0) fetch_list((i + LEAD) / 64 + 1);
-        if (brings_k && i + LEAD < tiles) fetch_keys(i + LEAD, ahead_k);
-        if (brings_v && i + LEAD - 1 < tiles) fetch_values(i + LEAD - 1, ahead_v);
-        ahead_v = W == 4 ? ahead_k : page_of(i + LEAD);
-        ahead_k = page_of(i + LEAD + 1);
+        next_values = source(i + 1, next_at, cache.v, G::kValuesAt);
+        if (((i + 2) & 63) == 0) look_up((i + 2) / 64);
+        next_at = lies_at(i + 2);
+        next_keys = source(i + 2, next_at, cache.k, G::kKeysAt);
         if (!I8 && masked_group(i)) {
-            if (brings_v) look_for_specials(i);
+            look_for_specials(i);
             __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
@@ -270,69 +264,92 @@ __global__ __launch_bounds__(W * 64, 2) void attention_tiles_kernel(AttnArgs a, 
             if (__builtin_amdgcn_readfirstlane(f[0] | f[1] | f[2] | f[3])) take_specials_out(i);
         }
     };
-    KeyFrags kf;                                                           // the first group of the next tile; with a longer lead read ahead of the barrier
+    // Tile i.  The probabilities of its first block are there already.  After the last tile the scores are of whatever lies in LDS, and not
+    // used: one block of instructions without a branch lets the compiler keep the order written here.
+    constexpr int XG = KB * KG, PER = 2 * L / XG;                          // groups of the first product; loads requested with each
+    KeyFrags kf;
     auto work = [&](int i) {
-        if (!AHEAD) read_keys(i + 1, 0, kf);
-        if (!unmasked(i)) mask(i);
-        if (maxima()) raise();
-        probabilities(0);
-        // (After the last tile the scores are of whatever lies in the ring, and not used: one block of instructions without a branch lets
-        // the compiler keep the order below.)
         ValueFrags vf;
 #pragma unroll
-        for (int x = 0; x < KB * KG; ++x) {
+        for (int x = 0; x < XG; ++x) {
             KeyFrags next;
-            if (x + 1 < KB * KG) read_keys(i + 1, x + 1, next);
-            else                 read_values(i, 0, vf);
-            __builtin_amdgcn_sched_barrier(0);                             // the reads of the next products stand ahead of these
+            if (x + 1 < XG) read_keys(i + 1, x + 1, next);
+            else            read_values(i, 0, vf);
+#pragma unroll
+            for (int j = x * PER; j < (x + 1) * PER; ++j) fetch(j < L ? next_values : next_keys, j % L);
+            __builtin_amdgcn_sched_barrier(0);                             // what is read for the next products stands ahead of these
             scores(x, kf);
-            if (x == 0) probabilities(1);
-            if (x + 1 < KB * KG) {
+            if (x == 0) l += probabilities(1);
+            if (x + 1 < XG) {
 #pragma unroll
                 for (int t = 0; t < KF; ++t) kf[t] = next[t];
             }
             if (x >= KG - 1) __builtin_amdgcn_sched_barrier(0);
         }
+        // (Used here, so that the compiler does not put off their sums and roundings.)
+        asm volatile("" : "+v"(l), "+v"(p[2]), "+v"(p[3]));
+        if (i + 1 < wave_tiles && !unmasked(i + 1)) mask(i + 1);
+        bool above = false;
+        float sum0 = 0.0f;
 #pragma unroll
         for (int x = 0; x < VG; ++x) {
             ValueFrags next;
             if (x + 1 < VG) read_values(i, x + 1, next);
-            else if (AHEAD) read_keys(i + 2, 0, kf);
             __builtin_amdgcn_sched_barrier(0);
             add_values(x, vf);
-            __builtin_amdgcn_sched_barrier(0);
+            if (x == 0) above = maxima();
+            if (x == VG / 2) sum0 = probabilities(0);                      // with the maximum as it is: of the next tile, whose first block's have gone in
+            if (x < VG / 2 || x == VG - 1) __builtin_amdgcn_sched_barrier(0);
+            if (x + 1 < VG) {
 #pragma unroll
-            for (int n = 0; n < 4; ++n) vf[n] = next[n];
+                for (int n = 0; n < 4; ++n) vf[n] = next[n];
+            }
         }
+        asm volatile("" : "+v"(sum0), "+v"(p[0]), "+v"(p[1]));
+        if (i + 1 >= wave_tiles) return;
+        if (above) {
+            raise();
+            sum0 = probabilities(0);
+        }
+        l += sum0;
     };
 
     if (tiles > 0) {
-        fetch_list(0);
-        fetch_list(1);
+        look_up(0);
         wait_loads<0>();                                                   // Q too: the loop's waits count the rings' loads alone
-        for (int i = 0; i < LEAD && i < tiles; ++i) {
-            if (brings_k) fetch_keys(i, page_of(i));
-            if (brings_v && i < LEAD - 1) fetch_values(i, page_of(i));
-        }
-        ahead_k = page_of(LEAD);
-        ahead_v = page_of(LEAD - 1);
-        if (AHEAD && tiles > 3)       wait_loads<2 * L>();                 // K(0), K(1)
-        else if (!AHEAD && tiles > 1) wait_loads<2 * L>();                 // K(0)
-        else                          wait_loads<0>();
+        next_at = lies_at(1);
+        const Source k0 = source(0, lies_at(0), cache.k, G::kKeysAt), v0 = source(0, lies_at(0), cache.v, G::kValuesAt), k1 = source(1, next_at, cache.k, G::kKeysAt);
+#pragma unroll
+        for (int j = 0; j < L; ++j) fetch(k0, j);
+#pragma unroll
+        for (int j = 0; j < L; ++j) fetch(v0, j);
+#pragma unroll
+        for (int j = 0; j < L; ++j) fetch(k1, j);
+        if (tiles > 1) wait_loads<2 * L>();
+        else           wait_loads<L>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         if (wave_tiles > 0) {
 #pragma unroll
-            for (int x = 0; x < KB * KG; ++x) {
+            for (int x = 0; x < XG; ++x) {
                 read_keys(0, x, kf);
                 scores(x, kf);
             }
-            if (AHEAD) read_keys(1, 0, kf);
+            if (!unmasked(0)) mask(0);
+            if (maxima()) raise();
+            l = probabilities(0);
         }
         for (int i = 0; i < tiles; ++i) {
             enter(i);
-            if (i < wave_tiles) work(i);
+            if (i < wave_tiles) {
+                read_keys(i + 1, 0, kf);
+                work(i);
+            } else {
+#pragma unroll
+                for (int j = 0; j < L; ++j) { fetch(next_values, j); fetch(next_keys, j); }
+            }
         }
+        wait_loads<0>();
     }
 
     float sum = l;
@@ -365,15 +382,12 @@ __global__ __launch_bounds__(W * 64, 2) void attention_tiles_kernel(AttnArgs a, 
 
 int attention_tiles_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& split, int few, int dim, bool int8, sasq_dtype dt, hipStream_t st)
 {
-    auto go = [&](auto kernel, int threads) {
-        launch_in_parts((int64_t)split.splits * s.batch * split.tiles * c.heads, threads,
-                        [&](unsigned n, int first) { hipLaunchKernelGGL(kernel, dim3(n), dim3(threads), 0, st, a, c, s, split, few, first); });
+    auto go = [&](auto kernel) {
+        launch_in_parts((int64_t)split.splits * s.batch * split.tiles * c.heads, kTileWaves * 64,
+                        [&](unsigned n, int first) { hipLaunchKernelGGL(kernel, dim3(n), dim3(kTileWaves * 64), 0, st, a, c, s, split, few, first); });
     };
     auto with = [&](auto dtv, auto dimv, auto i8v) {
-        constexpr int DT = decltype(dtv)::value, D = decltype(dimv)::value;
-        constexpr bool I8 = decltype(i8v)::value;
-        if (split.tile_rows == 128) go(attention_tiles_kernel<DT, D, I8, 4>, 256);
-        else                        go(attention_tiles_kernel<DT, D, I8, 8>, 512);
+        go(attention_tiles_kernel<decltype(dtv)::value, decltype(dimv)::value, decltype(i8v)::value>);
     };
     auto by_format = [&](auto dtv, auto dimv) {
         if (int8) with(dtv, dimv, std::true_type{});
