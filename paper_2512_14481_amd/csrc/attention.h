@@ -24,19 +24,21 @@ struct AttnArgs {
 };
 
 // A kv head's rows of a sequence are its new tokens times the query heads that share it: row r is token r / group, head r % group of
-// the group.  They are worked on in tiles of `tile_rows`, each over `splits` runs of `chunk` keys (the last one open-ended).  A tile
-// of more than one run leaves fp32 partial results in the workspace, joined by a kernel of their own.
+// the group.  A sequence with up to kFewRows of them is worked on in one piece, another in tiles of kTileRows, each over `splits` runs of
+// `chunk` keys (the last one open-ended).  Where there is more than one run each leaves fp32 partial results in the workspace, joined
+// by a kernel of their own.  The two kinds of sequences have runs and places of their own: single tokens are split finely.
+constexpr int kFewRows = 16, kTileRows = 128;
 struct AttnSplit {
-    int tile_rows, tiles, chunk, splits;
+    int tile_rows, rows, chunk, splits;                   // rows: the most that a sequence has (kFewRows at most, or any number)
     float2* ml;                                           // running maximum (of log2-scaled scores) and sum
     float* o;                                             // unnormalized sums of values
 };
-// Places of the partial results of row r of a sequence (rows kernel), and of token t and a head (tiles kernel).
-__device__ __forceinline__ int64_t rows_slot(const AttnSplit& s, int batch, int heads, int run, int b, int hk, int r)
+// Places of the partial results of row r of a sequence of few rows, and of token t and a head of the others.
+__device__ __forceinline__ int64_t few_slot(const AttnSplit& s, int batch, int heads, int run, int b, int hk, int r)
 {
-    return (((int64_t)run * batch + b) * heads + hk) * ((int64_t)s.tiles * s.tile_rows) + r;
+    return (((int64_t)run * batch + b) * heads + hk) * s.rows + r;
 }
-__device__ __forceinline__ int64_t tiles_slot(int tokens, int q_heads, int run, int t, int head) { return ((int64_t)run * tokens + t) * q_heads + head; }
+__device__ __forceinline__ int64_t token_slot(int tokens, int q_heads, int run, int t, int head) { return ((int64_t)run * tokens + t) * q_heads + head; }
 // Keys that a tile's last row sees, and how many runs they make.
 __device__ __forceinline__ int attn_end(const KvSeq& seq, int group, const AttnSplit& s, int tile)
 {
@@ -46,13 +48,12 @@ __device__ __forceinline__ int attn_end(const KvSeq& seq, int group, const AttnS
 __device__ __forceinline__ int attn_runs(const AttnSplit& s, int end) { return min(s.splits, max(1, (end + s.chunk - 1) / s.chunk)); }
 
 // 16 bytes a lane straight from global memory to LDS: lane i's go to lds_addr + 16 i.  The compiler does not know of the write: the
-// callers order it with s_waitcnt vmcnt.
-__device__ __forceinline__ void load_to_lds(uint32_t lds_addr, const void* base, uint32_t lane_off)
+// callers order it with s_waitcnt vmcnt.  Non-temporal, for what is read once (48 sequences of 70B 109 us without, 100 with).
+__device__ __forceinline__ void load_to_lds_once(uint32_t lds_addr, const void* base, uint32_t lane_off)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(lds_addr), "v"(lane_off), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" :: "s"(lds_addr), "v"(lane_off), "s"(base) : "memory");
 }
-
-// The same, or nothing where `on` is 0 (all ones otherwise): no branch, which would part the products that the load stands among.  For code that
+// The same with the ordinary policy, or nothing where `on` is 0 (all ones otherwise): no branch, which would part the products that the load stands among.  For code that
 // every lane of the wave runs.
 __device__ __forceinline__ void load_to_lds_if(int on, uint32_t lds_addr, const void* base, uint32_t lane_off)
 {
@@ -250,9 +251,10 @@ __device__ __forceinline__ void load_q(const AttnArgs& a, const uint16_t* src, b
     }
 }
 
-// Sequences of at most `few` rows of a kv head are the rows kernel's, the others the tiles kernel's.
-int attention_rows_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& split, int few, int dim, bool int8, sasq_dtype dt, hipStream_t st);
-int attention_tiles_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& split, int few, int dim, bool int8, sasq_dtype dt, hipStream_t st);
-int attention_join_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& split, bool tiled, int few, int dim, sasq_dtype dt, hipStream_t st);
+// Calls whose sequences all have few rows are the rows kernel's, any others the tiles kernel's.
+int attention_rows_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& few, int dim, bool int8, sasq_dtype dt, hipStream_t st);
+int attention_tiles_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& few, const AttnSplit& many, int64_t many_blocks, int64_t few_blocks,
+                           int dim, bool int8, sasq_dtype dt, hipStream_t st);
+int attention_join_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& split, bool many, int dim, sasq_dtype dt, hipStream_t st);
 
 }  // namespace sasq

@@ -3,16 +3,17 @@
 
 namespace sasq {
 
-// A wave for each row, D / 64 channels a lane.  Of the rows kernel: row r of a sequence and kv head, of the places of all sequences; of the
-// tiles kernel: a token and a head.
-template <int DTQ, int D, bool TILED>
-__global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, KvPages cache, KvSteps steps, AttnSplit split, int few, int first)
+// D / 64 channels a lane.  Sequences of few rows, whose runs may be many: a workgroup for each row of each sequence and kv head, its four waves
+// take every fourth run.  The others: a wave for each token and head.
+template <int DTQ, int D, bool MANY>
+__global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, KvPages cache, KvSteps steps, AttnSplit split, int first)
 {
     constexpr int E = D / 64;
     const int lane = (int)threadIdx.x & 63;
-    const int64_t row = ((int64_t)blockIdx.x + first) * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int64_t row = MANY ? ((int64_t)blockIdx.x + first) * 4 + wave : (int64_t)blockIdx.x + first;
     int b, hk, r;
-    if constexpr (TILED) {
+    if constexpr (MANY) {
         const int t = (int)(row / a.q_heads), head = (int)(row % a.q_heads);
         if (t >= steps.tokens) return;
         int before = 0;
@@ -23,19 +24,17 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, KvPages
         hk = head / a.group;
         r = (t - kv_seq(steps, b, cache.page_shift).row0) * a.group + head % a.group;
     } else {
-        const int rows = split.tiles * split.tile_rows;
-        r = (int)(row % rows);
-        hk = (int)(row / rows % cache.heads);
-        if (row / rows / cache.heads >= steps.batch) return;
-        b = (int)(row / rows / cache.heads);
+        r = (int)(row % split.rows);
+        hk = (int)(row / split.rows % cache.heads);
+        b = (int)(row / split.rows / cache.heads);
     }
     const KvSeq seq = kv_seq(steps, b, cache.page_shift);
-    if (r < 0 || r >= seq.rows * a.group || r >= split.tiles * split.tile_rows || (seq.rows * a.group > few) != TILED) return;
+    if (r < 0 || r >= seq.rows * a.group || (seq.rows * a.group > kFewRows) != MANY) return;
     if (attn_runs(split, attn_end(seq, a.group, split, r / split.tile_rows)) == 1) return;      // written already
     const int token = r / a.group, t = seq.row0 + token, head = hk * a.group + r % a.group;
     const int sees = seq.keys - seq.rows + token;
     const int runs = sees < 0 ? 0 : min(split.splits, sees / split.chunk + 1);                    // later ones have no key of this row
-    auto slot = [&](int i) -> int64_t { return TILED ? tiles_slot(steps.tokens, a.q_heads, i, t, head) : rows_slot(split, steps.batch, cache.heads, i, b, hk, r); };
+    auto slot = [&](int i) -> int64_t { return MANY ? token_slot(steps.tokens, a.q_heads, i, t, head) : few_slot(split, steps.batch, cache.heads, i, b, hk, r); };
     float top = -INFINITY;
     for (int i = lane; i < runs; i += kWave) top = fmaxf(top, split.ml[slot(i)].x);
 #pragma unroll
@@ -43,14 +42,25 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, KvPages
     float sum = 0.0f, x[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] = 0.0f;
-#pragma unroll 4
-    for (int i = 0; i < runs; ++i) {
+#pragma unroll 8
+    for (int i = MANY ? 0 : wave; i < runs; i += MANY ? 1 : 4) {
         const int64_t at = slot(i);
         const float2 f = split.ml[at];
         const float weight = part_weight(f, top);
         sum += f.y * weight;
 #pragma unroll
         for (int e = 0; e < E; ++e) x[e] = __builtin_fmaf(split.o[at * D + lane * E + e], weight, x[e]);
+    }
+    if constexpr (!MANY) {
+        __shared__ float parts[4][D + 1];
+#pragma unroll
+        for (int e = 0; e < E; ++e) parts[wave][lane * E + e] = x[e];
+        if (lane == 0) parts[wave][D] = sum;
+        __syncthreads();
+        if (wave != 0) return;
+        sum = (parts[0][D] + parts[1][D]) + (parts[2][D] + parts[3][D]);
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = (parts[0][lane * E + e] + parts[1][lane * E + e]) + (parts[2][lane * E + e] + parts[3][lane * E + e]);
     }
     const bool none = sum == 0.0f;
     const float f = none ? 0.0f : (cache.v_scale ? cache.v_scale[hk] : 1.0f) / sum;
@@ -60,16 +70,16 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, KvPages
     if (a.lse && lane == 0) a.lse[(int64_t)t * a.q_heads + head] = none ? -INFINITY : (top + log2f(sum)) * 0.693147180559945f;
 }
 
-int attention_join_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& split, bool tiled, int few, int dim, sasq_dtype dt, hipStream_t st)
+int attention_join_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& split, bool many, int dim, sasq_dtype dt, hipStream_t st)
 {
-    const int64_t rows = tiled ? (int64_t)s.tokens * a.q_heads : (int64_t)s.batch * c.heads * split.tiles * split.tile_rows;
+    const int64_t rows = many ? (int64_t)s.tokens * a.q_heads : (int64_t)s.batch * c.heads * split.rows;
     auto go = [&](auto kernel) {
-        launch_in_parts((rows + 3) / 4, 256, [&](unsigned n, int first) { hipLaunchKernelGGL(kernel, dim3(n), dim3(256), 0, st, a, c, s, split, few, first); });
+        launch_in_parts(many ? (rows + 3) / 4 : rows, 256, [&](unsigned n, int first) { hipLaunchKernelGGL(kernel, dim3(n), dim3(256), 0, st, a, c, s, split, first); });
     };
     auto with = [&](auto dtv, auto dimv) {
         constexpr int DT = decltype(dtv)::value, D = decltype(dimv)::value;
-        if (tiled) go(attention_join_kernel<DT, D, true>);
-        else       go(attention_join_kernel<DT, D, false>);
+        if (many) go(attention_join_kernel<DT, D, true>);
+        else      go(attention_join_kernel<DT, D, false>);
     };
     auto by_dim = [&](auto dtv) {
         if (dim == 64) with(dtv, std::integral_constant<int, 64>{});

@@ -1,16 +1,16 @@
 // Attention of few rows over the paged cache (single tokens, drafts): bound by the bytes of the cache.
 //
-// A workgroup has one kv head of one sequence, up to 16 RB rows of it (RB blocks of 16), and one run of keys; its four waves take
-// slabs of 32 keys in turn, each with its own running maximum, sum and output, joined at the end.  A wave streams its slabs through a
-// ring of two stages of its own in LDS (direct global-to-LDS loads, no barrier in the loop): one stage is always in flight.
+// A workgroup has one kv head of one sequence, up to 16 rows of it (its new tokens times the query heads that share the kv head), and one run
+// of keys; its four waves take slabs of 32 keys in turn, each with its own running maximum, sum and output, joined at the end.  A wave
+// streams its slabs through a ring of two stages of its own in LDS (direct global-to-LDS loads, no barrier in the loop): while one slab is
+// worked on the other is under way, and each half of a stage is asked for again as soon as its last reader is done.
 //
 // Products are taken transposed, so that a lane keeps one row from the scores to the output:
 //   S^T[key, row] = K Q^T     16x16x32: lane (row = l % 16, g = l / 16) gets keys 4g..4g+3 of each 16
 //   O^T[d, row]  += V^T P^T   the eight keys of a lane's slots are then the ones it has scores of (4g + j of both halves of the slab):
 //                             the probabilities go into the second product as they come out of the first, and V is read
 //                             transposed by ds_read_tr with the same order of keys.
-// The running maximum is moved only when a score passes it by more than 8 (in powers of two): probabilities then reach 2^8 at most, and
-// the common slab needs no reduction over lanes and no rescaling.
+// Fifteen of sixteen rows of the matrix units' work are idle with one row; they still have it done long before the next slab is there.
 #include "attention.h"
 
 namespace sasq {
@@ -29,8 +29,8 @@ struct RowsGeo : KvRow<D, I8> {
     static constexpr int kLds = kBody + kRowWaves * 16 * 8 + kSegment / 16 * 4;
 };
 
-template <int DTQ, int D, bool I8, int RB>
-__global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnArgs a, KvPages cache, KvSteps steps, AttnSplit split, int few, int first)
+template <int DTQ, int D, bool I8>
+__global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnArgs a, KvPages cache, KvSteps steps, AttnSplit split, int first)
 {
     using G = RowsGeo<D, I8>;
     constexpr int DT = I8 ? SASQ_F16 : DTQ;               // of the products
@@ -41,29 +41,28 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
 
     int rest = (int)blockIdx.x + first;
     const int hk = rest % cache.heads; rest /= cache.heads;
-    const int tile = rest % split.tiles; rest /= split.tiles;
     const int b = rest % steps.batch, run = rest / steps.batch;
+    // The first segment's pages, asked for together with the lengths that say how many of them count.
+    const int from = run * split.chunk, unit = (int)threadIdx.x;
+    auto page_of_unit = [&](int seg) -> int {
+        const int index = (int)(((int64_t)seg + 16 * unit) >> cache.page_shift);
+        return unit < kSegment / 16 && index < steps.max_pages ? kv_page(cache, steps, b, index) : -1;
+    };
+    int listed = page_of_unit(from);
     const KvSeq seq = kv_seq(steps, b, cache.page_shift);
-    const int rows = seq.rows * a.group, row0 = tile * 16 * RB;
-    if (rows > few || row0 >= rows) return;
-    const int end = attn_end(seq, a.group, split, tile), runs = attn_runs(split, end);
+    const int rows = seq.rows * a.group;
+    if (rows == 0 || rows > kFewRows) return;
+    const int end = attn_end(seq, a.group, split, 0), runs = attn_runs(split, end);
     if (run >= runs) return;
-    const int from = run * split.chunk, to = run == runs - 1 ? end : min(end, from + split.chunk);
-    const int sees_first = seq.keys - seq.rows + row0 / a.group;           // last key of the tile's first row: masks begin after it
+    const int to = run == runs - 1 ? end : min(end, from + split.chunk);
+    const int past = seq.keys - seq.rows;                                  // the first row's last key: masks begin after it
 
-    // The lane's rows: their last key, and Q as the second operand (8 channels of row l16 for each step).
-    int sees[RB];
-    float c[RB];                                                           // from a score to a power of two
-    u32x4 q[RB][DS];
-    const float k_scale = I8 ? cache.k_scale[hk] : 1.0f;
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-        const int r = row0 + 16 * rb + l16;
-        const bool there = r < rows;
-        const int token = (there ? r : row0) / a.group, head = (there ? r : row0) % a.group;
-        sees[rb] = seq.keys - seq.rows + token;
-        load_q<DTQ, D, I8, 16>(a, a.q + (int64_t)(seq.row0 + token) * a.q_stride + (int64_t)(hk * a.group + head) * D, there, g, k_scale, q[rb], c[rb]);
-    }
+    const bool row_there = l16 < rows;
+    const int my_token = (row_there ? l16 : 0) / a.group, my_head = hk * a.group + (row_there ? l16 : 0) % a.group;
+    const int sees = past + my_token;
+    float c;
+    u32x4 q[DS];
+    load_q<DTQ, D, I8, 16>(a, a.q + (int64_t)(seq.row0 + my_token) * a.q_stride + (int64_t)my_head * D, row_there, g, I8 ? cache.k_scale[hk] : 1.0f, q, c);
 
     uint32_t off[G::kLoads];
 #pragma unroll
@@ -72,22 +71,18 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
     const uint32_t ring_at = (uint32_t)(uintptr_t)(lds_ptr_t)ring;
     int* const pages = reinterpret_cast<int*>(lds + G::kBody + kRowWaves * 16 * 8);
 
-    f32x4 o[RB][DO];
-    float m[RB], l[RB];                                                    // maximum of the log2-scaled scores, sum
+    f32x4 o[DO];
+    float m = kNoMax, l = 0.0f;                                            // maximum of the log2-scaled scores, sum
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-        m[rb] = kNoMax; l[rb] = 0.0f;
-#pragma unroll
-        for (int i = 0; i < DO; ++i) o[rb][i] = f32x4{0, 0, 0, 0};
-    }
+    for (int n = 0; n < DO; ++n) o[n] = f32x4{0, 0, 0, 0};
 
     for (int seg = from; seg < to; seg += kSegment) {
         const int seg_end = min(to, seg + kSegment);
-        if (seg != from) __syncthreads();
-        for (int u = (int)threadIdx.x; u < kSegment / 16 && seg + 16 * u < seg_end; u += kRowWaves * 64) {
-            const int index = (seg + 16 * u) >> cache.page_shift;
-            pages[u] = index < steps.max_pages ? kv_page(cache, steps, b, index) : -1;
+        if (seg != from) {
+            __syncthreads();
+            listed = page_of_unit(seg);
         }
+        if (unit < kSegment / 16) pages[unit] = listed;
         __syncthreads();
         const int units = (seg_end - seg + 15) / 16, slabs = (units + 1) / 2;
         const int mine = (slabs - wave + kRowWaves - 1) / kRowWaves;       // slabs wave, wave + 4, ...
@@ -103,7 +98,7 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
                 const int page = page_of(i, h), place = (k0 + 16 * h) & ((1 << cache.page_shift) - 1);
                 const uint8_t* base = plane + (int64_t)hk * cache.head_stride + (page < 0 ? 0 : page * cache.page_stride + place * cache.token_stride);
 #pragma unroll
-                for (int j = 0; j < G::kLoads; ++j) load_to_lds(at + (h * G::kLoads + j) * G::kBlock, base, off[j]);
+                for (int j = 0; j < G::kLoads; ++j) load_to_lds_once(at + (h * G::kLoads + j) * G::kBlock, base, off[j]);
             }
         };
         wait_loads<0>();                                                   // Q has landed: the loop's waits count the ring's loads alone
@@ -116,9 +111,7 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
             const int k0 = seg + kSlab * (wave + i * kRowWaves);
             if (i + 1 < mine) wait_loads<3 * NL>();
             else              wait_loads<NL>();
-            f32x4 s[RB][2];
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb) s[rb][0] = s[rb][1] = f32x4{0, 0, 0, 0};
+            f32x4 s[2] = {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}};
 #pragma unroll
             for (int t = 0; t < (I8 ? DS / 2 : DS); ++t)
 #pragma unroll
@@ -127,14 +120,11 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
                     if constexpr (I8) {
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            const u32x2 x = codes_to_f16(w[2 * e]), y = codes_to_f16(w[2 * e + 1]);
-                            const u32x4 k = {x[0], x[1], y[0], y[1]};
-#pragma unroll
-                            for (int rb = 0; rb < RB; ++rb) s[rb][h] = mfma16<DT>(k, q[rb][2 * t + e], s[rb][h]);
+                            const u32x2 lo = codes_to_f16(w[2 * e]), hi = codes_to_f16(w[2 * e + 1]);
+                            s[h] = mfma16<DT>(u32x4{lo[0], lo[1], hi[0], hi[1]}, q[2 * t + e], s[h]);
                         }
                     } else {
-#pragma unroll
-                        for (int rb = 0; rb < RB; ++rb) s[rb][h] = mfma16<DT>(w, q[rb][t], s[rb][h]);
+                        s[h] = mfma16<DT>(w, q[t], s[h]);
                     }
                 }
             const int page0 = page_of(i, 0), page1 = page_of(i, 1);
@@ -142,47 +132,31 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
             asm volatile("" ::: "memory");
             if (i + kRing < mine) fetch(i + kRing, cache.k, 0);
 
-            const bool masked = k0 + kSlab - 1 > sees_first || page0 < 0 || page1 < 0;
+            const bool masked = k0 + kSlab - 1 > past || page0 < 0 || page1 < 0;
             if (masked) {
 #pragma unroll
-                for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if (page0 < 0 || k0 + 4 * g + j > sees[rb]) s[rb][0][j] = -INFINITY;
-                        if (page1 < 0 || k0 + 16 + 4 * g + j > sees[rb]) s[rb][1][j] = -INFINITY;
-                    }
-            }
-            u32x4 p[RB];
-            float top[RB];
-            bool above = false;
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb) {
-                top[rb] = fmaxf(fmaxf(fmaxf(s[rb][0][0], s[rb][0][1]), fmaxf(s[rb][0][2], s[rb][0][3])),
-                                fmaxf(fmaxf(s[rb][1][0], s[rb][1][1]), fmaxf(s[rb][1][2], s[rb][1][3])));
-                above |= __builtin_fmaf(top[rb], c[rb], -m[rb]) > kLazy;
-            }
-            if (__any(above)) {
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb) {
-                    float t = fmaxf(top[rb], __shfl_xor(top[rb], 16, kWave));
-                    t = fmaxf(t, __shfl_xor(t, 32, kWave));
-                    t = fmaxf(t * c[rb], m[rb]);
-                    const float keep = kept(m[rb], t);
-                    m[rb] = t;
-                    l[rb] *= keep;
-#pragma unroll
-                    for (int i2 = 0; i2 < DO; ++i2) o[rb][i2] *= keep;
+                for (int j = 0; j < 4; ++j) {
+                    if (page0 < 0 || k0 + 4 * g + j > sees) s[0][j] = -INFINITY;
+                    if (page1 < 0 || k0 + 16 + 4 * g + j > sees) s[1][j] = -INFINITY;
                 }
             }
+            float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+            if (__any(__builtin_fmaf(top, c, -m) > kLazy)) {
+                top = fmaxf(top, __shfl_xor(top, 16, kWave));
+                top = fmaxf(top, __shfl_xor(top, 32, kWave));
+                const float now = fmaxf(top * c, m), keep = kept(m, now);
+                m = now;
+                l *= keep;
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb) {
-                float e[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][j >> 2][j & 3], c[rb], -m[rb]));
-                l[rb] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-#pragma unroll
-                for (int j = 0; j < 4; ++j) p[rb][j] = Store16<DT>::pack(e[2 * j], e[2 * j + 1]);
+                for (int n = 0; n < DO; ++n) o[n] *= keep;
             }
+            float e[8];
+            u32x4 p;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j >> 2][j & 3], c, -m));
+            l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) p[j] = Store16<DT>::pack(e[2 * j], e[2 * j + 1]);
 
             if (i + kRing < mine)    wait_loads<3 * NL>();
             else if (i + 1 < mine)   wait_loads<2 * NL>();
@@ -200,18 +174,15 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
 #pragma unroll
                         for (int j = 0; j < 4; ++j) special |= any_special<DT>(v[n][j]);
                     if (__any(special)) {
+                        u32x4 seen;
 #pragma unroll
-                        for (int rb = 0; rb < RB; ++rb) {
-                            u32x4 seen;
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                const int key = k0 + (j < 2 ? 0 : 16) + 4 * g + 2 * (j & 1);
-                                const bool there = (j < 2 ? page0 : page1) >= 0;
-                                seen[j] = (there && key <= sees[rb] ? kSeen : 0u) | (there && key + 1 <= sees[rb] ? kSeen << 16 : 0u);
-                            }
-#pragma unroll
-                            for (int n = 0; n < DO; ++n) o[rb][n] = add_specials<DT>(v[n], seen, o[rb][n]);
+                        for (int j = 0; j < 4; ++j) {
+                            const int key = k0 + (j < 2 ? 0 : 16) + 4 * g + 2 * (j & 1);
+                            const bool there = (j < 2 ? page0 : page1) >= 0;
+                            seen[j] = (there && key <= sees ? kSeen : 0u) | (there && key + 1 <= sees ? kSeen << 16 : 0u);
                         }
+#pragma unroll
+                        for (int n = 0; n < DO; ++n) o[n] = add_specials<DT>(v[n], seen, o[n]);
 #pragma unroll
                         for (int n = 0; n < DO; ++n)
 #pragma unroll
@@ -220,80 +191,67 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
                 }
             }
 #pragma unroll
-            for (int n = 0; n < DO; ++n)
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb) o[rb][n] = mfma16<DT>(v[n], p[rb], o[rb][n]);
+            for (int n = 0; n < DO; ++n) o[n] = mfma16<DT>(v[n], p, o[n]);
             __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
             asm volatile("" ::: "memory");
             if (i + kRing < mine) fetch(i + kRing, cache.v, 1);
         }
     }
 
-    // Join the waves, one block of 16 rows at a time: thread (row, eight channels or four).
+    // Join the waves: sixteen threads for a row.
     constexpr int E = D / 16;
     float* const part = reinterpret_cast<float*>(lds);                     // [wave][row][D + 4]
     float2* const ml = reinterpret_cast<float2*>(lds + G::kBody);          // [wave][row]
-    const float v_scale = I8 ? cache.v_scale[hk] : 1.0f;
+    __syncthreads();
+    l += __shfl_xor(l, 16, kWave);
+    l += __shfl_xor(l, 32, kWave);
+    if (g == 0) ml[wave * 16 + l16] = make_float2(m == kNoMax ? -INFINITY : m, l);
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-        __syncthreads();
-        l[rb] += __shfl_xor(l[rb], 16, kWave);
-        l[rb] += __shfl_xor(l[rb], 32, kWave);
-        if (g == 0) ml[wave * 16 + l16] = make_float2(m[rb] == kNoMax ? -INFINITY : m[rb], l[rb]);
+    for (int n = 0; n < DO; ++n) *reinterpret_cast<f32x4*>(part + (wave * 16 + l16) * (D + 4) + 16 * n + 4 * g) = o[n];
+    __syncthreads();
+    const int r = (int)threadIdx.x / 16, d = (int)threadIdx.x % 16 * E;
+    if (r >= rows) return;
+    float top = -INFINITY, sum = 0.0f, x[E];
 #pragma unroll
-        for (int n = 0; n < DO; ++n) *reinterpret_cast<f32x4*>(part + (wave * 16 + l16) * (D + 4) + 16 * n + 4 * g) = o[rb][n];
-        __syncthreads();
-        const int rr = (int)threadIdx.x >> 4, d = ((int)threadIdx.x & 15) * E, r = row0 + 16 * rb + rr;
-        float top = -INFINITY, sum = 0.0f, x[E];
+    for (int w = 0; w < kRowWaves; ++w) top = fmaxf(top, ml[w * 16 + r].x);
 #pragma unroll
-        for (int w = 0; w < kRowWaves; ++w) top = fmaxf(top, ml[w * 16 + rr].x);
+    for (int e = 0; e < E; ++e) x[e] = 0.0f;
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = 0.0f;
+    for (int w = 0; w < kRowWaves; ++w) {
+        const float2 f = ml[w * 16 + r];
+        const float weight = part_weight(f, top);
+        sum += f.y * weight;
 #pragma unroll
-        for (int w = 0; w < kRowWaves; ++w) {
-            const float2 f = ml[w * 16 + rr];
-            const float weight = part_weight(f, top);
-            sum += f.y * weight;
+        for (int e = 0; e < E; ++e) x[e] = __builtin_fmaf(part[(w * 16 + r) * (D + 4) + d + e], weight, x[e]);
+    }
+    const int token = r / a.group, head = hk * a.group + r % a.group;
+    if (runs == 1) {
+        const bool none = sum == 0.0f;
+        const float f = none ? 0.0f : (I8 ? cache.v_scale[hk] : 1.0f) / sum;
+        uint16_t* dst = a.out + (int64_t)(seq.row0 + token) * a.out_stride + (int64_t)head * D + d;
+        uint32_t w[E / 2];
 #pragma unroll
-            for (int e = 0; e < E; ++e) x[e] = __builtin_fmaf(part[(w * 16 + rr) * (D + 4) + d + e], weight, x[e]);
-        }
-        if (r >= rows) continue;
-        const int token = r / a.group, head = hk * a.group + r % a.group;
-        if (runs == 1) {
-            const bool none = sum == 0.0f;
-            const float f = none ? 0.0f : v_scale / sum;
-            uint16_t* dst = a.out + (int64_t)(seq.row0 + token) * a.out_stride + (int64_t)head * D + d;
-            uint32_t w[E / 2];
+        for (int e = 0; e < E / 2; ++e) w[e] = none ? 0u : Store16<DTQ>::pack(x[2 * e] * f, x[2 * e + 1] * f);
+        __builtin_memcpy(dst, w, sizeof(w));
+        if (a.lse && d == 0) a.lse[(int64_t)(seq.row0 + token) * a.q_heads + head] = none ? -INFINITY : (top + log2f(sum)) * 0.693147180559945f;
+    } else {
+        const int64_t slot = few_slot(split, steps.batch, cache.heads, run, b, hk, r);
+        float* dst = split.o + slot * D + d;
 #pragma unroll
-            for (int e = 0; e < E / 2; ++e) w[e] = none ? 0u : Store16<DTQ>::pack(x[2 * e] * f, x[2 * e + 1] * f);
-            __builtin_memcpy(dst, w, sizeof(w));
-            if (a.lse && d == 0) a.lse[(int64_t)(seq.row0 + token) * a.q_heads + head] = none ? -INFINITY : (top + log2f(sum)) * 0.693147180559945f;
-        } else {
-            const int64_t slot = rows_slot(split, steps.batch, cache.heads, run, b, hk, r);
-            float* dst = split.o + slot * D + d;
-#pragma unroll
-            for (int e = 0; e < E; e += 4) *reinterpret_cast<f32x4*>(dst + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
-            if (d == 0) split.ml[slot] = make_float2(top, sum);
-        }
+        for (int e = 0; e < E; e += 4) *reinterpret_cast<f32x4*>(dst + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
+        if (d == 0) split.ml[slot] = make_float2(top, sum);
     }
 }
 
-int attention_rows_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& split, int few, int dim, bool int8, sasq_dtype dt, hipStream_t st)
+int attention_rows_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& split, int dim, bool int8, sasq_dtype dt, hipStream_t st)
 {
     auto go = [&](auto kernel) {
-        launch_in_parts((int64_t)split.splits * s.batch * split.tiles * c.heads, 256,
-                        [&](unsigned n, int first) { hipLaunchKernelGGL(kernel, dim3(n), dim3(256), 0, st, a, c, s, split, few, first); });
-    };
-    auto with = [&](auto dtv, auto dimv, auto i8v) {
-        constexpr int DT = decltype(dtv)::value, D = decltype(dimv)::value;
-        constexpr bool I8 = decltype(i8v)::value;
-        if (split.tile_rows == 16)      go(attention_rows_kernel<DT, D, I8, 1>);
-        else if (split.tile_rows == 32) go(attention_rows_kernel<DT, D, I8, 2>);
-        else                            go(attention_rows_kernel<DT, D, I8, 4>);
+        launch_in_parts((int64_t)split.splits * s.batch * c.heads, kRowWaves * 64,
+                        [&](unsigned n, int first) { hipLaunchKernelGGL(kernel, dim3(n), dim3(kRowWaves * 64), 0, st, a, c, s, split, first); });
     };
     auto by_format = [&](auto dtv, auto dimv) {
-        if (int8) with(dtv, dimv, std::true_type{});
-        else      with(dtv, dimv, std::false_type{});
+        if (int8) go(attention_rows_kernel<decltype(dtv)::value, decltype(dimv)::value, true>);
+        else      go(attention_rows_kernel<decltype(dtv)::value, decltype(dimv)::value, false>);
     };
     auto by_dim = [&](auto dtv) {
         if (dim == 64) by_format(dtv, std::integral_constant<int, 64>{});

@@ -22,7 +22,7 @@ struct TilesGeo : KvRow<D, I8> {
 };
 
 template <int DTQ, int D, bool I8>
-__global__ __launch_bounds__(kTileWaves * 64, 2) void attention_tiles_kernel(AttnArgs a, KvPages cache, KvSteps steps, AttnSplit split, int few, int first)
+__global__ __launch_bounds__(kTileWaves * 64, 2) void attention_tiles_kernel(AttnArgs a, KvPages cache, KvSteps steps, AttnSplit few, AttnSplit many, int many_blocks, int first)
 {
     using G = TilesGeo<D, I8>;
     constexpr int DT = I8 ? SASQ_F16 : DTQ;
@@ -32,14 +32,52 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void attention_tiles_kernel(Att
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int l32 = lane & 31, g = lane >> 5;
 
-    // The tiles of a sequence's last rows see the most keys: they come first.
+    // First the tiles of sequences of many rows, the last rows (which see the most keys) first, then the sequences of few rows.
     int rest = (int)blockIdx.x + first;
+    const bool is_few = rest >= many_blocks;
+    if (is_few) rest -= many_blocks;
+    const AttnSplit split = is_few ? few : many;
     const int hk = rest % cache.heads; rest /= cache.heads;
-    const int b = rest % steps.batch; rest /= steps.batch;
-    const int run = rest % split.splits, tile = split.tiles - 1 - rest / split.splits;
+    int b, run, tile;
+    if (is_few) {
+        b = rest % steps.batch;
+        run = rest / steps.batch;
+        tile = 0;
+    } else {
+        run = rest % split.splits;
+        rest /= split.splits;
+        // Tile `rest` from the end: the wave adds up the tiles of 64 sequences at a time, from the last one on.
+        bool found = false;
+        for (int i = 0; i < steps.batch && !found; i += kWave) {
+            const int at = steps.batch - 1 - i - lane;
+            int n = 0;
+            if (at >= 0) {
+                const int of = kv_seq(steps, at, cache.page_shift).rows * a.group;
+                n = of > kFewRows ? (of + kTileRows - 1) / kTileRows : 0;
+            }
+            int sum = n;
+#pragma unroll
+            for (int d = 1; d < kWave; d <<= 1) {
+                const int below = __shfl_up(sum, d, kWave);
+                if (lane >= d) sum += below;
+            }
+            const uint64_t past_it = __ballot(rest < sum);
+            if (past_it) {
+                const int where = __ffsll((unsigned long long)past_it) - 1;
+                found = true;
+                b = steps.batch - 1 - i - where;
+                tile = __builtin_amdgcn_readlane(sum, where) - 1 - rest;
+            } else {
+                rest -= __builtin_amdgcn_readlane(sum, kWave - 1);
+            }
+        }
+        if (!found) return;
+        b = __builtin_amdgcn_readfirstlane(b);
+        tile = __builtin_amdgcn_readfirstlane(tile);
+    }
     const KvSeq seq = kv_seq(steps, b, cache.page_shift);
-    const int rows = seq.rows * a.group, row0 = tile * R * kTileWaves;
-    if (rows <= few || row0 >= rows) return;
+    const int rows = seq.rows * a.group, row0 = tile * kTileRows;
+    if (rows == 0 || (rows <= kFewRows) != is_few) return;
     const int end = attn_end(seq, a.group, split, tile), runs = attn_runs(split, end);
     if (run >= runs) return;
     const int from = run * split.chunk, to = run == runs - 1 ? end : min(end, from + split.chunk);
@@ -370,7 +408,7 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void attention_tiles_kernel(Att
             }
         if (a.lse && g == 0) a.lse[t * a.q_heads + head] = none ? -INFINITY : (top + log2f(sum)) * 0.693147180559945f;
     } else {
-        const int64_t slot = tiles_slot(steps.tokens, a.q_heads, run, (int)t, head);
+        const int64_t slot = is_few ? few_slot(split, steps.batch, cache.heads, run, b, hk, r) : token_slot(steps.tokens, a.q_heads, run, (int)t, head);
         float* dst = split.o + slot * D + 4 * g;
 #pragma unroll
         for (int n = 0; n < DO; ++n)
@@ -380,18 +418,17 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void attention_tiles_kernel(Att
     }
 }
 
-int attention_tiles_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& split, int few, int dim, bool int8, sasq_dtype dt, hipStream_t st)
+int attention_tiles_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& few, const AttnSplit& many, int64_t many_blocks, int64_t few_blocks,
+                           int dim, bool int8, sasq_dtype dt, hipStream_t st)
 {
     auto go = [&](auto kernel) {
-        launch_in_parts((int64_t)split.splits * s.batch * split.tiles * c.heads, kTileWaves * 64,
-                        [&](unsigned n, int first) { hipLaunchKernelGGL(kernel, dim3(n), dim3(kTileWaves * 64), 0, st, a, c, s, split, few, first); });
-    };
-    auto with = [&](auto dtv, auto dimv, auto i8v) {
-        go(attention_tiles_kernel<decltype(dtv)::value, decltype(dimv)::value, decltype(i8v)::value>);
+        launch_in_parts(many_blocks + few_blocks, kTileWaves * 64, [&](unsigned n, int first) {
+            hipLaunchKernelGGL(kernel, dim3(n), dim3(kTileWaves * 64), 0, st, a, c, s, few, many, (int)many_blocks, first);
+        });
     };
     auto by_format = [&](auto dtv, auto dimv) {
-        if (int8) with(dtv, dimv, std::true_type{});
-        else      with(dtv, dimv, std::false_type{});
+        if (int8) go(attention_tiles_kernel<decltype(dtv)::value, decltype(dimv)::value, true>);
+        else      go(attention_tiles_kernel<decltype(dtv)::value, decltype(dimv)::value, false>);
     };
     auto by_dim = [&](auto dtv) {
         if (dim == 64) by_format(dtv, std::integral_constant<int, 64>{});

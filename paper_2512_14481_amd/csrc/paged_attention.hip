@@ -4,17 +4,12 @@
 #include <algorithm>
 #include <cmath>
 
-#ifndef SASQ_HEIGHT
-#define SASQ_HEIGHT 128
-#endif
 namespace sasq {
 
-constexpr int kFew = 64;                                 // rows of a kv head up to which a sequence is the rows kernel's
-
 struct Plan {
-    AttnSplit rows, tiles;
-    bool tiled;                                           // some sequences may have more than kFew rows
-    int64_t rows_slots, tiles_slots, most_blocks;
+    AttnSplit few, many;
+    bool tiled;                                           // some sequences may have more than kFewRows rows
+    int64_t few_blocks, many_blocks, few_slots, many_slots;
 };
 
 // Runs of `keys` keys: `runs` of them where possible, of whole tiles, at least `least` keys each and, unless that takes more than 256 runs, at most `most`.
@@ -32,23 +27,23 @@ static Plan plan_of(const sasq_kv_cache* c, const sasq_kv_batch* b, int64_t q_he
     Plan p{};
     const int64_t group = q_heads / c->heads, rows = std::min(b->max_q, b->tokens) * group;
     const int64_t keys = std::min(b->max_kv, b->max_pages * c->page_size);
-    p.tiled = rows > kFew;
+    p.tiled = rows > kFewRows;
     // Few rows: enough workgroups to fill the chip a few times over, and runs short enough that sequences of very different lengths end
     // at about the same time.
-    const int64_t tile = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
-    p.rows.tile_rows = (int)tile;
-    p.rows.tiles = 1;
-    cut(p.rows, keys, (1024 + b->batch * c->heads - 1) / (b->batch * c->heads), 256, 2048);
-    p.rows_slots = p.rows.splits > 1 ? p.rows.splits * b->batch * c->heads * tile : 0;
-    p.most_blocks = p.rows.splits * b->batch * c->heads;
+    const int64_t heads = b->batch * c->heads;
+    p.few.tile_rows = kFewRows;
+    p.few.rows = (int)std::min<int64_t>(rows, kFewRows);
+    cut(p.few, keys, (1024 + heads - 1) / heads, 256, 2048);
+    p.few_blocks = group <= kFewRows ? p.few.splits * heads : 0;
+    p.few_slots = p.few.splits > 1 ? p.few_blocks * p.few.rows : 0;
     if (p.tiled) {
-        // Many rows: runs only where the tiles would leave the chip half empty.
-        const int64_t height = SASQ_HEIGHT, about = std::max<int64_t>(1, b->tokens * group / height) * c->heads;
-        p.tiles.tile_rows = (int)height;
-        p.tiles.tiles = (int)((rows + height - 1) / height);
-        cut(p.tiles, keys, 512 / about, 1024, INT64_C(1) << 30);
-        p.tiles_slots = p.tiles.splits > 1 ? p.tiles.splits * b->tokens * q_heads : 0;
-        p.most_blocks = std::max(p.most_blocks, p.tiles.splits * b->batch * p.tiles.tiles * c->heads);
+        // Many rows: runs only where the tiles (about so many: a sequence's last one may be part empty) would leave the chip half empty.
+        const int64_t full = b->tokens * group / kTileRows, other = std::min(b->batch, b->tokens);
+        p.many.tile_rows = kTileRows;
+        p.many.rows = (int)rows;
+        cut(p.many, keys, 512 / (std::max(full, other) * c->heads), 1024, INT64_C(1) << 30);
+        p.many_blocks = p.many.splits * (full + other) * c->heads;
+        p.many_slots = p.many.splits > 1 ? p.many.splits * b->tokens * q_heads : 0;
     }
     return p;
 }
@@ -61,7 +56,7 @@ extern "C" size_t sasq_paged_attention_workspace(const sasq_kv_cache* cache, con
 {
     if (kv_check(cache, batch, q_heads, SASQ_F16) != SASQ_OK) return 0;
     const Plan p = plan_of(cache, batch, q_heads);
-    return (size_t)(p.rows_slots + p.tiles_slots) * (sizeof(float2) + sizeof(float) * cache->dim);
+    return (size_t)(p.few_slots + p.many_slots) * (sizeof(float2) + sizeof(float) * cache->dim);
 }
 
 extern "C" int sasq_paged_attention(const void* q, void* out, float* lse, int64_t q_stride, int64_t out_stride, int64_t q_heads, float scale,
@@ -80,23 +75,21 @@ extern "C" int sasq_paged_attention(const void* q, void* out, float* lse, int64_
     if (need && !aligned16(workspace)) return SASQ_ERR_ALIGN;
 
     Plan plan = plan_of(cache, batch, q_heads);
-    if (plan.most_blocks >= INT64_C(1) << 31) return SASQ_ERR_SHAPE;
-    float* o = static_cast<float*>(workspace);                             // the sums of both, then the maxima
-    float2* ml = reinterpret_cast<float2*>(o + (plan.rows_slots + plan.tiles_slots) * dim);
-    plan.rows.o = o;
-    plan.rows.ml = ml;
-    plan.tiles.o = o + plan.rows_slots * dim;
-    plan.tiles.ml = ml + plan.rows_slots;
+    if (plan.few_blocks + plan.many_blocks >= INT64_C(1) << 31) return SASQ_ERR_SHAPE;
+    float* o = static_cast<float*>(workspace);                             // the sums of both kinds, then the maxima
+    float2* ml = reinterpret_cast<float2*>(o + (plan.few_slots + plan.many_slots) * dim);
+    plan.few.o = o;
+    plan.few.ml = ml;
+    plan.many.o = o + plan.few_slots * dim;
+    plan.many.ml = ml + plan.few_slots;
     const AttnArgs a{static_cast<const uint16_t*>(q), static_cast<uint16_t*>(out), lse, q_stride, out_stride, (int)q_heads, (int)(q_heads / cache->heads), scale};
     const KvPages pages = kv_pages(cache);
     const KvSteps steps = kv_steps(batch);
     const bool int8 = cache->fmt == SASQ_KV_INT8;
-    const int few = plan.tiled ? kFew : INT32_MAX;
     hipStream_t st = as_stream(stream);
-    int rc = SASQ_OK;
-    if (plan.tiled) rc = attention_tiles_launch(a, pages, steps, plan.tiles, few, (int)dim, int8, dt, st);
-    if (rc == SASQ_OK) rc = attention_rows_launch(a, pages, steps, plan.rows, few, (int)dim, int8, dt, st);
-    if (rc == SASQ_OK && plan.tiles_slots) rc = attention_join_launch(a, pages, steps, plan.tiles, true, few, (int)dim, dt, st);
-    if (rc == SASQ_OK && plan.rows_slots) rc = attention_join_launch(a, pages, steps, plan.rows, false, few, (int)dim, dt, st);
+    int rc = plan.tiled ? attention_tiles_launch(a, pages, steps, plan.few, plan.many, plan.many_blocks, plan.few_blocks, (int)dim, int8, dt, st)
+                        : attention_rows_launch(a, pages, steps, plan.few, (int)dim, int8, dt, st);
+    if (rc == SASQ_OK && plan.many_slots) rc = attention_join_launch(a, pages, steps, plan.many, true, (int)dim, dt, st);
+    if (rc == SASQ_OK && plan.few_slots) rc = attention_join_launch(a, pages, steps, plan.few, false, (int)dim, dt, st);
     return rc;
 }
