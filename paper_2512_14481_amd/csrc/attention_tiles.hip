@@ -84,7 +84,9 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void attention_tiles_kernel(Att
     const int tiles = (to - from + kTileKeys - 1) / kTileKeys;
     const int past = seq.keys - seq.rows;
     const int sees_group = past + row0 / a.group;                          // last key of the workgroup's first row, of the wave's, of the wave's last row
-    const int wave_row = row0 + R * wave;
+    // Which 32 rows a wave has goes round with the workgroups that share a CU (they come 256 apart): a wave without rows, or with fewer keys to
+    // see, and one that has them then share a SIMD (drafts of 40 rows: two of four waves have any).
+    const int wave_row = row0 + R * ((wave + ((int)blockIdx.x >> 8)) % kTileWaves);
     const int sees_wave = past + wave_row / a.group;
     const int wave_end = past + (min(rows, wave_row + R) - 1) / a.group + 1;
     const int wave_tiles = wave_row < rows ? min(tiles, max(0, (wave_end - from + kTileKeys - 1) / kTileKeys)) : 0;
@@ -98,11 +100,13 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void attention_tiles_kernel(Att
     load_q<DTQ, D, I8, R>(a, a.q + (int64_t)(seq.row0 + token) * a.q_stride + (int64_t)head * D, row_there, g, I8 ? cache.k_scale[hk] : 1.0f, q, c);
 
     // A page that is not there makes every tile of the run a masked one (a rare thing: no list of which).
-    const int* const table = steps.table + (int64_t)b * steps.max_pages;
-    bool hole = false;
-    for (int u = (from >> cache.page_shift) + (int)threadIdx.x; u <= (to - 1) >> cache.page_shift; u += kTileWaves * 64)
-        hole |= u >= steps.max_pages || kv_page(cache, steps, b, u) < 0;
-    const bool holes = __builtin_amdgcn_readfirstlane(__syncthreads_or(hole));
+    bool holes = false;
+    auto missing = [&]() -> bool {
+        bool any = false;
+        for (int u = (from >> cache.page_shift) + (int)threadIdx.x; u <= (to - 1) >> cache.page_shift; u += kTileWaves * 64)
+            any |= u >= steps.max_pages || kv_page(cache, steps, b, u) < 0;
+        return any;
+    };
     auto there_is = [&](int i, int unit) -> bool {                         // keys 16 unit .. of tile i
         const int key = from + kTileKeys * i + 16 * unit;
         if (key >= to) return false;
@@ -353,8 +357,8 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void attention_tiles_kernel(Att
     };
 
     if (tiles > 0) {
+        const bool any_missing = missing();                                // (asked for beside the places, seen to while the first tiles are under way)
         look_up(0);
-        wait_loads<0>();                                                   // Q too: the loop's waits count the rings' loads alone
         next_at = lies_at(1);
         const Source k0 = source(0, lies_at(0), cache.k, G::kKeysAt), v0 = source(0, lies_at(0), cache.v, G::kValuesAt), k1 = source(1, next_at, cache.k, G::kKeysAt);
 #pragma unroll
@@ -363,10 +367,8 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void attention_tiles_kernel(Att
         for (int j = 0; j < L; ++j) fetch(v0, j);
 #pragma unroll
         for (int j = 0; j < L; ++j) fetch(k1, j);
-        if (tiles > 1) wait_loads<2 * L>();
-        else           wait_loads<L>();
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
+        wait_loads<0>();                                                   // Q too: from here on what is waited for is the loop's own
+        holes = __builtin_amdgcn_readfirstlane(__syncthreads_or(any_missing));
         if (wave_tiles > 0) {
 #pragma unroll
             for (int x = 0; x < XG; ++x) {
