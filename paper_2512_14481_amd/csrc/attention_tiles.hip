@@ -84,9 +84,7 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void attention_tiles_kernel(Att
     const int tiles = (to - from + kTileKeys - 1) / kTileKeys;
     const int past = seq.keys - seq.rows;
     const int sees_group = past + row0 / a.group;                          // last key of the workgroup's first row, of the wave's, of the wave's last row
-    // Which 32 rows a wave has goes round with the workgroups that share a CU (they come 256 apart): a wave without rows, or with fewer keys to
-    // see, and one that has them then share a SIMD (drafts of 40 rows: two of four waves have any).
-    const int wave_row = row0 + R * ((wave + ((int)blockIdx.x >> 8)) % kTileWaves);
+    const int wave_row = row0 + R * wave;
     const int sees_wave = past + wave_row / a.group;
     const int wave_end = past + (min(rows, wave_row + R) - 1) / a.group + 1;
     const int wave_tiles = wave_row < rows ? min(tiles, max(0, (wave_end - from + kTileKeys - 1) / kTileKeys)) : 0;

@@ -28,20 +28,22 @@ static Plan plan_of(const sasq_kv_cache* c, const sasq_kv_batch* b, int64_t q_he
     const int64_t group = q_heads / c->heads, rows = std::min(b->max_q, b->tokens) * group;
     const int64_t keys = std::min(b->max_kv, b->max_pages * c->page_size);
     p.tiled = rows > kFewRows;
-    // Few rows: enough workgroups to fill the chip a few times over, and runs short enough that sequences of very different lengths end
-    // at about the same time.
+    // Few rows: about 1024 workgroups, four or two rounds of what the chip holds at a time (512: chunks beside single tokens 107 us against
+    // 99), of 512 keys at least (one run and no join for up to 512 keys: 9.2 us for 301 keys of 7B; with 256 two runs, 10.5), and of 2048 at most,
+    // so that sequences of very different lengths end at about the same time (48 of 70B with 200 to 8190 keys: 109 us, with 4096 116).
     const int64_t heads = b->batch * c->heads;
     p.few.tile_rows = kFewRows;
     p.few.rows = (int)std::min<int64_t>(rows, kFewRows);
-    cut(p.few, keys, (1024 + heads - 1) / heads, 256, 2048);
+    cut(p.few, keys, (1024 + heads - 1) / heads, 512, 2048);
     p.few_blocks = group <= kFewRows ? p.few.splits * heads : 0;
     p.few_slots = p.few.splits > 1 ? p.few_blocks * p.few.rows : 0;
     if (p.tiled) {
-        // Many rows: runs only where the tiles (about so many: a sequence's last one may be part empty) would leave the chip half empty.
+        // Many rows: runs only where the tiles (about so many: a sequence's last one may be part empty) would leave the chip half empty: about
+        // 768 workgroups, one and a half times what it holds at a time (five tokens for each of 16 of 70B: 43 us, with 512 54, with 1024 52).
         const int64_t full = b->tokens * group / kTileRows, other = std::min(b->batch, b->tokens);
         p.many.tile_rows = kTileRows;
         p.many.rows = (int)rows;
-        cut(p.many, keys, 512 / (std::max(full, other) * c->heads), 1024, INT64_C(1) << 30);
+        cut(p.many, keys, 768 / (std::max(full, other) * c->heads), 512, INT64_C(1) << 30);
         p.many_blocks = p.many.splits * (full + other) * c->heads;
         p.many_slots = p.many.splits > 1 ? p.many.splits * b->tokens * q_heads : 0;
     }
