@@ -53,12 +53,14 @@ __device__ __forceinline__ void load_to_lds_once(uint32_t lds_addr, const void* 
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" :: "s"(lds_addr), "v"(lane_off), "s"(base) : "memory");
 }
-// The same with the ordinary policy, or nothing where `on` is 0 (all ones otherwise): no branch, which would part the products that the load stands among.  For code that
-// every lane of the wave runs.
+// The same with the ordinary policy, or nothing where `on` is 0 (all ones otherwise): no branch, which would part the products that the
+// load stands among.
 __device__ __forceinline__ void load_to_lds_if(int on, uint32_t lds_addr, const void* base, uint32_t lane_off)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_mov_b32 exec_lo, %3\n\ts_mov_b32 exec_hi, %3\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, -1"
-                 :: "s"(lds_addr), "v"(lane_off), "s"(base), "s"(__builtin_amdgcn_readfirstlane(on)) : "memory");
+    uint64_t lanes;
+    asm volatile("s_mov_b32 m0, %1\n\ts_mov_b64 %0, exec\n\ts_and_b32 exec_lo, exec_lo, %4\n\ts_and_b32 exec_hi, exec_hi, %4\n\t"
+                 "global_load_lds_dwordx4 %2, %3\n\ts_mov_b64 exec, %0"
+                 : "=&s"(lanes) : "s"(lds_addr), "v"(lane_off), "s"(base), "s"(__builtin_amdgcn_readfirstlane(on)) : "memory", "scc");
 }
 
 // Four int8 codes as fp16, exactly: a byte c + 128 in the low half of 0x6400 is 1152 + c.
