@@ -257,6 +257,6 @@ __device__ __forceinline__ void load_q(const AttnArgs& a, const uint16_t* src, b
 int attention_rows_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& few, int dim, bool int8, sasq_dtype dt, hipStream_t st);
 int attention_tiles_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& few, const AttnSplit& many, int64_t many_blocks, int64_t few_blocks,
                            int dim, bool int8, sasq_dtype dt, hipStream_t st);
-int attention_join_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& split, bool many, int dim, sasq_dtype dt, hipStream_t st);
+int attention_join_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& few, const AttnSplit& many, bool join_few, bool join_many, int dim, sasq_dtype dt, hipStream_t st);
 
 }  // namespace sasq

@@ -3,17 +3,20 @@
 
 namespace sasq {
 
-// D / 64 channels a lane.  Sequences of few rows, whose runs may be many: a workgroup for each row of each sequence and kv head, its four waves
-// take every fourth run.  The others: a wave for each token and head.
-template <int DTQ, int D, bool MANY>
-__global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, KvPages cache, KvSteps steps, AttnSplit split, int first)
+// D / 64 channels a lane.  First the sequences of many rows, a wave for each token and head, where these have runs; then those of few, whose
+// runs may be many: a workgroup for each row of each sequence and kv head, its four waves take every fourth run.
+template <int DTQ, int D>
+__global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, KvPages cache, KvSteps steps, AttnSplit few, AttnSplit all_of_many, int many_blocks, int first)
 {
     constexpr int E = D / 64;
     const int lane = (int)threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int64_t row = MANY ? ((int64_t)blockIdx.x + first) * 4 + wave : (int64_t)blockIdx.x + first;
+    const int block = (int)blockIdx.x + first;
+    const bool many = block < many_blocks;
+    const AttnSplit split = many ? all_of_many : few;
     int b, hk, r;
-    if constexpr (MANY) {
+    if (many) {
+        const int64_t row = (int64_t)block * 4 + wave;
         const int t = (int)(row / a.q_heads), head = (int)(row % a.q_heads);
         if (t >= steps.tokens) return;
         int before = 0;
@@ -24,17 +27,18 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, KvPages
         hk = head / a.group;
         r = (t - kv_seq(steps, b, cache.page_shift).row0) * a.group + head % a.group;
     } else {
-        r = (int)(row % split.rows);
-        hk = (int)(row / split.rows % cache.heads);
-        b = (int)(row / split.rows / cache.heads);
+        const int row = block - many_blocks;
+        r = row % split.rows;
+        hk = row / split.rows % cache.heads;
+        b = row / split.rows / cache.heads;
     }
     const KvSeq seq = kv_seq(steps, b, cache.page_shift);
-    if (r < 0 || r >= seq.rows * a.group || (seq.rows * a.group > kFewRows) != MANY) return;
+    if (r < 0 || r >= seq.rows * a.group || (seq.rows * a.group > kFewRows) != many) return;
     if (attn_runs(split, attn_end(seq, a.group, split, r / split.tile_rows)) == 1) return;      // written already
     const int token = r / a.group, t = seq.row0 + token, head = hk * a.group + r % a.group;
     const int sees = seq.keys - seq.rows + token;
     const int runs = sees < 0 ? 0 : min(split.splits, sees / split.chunk + 1);                    // later ones have no key of this row
-    auto slot = [&](int i) -> int64_t { return MANY ? token_slot(steps.tokens, a.q_heads, i, t, head) : few_slot(split, steps.batch, cache.heads, i, b, hk, r); };
+    auto slot = [&](int i) -> int64_t { return many ? token_slot(steps.tokens, a.q_heads, i, t, head) : few_slot(split, steps.batch, cache.heads, i, b, hk, r); };
     float top = -INFINITY;
     for (int i = lane; i < runs; i += kWave) top = fmaxf(top, split.ml[slot(i)].x);
 #pragma unroll
@@ -43,7 +47,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, KvPages
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] = 0.0f;
 #pragma unroll 8
-    for (int i = MANY ? 0 : wave; i < runs; i += MANY ? 1 : 4) {
+    for (int i = many ? 0 : wave; i < runs; i += many ? 1 : 4) {
         const int64_t at = slot(i);
         const float2 f = split.ml[at];
         const float weight = part_weight(f, top);
@@ -51,7 +55,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, KvPages
 #pragma unroll
         for (int e = 0; e < E; ++e) x[e] = __builtin_fmaf(split.o[at * D + lane * E + e], weight, x[e]);
     }
-    if constexpr (!MANY) {
+    if (!many) {
         __shared__ float parts[4][D + 1];
 #pragma unroll
         for (int e = 0; e < E; ++e) parts[wave][lane * E + e] = x[e];
@@ -70,20 +74,17 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, KvPages
     if (a.lse && lane == 0) a.lse[(int64_t)t * a.q_heads + head] = none ? -INFINITY : (top + log2f(sum)) * 0.693147180559945f;
 }
 
-int attention_join_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& split, bool many, int dim, sasq_dtype dt, hipStream_t st)
+int attention_join_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& few, const AttnSplit& many, bool join_few, bool join_many, int dim,
+                          sasq_dtype dt, hipStream_t st)
 {
-    const int64_t rows = many ? (int64_t)s.tokens * a.q_heads : (int64_t)s.batch * c.heads * split.rows;
+    const int64_t many_blocks = join_many ? ((int64_t)s.tokens * a.q_heads + 3) / 4 : 0, few_blocks = join_few ? (int64_t)s.batch * c.heads * few.rows : 0;
     auto go = [&](auto kernel) {
-        launch_in_parts(many ? (rows + 3) / 4 : rows, 256, [&](unsigned n, int first) { hipLaunchKernelGGL(kernel, dim3(n), dim3(256), 0, st, a, c, s, split, first); });
-    };
-    auto with = [&](auto dtv, auto dimv) {
-        constexpr int DT = decltype(dtv)::value, D = decltype(dimv)::value;
-        if (many) go(attention_join_kernel<DT, D, true>);
-        else      go(attention_join_kernel<DT, D, false>);
+        launch_in_parts(many_blocks + few_blocks, 256,
+                        [&](unsigned n, int first) { hipLaunchKernelGGL(kernel, dim3(n), dim3(256), 0, st, a, c, s, few, many, (int)many_blocks, first); });
     };
     auto by_dim = [&](auto dtv) {
-        if (dim == 64) with(dtv, std::integral_constant<int, 64>{});
-        else           with(dtv, std::integral_constant<int, 128>{});
+        if (dim == 64) go(attention_join_kernel<decltype(dtv)::value, 64>);
+        else           go(attention_join_kernel<decltype(dtv)::value, 128>);
     };
     if (dt == SASQ_F16) by_dim(std::integral_constant<int, SASQ_F16>{});
     else                by_dim(std::integral_constant<int, SASQ_BF16>{});

@@ -77,7 +77,7 @@ extern "C" int sasq_paged_attention(const void* q, void* out, float* lse, int64_
     if (need && !aligned16(workspace)) return SASQ_ERR_ALIGN;
 
     Plan plan = plan_of(cache, batch, q_heads);
-    if (plan.few_blocks + plan.many_blocks >= INT64_C(1) << 31) return SASQ_ERR_SHAPE;
+    if (plan.few_blocks + plan.many_blocks >= INT64_C(1) << 31 || batch->batch * cache->heads * kFewRows >= INT64_C(1) << 30) return SASQ_ERR_SHAPE;
     float* o = static_cast<float*>(workspace);                             // the sums of both kinds, then the maxima
     float2* ml = reinterpret_cast<float2*>(o + (plan.few_slots + plan.many_slots) * dim);
     plan.few.o = o;
@@ -91,7 +91,7 @@ extern "C" int sasq_paged_attention(const void* q, void* out, float* lse, int64_
     hipStream_t st = as_stream(stream);
     int rc = plan.tiled ? attention_tiles_launch(a, pages, steps, plan.few, plan.many, plan.many_blocks, plan.few_blocks, (int)dim, int8, dt, st)
                         : attention_rows_launch(a, pages, steps, plan.few, (int)dim, int8, dt, st);
-    if (rc == SASQ_OK && plan.many_slots) rc = attention_join_launch(a, pages, steps, plan.many, true, (int)dim, dt, st);
-    if (rc == SASQ_OK && plan.few_slots) rc = attention_join_launch(a, pages, steps, plan.few, false, (int)dim, dt, st);
+    if (rc == SASQ_OK && plan.few_slots + plan.many_slots)
+        rc = attention_join_launch(a, pages, steps, plan.few, plan.many, plan.few_slots > 0, plan.many_slots > 0, (int)dim, dt, st);
     return rc;
 }
