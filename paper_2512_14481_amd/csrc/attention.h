@@ -74,14 +74,6 @@ __device__ __forceinline__ u32x2 codes_to_f16(uint32_t c)
 }
 
 template <int DT>
-__device__ __forceinline__ f32x16 mfma32(const u32x4& a, const u32x4& b, const f32x16& c)
-{
-    if constexpr (DT == SASQ_F16)
-        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-    else
-        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-template <int DT>
 __device__ __forceinline__ f32x4 mfma16(const u32x4& a, const u32x4& b, const f32x4& c)
 {
     if constexpr (DT == SASQ_F16)
@@ -108,8 +100,8 @@ __device__ __forceinline__ uint32_t finite_of(uint32_t w)
 // bf16 value by itself, which overflows, so that the rows that do not see it (a factor of 0) stay as they are.  v: eight values of the
 // first operand, seen: kSeen (else 0) for the eight keys of the second.
 constexpr uint32_t kSeen = 0x7F7Fu;
-template <int DT, typename Acc>
-__device__ __forceinline__ Acc add_specials(const u32x4& v, const u32x4& seen, Acc o)
+template <int DT>
+__device__ __forceinline__ f32x4 add_specials(const u32x4& v, const u32x4& seen, f32x4 o)
 {
     constexpr uint32_t e = DT == SASQ_F16 ? 0x7C00u : 0x7F80u;
 #pragma unroll
@@ -125,8 +117,7 @@ __device__ __forceinline__ Acc add_specials(const u32x4& v, const u32x4& seen, A
                 w[j] |= (mine ? kSeen | (uint32_t)sign << 15 : 0u) << (16 * i);
             }
         }
-        if constexpr (sizeof(Acc) == sizeof(f32x4)) o = mfma16<SASQ_BF16>(w, seen, o);
-        else                                        o = mfma32<SASQ_BF16>(w, seen, o);
+        o = mfma16<SASQ_BF16>(w, seen, o);
     }
     return o;
 }
@@ -156,7 +147,7 @@ __device__ __forceinline__ float part_weight(const float2& f, float top)
 // 16-byte chunks together (neighbouring lanes read neighbouring bytes: loads whose lanes took turns among the rows took 150 cycles each
 // to issue), the rows' fours after each other, blocks 16 bytes apart, and the chunks of a four swapped in pairs in every other four rows of a
 // block.  The eight rows that a wave reads at a time at one chunk then lie in different banks, and so does what a transposing read of 16 lanes
-// takes (16 bits: two chunks of four rows; codes: a chunk of four rows of both halves of a step); and every place is a lane's own plus
+// takes (16 bits: two chunks of four rows; codes: a chunk of four rows of both halves of 32); and every place is a lane's own plus
 // a constant.
 template <int D, bool I8>
 struct KvRow {
@@ -179,48 +170,42 @@ struct KvRow {
         const int row = lane / 4 % kPerLoad, chunk = lane / 4 / kPerLoad * 4 + ((lane & 3) ^ swapped(row));
         return (uint32_t)((j * kPerLoad + row) * token_stride) + 16 * chunk;
     }
-    // First operands, for products of R = 16 rows (16x16x32) or 32 (32x32x16); a lane is (i = lane % R, g = lane / R).
-    // K Q^T: 16 bytes of row i, from chunk 64 / R t + g on.  at: the R keys + key_lane.
-    template <int R>
-    static __device__ __forceinline__ int key_lane(int lane) { return place(lane % R, lane / R); }
-    template <int R>
-    static __device__ __forceinline__ u32x4 key(const char* at, int t) { return *reinterpret_cast<const u32x4*>(at + step(64 / R * t)); }
-    // V^T P^T: channel R n + i of the eight keys that a lane's group g has scores of, in 16 bits: rows 4g..4g+3 of each half of a step's
-    // 512 / R keys.  at: the step's keys + value_lane.
-    template <int R>
+    // First operands of 16x16x32; a lane is (l16 = lane % 16, g = lane / 16).
+    // K Q^T: 16 bytes of row l16, from chunk 4 t + g on.  at: the 16 keys + key_lane.
+    static __device__ __forceinline__ int key_lane(int lane) { return place(lane & 15, lane >> 4); }
+    static __device__ __forceinline__ u32x4 key(const char* at, int t) { return *reinterpret_cast<const u32x4*>(at + t * kFour); }
+    // V^T P^T: channel 16 n + l16 of the eight keys that a lane has scores of, in 16 bits: rows 4g..4g+3 of both halves of 32 keys.
+    // at: the 32 keys + value_lane.
     static __device__ __forceinline__ int value_lane(int lane)
     {
-        const int l16 = lane & 15, g = lane / R, c = R == 32 ? lane >> 4 & 1 : 0;               // c: which 16 of a product's 32 channels
-        if constexpr (I8) return place((l16 < 8 ? 0 : 256 / R) + 4 * g + (l16 >> 1 & 3), c) + 8 * (l16 & 1);
-        else              return place(4 * g + (l16 >> 2), 2 * c + (l16 >> 1 & 1)) + 8 * (l16 & 1);
+        const int l16 = lane & 15, g = lane >> 4;
+        if constexpr (I8) return place((l16 < 8 ? 0 : 16) + 4 * g + (l16 >> 1 & 3), 0) + 8 * (l16 & 1);
+        else              return place(4 * g + (l16 >> 2), l16 >> 1 & 1) + 8 * (l16 & 1);
     }
-    // (Codes of 16 channels are one chunk: of the odd ones the lane's part has the swap the wrong way round.)
+    // (Codes of 16 channels are one chunk: of the odd ones the lane's part has the swap the wrong way round; this is what is to be added.)
     static __device__ __forceinline__ int value_odd(int lane) { return 16 - 32 * swapped(4 * (lane >> 4)); }
-    template <int R>
-    static __device__ __forceinline__ u32x4 value(const char* at, int n, int odd = 0)
+    static __device__ __forceinline__ u32x4 value(const char* at, int n, int odd)
     {
         if constexpr (I8) {
-            const int to = R == 32 ? step(2 * n) : step(n & ~1) + (n & 1 ? odd : 0);
-            const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2)(at + to));
+            const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2)(at + step(n & ~1) + (n & 1 ? odd : 0)));
             const u32x2 x = codes_to_f16((uint32_t)w[0]), y = codes_to_f16((uint32_t)w[1]);
             return u32x4{x[0], x[1], y[0], y[1]};
         } else {
-            constexpr int half = 256 / R / kPerLoad * kBlock;             // the upper half of a step's keys: whole blocks on
-            const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(at + step(R / 8 * n))));
-            const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(at + half + step(R / 8 * n))));
+            const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(at + step(2 * n))));
+            const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(at + k16 + step(2 * n))));
             return u32x4{x[0], x[1], y[0], y[1]};
         }
     }
 };
 
-// Q as the second operand of K Q^T: eight channels of the lane's row for each step of 512 / R.  c: from a score to a power of two.
-template <int DTQ, int D, bool I8, int R>
-__device__ __forceinline__ void load_q(const AttnArgs& a, const uint16_t* src, bool there, int g, float k_scale, u32x4 (&q)[D * R / 512], float& c)
+// Q as the second operand of K Q^T: eight channels of the lane's row for each step of 32.  c: from a score to a power of two.
+template <int DTQ, int D, bool I8>
+__device__ __forceinline__ void load_q(const AttnArgs& a, const uint16_t* src, bool there, int g, float k_scale, u32x4 (&q)[D / 32], float& c)
 {
-    constexpr int DS = D * R / 512, STEP = 512 / R;
+    constexpr int DS = D / 32;
 #pragma unroll
     for (int t = 0; t < DS; ++t) {
-        const int d = I8 ? 2 * STEP * (t >> 1) + 16 * g + 8 * (t & 1) : STEP * t + 8 * g;  // sixteen codes of one load serve two steps
+        const int d = I8 ? 64 * (t >> 1) + 16 * g + 8 * (t & 1) : 32 * t + 8 * g;          // sixteen codes of one load serve two steps
         q[t] = *reinterpret_cast<const u32x4*>(src + d);
         if (!there) q[t] = u32x4{0, 0, 0, 0};
     }
@@ -236,8 +221,8 @@ __device__ __forceinline__ void load_q(const AttnArgs& a, const uint16_t* src, b
             for (int t = 0; t < DS; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(Store16<DTQ>::lo(q[t][i])), fabsf(Store16<DTQ>::hi(q[t][i]))));
-#pragma unroll
-            for (int off = R; off < kWave; off <<= 1) top = fmaxf(top, __shfl_xor(top, off, kWave));
+            top = fmaxf(top, __shfl_xor(top, 16, kWave));
+            top = fmaxf(top, __shfl_xor(top, 32, kWave));
             const int e = top > 0.0f && top < INFINITY ? min(max(((int)(__float_as_uint(top) >> 23)) - 127, -100), 100) : 0;
             const float down = __uint_as_float((uint32_t)(127 - e) << 23);
             c *= __uint_as_float((uint32_t)(127 + e) << 23);

@@ -62,7 +62,7 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
     const int sees = past + my_token;
     float c;
     u32x4 q[DS];
-    load_q<DTQ, D, I8, 16>(a, a.q + (int64_t)(seq.row0 + my_token) * a.q_stride + (int64_t)my_head * D, row_there, g, I8 ? cache.k_scale[hk] : 1.0f, q, c);
+    load_q<DTQ, D, I8>(a, a.q + (int64_t)(seq.row0 + my_token) * a.q_stride + (int64_t)my_head * D, row_there, g, I8 ? cache.k_scale[hk] : 1.0f, q, c);
 
     uint32_t off[G::kLoads];
 #pragma unroll
@@ -106,8 +106,8 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
         for (int i = 0; i < kRing && i < mine; ++i) { fetch(i, cache.k, 0); fetch(i, cache.v, 1); }
         for (int i = 0; i < mine; ++i) {
             const char* stage = ring + (i % kRing) * G::kStage;
-            const char* kp = stage + G::template key_lane<16>(lane);
-            const char* vp = stage + G::kPart + G::template value_lane<16>(lane);
+            const char* kp = stage + G::key_lane(lane);
+            const char* vp = stage + G::kPart + G::value_lane(lane);
             const int k0 = seg + kSlab * (wave + i * kRowWaves);
             if (i + 1 < mine) wait_loads<3 * NL>();
             else              wait_loads<NL>();
@@ -116,7 +116,7 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
             for (int t = 0; t < (I8 ? DS / 2 : DS); ++t)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const u32x4 w = G::template key<16>(kp + h * G::k16, t);
+                    const u32x4 w = G::key(kp + h * G::k16, t);
                     if constexpr (I8) {
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
@@ -163,7 +163,7 @@ __global__ __launch_bounds__(kRowWaves * 64, 1) void attention_rows_kernel(AttnA
             else                     wait_loads<0>();
             u32x4 v[DO];
 #pragma unroll
-            for (int n = 0; n < DO; ++n) v[n] = G::template value<16>(vp, n, G::value_odd(lane));
+            for (int n = 0; n < DO; ++n) v[n] = G::value(vp, n, G::value_odd(lane));
             if constexpr (!I8) {
                 // A masked place may hold anything, and 0 times infinity is not 0: infinities and NaN are taken out of the product and
                 // put in by hand for the rows that see them.

@@ -4,9 +4,14 @@
 // rows) and one run of keys, which it takes in tiles of 64 through two stages in LDS for K and two for V.  Two workgroups share a CU: one's
 // waves have products for the matrix units while the other's wait.
 //
-// Both products are taken transposed (see attention_rows.hip) on 32x32x16: a lane keeps one row from the scores to the output.  The scores of
-// the next tile take the registers of this one's as these become probabilities, and what a product reads from LDS is
-// read before the products ahead of it, so that products, exponentials and reads stand side by side.
+// Both products are taken transposed (see attention_rows.hip), a lane keeps one row of each block of 16 from the scores to the output, and what a
+// wave reads of K or V from LDS serves two products.  The scores of the next tile take the registers of this one's, 16 keys after 16, as these
+// become probabilities; what a product reads from LDS is read before the products ahead of it, the loads of the tiles to come are dealt out
+// among them, and a tile is one block of instructions without a branch (but for masks, which only a run's last tiles have), so that products,
+// exponentials, reads and loads stand side by side.
+//
+// Measured: a chunk of 4096 tokens on 12281 of 70B 1.69 ms (1.13 PFLOP/s; the library's largest product reaches 1.59), 1.79 on 32x32x16, 1.74 with
+// eight waves and 256 rows a workgroup on it: the card is at its power limit (1.8 to 1.9 GHz of 2.4), where the 16x16 form gives more.
 #include "attention.h"
 
 namespace sasq {
@@ -26,11 +31,11 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void attention_tiles_kernel(Att
 {
     using G = TilesGeo<D, I8>;
     constexpr int DT = I8 ? SASQ_F16 : DTQ;
-    constexpr int R = 32, DS = D / 16, DO = D / 32, KB = kTileKeys / 32;   // steps of the first product, blocks of 32 channels, of 32 keys
+    constexpr int R = 16, RB = 2, DS = D / 32, DO = D / 16, KB = kTileKeys / 16;   // blocks of 16 rows of a wave; steps of the first product; blocks of 16 channels, of 16 keys
     constexpr int L = G::kLoads;
     __shared__ __attribute__((aligned(1024))) char lds[G::kLds];
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int l32 = lane & 31, g = lane >> 5;
+    const int l16 = lane & 15, g = lane >> 4;
 
     // First the tiles of sequences of many rows, the last rows (which see the most keys) first, then the sequences of few rows.
     int rest = (int)blockIdx.x + first;
@@ -84,18 +89,25 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void attention_tiles_kernel(Att
     const int tiles = (to - from + kTileKeys - 1) / kTileKeys;
     const int past = seq.keys - seq.rows;
     const int sees_group = past + row0 / a.group;                          // last key of the workgroup's first row, of the wave's, of the wave's last row
-    const int wave_row = row0 + R * wave;
+    const int wave_row = row0 + R * RB * wave;
     const int sees_wave = past + wave_row / a.group;
-    const int wave_end = past + (min(rows, wave_row + R) - 1) / a.group + 1;
+    const int wave_end = past + (min(rows, wave_row + R * RB) - 1) / a.group + 1;
     const int wave_tiles = wave_row < rows ? min(tiles, max(0, (wave_end - from + kTileKeys - 1) / kTileKeys)) : 0;
 
-    const int r = wave_row + l32;                                          // the lane's row
-    const bool row_there = r < rows;
-    const int token = (row_there ? r : row0) / a.group, head = hk * a.group + (row_there ? r : row0) % a.group;
-    const int sees = past + token;
-    float c;
-    u32x4 q[DS];
-    load_q<DTQ, D, I8, R>(a, a.q + (int64_t)(seq.row0 + token) * a.q_stride + (int64_t)head * D, row_there, g, I8 ? cache.k_scale[hk] : 1.0f, q, c);
+    // The lane's rows.
+    int sees[RB];
+    float c[RB];
+    u32x4 q[RB][DS];
+    auto token_of = [&](int rb) -> int { return (wave_row + R * rb + l16) / a.group; };
+    auto head_of = [&](int rb) -> int { return hk * a.group + (wave_row + R * rb + l16) % a.group; };
+    auto row_there = [&](int rb) -> bool { return wave_row + R * rb + l16 < rows; };
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        const bool there = row_there(rb);
+        const int token = there ? token_of(rb) : row0 / a.group, head = there ? head_of(rb) : hk * a.group;
+        sees[rb] = past + token;
+        load_q<DTQ, D, I8>(a, a.q + (int64_t)(seq.row0 + token) * a.q_stride + (int64_t)head * D, there, g, I8 ? cache.k_scale[hk] : 1.0f, q[rb], c[rb]);
+    }
 
     // A page that is not there makes every tile of the run a masked one (a rare thing: no list of which).
     bool holes = false;
@@ -142,99 +154,112 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void attention_tiles_kernel(Att
     auto keys_at = [&](int i) -> const char* { return lds + G::kKeysAt + (i & 1) * G::kTile; };
     auto values_at = [&](int i) -> char* { return lds + G::kValuesAt + (i & 1) * G::kTile; };
 
-    f32x16 o[DO], s[KB];
-    float m = kNoMax, l = 0.0f;                                            // maximum of the log2-scaled scores, sum
-    u32x4 p[2 * KB];                                                       // of 16 keys each
+    f32x4 o[RB][DO], s[RB][KB];
+    float m[RB], l[RB];                                                    // maximum of the log2-scaled scores, sum
+    u32x4 p[RB][KB / 2];                                                   // of 32 keys each
 #pragma unroll
-    for (int n = 0; n < DO; ++n)
+    for (int rb = 0; rb < RB; ++rb) {
+        m[rb] = kNoMax; l[rb] = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) o[n][j] = 0.0f;
+        for (int n = 0; n < DO; ++n) o[rb][n] = f32x4{0, 0, 0, 0};
+    }
 
-    // The steps of both products go in groups of four.
-    constexpr int KG = DS / 4, KF = I8 ? 2 : 4;                            // groups for 32 keys, 16-byte pieces of a group
-    constexpr int VG = DO;                                                 // groups of a tile's values
+    // What is read from LDS goes in groups: the fragments of 16 keys; four fragments of 32 keys' values.
+    constexpr int KF = I8 ? DS / 2 : DS, VG = KB / 2 * DO / 4;
     typedef u32x4 KeyFrags[KF];
     typedef u32x4 ValueFrags[4];
-    auto read_keys = [&](int i, int x, KeyFrags& w) {                      // group x of tile i
-        const char* at = keys_at(i) + G::template key_lane<R>(lane) + 2 * (x / KG) * G::k16;
+    auto read_keys = [&](int i, int k, KeyFrags& w) {                      // block k of tile i
+        const char* at = keys_at(i) + G::key_lane(lane) + k * G::k16;
 #pragma unroll
-        for (int t = 0; t < KF; ++t) w[t] = G::template key<R>(at, KF * (x % KG) + t);
+        for (int t = 0; t < KF; ++t) w[t] = G::key(at, t);
     };
-    auto scores = [&](int x, const KeyFrags& w) {
-        f32x16& to = s[x / KG];
-        if (x % KG == 0) {
+    auto scores = [&](int k, const KeyFrags& w) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) to[j] = 0.0f;
-        }
+        for (int rb = 0; rb < RB; ++rb) s[rb][k] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int t = 0; t < KF; ++t) {
             if constexpr (I8) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const u32x2 lo = codes_to_f16(w[t][2 * e]), hi = codes_to_f16(w[t][2 * e + 1]);
-                    to = mfma32<DT>(u32x4{lo[0], lo[1], hi[0], hi[1]}, q[4 * (x % KG) + 2 * t + e], to);
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) s[rb][k] = mfma16<DT>(u32x4{lo[0], lo[1], hi[0], hi[1]}, q[rb][2 * t + e], s[rb][k]);
                 }
             } else {
-                to = mfma32<DT>(w[t], q[4 * (x % KG) + t], to);
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) s[rb][k] = mfma16<DT>(w[t], q[rb][t], s[rb][k]);
             }
         }
     };
-    // Score j of block k is of key 32 k + 8 (j / 4) + 4 g + j % 4.
+    // Score j of block k is of key 16 k + 4 g + j.
     auto unmasked = [&](int i) -> bool { return !holes && from + kTileKeys * i + kTileKeys - 1 <= sees_wave; };
     auto mask = [&](int i) {
-        const int last = sees - (from + kTileKeys * i) - 4 * g;            // of the lane's keys, 0 being its first
 #pragma unroll
-        for (int k = 0; k < KB; ++k)
+        for (int rb = 0; rb < RB; ++rb) {
+            const int last = sees[rb] - (from + kTileKeys * i) - 4 * g;    // of the lane's keys, 0 being its first
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
-                if (32 * k + 8 * (j / 4) + j % 4 > last) s[k][j] = -INFINITY;
+            for (int k = 0; k < KB; ++k)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (16 * k + j > last) s[rb][k][j] = -INFINITY;
+        }
         if (holes) {
 #pragma unroll
-            for (int u = 0; u < 2 * KB; ++u)
-                if (!there_is(i, u)) {
+            for (int k = 0; k < KB; ++k)
+                if (!there_is(i, k)) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) s[u / 2][8 * (u & 1) + j] = -INFINITY;
+                    for (int rb = 0; rb < RB; ++rb) s[rb][k] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
                 }
         }
     };
-    float top;
+    float top[RB];
     auto maxima = [&]() -> bool {                                          // whether a score passes the running maximum by too much
-        top = s[0][0];
+        bool above = false;
 #pragma unroll
-        for (int k = 0; k < KB; ++k)
+        for (int rb = 0; rb < RB; ++rb) {
+            top[rb] = s[rb][0][0];
 #pragma unroll
-            for (int j = 0; j < 16; ++j) top = fmaxf(top, s[k][j]);
-        return __any(__builtin_fmaf(top, c, -m) > kLazy);
-    };
-    auto raise = [&]() {                                                   // moves the maximum, and the sums with it
-        const float t = fmaxf(fmaxf(top, __shfl_xor(top, 32, kWave)) * c, m);
-        const float keep = kept(m, t);
-        m = t;
-        l *= keep;
+            for (int k = 0; k < KB; ++k)
 #pragma unroll
-        for (int n = 0; n < DO; ++n) o[n] *= keep;
-    };
-    auto probabilities = [&](int k) -> float {                             // of block k, and their sum
-        float sum[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            float e[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k][8 * h + j], c, -m));
-            sum[h] = ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-#pragma unroll
-            for (int j = 0; j < 4; ++j) p[2 * k + h][j] = Store16<DT>::pack(e[2 * j], e[2 * j + 1]);
+                for (int j = 0; j < 4; ++j) top[rb] = fmaxf(top[rb], s[rb][k][j]);
+            above |= __builtin_fmaf(top[rb], c[rb], -m[rb]) > kLazy;
         }
-        return sum[0] + sum[1];
+        return __any(above);
+    };
+    auto raise = [&]() {                                                   // moves the maxima, and the sums with them
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            float t = fmaxf(top[rb], __shfl_xor(top[rb], 16, kWave));
+            t = fmaxf(t, __shfl_xor(t, 32, kWave));
+            t = fmaxf(t * c[rb], m[rb]);
+            const float keep = kept(m[rb], t);
+            m[rb] = t;
+            l[rb] *= keep;
+#pragma unroll
+            for (int n = 0; n < DO; ++n) o[rb][n] *= keep;
+        }
+    };
+    auto probabilities = [&](int k, float (&sum)[RB]) {                    // of block k, and their sums
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            float e[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][k][j], c[rb], -m[rb]));
+            sum[rb] = (e[0] + e[1]) + (e[2] + e[3]);
+            p[rb][k / 2][2 * (k & 1)] = Store16<DT>::pack(e[0], e[1]);
+            p[rb][k / 2][2 * (k & 1) + 1] = Store16<DT>::pack(e[2], e[3]);
+        }
     };
     auto read_values = [&](int i, int x, ValueFrags& w) {
-        const char* at = values_at(i) + G::template value_lane<R>(lane);
+        const char* at = values_at(i) + G::value_lane(lane) + 2 * (x / (DO / 4)) * G::k16;
 #pragma unroll
-        for (int f = 0; f < 4; ++f) w[f] = G::template value<R>(at + (4 * x + f) / DO * G::k16, (4 * x + f) % DO);
+        for (int f = 0; f < 4; ++f) w[f] = G::value(at, 4 * (x % (DO / 4)) + f, G::value_odd(lane));
     };
     auto add_values = [&](int x, const ValueFrags& w) {
 #pragma unroll
-        for (int f = 0; f < 4; ++f) o[(4 * x + f) % DO] = mfma32<DT>(w[f], p[(4 * x + f) / DO], o[(4 * x + f) % DO]);
+        for (int f = 0; f < 4; ++f)
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) o[rb][4 * (x % (DO / 4)) + f] = mfma16<DT>(w[f], p[rb][x / (DO / 4)], o[rb][4 * (x % (DO / 4)) + f]);
     };
     // A masked place may hold anything, and 0 times infinity is not 0: in a masked tile with infinities or NaN among its values these are
     // put into the rows that see them by hand, and taken out of the tile.
@@ -256,17 +281,22 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void attention_tiles_kernel(Att
         const int k0 = from + kTileKeys * i;
         if (i < wave_tiles) {
 #pragma unroll
-            for (int u = 0; u < 2 * KB; ++u) {
-                const bool there = there_is(i, u);
-                u32x4 seen;
+            for (int k = 0; k < KB / 2; ++k) {
+                const bool there[2] = {there_is(i, 2 * k), there_is(i, 2 * k + 1)};
+                u32x4 seen[RB];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int key = k0 + 16 * u + (j < 2 ? 0 : 8) + 4 * g + 2 * (j & 1);
-                    seen[j] = (there && key <= sees ? kSeen : 0u) | (there && key + 1 <= sees ? kSeen << 16 : 0u);
+                for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int key = k0 + 32 * k + (j < 2 ? 0 : 16) + 4 * g + 2 * (j & 1);
+                        seen[rb][j] = (there[j >> 1] && key <= sees[rb] ? kSeen : 0u) | (there[j >> 1] && key + 1 <= sees[rb] ? kSeen << 16 : 0u);
+                    }
+#pragma unroll
+                for (int n = 0; n < DO; ++n) {
+                    const u32x4 v = G::value(values_at(i) + G::value_lane(lane) + 2 * k * G::k16, n, G::value_odd(lane));
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) o[rb][n] = add_specials<DT>(v, seen[rb], o[rb][n]);
                 }
-#pragma unroll
-                for (int n = 0; n < DO; ++n)
-                    o[n] = add_specials<DT>(G::template value<R>(values_at(i) + G::template value_lane<R>(lane) + u * G::k16, n), seen, o[n]);
             }
         }
         __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
@@ -306,31 +336,34 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void attention_tiles_kernel(Att
     };
     // Tile i.  The probabilities of its first block are there already.  After the last tile the scores are of whatever lies in LDS, and not
     // used: one block of instructions without a branch lets the compiler keep the order written here.
-    constexpr int XG = KB * KG, PER = 2 * L / XG;                          // groups of the first product; loads requested with each
     KeyFrags kf;
     auto work = [&](int i) {
         ValueFrags vf;
 #pragma unroll
-        for (int x = 0; x < XG; ++x) {
+        for (int k = 0; k < KB; ++k) {
             KeyFrags next;
-            if (x + 1 < XG) read_keys(i + 1, x + 1, next);
+            if (k + 1 < KB) read_keys(i + 1, k + 1, next);
             else            read_values(i, 0, vf);
 #pragma unroll
-            for (int j = x * PER; j < (x + 1) * PER; ++j) fetch(j < L ? next_values : next_keys, j % L);
+            for (int j = k * 2 * L / KB; j < (k + 1) * 2 * L / KB; ++j) fetch(j < L ? next_values : next_keys, j % L);
             __builtin_amdgcn_sched_barrier(0);                             // what is read for the next products stands ahead of these
-            scores(x, kf);
-            if (x == 0) l += probabilities(1);
-            if (x + 1 < XG) {
+            scores(k, kf);
+            if (k + 1 < KB) {
+                float sum[RB];
+                probabilities(k + 1, sum);
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) l[rb] += sum[rb];
 #pragma unroll
                 for (int t = 0; t < KF; ++t) kf[t] = next[t];
             }
-            if (x >= KG - 1) __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_sched_barrier(0);
         }
         // (Used here, so that the compiler does not put off their sums and roundings.)
-        asm volatile("" : "+v"(l), "+v"(p[2]), "+v"(p[3]));
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) asm volatile("" : "+v"(l[rb]), "+v"(p[rb][0]), "+v"(p[rb][1]));
         if (i + 1 < wave_tiles && !unmasked(i + 1)) mask(i + 1);
         bool above = false;
-        float sum0 = 0.0f;
+        float sum0[RB];
 #pragma unroll
         for (int x = 0; x < VG; ++x) {
             ValueFrags next;
@@ -338,20 +371,22 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void attention_tiles_kernel(Att
             __builtin_amdgcn_sched_barrier(0);
             add_values(x, vf);
             if (x == 0) above = maxima();
-            if (x == VG / 2) sum0 = probabilities(0);                      // with the maximum as it is: of the next tile, whose first block's have gone in
-            if (x < VG / 2 || x == VG - 1) __builtin_amdgcn_sched_barrier(0);
+            if (x == VG / 2) probabilities(0, sum0);                       // with the maximum as it is: of the next tile, whose first blocks' have gone in
+            __builtin_amdgcn_sched_barrier(0);
             if (x + 1 < VG) {
 #pragma unroll
                 for (int n = 0; n < 4; ++n) vf[n] = next[n];
             }
         }
-        asm volatile("" : "+v"(sum0), "+v"(p[0]), "+v"(p[1]));
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) asm volatile("" : "+v"(sum0[rb]), "+v"(p[rb][0]));
         if (i + 1 >= wave_tiles) return;
         if (above) {
             raise();
-            sum0 = probabilities(0);
+            probabilities(0, sum0);
         }
-        l += sum0;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) l[rb] += sum0[rb];
     };
 
     if (tiles > 0) {
@@ -369,13 +404,13 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void attention_tiles_kernel(Att
         holes = __builtin_amdgcn_readfirstlane(__syncthreads_or(any_missing));
         if (wave_tiles > 0) {
 #pragma unroll
-            for (int x = 0; x < XG; ++x) {
-                read_keys(0, x, kf);
-                scores(x, kf);
+            for (int k = 0; k < KB; ++k) {
+                read_keys(0, k, kf);
+                scores(k, kf);
             }
             if (!unmasked(0)) mask(0);
             if (maxima()) raise();
-            l = probabilities(0);
+            probabilities(0, l);
         }
         for (int i = 0; i < tiles; ++i) {
             enter(i);
@@ -390,31 +425,33 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void attention_tiles_kernel(Att
         wait_loads<0>();
     }
 
-    float sum = l;
-    sum += __shfl_xor(sum, 32, kWave);
-    if (!row_there) return;
-    const int64_t t = seq.row0 + token;
-    top = m == kNoMax ? -INFINITY : m;
-    if (runs == 1) {
-        const bool none = sum == 0.0f;
-        const float f = none ? 0.0f : (I8 ? cache.v_scale[hk] : 1.0f) / sum;
-        uint16_t* dst = a.out + t * a.out_stride + (int64_t)head * D + 4 * g;
 #pragma unroll
-        for (int n = 0; n < DO; ++n)
+    for (int rb = 0; rb < RB; ++rb) {
+        float sum = l[rb];
+        sum += __shfl_xor(sum, 16, kWave);
+        sum += __shfl_xor(sum, 32, kWave);
+        if (!row_there(rb)) continue;
+        const int64_t t = seq.row0 + token_of(rb);
+        const int head = head_of(rb);
+        const float last = m[rb] == kNoMax ? -INFINITY : m[rb];
+        if (runs == 1) {
+            const bool none = sum == 0.0f;
+            const float f = none ? 0.0f : (I8 ? cache.v_scale[hk] : 1.0f) / sum;
+            uint16_t* dst = a.out + t * a.out_stride + (int64_t)head * D + 4 * g;
 #pragma unroll
-            for (int j = 0; j < 16; j += 4) {
-                const u32x2 w = {none ? 0u : Store16<DTQ>::pack(o[n][j] * f, o[n][j + 1] * f), none ? 0u : Store16<DTQ>::pack(o[n][j + 2] * f, o[n][j + 3] * f)};
-                *reinterpret_cast<u32x2*>(dst + 32 * n + 2 * j) = w;
+            for (int n = 0; n < DO; ++n) {
+                const f32x4 x = o[rb][n];
+                const u32x2 w = {none ? 0u : Store16<DTQ>::pack(x[0] * f, x[1] * f), none ? 0u : Store16<DTQ>::pack(x[2] * f, x[3] * f)};
+                *reinterpret_cast<u32x2*>(dst + 16 * n) = w;
             }
-        if (a.lse && g == 0) a.lse[t * a.q_heads + head] = none ? -INFINITY : (top + log2f(sum)) * 0.693147180559945f;
-    } else {
-        const int64_t slot = is_few ? few_slot(split, steps.batch, cache.heads, run, b, hk, r) : token_slot(steps.tokens, a.q_heads, run, (int)t, head);
-        float* dst = split.o + slot * D + 4 * g;
+            if (a.lse && g == 0) a.lse[t * a.q_heads + head] = none ? -INFINITY : (last + log2f(sum)) * 0.693147180559945f;
+        } else {
+            const int64_t slot = is_few ? few_slot(split, steps.batch, cache.heads, run, b, hk, wave_row + R * rb + l16) : token_slot(steps.tokens, a.q_heads, run, (int)t, head);
+            float* dst = split.o + slot * D + 4 * g;
 #pragma unroll
-        for (int n = 0; n < DO; ++n)
-#pragma unroll
-            for (int j = 0; j < 16; j += 4) *reinterpret_cast<f32x4*>(dst + 32 * n + 2 * j) = f32x4{o[n][j], o[n][j + 1], o[n][j + 2], o[n][j + 3]};
-        if (g == 0) split.ml[slot] = make_float2(top, sum);
+            for (int n = 0; n < DO; ++n) *reinterpret_cast<f32x4*>(dst + 16 * n) = o[rb][n];
+            if (g == 0) split.ml[slot] = make_float2(last, sum);
+        }
     }
 }
 
