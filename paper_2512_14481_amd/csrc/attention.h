@@ -24,9 +24,10 @@ struct AttnArgs {
 };
 
 // A kv head's rows of a sequence are its new tokens times the query heads that share it: row r is token r / group, head r % group of
-// the group.  A sequence with up to kFewRows of them is worked on in one piece, another in tiles of kTileRows, each over `splits` runs of
-// `chunk` keys (the last one open-ended).  Where there is more than one run each leaves fp32 partial results in the workspace, joined
-// by a kernel of their own.  The two kinds of sequences have runs and places of their own: single tokens are split finely.
+// the group.  A sequence with up to kFewRows of them is worked on in one piece, another in tiles of kTileRows (of half as many where no
+// sequence has more), each over `splits` runs of `chunk` keys (the last one open-ended).  Where there is more than one run each leaves fp32
+// partial results in the workspace, joined by a kernel of their own.  The two kinds of sequences have runs and places of their own: single
+// tokens are split finely.
 constexpr int kFewRows = 16, kTileRows = 128;
 struct AttnSplit {
     int tile_rows, rows, chunk, splits;                   // rows: the most that a sequence has (kFewRows at most, or any number)

@@ -1,11 +1,13 @@
 // Attention of many rows over the paged cache (chunks and prompts): bound by the matrix units and the exponentials beside them.
 //
-// A workgroup has one kv head of one sequence, 128 rows of it (32 for each of its four waves, the heads that share the kv head packed into the
-// rows) and one run of keys, which it takes in tiles of 64 through two stages in LDS for K and two for V.  Two workgroups share a CU: one's
-// waves have products for the matrix units while the other's wait.
+// A workgroup has one kv head of one sequence, 128 rows of it (RB = 2 blocks of 16 for each of its four waves, the heads that share the kv head
+// packed into the rows) and one run of keys, which it takes in tiles of 64 through two stages in LDS for K and two for V.  Two workgroups
+// share a CU: one's waves have products for the matrix units while the other's wait.  Where no sequence of the call has more than 64 rows
+// (drafts, short prompts) a tile has 64 and a wave one block: five tokens for each of 16 of 70B on 500 to 4000 keys in int8 37 us, with
+// 128 rows, of which two waves have none, 44; one prompt of 40 tokens on 300 of 7B 11.4 and 14.3.
 //
 // Both products are taken transposed (see attention_rows.hip), a lane keeps one row of each block of 16 from the scores to the output, and what a
-// wave reads of K or V from LDS serves two products.  The scores of the next tile take the registers of this one's, 16 keys after 16, as these
+// wave reads of K or V from LDS serves RB products.  The scores of the next tile take the registers of this one's, 16 keys after 16, as these
 // become probabilities; what a product reads from LDS is read before the products ahead of it, the loads of the tiles to come are dealt out
 // among them, and a tile is one block of instructions without a branch (but for masks, which only a run's last tiles have), so that products,
 // exponentials, reads and loads stand side by side.
@@ -26,12 +28,12 @@ struct TilesGeo : KvRow<D, I8> {
     static constexpr int kLds = kFlagsAt + 64;
 };
 
-template <int DTQ, int D, bool I8>
-__global__ __launch_bounds__(kTileWaves * 64, 2) void attention_tiles_kernel(AttnArgs a, KvPages cache, KvSteps steps, AttnSplit few, AttnSplit many, int many_blocks, int first)
+template <int DTQ, int D, bool I8, int RB>
+__global__ __launch_bounds__(kTileWaves * 64, RB == 1 && I8 ? 3 : 2) void attention_tiles_kernel(AttnArgs a, KvPages cache, KvSteps steps, AttnSplit few, AttnSplit many, int many_blocks, int first)
 {
     using G = TilesGeo<D, I8>;
     constexpr int DT = I8 ? SASQ_F16 : DTQ;
-    constexpr int R = 16, RB = 2, DS = D / 32, DO = D / 16, KB = kTileKeys / 16;   // blocks of 16 rows of a wave; steps of the first product; blocks of 16 channels, of 16 keys
+    constexpr int R = 16, Rows = R * RB * kTileWaves, DS = D / 32, DO = D / 16, KB = kTileKeys / 16;   // blocks of 16 rows of a wave; steps of the first product; blocks of 16 channels, of 16 keys
     constexpr int L = G::kLoads;
     __shared__ __attribute__((aligned(1024))) char lds[G::kLds];
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -58,7 +60,7 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void attention_tiles_kernel(Att
             int n = 0;
             if (at >= 0) {
                 const int of = kv_seq(steps, at, cache.page_shift).rows * a.group;
-                n = of > kFewRows ? (of + kTileRows - 1) / kTileRows : 0;
+                n = of > kFewRows ? (of + Rows - 1) / Rows : 0;
             }
             int sum = n;
 #pragma unroll
@@ -81,7 +83,7 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void attention_tiles_kernel(Att
         tile = __builtin_amdgcn_readfirstlane(tile);
     }
     const KvSeq seq = kv_seq(steps, b, cache.page_shift);
-    const int rows = seq.rows * a.group, row0 = tile * kTileRows;
+    const int rows = seq.rows * a.group, row0 = tile * Rows;
     if (rows == 0 || (rows <= kFewRows) != is_few) return;
     const int end = attn_end(seq, a.group, split, tile), runs = attn_runs(split, end);
     if (run >= runs) return;
@@ -464,8 +466,10 @@ int attention_tiles_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s
         });
     };
     auto by_format = [&](auto dtv, auto dimv) {
-        if (int8) go(attention_tiles_kernel<decltype(dtv)::value, decltype(dimv)::value, true>);
-        else      go(attention_tiles_kernel<decltype(dtv)::value, decltype(dimv)::value, false>);
+        constexpr int DTQ = decltype(dtv)::value, D = decltype(dimv)::value;
+        const bool half = many.tile_rows == kTileRows / 2;
+        if (int8) half ? go(attention_tiles_kernel<DTQ, D, true, 1>) : go(attention_tiles_kernel<DTQ, D, true, 2>);
+        else      half ? go(attention_tiles_kernel<DTQ, D, false, 1>) : go(attention_tiles_kernel<DTQ, D, false, 2>);
     };
     auto by_dim = [&](auto dtv) {
         if (dim == 64) by_format(dtv, std::integral_constant<int, 64>{});

@@ -39,9 +39,10 @@ static Plan plan_of(const sasq_kv_cache* c, const sasq_kv_batch* b, int64_t q_he
     p.few_slots = p.few.splits > 1 ? p.few_blocks * p.few.rows : 0;
     if (p.tiled) {
         // Many rows: runs only where the tiles (about so many: a sequence's last one may be part empty) would leave the chip half empty: about
-        // 768 workgroups, one and a half times what it holds at a time (five tokens for each of 16 of 70B: 43 us, with 512 54, with 1024 52).
-        const int64_t full = b->tokens * group / kTileRows, other = std::min(b->batch, b->tokens);
-        p.many.tile_rows = kTileRows;
+        // 768 workgroups, one and a half times what it holds at a time (five tokens for each of 16 of 70B: 39 us, with 1024 47; in tiles of
+        // 128 rows 43, with 512 54, with 1024 52).
+        p.many.tile_rows = rows <= kTileRows / 2 ? kTileRows / 2 : kTileRows;
+        const int64_t full = b->tokens * group / p.many.tile_rows, other = std::min(b->batch, b->tokens);
         p.many.rows = (int)rows;
         cut(p.many, keys, 768 / (std::max(full, other) * c->heads), 512, INT64_C(1) << 30);
         p.many_blocks = p.many.splits * (full + other) * c->heads;
