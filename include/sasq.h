@@ -425,7 +425,7 @@ int sasq_absmax_scale(const void* x, float* s, int64_t rows, int64_t cols, int b
  *                 value = code * k_scale[head], code = clamp(round(x / k_scale[head]), -128, 127) of the 16-bit x (any finite
  *                 non-zero factor, negative allowed).
  *   page_size     a power of two, 16 to 65536;  dim: 64 or 128;  pages * page_size may pass 2^31 (all offsets are 64 bits)
- *   strides       at least dim, multiples of 16 bytes; k and v 16-byte aligned
+ *   strides       at least dim, multiples of 16 bytes, token_stride at most 2^26 elements; k and v 16-byte aligned
  */
 typedef enum { SASQ_KV_16 = 0, SASQ_KV_INT8 = 1 } sasq_kvfmt;
 typedef struct {
@@ -445,7 +445,7 @@ typedef struct {
  *   cu_q          [batch + 1] device int32, ascending from 0;  a sequence may have no new token
  *   kv_len        [batch] device int32;  block_table  [batch, max_pages] device int32
  *   tokens        rows of q, k, v and the outputs; rows from cu_q[batch] on belong to no sequence and are not touched
- *   max_q         at least the most new tokens that a sequence has (tokens will do)
+ *   max_q         at least the most new tokens that a sequence has (tokens will do); sasq_paged_attention leaves one with more out
  *   max_kv        at least the longest kv_len (max_pages * page_size will do): how far the work is split, not which keys count
  *   max_pages * page_size at most 2^30
  * What lies on the device is not validated but bounded: an entry of block_table outside [0, pages) is a page that is not there (its
@@ -489,7 +489,7 @@ int sasq_kv_append(const void* q, const void* k, const void* v, void* q_out,
  *   q        [tokens, q_heads, dim] 16-bit `dt`, rows q_stride elements apart;  out: the same, rows out_stride apart, written;
  *            must not overlap q
  *   lse      [tokens, q_heads] device fp32 or NULL, written: ln sum_j exp S[j], with which results over parts of the keys are joined
- *   scale    finite, above 0
+ *   scale    finite, above 0;  tokens * q_heads under 2^31
  * Sums, maxima and the softmax are fp32; probabilities are rounded to 16 bits before they multiply the values (with an int8 cache:
  * to fp16, which holds every code exactly), and the output is rounded once.  Results do not change from run to run.
  *   workspace  >= sasq_paged_attention_workspace(...) bytes, 16-byte aligned (NULL allowed when that is 0), holds partial results of split sequences

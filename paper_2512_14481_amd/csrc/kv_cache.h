@@ -18,17 +18,17 @@ struct KvSteps {
     const int* __restrict__ cu_q;
     const int* __restrict__ kv_len;
     const int* __restrict__ table;
-    int batch, max_pages, tokens;
+    int batch, max_pages, tokens, max_q;
 };
 
-// A sequence's rows and keys, bounded whatever the device arrays hold.
+// A sequence's rows and keys, bounded whatever the device arrays hold.  (Places in the workspace are for max_q rows of it: one with more has none.)
 struct KvSeq {
     int row0, rows, keys;                                 // first new token's row, new tokens, length of the cache with them
 };
 __device__ __forceinline__ KvSeq kv_seq(const KvSteps& s, int b, int page_shift)
 {
     const int first = min(max(s.cu_q[b], 0), s.tokens), end = min(max(s.cu_q[b + 1], first), s.tokens);
-    return {first, end - first, min(max(s.kv_len[b], 0), s.max_pages << page_shift)};
+    return {first, end - first <= s.max_q ? end - first : 0, min(max(s.kv_len[b], 0), s.max_pages << page_shift)};
 }
 
 // Page of a sequence's position, -1 if it is not there; at >= 0 and inside the table's row is the caller's part.
@@ -70,7 +70,7 @@ inline KvPages kv_pages(const sasq_kv_cache* c)
 
 inline KvSteps kv_steps(const sasq_kv_batch* b)
 {
-    return {b->cu_q, b->kv_len, b->block_table, (int)b->batch, (int)b->max_pages, (int)b->tokens};
+    return {b->cu_q, b->kv_len, b->block_table, (int)b->batch, (int)b->max_pages, (int)b->tokens, (int)(b->max_q < b->tokens ? b->max_q : b->tokens)};
 }
 
 }  // namespace sasq

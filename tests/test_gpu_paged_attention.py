@@ -154,6 +154,24 @@ def test_lengths_that_do_not_fit_are_bounded():
     check(c)
 
 
+@pytest.mark.parametrize("max_q,lens", [(1, [(1, 3000), (2, 3000)]), (3, [(3, 3000), (4, 3000)]), (20, [(20, 3000), (1, 90), (40, 3000)])])
+def test_a_sequence_of_more_tokens_than_stated_is_left_out(max_q, lens):
+    c = Paged(lens, 8, 2, 128, 64, "f16", seed=31)
+    cache, batch = c.on_device(B, max_q=max_q, max_kv=max(n + p for n, p in c.lens))
+    need = B.sasq_paged_attention_workspace(cache, batch, c.heads)
+    ws = torch.full((need + (1 << 20),), 85, dtype=torch.uint8, device="cuda")
+    q = c.q.cuda()
+    out = torch.full((c.T, c.heads, c.dim), 7.0, dtype=q.dtype, device="cuda")
+    B.sasq_paged_attention(q, out, cache, batch, ws[:need], SCALE)
+    torch.cuda.synchronize()
+    assert bool((ws[need:] == 85).all())
+    last = int(c.cu[-2])
+    assert bool((out[last:] == 7.0).all())
+    whole, _ = run(c, lse=False)
+    assert bool((whole != 7.0).any(-1).all())
+    assert float((out[:last].float() - whole[:last].float()).abs().max()) <= 2 ** -8 * float(whole.float().abs().max())
+
+
 def test_rows_apart():
     c = Paged([(30, 10), (1, 200), (3, 77)], 8, 2, 128, 32, "bf16", seed=21)
     wide = torch.zeros((c.T, 13, 128), dtype=DT["bf16"], device="cuda")
