@@ -76,7 +76,10 @@ __device__ __forceinline__ u32x2 codes8(const u32x4& w, const QConst& k)
     return {pack_codes4(f[0], f[1], f[2], f[3]), pack_codes4(f[4], f[5], f[6], f[7])};
 }
 
-// A workgroup takes 256 units of one token: its queries, then its keys, then its values.
+// A workgroup takes 256 units of one token: its queries, then its keys, then its values; a lane reads, turns and writes 32 bytes, so that
+// nothing passes through LDS and a token's units are read and written in whole lines.  The sequence is found by the wave (64 of cu_q at a time,
+// from the cache) rather than by a list that a step before would have to make.  Bound by the bytes of long steps (4 x 2048 tokens of 70B: 60 us,
+// 5.6 TB/s; 2649 of 13B into int8 33 us) and by launch and waits of short ones (one token of 7B 4.2 us, 200 of 70B the same).
 template <int DT, int STYLE, bool I8>
 __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a, KvPages cache, KvSteps steps, int dim, int parts, int first)
 {
