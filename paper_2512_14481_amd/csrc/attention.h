@@ -237,6 +237,7 @@ __device__ __forceinline__ void load_q(const AttnArgs& a, const uint16_t* src, b
 #pragma unroll
             for (int i = 0; i < 4; ++i) q[t][i] ^= flip;
     }
+    c = fmaxf(c, 0x1p-149f);                              // a scale and a factor whose product is 0 in fp32: a masked score times it stays -inf
 }
 
 // Calls whose sequences all have few rows are the rows kernel's, any others the tiles kernel's.

@@ -3,7 +3,6 @@
 
 #include <algorithm>
 
-
 namespace sasq {
 
 // out = sum over runs of o 2^(m - top) / sum over runs of l 2^(m - top), D / 64 channels a lane.  First the sequences of many rows, a wave for

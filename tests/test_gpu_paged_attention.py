@@ -248,3 +248,13 @@ def test_big_scores():
     c.q *= 20
     out, lse = run(c, scale=1.0)
     assert_attention(c, out, lse, 1.0)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("lens", [[(1, 500), (3, 40)], [(40, 20), (1, 70)]])
+def test_a_scale_and_a_factor_whose_product_vanishes(lens, dtype):
+    """Scores of 0 in fp32: every key counts alike, and a masked one still does not."""
+    c = Paged(lens, 4, 2, 128, 16, dtype, True, seed=27)
+    c.k_scale.fill_(1e-30)
+    out, lse = run(c, scale=1e-30)
+    assert_attention(c, out, lse, 1e-30)
