@@ -44,7 +44,7 @@ __device__ __forceinline__ int64_t token_slot(int tokens, int q_heads, int run, 
 __device__ __forceinline__ int attn_end(const KvSeq& seq, int group, const AttnSplit& s, int tile)
 {
     const int last = min(seq.rows * group, (tile + 1) * s.tile_rows) - 1;
-    return max(seq.keys - seq.rows + last / group + 1, 0);
+    return max(kv_last(seq, last / group) + 1, 0);
 }
 __device__ __forceinline__ int attn_runs(const AttnSplit& s, int end) { return min(s.splits, max(1, (end + s.chunk - 1) / s.chunk)); }
 

@@ -49,7 +49,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, KvPages
     if (r >= rows || attn_runs(split, attn_end(seq, a.group, split, r / split.tile_rows)) == 1) return;      // nothing to do, or written already
     do {                                                                   // (a workgroup of the second kind goes through this as one)
         const int token = r / a.group, t = seq.row0 + token, head = hk * a.group + r % a.group;
-        const int sees = seq.keys - seq.rows + token;
+        const int sees = kv_last(seq, token);
         const int runs = sees < 0 ? 0 : min(split.splits, sees / split.chunk + 1);            // later ones have no key of this row
         auto slot = [&](int i) -> int64_t { return many ? token_slot(steps.tokens, a.q_heads, i, t, head) : few_slot(split, steps.batch, cache.heads, i, b, hk, r); };
         float top = -INFINITY;

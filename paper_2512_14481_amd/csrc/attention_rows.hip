@@ -60,11 +60,11 @@ __global__ __launch_bounds__(kRowWaves * 64, I8 ? 2 : 1) void attention_rows_ker
     const int end = attn_end(seq, a.group, split, 0), runs = attn_runs(split, end);
     if (run >= runs) return;
     const int to = run == runs - 1 ? end : min(end, from + split.chunk);
-    const int past = seq.keys - seq.rows;                                  // the first row's last key: masks begin after it
+    const int past = kv_last(seq, 0);                                      // the first row's last key: masks begin after it
 
     const bool row_there = l16 < rows;
     const int my_token = (row_there ? l16 : 0) / a.group, my_head = hk * a.group + (row_there ? l16 : 0) % a.group;
-    const int sees = past + my_token;
+    const int sees = kv_last(seq, my_token);
     float c;
     u32x4 q[DS];
     load_q<DTQ, D, I8>(a, a.q + (int64_t)(seq.row0 + my_token) * a.q_stride + (int64_t)my_head * D, row_there, g, I8 ? cache.k_scale[hk] : 1.0f, q, c);

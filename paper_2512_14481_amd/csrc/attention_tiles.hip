@@ -89,11 +89,10 @@ __global__ __launch_bounds__(kTileWaves * 64, RB == 1 && I8 ? 3 : 2) void attent
     if (run >= runs) return;
     const int from = run * split.chunk, to = run == runs - 1 ? end : min(end, from + split.chunk);
     const int tiles = (to - from + kTileKeys - 1) / kTileKeys;
-    const int past = seq.keys - seq.rows;
-    const int sees_group = past + row0 / a.group;                          // last key of the workgroup's first row, of the wave's, of the wave's last row
+    const int sees_group = kv_last(seq, row0 / a.group);                        // last key of the workgroup's first row, of the wave's, of the wave's last row
     const int wave_row = row0 + R * RB * wave;
-    const int sees_wave = past + wave_row / a.group;
-    const int wave_end = past + (min(rows, wave_row + R * RB) - 1) / a.group + 1;
+    const int sees_wave = kv_last(seq, wave_row / a.group);
+    const int wave_end = kv_last(seq, (min(rows, wave_row + R * RB) - 1) / a.group) + 1;
     const int wave_tiles = wave_row < rows ? min(tiles, max(0, (wave_end - from + kTileKeys - 1) / kTileKeys)) : 0;
 
     // The lane's rows.
@@ -107,7 +106,7 @@ __global__ __launch_bounds__(kTileWaves * 64, RB == 1 && I8 ? 3 : 2) void attent
     for (int rb = 0; rb < RB; ++rb) {
         const bool there = row_there(rb);
         const int token = there ? token_of(rb) : row0 / a.group, head = there ? head_of(rb) : hk * a.group;
-        sees[rb] = past + token;
+        sees[rb] = kv_last(seq, token);
         load_q<DTQ, D, I8>(a, a.q + (int64_t)(seq.row0 + token) * a.q_stride + (int64_t)head * D, there, g, I8 ? cache.k_scale[hk] : 1.0f, q[rb], c[rb]);
     }
 

@@ -23,13 +23,17 @@ struct KvSteps {
 
 // A sequence's rows and keys, bounded whatever the device arrays hold.  (Places in the workspace are for max_q rows of it: one with more has none.)
 struct KvSeq {
-    int row0, rows, keys;                                 // first new token's row, new tokens, length of the cache with them
+    int row0, rows, keys, past;                           // first new token's row, new tokens, keys that the table has places for, position of the first new token
 };
 __device__ __forceinline__ KvSeq kv_seq(const KvSteps& s, int b, int page_shift)
 {
     const int first = min(max(s.cu_q[b], 0), s.tokens), end = min(max(s.cu_q[b + 1], first), s.tokens);
-    return {first, end - first <= s.max_q ? end - first : 0, min(max(s.kv_len[b], 0), s.max_pages << page_shift)};
+    const int rows = end - first <= s.max_q ? end - first : 0, keys = max(s.kv_len[b], 0), places = s.max_pages << page_shift;
+    return {first, rows, min(keys, places), min(keys - rows, places)};
 }
+// The last key that new token i of the sequence sees, -1 (or less) if there is none.  A length past the table leaves the tokens where they
+// are: those past the table see all of it.
+__device__ __forceinline__ int kv_last(const KvSeq& seq, int i) { return min(seq.past + i, seq.keys - 1); }
 
 // Page of a sequence's position, -1 if it is not there; at >= 0 and inside the table's row is the caller's part.
 __device__ __forceinline__ int kv_page(const KvPages& c, const KvSteps& s, int b, int index)

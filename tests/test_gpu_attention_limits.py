@@ -1,0 +1,44 @@
+"""Attention over the paged cache at the limits of its contract: lengths past the table, structures with fields that do not count, values, scores
+and factors near the ends of their types."""
+from __future__ import annotations
+
+import math
+
+import pytest
+import torch
+
+from paper_2512_14481_amd import binding as B
+from tests.serving_ref import Paged, assert_attention
+from tests.test_gpu_paged_attention import SCALE, run
+
+pytestmark = pytest.mark.gpu
+
+
+def fill(c, b, k=None, v=None):
+    """Keys (their first channel, the others 0) and values (all channels) of sequence b's positions, one number each."""
+    j = torch.arange(int(c.kv_len[b]))
+    at = c.table[b].long()[j // c.page], j % c.page
+    if k is not None:
+        c.k[at] = 0
+        c.k[at[0], at[1], :, 0] = k.to(c.k.dtype)[:, None]
+    if v is not None:
+        c.v[at] = v.to(c.v.dtype)[:, None, None]
+
+
+def queries(c, x):
+    """Every query x in its first channel, 0 in the others: the score of a key is scale * x * its first channel."""
+    c.q.zero_()
+    c.q[..., 0] = x
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("by", [1, 3, 40, 1000, (1 << 31) - 1])
+@pytest.mark.parametrize("new,width", [(1, 21), (5, 21), (70, 21), (5, 190), (70, 190)])
+def test_a_length_past_the_table(new, width, by, int8):
+    """New tokens stay at the positions that the length gives, though the last ones are past the table: the others see the keys up to
+    theirs, those past it the whole table.  Rows, tiles, one run and several."""
+    c = Paged([(new, width * 16 - new), (2, 30)], 4, 2, 64, 16, "f16", int8, seed=41, width=width)
+    c.kv_len[0] = min(width * 16 + by, (1 << 31) - 1)
+    for max_kv in ("given", None):
+        out, lse = run(c, max_kv=max_kv)
+        assert_attention(c, out, lse, SCALE)
