@@ -65,10 +65,12 @@ inline int kv_check(const sasq_kv_cache* c, const sasq_kv_batch* b, int64_t q_he
     return SASQ_OK;
 }
 
+// (The factors are an int8 cache's: what another's fields hold does not count.)
 inline KvPages kv_pages(const sasq_kv_cache* c)
 {
-    const int64_t e = c->fmt == SASQ_KV_16 ? 2 : 1;
-    return {static_cast<uint8_t*>(c->k), static_cast<uint8_t*>(c->v), c->k_scale, c->v_scale, c->page_stride * e, c->token_stride * e,
+    const bool codes = c->fmt == SASQ_KV_INT8;
+    const int64_t e = codes ? 1 : 2;
+    return {static_cast<uint8_t*>(c->k), static_cast<uint8_t*>(c->v), codes ? c->k_scale : nullptr, codes ? c->v_scale : nullptr, c->page_stride * e, c->token_stride * e,
             c->head_stride * e, (int)c->pages, __builtin_ctz((unsigned)c->page_size), (int)c->heads};
 }
 

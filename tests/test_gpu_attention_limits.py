@@ -42,3 +42,16 @@ def test_a_length_past_the_table(new, width, by, int8):
     for max_kv in ("given", None):
         out, lse = run(c, max_kv=max_kv)
         assert_attention(c, out, lse, SCALE)
+
+
+@pytest.mark.parametrize("lens", [[(1, 300), (3, 40)], [(1, 3000), (3, 400)], [(40, 3000), (1, 900)]])
+def test_factors_of_a_16_bit_cache_are_not_read(lens):
+    """The structure's factors are an int8 cache's: whatever they are, a 16-bit cache gives the same, in one run of keys and in several."""
+    c = Paged(lens, 8, 2, 128, 16, "f16", seed=42)
+    ref, ref_lse = run(c)
+    cache, batch = c.on_device(B, max_q=max(n for n, _ in lens), max_kv=max(n + p for n, p in lens))
+    factors = torch.full((2,), 3.0, device="cuda")
+    cache._c.k_scale = cache._c.v_scale = factors.data_ptr()
+    q, out, lse = c.q.cuda(), torch.empty_like(ref), torch.empty_like(ref_lse)
+    B.sasq_paged_attention(q, out, cache, batch, B.new_workspace(B.sasq_paged_attention_workspace(cache, batch, 8)), SCALE, lse=lse)
+    assert torch.equal(out, ref) and torch.equal(lse, ref_lse)
