@@ -130,9 +130,14 @@ __device__ __forceinline__ void wait_loads()
     asm volatile("" ::: "memory");
 }
 
-// A score may pass the running maximum by so much (in powers of two) before the maximum is moved: probabilities then reach 2^8 at most,
-// their rounding is relative all the same, and the common step needs no reduction over lanes and no rescaling of the output.
-constexpr float kLazy = 8.0f;
+// A probability is 2^(score - m).  m is moved only when a score would pass `most`, and then to `below` under the row's largest: the common step
+// needs no reduction over lanes and no rescaling of the output, and rounding is relative all the same.  fp16 ends at 2^-24, so probabilities go as
+// high as it reaches with room for a score in between (2^7 to 2^15): what is rounded to 0 is under 2^-32 of the row's largest, 2^-15 of the row for
+// 131072 such keys (at 2^0 to 2^8 it was 2^-25 of each, 0.4 % of the row).
+template <int DT>
+struct Lazy {
+    static constexpr float below = DT == SASQ_F16 ? 7.0f : 0.0f, most = below + 8.0f;
+};
 // The maximum before any score: finite, so that a row whose scores are all masked gets probabilities of 0 and any other score moves it.
 constexpr float kNoMax = -1e30f;
 // What sums over an older maximum are multiplied by.  Never 0, which would make NaN of an infinite sum.

@@ -146,10 +146,10 @@ __global__ __launch_bounds__(kRowWaves * 64, I8 ? 2 : 1) void attention_rows_ker
                 }
             }
             float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-            if (__any(__builtin_fmaf(top, c, -m) > kLazy)) {
+            if (__any(__builtin_fmaf(top, c, -m) > Lazy<DT>::most)) {
                 top = fmaxf(top, __shfl_xor(top, 16, kWave));
                 top = fmaxf(top, __shfl_xor(top, 32, kWave));
-                const float now = fmaxf(top * c, m), keep = kept(m, now);
+                const float now = fmaxf(__builtin_fmaf(top, c, -Lazy<DT>::below), m), keep = kept(m, now);
                 m = now;
                 l *= keep;
 #pragma unroll

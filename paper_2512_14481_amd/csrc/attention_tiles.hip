@@ -223,7 +223,7 @@ __global__ __launch_bounds__(kTileWaves * 64, RB == 1 && I8 ? 3 : 2) void attent
             for (int k = 0; k < KB; ++k)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) top[rb] = fmaxf(top[rb], s[rb][k][j]);
-            above |= __builtin_fmaf(top[rb], c[rb], -m[rb]) > kLazy;
+            above |= __builtin_fmaf(top[rb], c[rb], -m[rb]) > Lazy<DT>::most;
         }
         return __any(above);
     };
@@ -232,7 +232,7 @@ __global__ __launch_bounds__(kTileWaves * 64, RB == 1 && I8 ? 3 : 2) void attent
         for (int rb = 0; rb < RB; ++rb) {
             float t = fmaxf(top[rb], __shfl_xor(top[rb], 16, kWave));
             t = fmaxf(t, __shfl_xor(t, 32, kWave));
-            t = fmaxf(t * c[rb], m[rb]);
+            t = fmaxf(__builtin_fmaf(t, c[rb], -Lazy<DT>::below), m[rb]);
             const float keep = kept(m[rb], t);
             m[rb] = t;
             l[rb] *= keep;

@@ -55,3 +55,25 @@ def test_factors_of_a_16_bit_cache_are_not_read(lens):
     q, out, lse = c.q.cuda(), torch.empty_like(ref), torch.empty_like(ref_lse)
     B.sasq_paged_attention(q, out, cache, batch, B.new_workspace(B.sasq_paged_attention_workspace(cache, batch, 8)), SCALE, lse=lse)
     assert torch.equal(out, ref) and torch.equal(lse, ref_lse)
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("max_kv", ["given", 64])
+@pytest.mark.parametrize("new", [1, 20])
+def test_many_keys_of_little_weight(new, max_kv, int8):
+    """One key 17.4 above 131071 others whose weight, 2^-25.1 of its each, is 0.36 % of the row in sum.  All values are 1, and so is the output:
+    off by the rounding of the large probability and of the output (2^-11 each), of the small ones (fp16 below 2^-14 has steps of 2^-24, and
+    probabilities reach 2^7 at least: 2^-32 of the largest for each), and of fp32 sums (a step of the product for every 32 keys, and a sum for every
+    16 of a lane's, taken as 2^-23 each)."""
+    n = 1 << 17
+    c = Paged([(new, n - new)], 1, 1, 64, 256, "f16", int8, seed=43)
+    queries(c, 1.0)
+    if int8:
+        c.k_scale[:], c.v_scale[:] = 0.2, 0.01
+    k = torch.zeros(n)
+    k[0] = 87 if int8 else 17.4
+    fill(c, 0, k, torch.full((n,), 100.0 if int8 else 1.0))
+    out, _ = run(c, max_kv=max_kv, scale=1.0)
+    bound = 2 * 1.01 * 2.0 ** -11 + n * 2.0 ** -32 + (n / 32 + n / 16) * 2.0 ** -23
+    assert bound < 0.7 * n * math.exp(-17.4)
+    assert float((out.double() - 1).abs().max()) <= bound
