@@ -140,6 +140,9 @@ struct Lazy {
 };
 // The maximum before any score: finite, so that a row whose scores are all masked gets probabilities of 0 and any other score moves it.
 constexpr float kNoMax = -1e30f;
+// m is a product of a score and c, rounded; from here on the exact product that a fused multiply-add subtracts it from is more than half a
+// power of two away (2^128 from about 2^32 on: probabilities of 0 or infinity for the largest score itself), and is to be rounded alike.
+constexpr float kExact = 0x1p24f;
 // What sums over an older maximum are multiplied by.  Never 0, which would make NaN of an infinite sum.
 __device__ __forceinline__ float kept(float before, float now) { return fmaxf(__builtin_amdgcn_exp2f(before - now), 1e-37f); }
 // The same for a part of a row's keys, f = (maximum, sum), joined with others under `top`: a part without keys has nothing to add, one whose

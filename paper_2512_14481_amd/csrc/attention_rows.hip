@@ -146,10 +146,10 @@ __global__ __launch_bounds__(kRowWaves * 64, I8 ? 2 : 1) void attention_rows_ker
                 }
             }
             float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-            if (__any(__builtin_fmaf(top, c, -m) > Lazy<DT>::most)) {
+            if (__any(top * c - m > Lazy<DT>::most)) {
                 top = fmaxf(top, __shfl_xor(top, 16, kWave));
                 top = fmaxf(top, __shfl_xor(top, 32, kWave));
-                const float now = fmaxf(__builtin_fmaf(top, c, -Lazy<DT>::below), m), keep = kept(m, now);
+                const float now = fmaxf(top * c - Lazy<DT>::below, m), keep = kept(m, now);
                 m = now;
                 l *= keep;
 #pragma unroll
@@ -158,7 +158,7 @@ __global__ __launch_bounds__(kRowWaves * 64, I8 ? 2 : 1) void attention_rows_ker
             float e[8];
             u32x4 p;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j >> 2][j & 3], c, -m));
+            for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(s[j >> 2][j & 3] * c - m);      // the product rounded as in m (kExact); bound by bytes
             l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
 #pragma unroll
             for (int j = 0; j < 4; ++j) p[j] = Store16<DT>::pack(e[2 * j], e[2 * j + 1]);

@@ -192,9 +192,22 @@ __global__ __launch_bounds__(kTileWaves * 64, RB == 1 && I8 ? 3 : 2) void attent
             }
         }
     };
+    // A wave that has met a score of kExact or more multiplies its scores by c ahead of everything else, and c is 1 from then on.  (Products rounded
+    // in every tile: a chunk of 4096 on 12281 tokens 1846 us against 1803.)
+    bool coarse = false;
+    float by[RB];
+    auto multiply = [&]() {
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+            for (int k = 0; k < KB; ++k)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[rb][k][j] *= by[rb];
+    };
     // Score j of block k is of key 16 k + 4 g + j.
-    auto unmasked = [&](int i) -> bool { return !holes && from + kTileKeys * i + kTileKeys - 1 <= sees_wave; };
+    auto unmasked = [&](int i) -> bool { return !coarse && !holes && from + kTileKeys * i + kTileKeys - 1 <= sees_wave; };
     auto mask = [&](int i) {
+        if (coarse) multiply();
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
             const int last = sees[rb] - (from + kTileKeys * i) - 4 * g;    // of the lane's keys, 0 being its first
@@ -215,7 +228,7 @@ __global__ __launch_bounds__(kTileWaves * 64, RB == 1 && I8 ? 3 : 2) void attent
     };
     float top[RB];
     auto maxima = [&]() -> bool {                                          // whether a score passes the running maximum by too much
-        bool above = false;
+        bool passes = false;
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
             top[rb] = s[rb][0][0];
@@ -223,16 +236,31 @@ __global__ __launch_bounds__(kTileWaves * 64, RB == 1 && I8 ? 3 : 2) void attent
             for (int k = 0; k < KB; ++k)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) top[rb] = fmaxf(top[rb], s[rb][k][j]);
-            above |= __builtin_fmaf(top[rb], c[rb], -m[rb]) > Lazy<DT>::most;
+            passes |= __builtin_fmaf(top[rb], c[rb], -m[rb]) > Lazy<DT>::most;
         }
-        return __any(above);
+        return __any(passes);
     };
     auto raise = [&]() {                                                   // moves the maxima, and the sums with them
+        bool large = false;
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
-            float t = fmaxf(top[rb], __shfl_xor(top[rb], 16, kWave));
-            t = fmaxf(t, __shfl_xor(t, 32, kWave));
-            t = fmaxf(__builtin_fmaf(t, c[rb], -Lazy<DT>::below), m[rb]);
+            top[rb] = fmaxf(top[rb], __shfl_xor(top[rb], 16, kWave));
+            top[rb] = fmaxf(top[rb], __shfl_xor(top[rb], 32, kWave));
+            large |= top[rb] > -INFINITY && fabsf(top[rb] * c[rb]) >= kExact;
+        }
+        if (!coarse && __any(large)) {
+            coarse = true;
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                by[rb] = c[rb];
+                c[rb] = 1.0f;
+                top[rb] *= by[rb];
+            }
+            multiply();
+        }
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            const float t = fmaxf(top[rb] * c[rb] - Lazy<DT>::below, m[rb]);
             const float keep = kept(m[rb], t);
             m[rb] = t;
             l[rb] *= keep;
@@ -363,7 +391,7 @@ __global__ __launch_bounds__(kTileWaves * 64, RB == 1 && I8 ? 3 : 2) void attent
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) asm volatile("" : "+v"(l[rb]), "+v"(p[rb][0]), "+v"(p[rb][1]));
         if (i + 1 < wave_tiles && !unmasked(i + 1)) mask(i + 1);
-        bool above = false;
+        bool passes = false;
         float sum0[RB];
 #pragma unroll
         for (int x = 0; x < VG; ++x) {
@@ -371,7 +399,7 @@ __global__ __launch_bounds__(kTileWaves * 64, RB == 1 && I8 ? 3 : 2) void attent
             if (x + 1 < VG) read_values(i, x + 1, next);
             __builtin_amdgcn_sched_barrier(0);
             add_values(x, vf);
-            if (x == 0) above = maxima();
+            if (x == 0) passes = maxima();
             if (x == VG / 2) probabilities(0, sum0);                       // with the maximum as it is: of the next tile, whose first blocks' have gone in
             __builtin_amdgcn_sched_barrier(0);
             if (x + 1 < VG) {
@@ -382,7 +410,7 @@ __global__ __launch_bounds__(kTileWaves * 64, RB == 1 && I8 ? 3 : 2) void attent
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) asm volatile("" : "+v"(sum0[rb]), "+v"(p[rb][0]));
         if (i + 1 >= wave_tiles) return;
-        if (above) {
+        if (passes) {
             raise();
             probabilities(0, sum0);
         }

@@ -77,3 +77,22 @@ def test_many_keys_of_little_weight(new, max_kv, int8):
     bound = 2 * 1.01 * 2.0 ** -11 + n * 2.0 ** -32 + (n / 32 + n / 16) * 2.0 ** -23
     assert bound < 0.7 * n * math.exp(-17.4)
     assert float((out.double() - 1).abs().max()) <= bound
+
+
+@pytest.mark.parametrize("q,base", [(2.0 ** 60, 44), (-1.0, 20), (1.0, 20)])
+@pytest.mark.parametrize("new,n", [(1, 500), (1, 2800), (30, 500), (30, 2800)])
+def test_scores_far_from_zero(new, n, q, base):
+    """Scores from 2e30 to 1e37, or from 1e5 to 5e11 of either sign, all different: a row's output is the value of its largest, to the bit, and
+    lse that score."""
+    c = Paged([(new, n - new), (1, 7)], 1, 1, 64, 64, "bf16", seed=44)
+    queries(c, q)
+    rank = torch.randperm(n, generator=torch.Generator().manual_seed(44))
+    size = (1 + (rank % 128) / 128.0) * 2.0 ** (base + rank // 128)
+    fill(c, 0, size)
+    out, lse = run(c)
+    for i in range(new):
+        p = n - new + i
+        best = int((rank[:p + 1] * q).argmax())
+        at = int(c.table[0, best // 64]), best % 64
+        score = SCALE * q * float(size[best])
+        assert torch.equal(out[i, 0].cpu(), c.v[at][0]) and abs(float(lse[i, 0]) - score) <= 2.0 ** -21 * abs(score)
