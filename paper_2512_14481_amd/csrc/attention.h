@@ -138,8 +138,9 @@ template <int DT>
 struct Lazy {
     static constexpr float below = DT == SASQ_F16 ? 7.0f : 0.0f, most = below + 8.0f;
 };
-// The maximum before any score: finite, so that a row whose scores are all masked gets probabilities of 0 and any other score moves it.
-constexpr float kNoMax = -1e30f;
+// m before any score: finite, so that a row whose scores are all masked gets probabilities of 0, and the lowest that is, so that any other
+// score moves it (or is that value, with a probability of 1).
+constexpr float kNoMax = -0x1.fffffep127f;
 // m is a product of a score and c, rounded; from here on the exact product that a fused multiply-add subtracts it from is more than half a
 // power of two away (2^128 from about 2^32 on: probabilities of 0 or infinity for the largest score itself), and is to be rounded alike.
 constexpr float kExact = 0x1p24f;

@@ -210,7 +210,7 @@ __global__ __launch_bounds__(kRowWaves * 64, I8 ? 2 : 1) void attention_rows_ker
     __syncthreads();
     l += __shfl_xor(l, 16, kWave);
     l += __shfl_xor(l, 32, kWave);
-    if (g == 0) ml[wave * 16 + l16] = make_float2(m == kNoMax ? -INFINITY : m, l);
+    if (g == 0) ml[wave * 16 + l16] = make_float2(l == 0.0f ? -INFINITY : m, l);
 #pragma unroll
     for (int n = 0; n < DO; ++n) *reinterpret_cast<f32x4*>(part + (wave * 16 + l16) * (D + 4) + 16 * n + 4 * g) = o[n];
     __syncthreads();

@@ -462,7 +462,7 @@ __global__ __launch_bounds__(kTileWaves * 64, RB == 1 && I8 ? 3 : 2) void attent
         if (!row_there(rb)) continue;
         const int64_t t = seq.row0 + token_of(rb);
         const int head = head_of(rb);
-        const float last = m[rb] == kNoMax ? -INFINITY : m[rb];
+        const float last = sum == 0.0f ? -INFINITY : m[rb];
         if (runs == 1) {
             const bool none = sum == 0.0f;
             const float f = none ? 0.0f : (I8 ? cache.v_scale[hk] : 1.0f) / sum;

@@ -79,10 +79,10 @@ def test_many_keys_of_little_weight(new, max_kv, int8):
     assert float((out.double() - 1).abs().max()) <= bound
 
 
-@pytest.mark.parametrize("q,base", [(2.0 ** 60, 44), (-1.0, 20), (1.0, 20)])
+@pytest.mark.parametrize("q,base", [(-2.0 ** 60, 44), (2.0 ** 60, 44), (-1.0, 20), (1.0, 20)])
 @pytest.mark.parametrize("new,n", [(1, 500), (1, 2800), (30, 500), (30, 2800)])
 def test_scores_far_from_zero(new, n, q, base):
-    """Scores from 2e30 to 1e37, or from 1e5 to 5e11 of either sign, all different: a row's output is the value of its largest, to the bit, and
+    """Scores from 2e30 to 1e37, or from 1e5 to 5e11, of either sign, all different: a row's output is the value of its largest, to the bit, and
     lse that score."""
     c = Paged([(new, n - new), (1, 7)], 1, 1, 64, 64, "bf16", seed=44)
     queries(c, q)
@@ -96,3 +96,19 @@ def test_scores_far_from_zero(new, n, q, base):
         at = int(c.table[0, best // 64]), best % 64
         score = SCALE * q * float(size[best])
         assert torch.equal(out[i, 0].cpu(), c.v[at][0]) and abs(float(lse[i, 0]) - score) <= 2.0 ** -21 * abs(score)
+
+
+@pytest.mark.parametrize("new", [1, 30])
+@pytest.mark.parametrize("dtype,q,factor", [("f16", -1.0, 2.0 ** 110), ("bf16", -2.0 ** 60, 2.0 ** 50)])
+def test_scores_of_codes_far_below_zero(new, dtype, q, factor):
+    c = Paged([(new, 120 - new)], 1, 1, 64, 16, dtype, True, seed=45)
+    queries(c, q)
+    c.k_scale[:], c.v_scale[:] = factor, 0.5
+    code = 1 + torch.randperm(120, generator=torch.Generator().manual_seed(45))
+    fill(c, 0, code)
+    out, lse = run(c)
+    for i in range(new):
+        best = int(code[:121 - new + i].argmin())
+        score = SCALE * q * factor * int(code[best])
+        value = c.v[int(c.table[0, best // 16]), best % 16, 0].float() * 0.5
+        assert torch.equal(out[i, 0].cpu().float(), value.to(c.q.dtype).float()) and abs(float(lse[i, 0]) - score) <= 2.0 ** -21 * -score
