@@ -233,13 +233,12 @@ __device__ __forceinline__ void load_q(const AttnArgs& a, const uint16_t* src, b
                 for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(Store16<DTQ>::lo(q[t][i])), fabsf(Store16<DTQ>::hi(q[t][i]))));
             top = fmaxf(top, __shfl_xor(top, 16, kWave));
             top = fmaxf(top, __shfl_xor(top, 32, kWave));
-            const int e = top > 0.0f && top < INFINITY ? min(max(((int)(__float_as_uint(top) >> 23)) - 127, -100), 100) : 0;
-            const float down = __uint_as_float((uint32_t)(127 - e) << 23);
-            c *= __uint_as_float((uint32_t)(127 + e) << 23);
+            const int e = top > 0.0f && top < INFINITY ? __builtin_amdgcn_frexp_expf(top) - 1 : 0;      // -133 to 127: no single factor reaches both ends
+            c = __builtin_ldexpf(c, e);
 #pragma unroll
             for (int t = 0; t < DS; ++t)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) q[t][i] = Store16<SASQ_F16>::pack(Store16<DTQ>::lo(q[t][i]) * down, Store16<DTQ>::hi(q[t][i]) * down);
+                for (int i = 0; i < 4; ++i) q[t][i] = Store16<SASQ_F16>::pack(__builtin_ldexpf(Store16<DTQ>::lo(q[t][i]), -e), __builtin_ldexpf(Store16<DTQ>::hi(q[t][i]), -e));
         }
 #pragma unroll
         for (int t = 0; t < DS; ++t)

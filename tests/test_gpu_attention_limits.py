@@ -112,3 +112,15 @@ def test_scores_of_codes_far_below_zero(new, dtype, q, factor):
         score = SCALE * q * factor * int(code[best])
         value = c.v[int(c.table[0, best // 16]), best % 16, 0].float() * 0.5
         assert torch.equal(out[i, 0].cpu().float(), value.to(c.q.dtype).float()) and abs(float(lse[i, 0]) - score) <= 2.0 ** -21 * -score
+
+
+@pytest.mark.parametrize("lens", [[(1, 500), (3, 40)], [(40, 20), (1, 70)]])
+@pytest.mark.parametrize("query,factor,scale", [(118, -118, 0), (125, -120, -5), (-110, 110, 0), (-120, 120, 0)])
+def test_queries_of_any_size(query, factor, scale, lens):
+    """bf16 queries near either end of their type over an int8 cache whose factor makes up for it."""
+    c = Paged(lens, 4, 2, 128, 16, "bf16", True, seed=46)
+    c.q = (c.q.float() * 2.0 ** query).to(c.q.dtype)
+    c.k_scale *= 2.0 ** factor
+    assert bool(torch.isfinite(c.q).all()) and bool((c.k_scale != 0).all()) and bool(torch.isfinite(c.k_scale).all())
+    out, lse = run(c, scale=SCALE * 2.0 ** scale)
+    assert_attention(c, out, lse, SCALE * 2.0 ** scale)
