@@ -221,9 +221,9 @@ __device__ __forceinline__ void load_q(const AttnArgs& a, const uint16_t* src, b
     }
     c = a.scale * 1.44269504088896f;
     if constexpr (I8) {
+        int e = 0;
         // fp16 products: a bf16 row is brought to at most 2 by a power of two (exact but for values 2^-14 and more below its largest),
         // and the sign of the factor goes into Q, so that larger products stay larger scores.
-        c *= fabsf(k_scale);
         const uint32_t flip = k_scale < 0.0f ? 0x80008000u : 0u;
         if constexpr (DTQ == SASQ_BF16) {
             float top = 0.0f;
@@ -233,8 +233,7 @@ __device__ __forceinline__ void load_q(const AttnArgs& a, const uint16_t* src, b
                 for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(Store16<DTQ>::lo(q[t][i])), fabsf(Store16<DTQ>::hi(q[t][i]))));
             top = fmaxf(top, __shfl_xor(top, 16, kWave));
             top = fmaxf(top, __shfl_xor(top, 32, kWave));
-            const int e = top > 0.0f && top < INFINITY ? __builtin_amdgcn_frexp_expf(top) - 1 : 0;      // -133 to 127: no single factor reaches both ends
-            c = __builtin_ldexpf(c, e);
+            e = top > 0.0f && top < INFINITY ? __builtin_amdgcn_frexp_expf(top) - 1 : 0;      // -133 to 127: no single factor reaches both ends
 #pragma unroll
             for (int t = 0; t < DS; ++t)
 #pragma unroll
@@ -244,6 +243,11 @@ __device__ __forceinline__ void load_q(const AttnArgs& a, const uint16_t* src, b
         for (int t = 0; t < DS; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) q[t][i] ^= flip;
+        // The three are multiplied with their powers of two apart: two of them may leave fp32 where all three do not.  Where these do, scores
+        // are infinite, but a score of 0 stays that.
+        c = __builtin_ldexpf(__builtin_amdgcn_frexp_mantf(c) * __builtin_amdgcn_frexp_mantf(fabsf(k_scale)),
+                             __builtin_amdgcn_frexp_expf(c) + __builtin_amdgcn_frexp_expf(k_scale) + e);
+        c = fminf(c, 0x1.fffffep127f);
     }
     c = fmaxf(c, 0x1p-149f);                              // a scale and a factor whose product is 0 in fp32: a masked score times it stays -inf
 }

@@ -124,3 +124,17 @@ def test_queries_of_any_size(query, factor, scale, lens):
     assert bool(torch.isfinite(c.q).all()) and bool((c.k_scale != 0).all()) and bool(torch.isfinite(c.k_scale).all())
     out, lse = run(c, scale=SCALE * 2.0 ** scale)
     assert_attention(c, out, lse, SCALE * 2.0 ** scale)
+
+
+@pytest.mark.parametrize("lens", [[(1, 500), (3, 40)], [(40, 20), (1, 70)]])
+@pytest.mark.parametrize("dtype,query,factor,scale", [("bf16", -126, 70, 68), ("bf16", 100, -110, 10), ("bf16", -120, -5, 125)] +
+                         [(dtype, *powers) for dtype in ("f16", "bf16") for powers in ((-10, 120, -110), (0, -120, 120), (10, -140, 126))])
+def test_products_of_scale_factor_and_query_of_any_size(query, factor, scale, lens, dtype):
+    """Scores are finite though the product of two of the three leaves fp32 at one end or the other."""
+    c = Paged(lens, 4, 2, 128, 16, dtype, True, seed=46)
+    c.q = (c.q.float() * 2.0 ** query).to(c.q.dtype)
+    c.k_scale *= 2.0 ** factor
+    factor, scale = c.k_scale, SCALE * 2.0 ** scale
+    assert bool(torch.isfinite(c.q).all()) and bool((factor != 0).all()) and bool(torch.isfinite(factor).all()) and scale < 2.0 ** 127
+    out, lse = run(c, scale=scale)
+    assert_attention(c, out, lse, scale)
