@@ -2,7 +2,6 @@
 #include "attention.h"
 
 #include <algorithm>
-#include <cmath>
 
 namespace sasq {
 
@@ -68,7 +67,7 @@ extern "C" int sasq_paged_attention(const void* q, void* out, float* lse, int64_
 {
     if (!q || !out) return SASQ_ERR_NULL;
     if (const int rc = kv_check(cache, batch, q_heads, dt)) return rc;
-    if (!std::isfinite(scale) || scale <= 0.0f) return SASQ_ERR_UNSUPPORTED;
+    if (!(scale > 0.0f && scale <= 0x1p127f)) return SASQ_ERR_UNSUPPORTED;      // scale / ln 2 has to be finite too
     const int64_t dim = cache->dim, most = INT64_C(1) << 40;
     if (q_stride < q_heads * dim || out_stride < q_heads * dim || q_stride % 8 || out_stride % 8 || q_stride > most || out_stride > most) return SASQ_ERR_SHAPE;
     if (batch->tokens * q_heads >= INT64_C(1) << 31) return SASQ_ERR_SHAPE;

@@ -138,3 +138,12 @@ def test_products_of_scale_factor_and_query_of_any_size(query, factor, scale, le
     assert bool(torch.isfinite(c.q).all()) and bool((factor != 0).all()) and bool(torch.isfinite(factor).all()) and scale < 2.0 ** 127
     out, lse = run(c, scale=scale)
     assert_attention(c, out, lse, scale)
+
+
+@pytest.mark.parametrize("lens", [[(1, 500), (3, 40)], [(40, 20), (1, 70)]])
+def test_the_largest_scale(lens):
+    c = Paged(lens, 4, 2, 128, 16, "bf16", seed=50)
+    c.q = (c.q.float() * 2.0 ** -65).to(c.q.dtype)
+    c.k = (c.k.float() * 2.0 ** -65).to(c.k.dtype)
+    out, lse = run(c, scale=2.0 ** 127)
+    assert_attention(c, out, lse, 2.0 ** 127)
