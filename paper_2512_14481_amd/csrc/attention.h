@@ -132,11 +132,12 @@ __device__ __forceinline__ void wait_loads()
 
 // A probability is 2^(score - m).  m is moved only when a score would pass `most`, and then to `below` under the row's largest: the common step
 // needs no reduction over lanes and no rescaling of the output, and rounding is relative all the same.  fp16 ends at 2^-24, so probabilities go as
-// high as it reaches with room for a score in between (2^7 to 2^15): what is rounded to 0 is under 2^-32 of the row's largest, 2^-15 of the row for
-// 131072 such keys (at 2^0 to 2^8 it was 2^-25 of each, 0.4 % of the row).
+// high as it reaches with room for a score in between (the largest 2^7 to 2^15): what is rounded to 0 is under 2^-32 of the row's largest, 2^-15 of
+// the row for 131072 such keys (at 2^0 to 2^8 it was 2^-25 of each, 0.4 % of the row).  bf16 has room below but values as large as fp32's:
+// probabilities of 1 at most (the largest 2^-8 to 2^0) times them stay in it.
 template <int DT>
 struct Lazy {
-    static constexpr float below = DT == SASQ_F16 ? 7.0f : 0.0f, most = below + 8.0f;
+    static constexpr float below = DT == SASQ_F16 ? 7.0f : -8.0f, most = below + 8.0f;
 };
 // m before any score: finite, so that a row whose scores are all masked gets probabilities of 0, and the lowest that is, so that any other
 // score moves it (or is that value, with a probability of 1).

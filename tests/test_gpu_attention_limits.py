@@ -147,3 +147,16 @@ def test_the_largest_scale(lens):
     c.k = (c.k.float() * 2.0 ** -65).to(c.k.dtype)
     out, lse = run(c, scale=2.0 ** 127)
     assert_attention(c, out, lse, 2.0 ** 127)
+
+
+@pytest.mark.parametrize("new", [1, 30])
+def test_large_values_at_scores_a_little_above_the_first(new):
+    """Values near 2^117, first keys of score 0, the rest of 4.84 (2^7 times the weight): the sums over probabilities of 1 at most are finite."""
+    n = 256
+    c = Paged([(new, n - new)], 1, 1, 64, 64, "bf16", seed=47)
+    queries(c, 1.0)
+    k = torch.full((n,), 4.84375)
+    k[:128 if new == 1 else 64] = 0
+    fill(c, 0, k, 2.0 ** 117 * (1 + torch.rand(n, generator=torch.Generator().manual_seed(47))))
+    out, lse = run(c, scale=1.0)
+    assert_attention(c, out, lse, 1.0)
