@@ -145,8 +145,9 @@ constexpr float kNoMax = -0x1.fffffep127f;
 // m is a product of a score and c, rounded; from here on the exact product that a fused multiply-add subtracts it from is more than half a
 // power of two away (2^128 from about 2^32 on: probabilities of 0 or infinity for the largest score itself), and is to be rounded alike.
 constexpr float kExact = 0x1p24f;
-// What sums over an older maximum are multiplied by.  Never 0, which would make NaN of an infinite sum.
-__device__ __forceinline__ float kept(float before, float now) { return fmaxf(__builtin_amdgcn_exp2f(before - now), 1e-37f); }
+// What sums over an older maximum are multiplied by.  Never 0, which would make NaN of an infinite sum, but the least there is: of a sum of 2^120
+// (bf16 values) 1e-37 would be 0.1 of what has no weight.
+__device__ __forceinline__ float kept(float before, float now) { return fmaxf(__builtin_amdgcn_exp2f(before - now), 0x1p-149f); }
 // The same for a part of a row's keys, f = (maximum, sum), joined with others under `top`: a part without keys has nothing to add, one whose
 // maximum is infinite or whose sum is NaN hands that on.
 __device__ __forceinline__ float part_weight(const float2& f, float top)

@@ -160,3 +160,17 @@ def test_large_values_at_scores_a_little_above_the_first(new):
     fill(c, 0, k, 2.0 ** 117 * (1 + torch.rand(n, generator=torch.Generator().manual_seed(47))))
     out, lse = run(c, scale=1.0)
     assert_attention(c, out, lse, 1.0)
+
+
+@pytest.mark.parametrize("new,n,low", [(1, 256, 128), (30, 256, 64), (1, 3000, 1500), (30, 3000, 1500)])
+def test_large_values_of_no_weight(new, n, low):
+    """The first keys' scores are 180 below the others' (a weight of 2^-259) and their values 2^120: nothing of them is in the output."""
+    c = Paged([(new, n - new)], 1, 1, 64, 64, "bf16", seed=48)
+    queries(c, 1.0)
+    k = torch.zeros(n)
+    k[:low] = -180
+    v = torch.randn(n, generator=torch.Generator().manual_seed(48))
+    v[:low] = 2.0 ** 120
+    fill(c, 0, k, v)
+    out, lse = run(c, scale=1.0)
+    assert_attention(c, out, lse, 1.0)
