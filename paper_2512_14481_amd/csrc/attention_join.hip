@@ -81,10 +81,10 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, KvPages
         }
         if (many || wave == 0) {
             const bool none = sum == 0.0f;
-            const float f = none ? 0.0f : (cache.v_scale ? cache.v_scale[hk] : 1.0f) / sum;
+            const float f = none ? 0.0f : 1.0f / sum, v = cache.v_scale ? cache.v_scale[hk] : 1.0f;      // (apart, as in attention_rows.hip)
             uint16_t* dst = a.out + (int64_t)t * a.out_stride + (int64_t)head * D + lane * E;
 #pragma unroll
-            for (int e = 0; e < E; ++e) dst[e] = none ? (uint16_t)0 : Store16<DTQ>::enc(x[e] * f);
+            for (int e = 0; e < E; ++e) dst[e] = none ? (uint16_t)0 : Store16<DTQ>::enc(x[e] * f * v);
             if (a.lse && lane == 0) a.lse[(int64_t)t * a.q_heads + head] = none ? -INFINITY : (top + log2f(sum)) * 0.693147180559945f;
         }
         r += step;

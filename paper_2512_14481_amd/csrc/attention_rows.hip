@@ -232,11 +232,11 @@ __global__ __launch_bounds__(kRowWaves * 64, I8 ? 2 : 1) void attention_rows_ker
     const int token = r / a.group, head = hk * a.group + r % a.group;
     if (runs == 1) {
         const bool none = sum == 0.0f;
-        const float f = none ? 0.0f : (I8 ? cache.v_scale[hk] : 1.0f) / sum;
+        const float f = none ? 0.0f : 1.0f / sum, v = I8 ? cache.v_scale[hk] : 1.0f;       // (apart: a small factor over a large sum may be no number of fp32's)
         uint16_t* dst = a.out + (int64_t)(seq.row0 + token) * a.out_stride + (int64_t)head * D + d;
         uint32_t w[E / 2];
 #pragma unroll
-        for (int e = 0; e < E / 2; ++e) w[e] = none ? 0u : Store16<DTQ>::pack(x[2 * e] * f, x[2 * e + 1] * f);
+        for (int e = 0; e < E / 2; ++e) w[e] = none ? 0u : Store16<DTQ>::pack(x[2 * e] * f * v, x[2 * e + 1] * f * v);
         __builtin_memcpy(dst, w, sizeof(w));
         if (a.lse && d == 0) a.lse[(int64_t)(seq.row0 + token) * a.q_heads + head] = none ? -INFINITY : (top + log2f(sum)) * 0.693147180559945f;
     } else {

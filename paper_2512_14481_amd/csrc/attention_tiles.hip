@@ -465,12 +465,12 @@ __global__ __launch_bounds__(kTileWaves * 64, RB == 1 && I8 ? 3 : 2) void attent
         const float last = sum == 0.0f ? -INFINITY : m[rb];
         if (runs == 1) {
             const bool none = sum == 0.0f;
-            const float f = none ? 0.0f : (I8 ? cache.v_scale[hk] : 1.0f) / sum;
+            const float f = none ? 0.0f : 1.0f / sum, v = I8 ? cache.v_scale[hk] : 1.0f;       // (apart, as in attention_rows.hip)
             uint16_t* dst = a.out + t * a.out_stride + (int64_t)head * D + 4 * g;
 #pragma unroll
             for (int n = 0; n < DO; ++n) {
                 const f32x4 x = o[rb][n];
-                const u32x2 w = {none ? 0u : Store16<DTQ>::pack(x[0] * f, x[1] * f), none ? 0u : Store16<DTQ>::pack(x[2] * f, x[3] * f)};
+                const u32x2 w = {none ? 0u : Store16<DTQ>::pack(x[0] * f * v, x[1] * f * v), none ? 0u : Store16<DTQ>::pack(x[2] * f * v, x[3] * f * v)};
                 *reinterpret_cast<u32x2*>(dst + 16 * n) = w;
             }
             if (a.lse && g == 0) a.lse[t * a.q_heads + head] = none ? -INFINITY : (last + log2f(sum)) * 0.693147180559945f;

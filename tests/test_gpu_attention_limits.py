@@ -174,3 +174,17 @@ def test_large_values_of_no_weight(new, n, low):
     fill(c, 0, k, v)
     out, lse = run(c, scale=1.0)
     assert_attention(c, out, lse, 1.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16"])
+@pytest.mark.parametrize("power", [-118, 118])
+@pytest.mark.parametrize("lens", [[(1, 500), (3, 40)], [(1, 3000), (2, 1400)], [(40, 600), (1, 70)], [(40, 3000), (1, 900)]])
+def test_value_factors_of_any_size(lens, power, dtype):
+    """A power of two in the factors of the values is the same power of two in the output, to the bit where that is a normal number."""
+    c = Paged(lens, 4, 2, 128, 16, dtype, True, seed=49)
+    ref, _ = run(c)
+    c.v_scale *= 2.0 ** power
+    out, _ = run(c)
+    want = ref.double() * 2.0 ** power
+    normal = want.abs() >= 2.0 ** -126
+    assert float(normal.double().mean()) > 0.9 and torch.equal(out.double()[normal], want[normal])
