@@ -489,7 +489,7 @@ int sasq_kv_append(const void* q, const void* k, const void* v, void* q_out,
  *   q        [tokens, q_heads, dim] 16-bit `dt`, rows q_stride elements apart;  out: the same, rows out_stride apart, written;
  *            must not overlap q
  *   lse      [tokens, q_heads] device fp32 or NULL, written: ln sum_j exp S[j], with which results over parts of the keys are joined
- *   scale    above 0, at most 2^127;  tokens * q_heads under 2^31
+ *   scale    above 0, at most 2^127;  tokens * q_heads under 2^31;  batch * heads at most 2^22 (up to 2^26 where max_kv makes few runs)
  * Sums, maxima and the softmax are fp32; probabilities are rounded to 16 bits before they multiply the values (with an int8 cache:
  * to fp16, which holds every code exactly), and the output is rounded once.  Results do not change from run to run.
  *   workspace  >= sasq_paged_attention_workspace(...) bytes, 16-byte aligned (NULL allowed when that is 0), holds partial results of split sequences

@@ -50,6 +50,12 @@ static Plan plan_of(const sasq_kv_cache* c, const sasq_kv_batch* b, int64_t q_he
     return p;
 }
 
+// Rows, and workgroups, are numbered in 32 bits.
+static bool numbered(const Plan& p, const sasq_kv_cache* c, const sasq_kv_batch* b, int64_t q_heads)
+{
+    return b->tokens * q_heads < INT64_C(1) << 31 && p.few_blocks + p.many_blocks < INT64_C(1) << 31 && b->batch * c->heads * kFewRows < INT64_C(1) << 30;
+}
+
 }  // namespace sasq
 
 using namespace sasq;
@@ -58,6 +64,7 @@ extern "C" size_t sasq_paged_attention_workspace(const sasq_kv_cache* cache, con
 {
     if (kv_check(cache, batch, q_heads, SASQ_F16) != SASQ_OK) return 0;
     const Plan p = plan_of(cache, batch, q_heads);
+    if (!numbered(p, cache, batch, q_heads)) return 0;
     return (size_t)(p.few_slots + p.many_slots) * (sizeof(float2) + sizeof(float) * cache->dim);
 }
 
@@ -70,14 +77,13 @@ extern "C" int sasq_paged_attention(const void* q, void* out, float* lse, int64_
     if (!(scale > 0.0f && scale <= 0x1p127f)) return SASQ_ERR_UNSUPPORTED;      // scale / ln 2 has to be finite too
     const int64_t dim = cache->dim, most = INT64_C(1) << 40;
     if (q_stride < q_heads * dim || out_stride < q_heads * dim || q_stride % 8 || out_stride % 8 || q_stride > most || out_stride > most) return SASQ_ERR_SHAPE;
-    if (batch->tokens * q_heads >= INT64_C(1) << 31) return SASQ_ERR_SHAPE;
+    Plan plan = plan_of(cache, batch, q_heads);
+    if (!numbered(plan, cache, batch, q_heads)) return SASQ_ERR_SHAPE;
     if (!aligned16(q) || !aligned16(out)) return SASQ_ERR_ALIGN;
     const size_t need = sasq_paged_attention_workspace(cache, batch, q_heads);
     if (need && (!workspace || workspace_bytes < need)) return SASQ_ERR_WORKSPACE;
     if (need && !aligned16(workspace)) return SASQ_ERR_ALIGN;
 
-    Plan plan = plan_of(cache, batch, q_heads);
-    if (plan.few_blocks + plan.many_blocks >= INT64_C(1) << 31 || batch->batch * cache->heads * kFewRows >= INT64_C(1) << 30) return SASQ_ERR_SHAPE;
     float* o = static_cast<float*>(workspace);                             // the sums of both kinds, then the maxima
     float2* ml = reinterpret_cast<float2*>(o + (plan.few_slots + plan.many_slots) * dim);
     plan.few.o = o;
