@@ -492,7 +492,9 @@ int sasq_kv_append(const void* q, const void* k, const void* v, void* q_out,
  *   scale    above 0, at most 2^127;  tokens * q_heads under 2^31;  batch * heads at most 2^22 (up to 2^26 where max_kv makes few runs)
  * Sums, maxima and the softmax are fp32; probabilities are rounded to 16 bits before they multiply the values (with an int8 cache:
  * to fp16, which holds every code exactly), and the output is rounded once.  Results do not change from run to run.
- *   workspace  >= sasq_paged_attention_workspace(...) bytes, 16-byte aligned (NULL allowed when that is 0), holds partial results of split sequences
+ *   workspace  >= sasq_paged_attention_workspace(...) bytes, 16-byte aligned (NULL allowed when that is 0), holds partial results of split sequences.
+ *            The size is that of one combination of batch, tokens, max_q, max_kv, max_pages and heads, to be asked for each: keys are cut into
+ *            as many runs as fill the chip, so a step of fewer sequences or tokens may need more than a larger one
  */
 size_t sasq_paged_attention_workspace(const sasq_kv_cache* cache, const sasq_kv_batch* batch, int64_t q_heads);
 int sasq_paged_attention(const void* q, void* out, float* lse, int64_t q_stride, int64_t out_stride, int64_t q_heads, float scale,
