@@ -30,7 +30,8 @@ def test_a_smaller_step_may_need_a_larger_workspace():
 
 
 def test_sequences_times_heads():
-    """Rows of all sequences and kv heads are numbered in 30 bits."""
+    """Rows of all sequences and kv heads are numbered in 30 bits, workgroups in 31."""
     c = cache(heads=64, token_stride=64 * 128, page_stride=16 * 64 * 128)
-    call = lambda n: attend(c=c, b=batch(batch=n, tokens=n, max_q=1, max_kv=1 << 20, max_pages=1 << 16), heads=64, q_stride=8192, out_stride=8192, ws=None, wsb=0)
-    assert call((1 << 20) - 1) == WORKSPACE and call(1 << 20) == SHAPE
+    call = lambda n, keys: attend(c=c, b=batch(batch=n, tokens=n, max_q=1, max_kv=keys, max_pages=1 << 16), heads=64, q_stride=8192, out_stride=8192, ws=None, wsb=0)
+    assert call((1 << 20) - 1, 4096) == WORKSPACE and call(1 << 20, 4096) == SHAPE
+    assert call(1 << 15, 1 << 20) == WORKSPACE and call(1 << 17, 1 << 20) == SHAPE                 # 2^29 and 2^31 workgroups
