@@ -21,9 +21,8 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, KvPages
     const int block = (int)blockIdx.x + first;
     const bool many = block < many_blocks;
     const AttnSplit split = many ? all_of_many : few;
-    constexpr int kAlone = 1 << 30;                       // the only row
     __shared__ float parts[4][D + 1];
-    int b, hk, r, step;
+    int b, hk, r;
     if (many) {
         const int64_t row = (int64_t)block * 4 + wave;
         const int t = (int)(row / a.q_heads), head = (int)(row % a.q_heads);
@@ -35,13 +34,11 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, KvPages
         if (b < 0 || b >= steps.batch) return;
         hk = head / a.group;
         r = (t - kv_seq(steps, b, cache.page_shift).row0) * a.group + head % a.group;
-        step = kAlone;
     } else {
         const int at = block - many_blocks;
         r = at % few_parts;
         hk = at / few_parts % cache.heads;
         b = at / few_parts / cache.heads;
-        step = few_parts;
     }
     const KvSeq seq = kv_seq(steps, b, cache.page_shift);
     const int rows = seq.rows * a.group;
@@ -87,8 +84,8 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, KvPages
             for (int e = 0; e < E; ++e) dst[e] = none ? (uint16_t)0 : Store16<DTQ>::enc(x[e] * f * v);
             if (a.lse && lane == 0) a.lse[(int64_t)t * a.q_heads + head] = none ? -INFINITY : (top + log2f(sum)) * 0.693147180559945f;
         }
-        r += step;
-    } while (LOOP && r < rows);
+        r += few_parts;
+    } while (LOOP && !many && r < rows);
 }
 
 int attention_join_launch(const AttnArgs& a, const KvPages& c, const KvSteps& s, const AttnSplit& few, const AttnSplit& many, bool join_few, bool join_many, int dim,
