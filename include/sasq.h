@@ -491,7 +491,8 @@ int sasq_kv_append(const void* q, const void* k, const void* v, void* q_out,
  *   lse      [tokens, q_heads] device fp32 or NULL, written: ln sum_j exp S[j], with which results over parts of the keys are joined
  *   scale    above 0, at most 2^127;  tokens * q_heads under 2^31;  batch * heads at most 2^22 (up to 2^26 where max_kv makes few runs)
  * Sums, maxima and the softmax are fp32; probabilities are rounded to 16 bits before they multiply the values (with an int8 cache:
- * to fp16, which holds every code exactly), and the output is rounded once.  Results do not change from run to run.
+ * to fp16, which holds every code exactly; in fp16 one under 2^-32 of the row's largest is 0), and the output is rounded once.  The sums over d
+ * and the scores may be any that fp32 holds.  Results do not change from run to run.
  *   workspace  >= sasq_paged_attention_workspace(...) bytes, 16-byte aligned (NULL allowed when that is 0), holds partial results of split sequences.
  *            The size is that of one combination of batch, tokens, max_q, max_kv, max_pages and heads, to be asked for each: keys are cut into
  *            as many runs as fill the chip, so a step of fewer sequences or tokens may need more than a larger one

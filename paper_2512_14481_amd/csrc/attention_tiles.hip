@@ -12,8 +12,9 @@
 // among them, and a tile is one block of instructions without a branch (but for masks, which only a run's last tiles have), so that products,
 // exponentials, reads and loads stand side by side.
 //
-// Measured: a chunk of 4096 tokens on 12281 of 70B 1.69 ms (1.13 PFLOP/s; the library's largest product reaches 1.59), 1.79 on 32x32x16, 1.74 with
-// eight waves and 256 rows a workgroup on it: the card is at its power limit (1.8 to 1.9 GHz of 2.4), where the 16x16 form gives more.
+// Measured: a chunk of 4096 tokens on 12281 of 70B 1.69 to 1.81 ms by card (1.14 to 1.06 PFLOP/s; the library's largest product reaches 1.59); on the
+// card with 1.69, 1.79 on 32x32x16, 1.74 with eight waves and 256 rows a workgroup on it: the card is at its power limit (1.8 to 2.1 GHz of 2.4),
+// where the 16x16 form gives more.  On an int8 cache 2.27 where it is 1.74 in 16 bits: each wave turns the codes of the whole tile to fp16.
 #include "attention.h"
 
 namespace sasq {

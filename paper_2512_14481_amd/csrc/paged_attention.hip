@@ -11,7 +11,8 @@ struct Plan {
     int64_t few_blocks, many_blocks, few_slots, many_slots;
 };
 
-// Runs of `keys` keys: `runs` of them where possible, of whole tiles, at least `least` keys each and, unless that takes more than 256 runs, at most `most`.
+// Runs of `keys` keys, of whole tiles: `runs` of them, but no more than one for every `least` keys begun (all but the last then have three quarters of that
+// at least) and, up to 256, no fewer than one for every `most`.
 static void cut(AttnSplit& s, int64_t keys, int64_t runs, int64_t least, int64_t most)
 {
     runs = std::min(runs, (keys + least - 1) / least);
@@ -28,7 +29,7 @@ static Plan plan_of(const sasq_kv_cache* c, const sasq_kv_batch* b, int64_t q_he
     const int64_t keys = std::min(b->max_kv, b->max_pages * c->page_size);
     p.tiled = rows > kFewRows;
     // Few rows: about 1024 workgroups, four or two rounds of what the chip holds at a time (512: chunks beside single tokens 107 us against
-    // 99), of 512 keys at least (one run and no join for up to 512 keys: 9.2 us for 301 keys of 7B; with 256 two runs, 10.5), and of 2048 at most,
+    // 99), one for 512 keys begun at most (up to 512 no join: 9.2 us for 301 keys of 7B; with 256 two runs, 10.5), and of 2048 keys at most,
     // so that sequences of very different lengths end at about the same time (48 of 70B with 200 to 8190 keys: 109 us, with 4096 116).
     const int64_t heads = b->batch * c->heads;
     p.few.tile_rows = kFewRows;
