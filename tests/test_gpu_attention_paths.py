@@ -5,7 +5,6 @@ from __future__ import annotations
 import math
 
 import pytest
-import torch
 
 from paper_2512_14481_amd import binding as B
 from tests.serving_ref import Paged, assert_attention
