@@ -8,6 +8,7 @@
  *   training:   x' = fakequant(x; s)                     sasq_fakequant_fwd
  *               dx, ds = backward(x, dy; s)              sasq_fakequant_bwd
  *               s <- s - lr * ds                         sasq_scale_sgd
+ *               loss, dx at the frozen output head       sasq_linear_ce
  *   inference:  Y = s * (q(X) . Wq^T) * s_w (+ bias)     sasq_static_linear
  *   set-up:     Wq, s_w from frozen fp32 weights         sasq_quantize_weight
  *               s0 = max|X| / (2^(bits-1) - 1)           sasq_absmax_scale
@@ -402,6 +403,39 @@ int sasq_prepare_bwd_weight(const void* wq, const float* s_w, void* wt, int64_t 
                             sasq_wfmt wf, sasq_dtype dt, void* stream);
 int sasq_linear_bwd_input(const void* dy, const void* wt, void* dx, float* acc_out,
                           int64_t M, int64_t N, int64_t K, sasq_dtype dt, void* stream);
+
+/*
+ * Cross entropy of a frozen output head, the loss of scale training and the measure of evaluation (Sec. 5: perplexity is exp of its mean), and
+ * the gradient that the layers' backward starts from.  For row i of x with target t = targets[i] in [0, V):
+ *     z[v] = sum_h x[i,h] W[v,h]      lse[i] = ln sum_v exp z[v]      loss[i] = lse[i] - z[t]      *mean = sum of loss / counted rows
+ *     dx[i] = scale * g[i] * (sum_v p[v] W[v] - W[t])                  p[v] = exp(z[v] - lse[i])
+ * with g[i] = row_weight[i], or 1 / counted rows (the gradient of the mean) where row_weight is NULL.  The logits are not stored: the vocabulary
+ * goes by in pieces, and both products of a piece are done before the next.  The head is frozen and has no gradient.
+ * A row whose target lies outside [0, V) is left out: loss = lse = 0, dx = 0, whatever its x holds, and no product is done for it.  No counted
+ * row: *mean = 0.
+ *   x          [T, H] device 16-bit `dt`, rows x_stride elements apart
+ *   head       W as sasq_prepare_head laid it out with SASQ_HEAD_LOGITS;  head_grad: with SASQ_HEAD_GRAD, or NULL without dx
+ *   targets    [T] device int32;  row_weight  [T] device fp32 or NULL;  scale: a factor on the gradient (loss scaling), 1 otherwise
+ *   loss       [T] device fp32, written;  lse  [T] device fp32 or NULL, written;  mean  device fp32 scalar or NULL, written
+ *   dx         [T, H] device 16-bit `dt`, rows dx_stride apart, written, or NULL: no gradient; may be x itself (with its stride)
+ *   T, V       at most 2^23;  H at most 2^20;  any sizes, multiples of 64 of H cost nothing extra
+ *   piece      columns of the vocabulary at a time, a multiple of 256, or 0: the library's choice (128 MB of the workspace)
+ *   workspace  >= sasq_linear_ce_workspace(T, V, H, dx != NULL, piece) bytes, 16-byte aligned; needs no initialisation
+ * Sums are fp32, those over a row's losses fp64; the exponentials that the gradient contracts with W are rounded to 16 bits, relative to the
+ * largest of their row but for the target's, which is kept apart: rows whose target is all but certain lose nothing.  Results do not change from
+ * run to run.  Logits must be finite.
+ *
+ * sasq_prepare_head lays W [V, H] (16-bit, rows w_stride elements apart) out for the two products, once for a head: 1 KB blocks of 16 rows x 32
+ * columns as in sasq_prepare_bwd_weight, rows v and columns h (SASQ_HEAD_LOGITS), or rows h and columns v (SASQ_HEAD_GRAD), the columns padded to
+ * 64 and the rows to 16 with zeros.  sasq_head_bytes is a pure host function; 0 for sizes that are not supported.
+ */
+typedef enum { SASQ_HEAD_LOGITS = 0, SASQ_HEAD_GRAD = 1 } sasq_head_form;
+size_t sasq_head_bytes(int64_t V, int64_t H, sasq_head_form form);
+int sasq_prepare_head(const void* w, int64_t w_stride, void* head, int64_t V, int64_t H, sasq_head_form form, sasq_dtype dt, void* stream);
+size_t sasq_linear_ce_workspace(int64_t T, int64_t V, int64_t H, int grad, int64_t piece);
+int sasq_linear_ce(const void* x, int64_t x_stride, const void* head, const void* head_grad, const int32_t* targets,
+                   const float* row_weight, float scale, float* loss, float* lse, float* mean, void* dx, int64_t dx_stride,
+                   int64_t T, int64_t V, int64_t H, int64_t piece, sasq_dtype dt, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Bytes of workspace sasq_absmax_scale needs (pure function, host only). */
 size_t sasq_absmax_scale_workspace(int64_t rows, int64_t cols);

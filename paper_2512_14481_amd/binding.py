@@ -30,6 +30,8 @@ SASQ_W_INT8, SASQ_W_INT4_PACKED, SASQ_W_INT8_BLOCKED, SASQ_W_INT4_BLOCKED = 0, 1
 SASQ_KV_16, SASQ_KV_INT8 = 0, 1
 SASQ_ROPE_HALVES, SASQ_ROPE_PAIRS = 0, 1
 
+SASQ_HEAD_LOGITS, SASQ_HEAD_GRAD = 0, 1
+
 SASQ_MAX_BATCH = 8
 
 _DT = {torch.float16: SASQ_F16, torch.bfloat16: SASQ_BF16}
@@ -160,6 +162,12 @@ def _lib() -> ctypes.CDLL:
         L.sasq_bwd_weight_bytes.argtypes = [i64, i64]
         L.sasq_prepare_bwd_weight.argtypes = [vp, vp, vp, i64, i64, i32, i32, vp]
         L.sasq_linear_bwd_input.argtypes = [vp, vp, vp, vp, i64, i64, i64, i32, vp]
+        L.sasq_head_bytes.restype = sz
+        L.sasq_head_bytes.argtypes = [i64, i64, i32]
+        L.sasq_prepare_head.argtypes = [vp, i64, vp, i64, i64, i32, i32, vp]
+        L.sasq_linear_ce_workspace.restype = sz
+        L.sasq_linear_ce_workspace.argtypes = [i64, i64, i64, i32, i64]
+        L.sasq_linear_ce.argtypes = [vp, i64] + [vp] * 4 + [f32] + [vp] * 4 + [i64] * 5 + [i32, vp, sz, vp]
         L.sasq_absmax_scale_workspace.restype = sz
         L.sasq_absmax_scale_workspace.argtypes = [i64, i64]
         L.sasq_absmax_scale.argtypes = [vp, vp, i64, i64, i32, i32, vp, sz, vp]
@@ -602,6 +610,62 @@ def sasq_linear_bwd_input(dy: torch.Tensor, wt: torch.Tensor, dx: torch.Tensor, 
         raise ValueError("wt must have sasq_bwd_weight_bytes(N, K) bytes")
     _check(_lib().sasq_linear_bwd_input(_ptr(dy), _ptr(wt), _ptr(dx), _ptr(acc_out), M, N, K, _dt(dy), _stream()),
            "sasq_linear_bwd_input")
+
+
+def _row_stride(t: torch.Tensor, name: str) -> int:
+    """The distance of the rows of a [rows, cols] operand in elements."""
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be a matrix, got {tuple(t.shape)}")
+    if not t.is_cuda:
+        raise ValueError("SASQ entry points take device tensors")
+    if t.stride(1) != 1 and t.shape[1] > 1:
+        raise ValueError(f"the elements of a row of {name} must be next to each other")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def sasq_head_bytes(V: int, H: int, form: int) -> int:
+    return int(_lib().sasq_head_bytes(V, H, form))
+
+
+def sasq_prepare_head(w: torch.Tensor, head: torch.Tensor, form: int) -> None:
+    """w: [V, H], rows may be apart; head: sasq_head_bytes(V, H, form) bytes, written."""
+    stride = _row_stride(w, "w")
+    V, H = w.shape
+    if head.numel() * head.element_size() != sasq_head_bytes(V, H, form):
+        raise ValueError("head must have sasq_head_bytes(V, H, form) bytes")
+    _check(_lib().sasq_prepare_head(_at(w), stride, _ptr(head), V, H, form, _dt(w), _stream()), "sasq_prepare_head")
+
+
+def sasq_linear_ce_workspace(T: int, V: int, H: int, grad: bool, piece: int = 0) -> int:
+    return int(_lib().sasq_linear_ce_workspace(T, V, H, int(grad), piece))
+
+
+def sasq_linear_ce(x: torch.Tensor, head: torch.Tensor, targets: torch.Tensor, loss: torch.Tensor, V: int, workspace: torch.Tensor,
+                   lse: Optional[torch.Tensor] = None, mean: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None,
+                   head_grad: Optional[torch.Tensor] = None, row_weight: Optional[torch.Tensor] = None, scale: float = 1.0,
+                   piece: int = 0) -> None:
+    """x, dx: [T, H], rows may be apart; targets: [T] int32; loss, lse, row_weight: [T] float32; mean: one float32.  head, head_grad: the
+    layouts that sasq_prepare_head made of a [V, H] head (head_grad goes with dx)."""
+    x_stride, dx_stride = _row_stride(x, "x"), 0 if dx is None else _row_stride(dx, "dx")
+    T, H = x.shape
+    if dx is not None and (dx.shape != x.shape or dx.dtype != x.dtype):
+        raise ValueError("dx must match x")
+    if dx is not None and head_grad is None:
+        raise ValueError("dx goes with head_grad")
+    _want(targets, torch.int32, "targets")
+    for t, n, name in ((loss, T, "loss"), (lse, T, "lse"), (mean, 1, "mean"), (row_weight, T, "row_weight")):
+        _want(t, torch.float32, name)
+        if t is not None and t.numel() != n:
+            raise ValueError(f"{name} must have {n} elements")
+    if targets.numel() != T:
+        raise ValueError("targets must have one element per row of x")
+    if head.numel() * head.element_size() != sasq_head_bytes(V, H, SASQ_HEAD_LOGITS):
+        raise ValueError("head must have sasq_head_bytes(V, H, SASQ_HEAD_LOGITS) bytes")
+    if head_grad is not None and head_grad.numel() * head_grad.element_size() != sasq_head_bytes(V, H, SASQ_HEAD_GRAD):
+        raise ValueError("head_grad must have sasq_head_bytes(V, H, SASQ_HEAD_GRAD) bytes")
+    _check(_lib().sasq_linear_ce(_at(x), x_stride, _ptr(head), _ptr(head_grad), _ptr(targets), _ptr(row_weight), ctypes.c_float(scale), _ptr(loss),
+                                 _ptr(lse), _ptr(mean), _at(dx), dx_stride, T, V, H, piece, _dt(x), _ptr(workspace),
+                                 workspace.numel() * workspace.element_size(), _stream()), "sasq_linear_ce")
 
 
 def sasq_absmax_scale_workspace(rows: int, cols: int) -> int:

@@ -1,0 +1,62 @@
+// Cross entropy of a frozen output head (sasq_linear_ce): what its kernels share.
+//
+// Row i (of the counted ones, packed together), vocabulary entry v, target t:  z_v = x . W_v.  With lg = log2(e) and any number M of the row
+//     a_v = 2^(z_v lg - M) for v != t,   S = sum a_v,   d = ln(sum_{v != t} e^{z_v}) - z_t = (M + log2 S - z_t lg) / lg
+//     loss = ln(1 + e^d)     lse = z_t + loss     u = 1 - p_t = 1 / (1 + e^-d)
+//     dx = g u (sum a_v W_v / S - W_t)
+// The target is kept out of the sums, so that nothing cancels in a row whose target is all but certain.  The vocabulary goes by in pieces:
+//     logits GEMM   z of a piece; each wave reduces its rows over its columns to (M, S), with M a whole number, and stores a_v in 16 bits
+//     join          M of the row so far: the running sums are scaled by 2^(M_old - M), and so (exactly) are the a_v of every wave's columns
+//     gradient GEMM the running sums over v of a_v W_v, fp32
+// and at last one kernel divides, subtracts W_t and rounds.  A pass costs the two products that the formulas have and no third; the logits
+// themselves are never stored.
+#pragma once
+
+#include "gemm_tile.h"
+
+namespace sasq {
+
+constexpr float kLog2e = 1.44269504088896340736f, kLog2eLow = 1.92596299112661746887e-8f;    // their sum is log2(e) to 49 bits
+constexpr float kLn2 = 0.693147180559945309417f;
+
+// 16-bit a_v are at most 2^kTopExp: fp16 has 2^-24 .. 2^15 to offer, bf16 the exponents of fp32.
+template <int DT> constexpr int kTopExp = DT == SASQ_F16 ? 15 : 0;
+
+struct RowStat { float m, s; };                 // M (a whole number; -inf: no column yet) and S
+
+struct CeArgs {
+    // sizes
+    int64_t T, V, H;
+    int Hp, Vp;                                 // H and V in whole multiples of 64
+    int piece, splits;                          // columns of a piece, parts that its contraction is cut into
+    int tile, grad_tile;                        // 0: 256x256, 1: 128x256, 2: 128x128
+    bool grad;
+    // operands
+    const void* x; int64_t x_stride;
+    const uint8_t* head; const uint8_t* head_grad;
+    const int32_t* targets;
+    const float* row_weight; float scale;
+    float* loss; float* lse; float* mean;
+    void* dx; int64_t dx_stride;
+    // workspace
+    int32_t* count;                             // counted rows
+    int32_t* pos;                               // [T] place of a row among them, -1: left out
+    int32_t* row;                               // [T] packed: the row
+    int32_t* tgt;                               // [T] packed: target
+    float* zt;                                  // [T] packed: z_t
+    RowStat* run;                               // [T] packed: M and S of the pieces so far
+    float* beta;                                // [T] packed: 2^(M_old - M)
+    float* coef;                                // [T] packed: u / S
+    float* u;                                   // [T] packed: u
+    float* row_loss;                            // [T] packed: loss, for the mean
+    RowStat* stats;                             // [columns of a piece / stat_cols][T]
+    uint16_t* xs;                               // [T][Hp] packed rows of x, zeros past H
+    uint16_t* a;                                // [T][piece]
+    float* acc;                                 // [splits][T][Hp]
+};
+constexpr int stat_cols(int tile) { return tile == 2 ? 64 : 128; }     // half a tile's columns: what a wave has
+
+void launch_ce_logits(const CeArgs& c, sasq_dtype dt, int64_t col0, int64_t cols, hipStream_t st);
+void launch_ce_grad(const CeArgs& c, sasq_dtype dt, int64_t col0, int64_t cols, hipStream_t st);
+
+}  // namespace sasq

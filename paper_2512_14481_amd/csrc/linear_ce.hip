@@ -1,0 +1,429 @@
+// Cross entropy of a frozen output head (linear_ce.h): laying the head out, the rows that count, the steps between the two products, entry points.
+#include "sasq_device.h"
+#include "gemm_tile.h"
+#include "linear_ce.h"
+#include <math.h>
+
+namespace sasq {
+
+constexpr int64_t kCeMaxTokens = INT64_C(1) << 23, kCeMaxVocab = INT64_C(1) << 23, kCeMaxHidden = INT64_C(1) << 20;
+constexpr int64_t kCeMaxProduct = INT64_C(1) << 37;                 // elements of x and of the head
+constexpr int kPieceStep = 256;
+
+static int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
+
+// ---- the head's two layouts: 1 KB blocks of 16 rows x 32 columns, chunks swizzled as in every operand of the GEMMs ----
+__device__ __forceinline__ uint16_t head_at(const uint16_t* w, int64_t stride, int64_t v, int64_t h, int64_t V, int64_t H)
+{
+    return v < V && h < H ? w[v * stride + h] : (uint16_t)0;
+}
+
+// Rows v, columns h.  A thread takes one 16-byte chunk.
+__global__ __launch_bounds__(256) void head_logits_kernel(const uint16_t* __restrict__ w, int64_t stride, u32x4* __restrict__ out, int64_t V, int64_t H,
+                                                         int64_t kt, int64_t chunks, bool vec)
+{
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < chunks; i += (int64_t)gridDim.x * 256) {
+        const int64_t block = i >> 6;
+        const int r = (int)(i & 63) >> 2, c = ((int)i & 3) ^ swz64(r);
+        const int64_t v = block / kt * 16 + r, h = block % kt * 32 + 8 * c;
+        u32x4 o = {0u, 0u, 0u, 0u};
+        if (vec && v < V && h + 8 <= H) {
+            o = *reinterpret_cast<const u32x4*>(w + v * stride + h);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                o[e] = head_at(w, stride, v, h + 2 * e, V, H) | (uint32_t)head_at(w, stride, v, h + 2 * e + 1, V, H) << 16;
+        }
+        out[i] = o;
+    }
+}
+
+// Rows h, columns v: 64 x 64 elements at a time through LDS.
+__global__ __launch_bounds__(256) void head_grad_kernel(const uint16_t* __restrict__ w, int64_t stride, u32x4* __restrict__ out, int64_t V, int64_t H,
+                                                       int64_t hb, int64_t kt, int64_t tiles, bool vec)
+{
+    __shared__ uint16_t tile[64][64 + 8];
+    const int64_t tiles_h = (H + 63) / 64;
+    for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
+        const int64_t v0 = t / tiles_h * 64, h0 = t % tiles_h * 64;
+        __syncthreads();
+        for (int i = threadIdx.x; i < 64 * 8; i += 256) {
+            const int r = i >> 3, c = (i & 7) * 8;
+            const int64_t v = v0 + r, h = h0 + c;
+            u32x4 o = {0u, 0u, 0u, 0u};
+            if (vec && v < V && h + 8 <= H) {
+                o = *reinterpret_cast<const u32x4*>(w + v * stride + h);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    o[e] = head_at(w, stride, v, h + 2 * e, V, H) | (uint32_t)head_at(w, stride, v, h + 2 * e + 1, V, H) << 16;
+            }
+            *reinterpret_cast<u32x4*>(&tile[r][c]) = o;
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < 8 * 64; i += 256) {                      // 4 x 2 blocks of 64 chunks
+            const int b = i >> 6, r = (i & 63) >> 2, c = (i & 3) ^ swz64(r);
+            const int h = (b >> 1) * 16 + r, v = (b & 1) * 32 + 8 * c;
+            const int64_t hblock = (h0 >> 4) + (b >> 1);
+            if (hblock >= hb) continue;
+            u32x4 o;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = tile[v + 2 * e][h] | (uint32_t)tile[v + 2 * e + 1][h] << 16;
+            out[(hblock * kt + (v0 >> 5) + (b & 1)) * 64 + (i & 63)] = o;
+        }
+    }
+}
+
+// ---- the rows that count, packed together ----
+constexpr int kPackThreads = 1024;
+__global__ __launch_bounds__(kPackThreads) void ce_pack_kernel(const int32_t* __restrict__ targets, int T, int V, int32_t* __restrict__ count,
+                                                              int32_t* __restrict__ pos, int32_t* __restrict__ row, int32_t* __restrict__ tgt,
+                                                              RowStat* __restrict__ run, float* __restrict__ loss, float* __restrict__ lse)
+{
+    __shared__ int wave_count[kPackThreads / kWave];
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    int base = 0;
+    for (int r0 = 0; r0 < T; r0 += kPackThreads) {
+        const int r = r0 + t;
+        const int v = r < T ? targets[r] : -1;
+        const bool counts = v >= 0 && v < V;
+        const uint64_t mask = __builtin_amdgcn_ballot_w64(counts);
+        if (lane == 0) wave_count[wave] = __popcll(mask);
+        __syncthreads();
+        int before = 0, all = 0;
+#pragma unroll
+        for (int w = 0; w < kPackThreads / kWave; ++w) {
+            before += w < wave ? wave_count[w] : 0;
+            all += wave_count[w];
+        }
+        __syncthreads();
+        if (counts) {
+            const int p = base + before + __popcll(mask & ((UINT64_C(1) << lane) - 1));
+            pos[r] = p;
+            row[p] = r;
+            tgt[p] = v;
+            run[p] = RowStat{0.0f, 0.0f};
+        } else if (r < T) {
+            pos[r] = -1;
+            loss[r] = 0.0f;
+            if (lse) lse[r] = 0.0f;
+        }
+        base += all;
+    }
+    if (t == 0) *count = base;
+}
+
+// A wave copies one counted row of x to its packed place, with zeros past H.
+template <bool VEC>
+__global__ __launch_bounds__(256) void ce_stage_kernel(const uint16_t* __restrict__ x, int64_t stride, uint16_t* __restrict__ xs, const int32_t* __restrict__ count,
+                                                      const int32_t* __restrict__ row, int H, int Hp)
+{
+    const int p = (int)blockIdx.x * 4 + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (p >= *count) return;
+    const uint16_t* src = x + (int64_t)row[p] * stride;
+    uint16_t* dst = xs + (int64_t)p * Hp;
+    for (int h = lane * 8; h < Hp; h += 512) {
+        u32x4 o = {0u, 0u, 0u, 0u};
+        if (VEC && h < H) {
+            o = *reinterpret_cast<const u32x4*>(src + h);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t lo = h + 2 * e < H ? src[h + 2 * e] : 0u, hi = h + 2 * e + 1 < H ? src[h + 2 * e + 1] : 0u;
+                o[e] = lo | hi << 16;
+            }
+        }
+        *reinterpret_cast<u32x4*>(dst + h) = o;
+    }
+}
+
+// ---- between the products: M and S of each row so far ----
+// 16 rows a workgroup, 16 threads a row, each for every sixteenth group of columns.  The factors 2^(M_old - M) are exact.
+constexpr int kJoinRows = 16, kJoinLanes = 16;
+__global__ __launch_bounds__(256) void ce_join_kernel(const RowStat* __restrict__ stats, int groups, int64_t T, const int32_t* __restrict__ count,
+                                                     RowStat* __restrict__ run, float* __restrict__ beta, const float* __restrict__ zt,
+                                                     const int32_t* __restrict__ row, float* __restrict__ coef, float* __restrict__ u_out,
+                                                     float* __restrict__ row_loss, float* __restrict__ loss, float* __restrict__ lse, int last)
+{
+    __shared__ float part[kJoinLanes][kJoinRows];
+    const int r = threadIdx.x % kJoinRows, k = threadIdx.x / kJoinRows, p = (int)blockIdx.x * kJoinRows + r;
+    const int n = *count;
+    if ((int)blockIdx.x * kJoinRows >= n) return;
+    const RowStat* mine = stats + min(p, n - 1);
+    const RowStat old = run[min(p, n - 1)];
+    float top = -__builtin_inff();
+    for (int g = k; g < groups; g += kJoinLanes) {
+        const RowStat s = mine[(int64_t)g * T];
+        if (s.s != 0.0f) top = fmaxf(top, s.m);
+    }
+    part[k][r] = top;
+    __syncthreads();
+    float m = old.s != 0.0f ? old.m : -__builtin_inff();
+#pragma unroll
+    for (int j = 0; j < kJoinLanes; ++j) m = fmaxf(m, part[j][r]);
+    if (m == -__builtin_inff()) m = 0.0f;
+    __syncthreads();
+    float sum = 0.0f;
+    for (int g = k; g < groups; g += kJoinLanes) {
+        const RowStat s = mine[(int64_t)g * T];
+        if (s.s != 0.0f) sum += s.s * exp2f(s.m - m);
+    }
+    part[k][r] = sum;
+    __syncthreads();
+    if (k != 0 || p >= n) return;
+    const float f = old.s != 0.0f ? exp2f(old.m - m) : 0.0f;
+    float all = old.s * f;
+#pragma unroll
+    for (int j = 0; j < kJoinLanes; ++j) all += part[j][r];
+    run[p] = RowStat{m, all};
+    beta[p] = f;
+    if (!last) return;
+    // In fp64: a small loss is the exponential of a difference.
+    const double z = (double)zt[p];
+    const double d = all == 0.0f ? -(double)__builtin_inff() : ((double)m + log2((double)all)) * 0.69314718055994530942 - z;
+    const double l = d > 0.0 ? d + log1p(exp(-d)) : log1p(exp(d));
+    const double u = 1.0 / (1.0 + exp(-d));
+    loss[row[p]] = (float)l;
+    row_loss[p] = (float)l;
+    if (lse) lse[row[p]] = (float)(z + l);
+    u_out[p] = (float)u;
+    coef[p] = all == 0.0f ? 0.0f : (float)(u / (double)all);
+}
+
+// a_v of a group of columns from its M to the row's, in place.
+template <int DT>
+__global__ __launch_bounds__(256) void ce_scale_kernel(uint16_t* __restrict__ a, int64_t pitch, int cols, int stat_cols, const RowStat* __restrict__ stats,
+                                                      const RowStat* __restrict__ run, int64_t T, const int32_t* __restrict__ count)
+{
+    using S = Store16<DT>;
+    const int p = (int)blockIdx.x;
+    if (p >= *count) return;
+    const float m = run[p].m;
+    for (int c = threadIdx.x * 8; c < cols; c += 256 * 8) {
+        const float f = exp2f(stats[(int64_t)(c / stat_cols) * T + p].m - m);
+        u32x4* at = reinterpret_cast<u32x4*>(a + (int64_t)p * pitch + c);
+        u32x4 v = *at;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = S::pack(S::lo(v[e]) * f, S::hi(v[e]) * f);
+        *at = v;
+    }
+}
+
+// ---- the end: dx of every row; left-out ones are 0 ----
+template <int DT, bool VEC>
+__global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ acc, int splits, int64_t T, const int32_t* __restrict__ count,
+                                                   const int32_t* __restrict__ pos, const int32_t* __restrict__ tgt, const float* __restrict__ coef,
+                                                   const float* __restrict__ u, const uint8_t* __restrict__ head, const float* __restrict__ row_weight,
+                                                   float scale, uint16_t* __restrict__ dx, int64_t stride, int H, int Hp)
+{
+    using S = Store16<DT>;
+    const int r = (int)blockIdx.x;
+    const int p = pos[r];
+    float g = 0.0f, cf = 0.0f, uu = 0.0f;
+    int t = 0;
+    if (p >= 0) {
+        g = scale * (row_weight ? row_weight[r] : 1.0f / (float)*count);
+        cf = coef[p];
+        uu = u[p];
+        t = tgt[p];
+    }
+    const int tr = t & 15;
+    const uint8_t* blocks = head + (int64_t)(t >> 4) * (Hp / 32) * 1024 + tr * 64;
+    for (int h = threadIdx.x * 8; h < H; h += 256 * 8) {
+        float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (p >= 0) {
+            for (int s = 0; s < splits; ++s) {
+                const float* at = acc + ((int64_t)s * T + p) * Hp + h;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] += at[e];
+            }
+            const u32x4 w = *reinterpret_cast<const u32x4*>(blocks + (int64_t)(h >> 5) * 1024 + ((((h >> 3) & 3) ^ swz64(tr)) << 4));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = g * __builtin_fmaf(cf, v[e], -uu * ((e & 1) ? S::hi(w[e >> 1]) : S::lo(w[e >> 1])));
+        }
+        uint16_t* dst = dx + (int64_t)r * stride + h;
+        if (VEC) {
+            *reinterpret_cast<u32x4*>(dst) = u32x4{S::pack(v[0], v[1]), S::pack(v[2], v[3]), S::pack(v[4], v[5]), S::pack(v[6], v[7])};
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (h + e < H) dst[e] = S::enc(v[e]);
+        }
+    }
+}
+
+// Mean over the counted rows, fp64, in a fixed order.
+__global__ __launch_bounds__(1024) void ce_mean_kernel(const float* __restrict__ row_loss, const int32_t* __restrict__ count, float* __restrict__ mean)
+{
+    __shared__ double part[16];
+    const int n = *count;
+    double sum = 0.0;
+    for (int p = threadIdx.x; p < n; p += 1024) sum += (double)row_loss[p];
+    sum = wave_sum(sum);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x) return;
+    double all = 0.0;
+    for (int w = 0; w < 16; ++w) all += part[w];
+    *mean = n ? (float)(all / (double)n) : 0.0f;
+}
+
+// ---- plan ----
+// Columns of a piece: 128 MB of a_v, at least 256.
+static int64_t ce_piece(int64_t T, int64_t V)
+{
+    int64_t most = (INT64_C(1) << 26) / T / kPieceStep * kPieceStep;
+    if (most < kPieceStep) most = kPieceStep;
+    const int64_t pieces = (V + most - 1) / most;
+    return up((V + pieces - 1) / pieces, kPieceStep);
+}
+
+static int ce_tile(int64_t M, int64_t N)
+{
+    auto tiles = [&](int64_t bm, int64_t bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
+    const int64_t t128 = tiles(128, 128), rest = t128 % 512;
+    const double c0 = (double)((tiles(256, 256) + 255) / 256), c1 = 0.68 * (double)((tiles(128, 256) + 255) / 256);
+    const double c2 = 0.8 * (double)(t128 / 512) + (rest == 0 ? 0.0 : rest <= 256 ? 0.44 : 0.8);
+    return c0 <= c1 && c0 <= c2 ? 0 : c1 < c2 ? 1 : 2;
+}
+
+// Sizes and the workspace's parts, from `base` (0: only how long they are).
+static size_t ce_plan(CeArgs& c, int64_t piece, char* base)
+{
+    c.Hp = (int)up(c.H, 64);
+    c.Vp = (int)up(c.V, 64);
+    c.piece = (int)(piece ? (piece < up(c.V, kPieceStep) ? piece : up(c.V, kPieceStep)) : ce_piece(c.T, c.V));
+    c.tile = ce_tile(c.T, c.piece);
+    c.grad_tile = ce_tile(c.T, c.H);
+    const int64_t bm = c.grad_tile == 0 ? 256 : 128, bn = c.grad_tile == 2 ? 128 : 256;
+    const int64_t tiles = ((c.T + bm - 1) / bm) * ((c.H + bn - 1) / bn), slots = c.grad_tile == 2 ? 512 : 256;
+    int64_t splits = slots / tiles;
+    if (splits > c.piece / 512) splits = c.piece / 512;
+    c.splits = (int)(splits < 1 ? 1 : splits);
+    size_t at = 0;
+    auto part = [&](auto*& p, size_t bytes) {
+        p = reinterpret_cast<std::remove_reference_t<decltype(p)>>(base + at);
+        at += (bytes + 255) / 256 * 256;
+    };
+    const size_t T = (size_t)c.T;
+    part(c.count, 4);
+    part(c.pos, T * 4);
+    part(c.row, T * 4);
+    part(c.tgt, T * 4);
+    part(c.zt, T * 4);
+    part(c.run, T * 8);
+    part(c.beta, T * 4);
+    part(c.coef, T * 4);
+    part(c.u, T * 4);
+    part(c.row_loss, T * 4);
+    part(c.stats, (size_t)(c.piece / stat_cols(c.tile)) * T * 8);
+    part(c.xs, T * (size_t)c.Hp * 2);
+    if (c.grad) {
+        part(c.a, T * (size_t)c.piece * 2);
+        part(c.acc, (size_t)c.splits * T * (size_t)c.Hp * 4);
+    }
+    return at;
+}
+
+static bool ce_sizes_ok(int64_t T, int64_t V, int64_t H, int64_t piece)
+{
+    return T > 0 && V > 0 && H > 0 && T <= kCeMaxTokens && V <= kCeMaxVocab && H <= kCeMaxHidden && up(H, 64) <= kCeMaxProduct / T &&
+           up(H, 64) <= kCeMaxProduct / V && piece >= 0 && piece % kPieceStep == 0;
+}
+
+template <int DT>
+static void ce_run(const CeArgs& c, sasq_dtype dt, hipStream_t st)
+{
+    const int T = (int)c.T, H = (int)c.H;
+    ce_pack_kernel<<<1, kPackThreads, 0, st>>>(c.targets, T, (int)c.V, c.count, c.pos, c.row, c.tgt, c.run, c.loss, c.lse);
+    if (c.x_stride % 8 == 0 && H % 8 == 0)
+        ce_stage_kernel<true><<<(T + 3) / 4, 256, 0, st>>>(static_cast<const uint16_t*>(c.x), c.x_stride, c.xs, c.count, c.row, H, c.Hp);
+    else
+        ce_stage_kernel<false><<<(T + 3) / 4, 256, 0, st>>>(static_cast<const uint16_t*>(c.x), c.x_stride, c.xs, c.count, c.row, H, c.Hp);
+    const int sc = stat_cols(c.tile), bn = 2 * sc;
+    for (int64_t col0 = 0; col0 < c.V; col0 += c.piece) {
+        const int64_t cols = c.V - col0 < c.piece ? c.V - col0 : c.piece;
+        const int groups = (int)((cols + bn - 1) / bn) * 2;
+        launch_ce_logits(c, dt, col0, cols, st);
+        ce_join_kernel<<<(T + kJoinRows - 1) / kJoinRows, 256, 0, st>>>(c.stats, groups, c.T, c.count, c.run, c.beta, c.zt, c.row, c.coef, c.u, c.row_loss,
+                                                                       c.loss, c.lse, col0 + cols >= c.V);
+        if (c.grad) {
+            ce_scale_kernel<DT><<<T, 256, 0, st>>>(c.a, c.piece, (int)up(cols, 64), sc, c.stats, c.run, c.T, c.count);
+            launch_ce_grad(c, dt, col0, cols, st);
+        }
+    }
+    if (c.grad) {
+        if (c.dx_stride % 8 == 0 && H % 8 == 0)
+            ce_dx_kernel<DT, true><<<T, 256, 0, st>>>(c.acc, c.splits, c.T, c.count, c.pos, c.tgt, c.coef, c.u, c.head, c.row_weight, c.scale,
+                                                      static_cast<uint16_t*>(c.dx), c.dx_stride, H, c.Hp);
+        else
+            ce_dx_kernel<DT, false><<<T, 256, 0, st>>>(c.acc, c.splits, c.T, c.count, c.pos, c.tgt, c.coef, c.u, c.head, c.row_weight, c.scale,
+                                                       static_cast<uint16_t*>(c.dx), c.dx_stride, H, c.Hp);
+    }
+    if (c.mean) ce_mean_kernel<<<1, 1024, 0, st>>>(c.row_loss, c.count, c.mean);
+}
+
+}  // namespace sasq
+
+using namespace sasq;
+
+extern "C" size_t sasq_head_bytes(int64_t V, int64_t H, sasq_head_form form)
+{
+    if (V <= 0 || H <= 0 || V > kCeMaxVocab || H > kCeMaxHidden || up(H, 64) > kCeMaxProduct / V) return 0;
+    if (form == SASQ_HEAD_LOGITS) return (size_t)up(V, 16) * (size_t)up(H, 64) * 2;
+    if (form == SASQ_HEAD_GRAD) return (size_t)up(V, 64) * (size_t)up(H, 16) * 2;
+    return 0;
+}
+
+extern "C" int sasq_prepare_head(const void* w, int64_t w_stride, void* head, int64_t V, int64_t H, sasq_head_form form, sasq_dtype dt, void* stream)
+{
+    if (!w || !head) return SASQ_ERR_NULL;
+    if (form != SASQ_HEAD_LOGITS && form != SASQ_HEAD_GRAD) return SASQ_ERR_UNSUPPORTED;
+    if (dt != SASQ_F16 && dt != SASQ_BF16) return SASQ_ERR_UNSUPPORTED;
+    if (sasq_head_bytes(V, H, form) == 0 || w_stride < H) return SASQ_ERR_SHAPE;
+    if (!aligned16(w) || !aligned16(head)) return SASQ_ERR_ALIGN;
+    hipStream_t st = as_stream(stream);
+    auto W = static_cast<const uint16_t*>(w);
+    auto O = static_cast<u32x4*>(head);
+    const bool vec = w_stride % 8 == 0;
+    if (form == SASQ_HEAD_LOGITS) {
+        const int64_t kt = up(H, 64) / 32, chunks = up(V, 16) / 16 * kt * 64, blocks = (chunks + 255) / 256;
+        head_logits_kernel<<<(int)(blocks < 8192 ? blocks : 8192), 256, 0, st>>>(W, w_stride, O, V, H, kt, chunks, vec);
+    } else {
+        const int64_t tiles = up(V, 64) / 64 * (up(H, 64) / 64);
+        head_grad_kernel<<<(int)(tiles < 8192 ? tiles : 8192), 256, 0, st>>>(W, w_stride, O, V, H, up(H, 16) / 16, up(V, 64) / 32, tiles, vec);
+    }
+    return hipGetLastError() == hipSuccess ? SASQ_OK : SASQ_ERR_LAUNCH;
+}
+
+extern "C" size_t sasq_linear_ce_workspace(int64_t T, int64_t V, int64_t H, int grad, int64_t piece)
+{
+    if (!ce_sizes_ok(T, V, H, piece)) return 0;
+    CeArgs c{};
+    c.T = T; c.V = V; c.H = H; c.grad = grad != 0;
+    return ce_plan(c, piece, nullptr);
+}
+
+extern "C" int sasq_linear_ce(const void* x, int64_t x_stride, const void* head, const void* head_grad, const int32_t* targets,
+                              const float* row_weight, float scale, float* loss, float* lse, float* mean, void* dx, int64_t dx_stride,
+                              int64_t T, int64_t V, int64_t H, int64_t piece, sasq_dtype dt, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!x || !head || !targets || !loss || (dx && !head_grad)) return SASQ_ERR_NULL;
+    if (!ce_sizes_ok(T, V, H, piece) || x_stride < H || (dx && dx_stride < H)) return SASQ_ERR_SHAPE;
+    if (dt != SASQ_F16 && dt != SASQ_BF16) return SASQ_ERR_UNSUPPORTED;
+    if (!aligned16(x) || !aligned16(head) || (dx && (!aligned16(dx) || !aligned16(head_grad)))) return SASQ_ERR_ALIGN;
+    if (!workspace || workspace_bytes < sasq_linear_ce_workspace(T, V, H, dx != nullptr, piece)) return SASQ_ERR_WORKSPACE;
+    if (!aligned16(workspace)) return SASQ_ERR_ALIGN;
+    CeArgs c{};
+    c.T = T; c.V = V; c.H = H; c.grad = dx != nullptr;
+    c.x = x; c.x_stride = x_stride;
+    c.head = static_cast<const uint8_t*>(head); c.head_grad = static_cast<const uint8_t*>(head_grad);
+    c.targets = targets; c.row_weight = row_weight; c.scale = scale;
+    c.loss = loss; c.lse = lse; c.mean = mean;
+    c.dx = dx; c.dx_stride = dx_stride;
+    ce_plan(c, piece, static_cast<char*>(workspace));
+    hipStream_t st = as_stream(stream);
+    if (dt == SASQ_F16) ce_run<SASQ_F16>(c, dt, st);
+    else                ce_run<SASQ_BF16>(c, dt, st);
+    return hipGetLastError() == hipSuccess ? SASQ_OK : SASQ_ERR_LAUNCH;
+}

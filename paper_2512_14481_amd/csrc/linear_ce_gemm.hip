@@ -1,0 +1,248 @@
+// The two products of sasq_linear_ce (linear_ce.h) on the tile body of the 16-bit GEMMs (gemm_k64_body.h).
+#include "sasq_device.h"
+#include "gemm_tile.h"
+#include "gemm_k64_body.h"
+#include "linear_ce.h"
+
+namespace sasq {
+
+// The tile of a workgroup among those of the rows that count, whose number only the device knows: the mapping of tile_of_block, ids past the
+// last tile have nothing to do.
+__device__ __forceinline__ bool tile_of_counted(int tiles_m, int tiles_n, int& tm, int& tn)
+{
+    const int per = (tiles_m * tiles_n + 7) >> 3;
+    return (int)(blockIdx.x >> 3) < per && tile_of_block((int)blockIdx.x, tiles_m, tiles_n, tm, tn);
+}
+
+// ---- logits: z of a tile, reduced and stored as a_v ----
+template <int DT, bool GRAD>
+struct LogitsExt {
+    static constexpr bool kOn = true;
+    int x_pitch, w_kt;
+    const int32_t* tgt;
+    float* zt;
+    RowStat* stats;
+    int64_t T;                                  // rows of `stats`
+    uint16_t* a;
+    int64_t a_pitch;
+    int col0;                                   // first column of the piece
+
+    // Lane (fq, frow) of a wave holds, for each of its MF rows b * 16 + frow, the columns 16 g + 4 fq + e: a row's columns lie in the four lanes
+    // of equal frow.
+    template <int BM, int BN, class ACC>
+    __device__ __forceinline__ void finish(ACC& acc, int m0, int n0, int M, int N, char* lds) const
+    {
+        using S = Store16<DT>;
+        constexpr int MF = BM / 32, NF = BN / 32, kStride = BN + 16;
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int wm = wave & 1, wn = wave >> 1, frow = lane & 15, fq = lane >> 4;
+        const int wn0 = n0 + wn * (BN / 2), wm0 = m0 + wm * (BM / 2);
+        const bool edge = wn0 + BN / 2 > N;                   // columns past the vocabulary
+        char* stage = lds + wave * 16 * kStride;
+        constexpr int kChunksPerRow = BN / 16, kRowsPerPass = 64 / kChunksPerRow, kPasses = 16 / kRowsPerPass;
+        const int crow = lane / kChunksPerRow, cchunk = lane % kChunksPerRow;
+#pragma unroll
+        for (int b = 0; b < MF; ++b) {
+            const int m = wm0 + b * 16 + frow;
+            __builtin_amdgcn_sched_barrier(0);                 // a row of tiles at a time: all of them at once need more registers than there are
+            float zv[NF][4];
+#pragma unroll
+            for (int g = 0; g < NF; ++g)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) zv[g][e] = acc[g][b][e];
+            if (edge) {
+#pragma unroll
+                for (int g = 0; g < NF; ++g)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (wn0 + 16 * g + 4 * fq + e >= N) zv[g][e] = -__builtin_inff();
+            }
+            const int t = tgt[min(m, M - 1)] - wn0;            // the target's place among the wave's columns
+            const bool here = t >= 0 && t < BN / 2 && ((t >> 2) & 3) == fq;
+            if (__builtin_amdgcn_ballot_w64(here)) {
+                float z = 0.0f;
+#pragma unroll
+                for (int g = 0; g < NF; ++g)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (here && t == 16 * g + 4 * fq + e) { z = zv[g][e]; zv[g][e] = -__builtin_inff(); }
+                if (here && m < M) zt[m] = z;
+            }
+            float top = zv[0][0];
+#pragma unroll
+            for (int g = 0; g < NF; ++g)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) top = fmaxf(top, zv[g][e]);
+            top = fmaxf(top, __shfl_xor(top, 16, kWave));
+            top = fmaxf(top, __shfl_xor(top, 32, kWave));
+            // whole numbers, so that one M takes another's place by an exact factor
+            const float mm = top == -__builtin_inff() ? 0.0f : ceilf(top * kLog2e) - (float)kTopExp<DT>;
+            float sum = 0.0f;
+            u32x2 pk[NF];
+#pragma unroll
+            for (int g = 0; g < NF; ++g) {
+                float av[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float z = zv[g][e];
+                    av[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z, kLog2eLow, __builtin_fmaf(z, kLog2e, -mm)));
+                    sum += av[e];
+                }
+                pk[g] = u32x2{S::pack(av[0], av[1]), S::pack(av[2], av[3])};
+            }
+            sum += __shfl_xor(sum, 16, kWave);
+            sum += __shfl_xor(sum, 32, kWave);
+            if (fq == 0 && m < M) stats[(int64_t)((wn0 - col0) / (BN / 2)) * T + m] = RowStat{mm, sum};
+            if constexpr (GRAD) {
+                // sixteen rows through the wave's own LDS, out in 128-bit stores; LDS serves a wave's requests in order
+#pragma unroll
+                for (int g = 0; g < NF; ++g) *reinterpret_cast<u32x2*>(stage + frow * kStride + (16 * g + 4 * fq) * 2) = pk[g];
+                asm volatile("" ::: "memory");
+                u32x4 back[kPasses];
+#pragma unroll
+                for (int p = 0; p < kPasses; ++p) back[p] = *reinterpret_cast<const u32x4*>(stage + (p * kRowsPerPass + crow) * kStride + cchunk * 16);
+                asm volatile("" ::: "memory");
+#pragma unroll
+                for (int p = 0; p < kPasses; ++p) {
+                    const int row = wm0 + b * 16 + p * kRowsPerPass + crow;
+                    if (row < M) *reinterpret_cast<u32x4*>(a + (int64_t)row * a_pitch + (wn0 - col0) + cchunk * 8) = back[p];
+                }
+            }
+        }
+    }
+};
+
+template <int DT, int BM, int BN, bool GRAD>
+__global__ __launch_bounds__(kGemmThreads)
+__attribute__((amdgpu_waves_per_eu(Tile<BM, BN>::kWavesPerSimd, Tile<BM, BN>::kWavesPerSimd)))
+void ce_logits_kernel(const uint16_t* __restrict__ xs, const uint8_t* __restrict__ head, const int32_t* __restrict__ count, int V, int Hp,
+                      int tiles_n, LogitsExt<DT, GRAD> ext)
+{
+    __shared__ __attribute__((aligned(1024))) char lds[lds_bytes_lines<BM, BN>()];
+    const int M = *count;
+    int tm, tn;
+    if (!tile_of_counted((M + BM - 1) / BM, tiles_n, tm, tn)) return;
+    gemm_k64_body<DT, KW_I8B, BM, BN, false, GR_NONE, 2, LogitsExt<DT, GRAD>>(
+        reinterpret_cast<const int8_t*>(xs), head, nullptr, nullptr, nullptr, nullptr, nullptr, M, V, Hp * 2, tm, ext.col0 / BN + tn, lds, 0, ext);
+}
+
+// ---- gradient: running sums over v of a_v W_v ----
+struct SumsExt {
+    static constexpr bool kOn = true;
+    int x_pitch, w_kt;
+    float* acc;                                 // [T][Hp]
+    const float* beta;                          // NULL: the first piece
+    int Hp;
+
+    template <int BM, int BN, class ACC>
+    __device__ __forceinline__ void finish(ACC& sums, int m0, int n0, int M, int N, char*) const
+    {
+        constexpr int MF = BM / 32, NF = BN / 32;
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int wm = wave & 1, wn = wave >> 1, frow = lane & 15, fq = lane >> 4;
+        const int wn0 = n0 + wn * (BN / 2), wm0 = m0 + wm * (BM / 2);
+#pragma unroll
+        for (int b = 0; b < MF; ++b) {
+            const int m = wm0 + b * 16 + frow;
+            __builtin_amdgcn_sched_barrier(0);
+            if (m >= M) continue;
+            const float f = beta ? beta[m] : 0.0f;
+            float* row = acc + (int64_t)m * Hp + wn0 + 4 * fq;
+#pragma unroll
+            for (int g = 0; g < NF; ++g) {
+                if (wn0 + 16 * g >= Hp) break;
+                f32x4 v = sums[g][b];
+                if (beta) {
+                    const f32x4 old = *reinterpret_cast<const f32x4*>(row + 16 * g);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(old[e], f, v[e]);
+                }
+                *reinterpret_cast<f32x4*>(row + 16 * g) = v;
+            }
+        }
+    }
+};
+
+// The contraction over the piece's columns is cut into `splits` parts of whole 64 columns, each with running sums of its own.
+template <int DT, int BM, int BN>
+__global__ __launch_bounds__(kGemmThreads)
+__attribute__((amdgpu_waves_per_eu(Tile<BM, BN>::kWavesPerSimd, Tile<BM, BN>::kWavesPerSimd)))
+void ce_grad_kernel(const uint16_t* __restrict__ a, const uint8_t* __restrict__ head_grad, const int32_t* __restrict__ count, int64_t T, int H, int Hp,
+                    int cols64, int kt0, int tiles_n, int splits, SumsExt ext)
+{
+    __shared__ __attribute__((aligned(1024))) char lds[lds_bytes_lines<BM, BN>()];
+    const int M = *count;
+    int tm, tn;
+    if (!tile_of_counted((M + BM - 1) / BM, tiles_n * splits, tm, tn)) return;
+    const int part = tn / tiles_n;
+    tn -= part * tiles_n;
+    const int c0 = (int)((int64_t)cols64 * part / splits), c1 = (int)((int64_t)cols64 * (part + 1) / splits);
+    ext.acc += (int64_t)part * T * Hp;
+    if (c0 == c1) {                             // a last piece of fewer columns than parts
+        for (int i = threadIdx.x; i < BM * (BN / 4); i += kGemmThreads) {
+            const int m = tm * BM + i / (BN / 4), n = tn * BN + i % (BN / 4) * 4;
+            if (m >= M || n >= Hp) continue;
+            f32x4* at = reinterpret_cast<f32x4*>(ext.acc + (int64_t)m * Hp + n);
+            f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (ext.beta) {
+                const float f = ext.beta[m];
+                v = *at;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] *= f;
+            }
+            *at = v;
+        }
+        return;
+    }
+    gemm_k64_body<DT, KW_I8B, BM, BN, false, GR_NONE, 2, SumsExt>(
+        reinterpret_cast<const int8_t*>(a) + (int64_t)c0 * 128, head_grad + (int64_t)(kt0 + 2 * c0) * 1024, nullptr, nullptr, nullptr, nullptr, nullptr,
+        M, H, (c1 - c0) * 128, tm, tn, lds, 0, ext);
+}
+
+template <int DT, int BM, int BN>
+static void launch_logits(const CeArgs& c, int64_t col0, int64_t cols, hipStream_t st)
+{
+    const int tiles_m = (int)((c.T + BM - 1) / BM), tiles_n = (int)((cols + BN - 1) / BN);
+    const int grid = ((tiles_m * tiles_n + 7) / 8) * 8;
+    auto go = [&](auto grad_tag) {
+        constexpr bool GRAD = decltype(grad_tag)::value;
+        const LogitsExt<DT, GRAD> ext{c.Hp * 2, c.Hp / 32, c.tgt, c.zt, c.stats, c.T, c.a, c.piece, (int)col0};
+        ce_logits_kernel<DT, BM, BN, GRAD><<<grid, kGemmThreads, 0, st>>>(c.xs, c.head, c.count, (int)c.V, c.Hp, tiles_n, ext);
+    };
+    if (c.grad) go(std::true_type{});
+    else        go(std::false_type{});
+}
+
+template <int DT, int BM, int BN>
+static void launch_grad(const CeArgs& c, int64_t col0, int64_t cols, hipStream_t st)
+{
+    const int tiles_m = (int)((c.T + BM - 1) / BM), tiles_n = (int)((c.H + BN - 1) / BN);
+    const int grid = ((tiles_m * tiles_n * c.splits + 7) / 8) * 8;
+    const SumsExt ext{c.piece * 2, c.Vp / 32, c.acc, col0 ? c.beta : nullptr, c.Hp};
+    ce_grad_kernel<DT, BM, BN><<<grid, kGemmThreads, 0, st>>>(c.a, c.head_grad, c.count, c.T, (int)c.H, c.Hp, (int)((cols + 63) / 64), (int)(col0 / 32),
+                                                              tiles_n, c.splits, ext);
+}
+
+template <int DT, typename Go>
+static void by_tile(int tile, Go&& go)
+{
+    if (tile == 0)      go(std::integral_constant<int, DT>{}, std::integral_constant<int, 256>{}, std::integral_constant<int, 256>{});
+    else if (tile == 1) go(std::integral_constant<int, DT>{}, std::integral_constant<int, 128>{}, std::integral_constant<int, 256>{});
+    else                go(std::integral_constant<int, DT>{}, std::integral_constant<int, 128>{}, std::integral_constant<int, 128>{});
+}
+
+void launch_ce_logits(const CeArgs& c, sasq_dtype dt, int64_t col0, int64_t cols, hipStream_t st)
+{
+    auto go = [&](auto d, auto bm, auto bn) { launch_logits<decltype(d)::value, decltype(bm)::value, decltype(bn)::value>(c, col0, cols, st); };
+    if (dt == SASQ_F16) by_tile<SASQ_F16>(c.tile, go);
+    else                by_tile<SASQ_BF16>(c.tile, go);
+}
+
+void launch_ce_grad(const CeArgs& c, sasq_dtype dt, int64_t col0, int64_t cols, hipStream_t st)
+{
+    auto go = [&](auto d, auto bm, auto bn) { launch_grad<decltype(d)::value, decltype(bm)::value, decltype(bn)::value>(c, col0, cols, st); };
+    if (dt == SASQ_F16) by_tile<SASQ_F16>(c.grad_tile, go);
+    else                by_tile<SASQ_BF16>(c.grad_tile, go);
+}
+
+}  // namespace sasq

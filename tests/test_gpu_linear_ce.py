@@ -1,0 +1,217 @@
+"""Cross entropy of a frozen head against its definition in 64 bits: sizes, masks, strides, weights, pieces, graphs."""
+from __future__ import annotations
+
+import math
+
+import pytest
+import torch
+
+from paper_2512_14481_amd import binding as B
+from tests.ce_ref import DT, Head, check
+
+pytestmark = pytest.mark.gpu
+
+
+def heads(w, grad=True):
+    w = w.cuda()
+    V, H = w.shape
+    made = []
+    for form in (B.SASQ_HEAD_LOGITS, B.SASQ_HEAD_GRAD):
+        h = torch.full((B.sasq_head_bytes(V, H, form),), 0xFF, dtype=torch.uint8, device="cuda")
+        B.sasq_prepare_head(w, h, form)
+        made.append(h)
+    return made
+
+
+def call(p, piece=0, grad=True, lse=True, mean=True, row_weight=None, scale=1.0, x=None, dx=None, hw=None):
+    hl, hg = hw or heads(p.w)
+    x = p.x.cuda() if x is None else x
+    nan = lambda n: torch.full((n,), math.nan, device="cuda")
+    out = {"loss": nan(p.T), "lse": nan(p.T) if lse else None, "mean": nan(1) if mean else None,
+           "dx": (torch.full((p.T, p.H), math.nan, dtype=DT[p.dtype], device="cuda") if dx is None else dx) if grad else None}
+    need = B.sasq_linear_ce_workspace(p.T, p.V, p.H, grad, piece)
+    ws = torch.full((need + 64,), 0xFF, dtype=torch.uint8, device="cuda")       # NaN wherever nothing was written
+    B.sasq_linear_ce(x, hl, p.t.cuda(), out["loss"], p.V, ws[:need], lse=out["lse"], mean=out["mean"], dx=out["dx"],
+                     head_grad=hg if grad else None, row_weight=None if row_weight is None else row_weight.cuda(), scale=scale, piece=piece)
+    torch.cuda.synchronize()
+    assert (ws[need:] == 0xFF).all()
+    return out
+
+
+SIZES = [(1, 1, 1), (1, 7, 64), (3, 257, 8), (2, 2, 3), (5, 1000, 100), (16, 1000, 256), (17, 513, 72), (64, 1000, 256), (65, 2050, 192), (130, 513, 65), (257, 2049, 320),
+         (300, 5000, 640), (1, 5003, 1000)]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("T,V,H", SIZES)
+def test_sizes(T, V, H, dtype):
+    p = Head(T, V, H, dtype, seed=T + V)
+    scale = 64.0
+    check(call(p, scale=scale), p.reference(scale=scale))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("T,V,H", [(1, 1, 1), (16, 1000, 256), (300, 5000, 640)])
+def test_without_gradient(T, V, H, dtype):
+    p = Head(T, V, H, dtype, seed=3, left_out=0.2)
+    check(call(p, grad=False), p.reference())
+    check(call(p, grad=False, lse=False, mean=False), p.reference())
+
+
+@pytest.mark.parametrize("left_out", [0.3, 0.95, 1.0])
+@pytest.mark.parametrize("T,V,H", [(1, 300, 64), (40, 300, 100), (700, 1030, 128), (2500, 300, 64)])
+def test_left_out_rows(T, V, H, left_out):
+    """Left-out rows are 0 whatever they hold; the others do not see them."""
+    p = Head(T, V, H, "bf16", seed=5, left_out=left_out)
+    ref = p.reference()
+    out = (p.t < 0) | (p.t >= V)
+    p.x[out] = math.nan
+    p.x[out & (torch.arange(T) % 3 == 0)] = math.inf
+    check(call(p), ref)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("T,V,H,piece", [(7, 3000, 128, 256), (7, 3000, 128, 1024), (300, 1500, 200, 256), (300, 2817, 192, 512), (600, 2561, 640, 2560), (20, 1000, 64, 4096)])
+def test_pieces(T, V, H, piece, dtype):
+    """Each piece may raise a row's maximum or not; the last may hold a single column."""
+    p = Head(T, V, H, dtype, seed=11, left_out=0.1)
+    check(call(p, piece=piece, scale=32.0), p.reference(scale=32.0))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("order", ["up", "down"])
+def test_pieces_with_steep_maxima(dtype, order):
+    """Logits over a range of 120, ascending or descending from piece to piece: sums of earlier pieces vanish, or those of later ones."""
+    p = Head(40, 1500, 64, dtype, seed=2, sure=0.0)
+    ramp = torch.linspace(-60, 60, 1500)
+    p.x[:, 0] = 1.0
+    p.w[:, 0] = (ramp if order == "up" else ramp.flip(0)).to(DT[dtype])
+    check(call(p, piece=256), p.reference())
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_sure_rows(dtype):
+    """Targets that are all but certain: losses down to 1e-7 and less, and gradients as small; also targets all but excluded."""
+    p = Head(64, 600, 128, dtype, seed=9, sure=0.0)
+    size = torch.linspace(-12, 26, 64)
+    x = torch.randn((64, 128), generator=torch.Generator().manual_seed(4)) * 0.3
+    w = p.w.float()
+    p.x = (x + size[:, None] * w[p.t.long()] / (w[p.t.long()] ** 2).sum(1, keepdim=True)).to(DT[dtype])
+    ref = p.reference(scale=2.0 ** 14)
+    assert ref["loss"][0].min() < 1e-7 and ref["loss"][0].max() > 10
+    check(call(p, scale=2.0 ** 14), ref)
+
+
+def test_row_weights_and_scale():
+    p = Head(90, 700, 96, "bf16", seed=1, left_out=0.2)
+    rw = torch.randn(90, generator=torch.Generator().manual_seed(8))
+    rw[3] = 0.0
+    check(call(p, row_weight=rw, scale=-3.0), p.reference(row_weight=rw, scale=-3.0))
+
+
+@pytest.mark.parametrize("x_pad,dx_pad,H", [(8, 16, 64), (3, 0, 64), (0, 5, 64), (64, 64, 100), (1, 1, 33)])
+def test_rows_apart(x_pad, dx_pad, H):
+    p = Head(50, 400, H, "f16", seed=6)
+    x = torch.full((50, H + x_pad), math.nan, dtype=DT["f16"], device="cuda")
+    x[:, :H] = p.x.cuda()
+    dx = torch.full((50, H + dx_pad), 7.0, dtype=DT["f16"], device="cuda")
+    check(call(p, x=x[:, :H], dx=dx[:, :H]), p.reference())
+    assert (dx[:, H:] == 7.0).all()
+    w = torch.full((400, H + x_pad), math.nan, dtype=DT["f16"], device="cuda")
+    w[:, :H] = p.w.cuda()
+    for a, b in zip(heads(p.w), heads(w[:, :H])):
+        assert torch.equal(a, b)
+
+
+def test_gradient_in_place_of_x():
+    p = Head(70, 900, 128, "bf16", seed=7, left_out=0.2)
+    apart = call(p)
+    x = p.x.cuda()
+    same = call(p, x=x, dx=x)
+    for k in apart:
+        assert torch.equal(apart[k], same[k]), k
+
+
+@pytest.mark.parametrize("V,H", [(1, 1), (40, 33), (130, 64), (1000, 200)])
+def test_layouts(V, H):
+    """Both layouts element by element; places past the matrix hold zeros."""
+    w = torch.randn((V, H), generator=torch.Generator().manual_seed(V)).to(torch.float16)
+    up = lambda n, m: -(-n // m) * m
+    for got, rows, cols, m in zip(heads(w), (V, H), (H, V), (w, w.t())):
+        R, C = up(rows, 16), up(cols, 64)
+        assert got.numel() == R * C * 2
+        full = torch.zeros((R, C), dtype=torch.float16)
+        full[:rows, :cols] = m
+        r, c = torch.arange(R)[:, None], torch.arange(C)[None]
+        swz = ((r >> 1) & 3) ^ ((r >> 3) & 1)
+        at = ((r // 16) * (C // 32) + c // 32) * 512 + ((4 * (r % 16) + (((c >> 3) & 3) ^ swz)) << 3) + (c & 7)
+        assert torch.equal(got.cpu().view(torch.float16)[at], full)
+
+
+def test_same_from_run_to_run():
+    p = Head(333, 5003, 200, "f16", seed=12, left_out=0.1)
+    hw = heads(p.w)
+    first = call(p, hw=hw)
+    for _ in range(3):
+        again = call(p, hw=hw)
+        for k in first:
+            assert torch.equal(first[k], again[k]), k
+
+
+def test_differences():
+    """dx against differences of the loss itself, in the direction of dx and in a random one."""
+    p = Head(4, 300, 64, "f16", seed=13, sure=4.0)
+    hw = heads(p.w)
+    got = call(p, hw=hw, row_weight=torch.ones(4))
+    base = p.x.double()
+    for direction in (got["dx"].cpu().double(), torch.randn((4, 64), generator=torch.Generator().manual_seed(1)).double()):
+        step = 0.25 * direction / direction.norm(dim=1, keepdim=True)
+        ends = []
+        for sign in (1, -1):
+            q = Head(4, 300, 64, "f16", seed=13, sure=4.0)
+            q.x = (base + sign * step).to(torch.float16)
+            ends.append((q.x.double(), call(q, hw=hw, grad=False)["loss"].cpu().double()))
+        moved = ends[0][0] - ends[1][0]
+        slope = (got["dx"].cpu().double() * moved).sum(1)
+        # third-order term of the central difference: the third derivative along a unit direction is at most 2 max|W_v - W_t|^3, times (step^3) / 24 * 2
+        third = 2 * (2 * p.w.double().norm(dim=1).max()) ** 3 * (0.26 ** 3) / 12
+        assert ((ends[0][1] - ends[1][1]) - slope).abs().max() < third + 0.51 * 2.0 ** -9
+
+
+def test_captured_and_replayed():
+    """A graph of two calls, replayed with new inputs between, gives what eager calls on a workspace of their own give."""
+    a, b = Head(37, 700, 96, "bf16", seed=20, left_out=0.3), Head(37, 700, 96, "bf16", seed=21, left_out=0.6)
+    b.w = a.w
+    hl, hg = heads(a.w)
+    x, t = a.x.cuda(), a.t.cuda()
+    ws = B.new_workspace(B.sasq_linear_ce_workspace(37, 700, 96, True))
+    loss, lse, mean = torch.empty(37, device="cuda"), torch.empty(37, device="cuda"), torch.empty(1, device="cuda")
+    dx = torch.empty_like(x)
+    run = lambda: B.sasq_linear_ce(x, hl, t, loss, 700, ws, lse=lse, mean=mean, dx=dx, head_grad=hg)
+    run()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        run()
+        run()
+    for p in (a, b, a, b):
+        x.copy_(p.x.cuda())
+        t.copy_(p.t.cuda())
+        g.replay()
+        torch.cuda.synchronize()
+        want = call(p, hw=(hl, hg))
+        for got, k in ((loss, "loss"), (lse, "lse"), (mean, "mean"), (dx, "dx")):
+            assert torch.equal(got, want[k]), k
+
+
+def test_other_stream():
+    p = Head(128, 3000, 256, "f16", seed=30)
+    want = call(p)
+    hw = heads(p.w)
+    torch.cuda.synchronize()
+    st = torch.cuda.Stream()
+    with torch.cuda.stream(st):
+        got = call(p, hw=hw)
+    st.synchronize()
+    for k in want:
+        assert torch.equal(want[k], got[k]), k

@@ -1,0 +1,65 @@
+"""What the cross entropy refuses: at the C entry points on the host before anything is launched, and in the binding."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+from paper_2512_14481_amd import binding as B
+
+P = 0x10000                       # never read: every call below is refused first
+NULL, SHAPE, ALIGN, UNSUPPORTED, WORKSPACE = 1, 2, 3, 4, 5
+
+
+def ce(x=P, x_stride=64, head=P, head_grad=P, targets=P, row_weight=None, scale=1.0, loss=P, lse=P, mean=P, dx=P, dx_stride=64, T=8, V=100, H=64, piece=0, dt=0, ws=P,
+       wsb=1 << 40):
+    return B._lib().sasq_linear_ce(x, x_stride, head, head_grad, targets, row_weight, scale, loss, lse, mean, dx, dx_stride, T, V, H, piece, dt, ws, wsb, None)
+
+
+def test_loss():
+    for change, rc in [(dict(x=None), NULL), (dict(head=None), NULL), (dict(targets=None), NULL), (dict(loss=None), NULL), (dict(head_grad=None), NULL),
+                       (dict(T=0), SHAPE), (dict(V=0), SHAPE), (dict(H=0), SHAPE), (dict(T=-1), SHAPE), (dict(T=(1 << 23) + 1), SHAPE), (dict(V=(1 << 23) + 1), SHAPE),
+                       (dict(H=(1 << 20) + 1, x_stride=1 << 21, dx_stride=1 << 21), SHAPE), (dict(T=1 << 23, H=1 << 15, x_stride=1 << 15, dx_stride=1 << 15), SHAPE),
+                       (dict(V=1 << 23, H=1 << 15, x_stride=1 << 15, dx_stride=1 << 15), SHAPE), (dict(x_stride=63), SHAPE), (dict(dx_stride=63), SHAPE),
+                       (dict(piece=-256), SHAPE), (dict(piece=100), SHAPE), (dict(dt=2), UNSUPPORTED), (dict(dt=-1), UNSUPPORTED), (dict(x=P + 2), ALIGN),
+                       (dict(head=P + 8), ALIGN), (dict(head_grad=P + 8), ALIGN), (dict(dx=P + 2), ALIGN), (dict(ws=None), WORKSPACE), (dict(ws=P + 8), ALIGN)]:
+        assert ce(**change) == rc, change
+    for grad in (0, 1):
+        need = B.sasq_linear_ce_workspace(8, 100, 64, bool(grad))
+        assert ce(wsb=need - 1, dx=P if grad else None) == WORKSPACE
+    assert B.sasq_linear_ce_workspace(8, 100, 64, True) > B.sasq_linear_ce_workspace(8, 100, 64, False) > 0
+    for sizes in ((0, 1, 1), (1, 0, 1), (1, 1, 0), (1 << 24, 1, 1), (1, 1 << 24, 1), (1, 1, 1 << 21)):
+        assert B.sasq_linear_ce_workspace(*sizes, True) == 0
+    assert B.sasq_linear_ce_workspace(8, 100, 64, True, 100) == 0
+
+
+def test_workspace_follows_the_piece():
+    """A smaller piece needs less; sizes near the limits do not wrap."""
+    lib = B._lib()
+    sizes = [lib.sasq_linear_ce_workspace(4096, 128000, 4096, 1, p) for p in (256, 1024, 4096, 16384, 65536)]
+    assert sizes == sorted(sizes) and sizes[-1] >= 4096 * 65536 * 2
+    assert lib.sasq_linear_ce_workspace(1 << 23, 1 << 23, 1 << 14, 1, 0) > (1 << 37) * 6
+    assert lib.sasq_linear_ce_workspace(8, 1000, 64, 1, 1 << 20) == lib.sasq_linear_ce_workspace(8, 1000, 64, 1, 1024)
+
+
+def test_head():
+    lib = B._lib()
+
+    def prep(w=P, stride=64, head=P, V=100, H=64, form=0, dt=0):
+        return lib.sasq_prepare_head(w, stride, head, V, H, form, dt, None)
+    for change, rc in [(dict(w=None), NULL), (dict(head=None), NULL), (dict(form=2), UNSUPPORTED), (dict(dt=2), UNSUPPORTED), (dict(V=0), SHAPE), (dict(H=0), SHAPE),
+                       (dict(stride=63), SHAPE), (dict(V=(1 << 23) + 1), SHAPE), (dict(w=P + 2), ALIGN), (dict(head=P + 8), ALIGN)]:
+        assert prep(**change) == rc, change
+    assert B.sasq_head_bytes(100, 65, B.SASQ_HEAD_LOGITS) == 112 * 128 * 2 and B.sasq_head_bytes(100, 65, B.SASQ_HEAD_GRAD) == 128 * 80 * 2
+    assert B.sasq_head_bytes(0, 64, 0) == B.sasq_head_bytes(64, 0, 0) == B.sasq_head_bytes(64, 64, 2) == 0
+
+
+def test_binding():
+    x, t, loss = torch.zeros((4, 64), dtype=torch.float16), torch.zeros(4, dtype=torch.int32), torch.zeros(4)
+    head = torch.zeros(B.sasq_head_bytes(10, 64, 0), dtype=torch.uint8)
+    ws = torch.zeros(16, dtype=torch.uint8)
+    with pytest.raises(ValueError):
+        B.sasq_linear_ce(x, head, t, loss, 10, ws)                   # host tensors
+    with pytest.raises(ValueError):
+        B.sasq_linear_ce(x[0], head, t, loss, 10, ws)
+    with pytest.raises(ValueError):
+        B.sasq_prepare_head(x, head, B.SASQ_HEAD_LOGITS)
