@@ -8,6 +8,7 @@
  *   training:   x' = fakequant(x; s)                     sasq_fakequant_fwd
  *               dx, ds = backward(x, dy; s)              sasq_fakequant_bwd
  *               s <- s - lr * ds                         sasq_scale_sgd
+ *               the same with a byte in x's place    sasq_fakequant_fwd_ckpt, sasq_fakequant_bwd_ckpt
  *               loss, dx at the frozen output head       sasq_linear_ce
  *   inference:  Y = s * (q(X) . Wq^T) * s_w (+ bias)     sasq_static_linear
  *   set-up:     Wq, s_w from frozen fp32 weights         sasq_quantize_weight
@@ -216,6 +217,45 @@ int sasq_fakequant_fwd_pc_batch(const sasq_fq_item* items, int count, int bits, 
 size_t sasq_fakequant_bwd_pc_batch_workspace(const sasq_fq_item* items, int count);
 int sasq_fakequant_bwd_pc_batch(const sasq_fq_item* items, int count, int bits, sasq_dtype dt,
                                 void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Fake quantization that keeps ONE BYTE an element for its backward: a scale-training step then holds [rows, cols] bytes per operator between
+ * forward and backward, and x is free (y may overwrite it).  q, y, m and dx are those of sasq_fakequant_fwd / _bwd; with p = x / s as there,
+ *     inside the range (m = 1):  e = fl32(q - p),  kept = round(252 e), in [-126, 126]           above it: kept = 127      below it: kept = -128
+ *     dx = dy * m        ds = sum dy * v,   v = kept / 252 inside,  2^(bits-1) - 1 above,  -2^(bits-1) below
+ * so that dx is that of the form which keeps x, and ds off from it by at most sum |dy| / 504 (the bytes' rounding, without bias).  The backward
+ * reads neither x nor s.
+ *   x, y, dy, dx   [rows, cols] device 16-bit `dt`;  y may alias x, dx may alias dy or be NULL (ds only)
+ *   kept       [rows, cols] device int8, 16-byte aligned, written by the forward, read by the backward
+ *   s, ds      device fp32: a scalar, or (pc) [cols];  ds is overwritten, its terms are summed in an order that follows from the sizes
+ *   bits       2..8, the same in both directions;  cols (pc): any up to 2^24, multiples of 8 are fast
+ *   workspace (backward)  >= the matching query's bytes, 16-byte aligned; needs no initialisation
+ * The batch forms do up to SASQ_MAX_BATCH tensors in one launch, with the results of the single calls (pc: bit for bit; ds of a whole tensor may
+ * differ in the last bits).  items: HOST array, read before the call returns; items must not overlap each other's outputs.
+ */
+typedef struct {
+    const void* x;      /* forward                                                */
+    const float* s;     /* forward                                                */
+    void* out;          /* forward: y; backward: dx or NULL                       */
+    int8_t* kept;       /* forward: written; backward: read                       */
+    const void* dy;     /* backward                                               */
+    float* ds;          /* backward, overwritten                                  */
+    int64_t rows, cols;
+} sasq_ckpt_item;
+int sasq_fakequant_fwd_ckpt(const void* x, const float* s, void* y, int8_t* kept, int64_t rows, int64_t cols, int bits, sasq_dtype dt, void* stream);
+size_t sasq_fakequant_bwd_ckpt_workspace(int64_t rows, int64_t cols);
+int sasq_fakequant_bwd_ckpt(const int8_t* kept, const void* dy, void* dx, float* ds, int64_t rows, int64_t cols, int bits, sasq_dtype dt,
+                            void* workspace, size_t workspace_bytes, void* stream);
+int sasq_fakequant_fwd_pc_ckpt(const void* x, const float* s, void* y, int8_t* kept, int64_t rows, int64_t cols, int bits, sasq_dtype dt, void* stream);
+size_t sasq_fakequant_bwd_pc_ckpt_workspace(int64_t rows, int64_t cols);
+int sasq_fakequant_bwd_pc_ckpt(const int8_t* kept, const void* dy, void* dx, float* ds, int64_t rows, int64_t cols, int bits, sasq_dtype dt,
+                               void* workspace, size_t workspace_bytes, void* stream);
+int sasq_fakequant_fwd_ckpt_batch(const sasq_ckpt_item* items, int count, int bits, sasq_dtype dt, void* stream);
+size_t sasq_fakequant_bwd_ckpt_batch_workspace(const sasq_ckpt_item* items, int count);
+int sasq_fakequant_bwd_ckpt_batch(const sasq_ckpt_item* items, int count, int bits, sasq_dtype dt, void* workspace, size_t workspace_bytes, void* stream);
+int sasq_fakequant_fwd_pc_ckpt_batch(const sasq_ckpt_item* items, int count, int bits, sasq_dtype dt, void* stream);
+size_t sasq_fakequant_bwd_pc_ckpt_batch_workspace(const sasq_ckpt_item* items, int count);
+int sasq_fakequant_bwd_pc_ckpt_batch(const sasq_ckpt_item* items, int count, int bits, sasq_dtype dt, void* workspace, size_t workspace_bytes, void* stream);
 
 /* SGD step of sasq_scale_sgd on a vector of n scales (the scales of one layer in one launch). */
 int sasq_scale_sgd_vec(float* s, const float* ds, int64_t n, float lr, void* stream);

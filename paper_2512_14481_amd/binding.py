@@ -48,6 +48,11 @@ class _FqItem(ctypes.Structure):
                 ("ds", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64)]
 
 
+class _CkptItem(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("s", ctypes.c_void_p), ("out", ctypes.c_void_p), ("kept", ctypes.c_void_p), ("dy", ctypes.c_void_p),
+                ("ds", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64)]
+
+
 class _KvCache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
                 ("pages", ctypes.c_int64), ("page_size", ctypes.c_int64), ("heads", ctypes.c_int64), ("dim", ctypes.c_int64),
@@ -162,6 +167,16 @@ def _lib() -> ctypes.CDLL:
         L.sasq_bwd_weight_bytes.argtypes = [i64, i64]
         L.sasq_prepare_bwd_weight.argtypes = [vp, vp, vp, i64, i64, i32, i32, vp]
         L.sasq_linear_bwd_input.argtypes = [vp, vp, vp, vp, i64, i64, i64, i32, vp]
+        for pc in ("", "_pc"):
+            f = lambda name: getattr(L, name.replace("@", pc))
+            f("sasq_fakequant_fwd@_ckpt").argtypes = [vp, vp, vp, vp, i64, i64, i32, i32, vp]
+            f("sasq_fakequant_bwd@_ckpt_workspace").restype = sz
+            f("sasq_fakequant_bwd@_ckpt_workspace").argtypes = [i64, i64]
+            f("sasq_fakequant_bwd@_ckpt").argtypes = [vp, vp, vp, vp, i64, i64, i32, i32, vp, sz, vp]
+            f("sasq_fakequant_fwd@_ckpt_batch").argtypes = [ctypes.POINTER(_CkptItem), i32, i32, i32, vp]
+            f("sasq_fakequant_bwd@_ckpt_batch_workspace").restype = sz
+            f("sasq_fakequant_bwd@_ckpt_batch_workspace").argtypes = [ctypes.POINTER(_CkptItem), i32]
+            f("sasq_fakequant_bwd@_ckpt_batch").argtypes = [ctypes.POINTER(_CkptItem), i32, i32, i32, vp, sz, vp]
         L.sasq_head_bytes.restype = sz
         L.sasq_head_bytes.argtypes = [i64, i64, i32]
         L.sasq_prepare_head.argtypes = [vp, i64, vp, i64, i64, i32, i32, vp]
@@ -384,6 +399,121 @@ def sasq_fakequant_bwd_pc_batch(items, workspace: torch.Tensor, bits: int = 8) -
     _check(_lib().sasq_fakequant_bwd_pc_batch(arr, len(items), bits, dt, _ptr(workspace),
                                               workspace.numel() * workspace.element_size(), _stream()),
            "sasq_fakequant_bwd_pc_batch")
+
+
+def _ckpt_items(items, backward: bool, pc: bool):
+    """items: sequence of (x, s, y, kept) for the forward or (kept, dy, dx_or_None, ds) for the backward."""
+    if not 1 <= len(items) <= SASQ_MAX_BATCH:
+        raise ValueError(f"a batch holds 1..{SASQ_MAX_BATCH} tensors")
+    arr = (_CkptItem * len(items))()
+    dt = None
+    for i, it in enumerate(items):
+        if backward:
+            kept, like, out, f = it
+            arr[i].dy, arr[i].ds = _ptr(like).value, _ptr(f).value
+        else:
+            like, f, out, kept = it
+            arr[i].x, arr[i].s = _ptr(like).value, _ptr(f).value
+        _want(kept, torch.int8, "kept"); _want(f, torch.float32, "ds" if backward else "s")
+        if out is not None and (out.dtype != like.dtype or out.shape != like.shape):
+            raise ValueError("dx must match dy" if backward else "y must match x")
+        if kept.shape != like.shape or like.dim() < 1 or (pc and like.dim() != 2):
+            raise ValueError("kept must have one byte per element, and per-channel tensors are matrices")
+        rows, cols = like.shape[0], like.numel() // max(like.shape[0], 1)
+        if f.numel() != (cols if pc else 1):
+            raise ValueError("s and ds hold one element, or (per channel) one per column")
+        if dt is None:
+            dt = _dt(like)
+        elif _dt(like) != dt:
+            raise TypeError("all tensors of a batch must have the same dtype")
+        arr[i].out, arr[i].kept = None if out is None else _ptr(out).value, _ptr(kept).value
+        arr[i].rows, arr[i].cols = rows, cols
+    return arr, dt
+
+
+def _ckpt_fwd(name: str, items, bits: int, pc: bool) -> None:
+    arr, dt = _ckpt_items(items, False, pc)
+    _check(getattr(_lib(), name)(arr, len(items), bits, dt, _stream()), name)
+
+
+def _ckpt_bwd(name: str, items, workspace: torch.Tensor, bits: int, pc: bool) -> None:
+    arr, dt = _ckpt_items(items, True, pc)
+    _check(getattr(_lib(), name)(arr, len(items), bits, dt, _ptr(workspace), workspace.numel() * workspace.element_size(), _stream()), name)
+
+
+def sasq_fakequant_fwd_ckpt(x: torch.Tensor, s: torch.Tensor, y: torch.Tensor, kept: torch.Tensor, bits: int = 8) -> None:
+    """kept: int8 of x's shape, written: what sasq_fakequant_bwd_ckpt needs of x."""
+    _want(s, torch.float32, "s"); _want(kept, torch.int8, "kept")
+    if y.dtype != x.dtype or y.shape != x.shape or kept.shape != x.shape or s.numel() != 1:
+        raise ValueError("y and kept must match x, and s holds one element")
+    rows, cols = x.shape[0], x.numel() // max(x.shape[0], 1)
+    _check(_lib().sasq_fakequant_fwd_ckpt(_ptr(x), _ptr(s), _ptr(y), _ptr(kept), rows, cols, bits, _dt(x), _stream()), "sasq_fakequant_fwd_ckpt")
+
+
+def sasq_fakequant_bwd_ckpt_workspace(rows: int, cols: int) -> int:
+    return int(_lib().sasq_fakequant_bwd_ckpt_workspace(rows, cols))
+
+
+def sasq_fakequant_bwd_ckpt(kept: torch.Tensor, dy: torch.Tensor, dx: Optional[torch.Tensor], ds: torch.Tensor, workspace: torch.Tensor,
+                            bits: int = 8) -> None:
+    _want(ds, torch.float32, "ds"); _want(kept, torch.int8, "kept")
+    if kept.shape != dy.shape or (dx is not None and (dx.dtype != dy.dtype or dx.shape != dy.shape)) or ds.numel() != 1:
+        raise ValueError("kept and dx must match dy, and ds holds one element")
+    rows, cols = dy.shape[0], dy.numel() // max(dy.shape[0], 1)
+    _check(_lib().sasq_fakequant_bwd_ckpt(_ptr(kept), _ptr(dy), _ptr(dx), _ptr(ds), rows, cols, bits, _dt(dy), _ptr(workspace),
+                                          workspace.numel() * workspace.element_size(), _stream()), "sasq_fakequant_bwd_ckpt")
+
+
+def sasq_fakequant_fwd_pc_ckpt(x: torch.Tensor, s: torch.Tensor, y: torch.Tensor, kept: torch.Tensor, bits: int = 8) -> None:
+    _want(s, torch.float32, "s"); _want(kept, torch.int8, "kept")
+    rows, cols = x.shape
+    if y.dtype != x.dtype or y.shape != x.shape or kept.shape != x.shape or s.numel() != cols:
+        raise ValueError("y and kept must match x, and s must have one element per column")
+    _check(_lib().sasq_fakequant_fwd_pc_ckpt(_ptr(x), _ptr(s), _ptr(y), _ptr(kept), rows, cols, bits, _dt(x), _stream()), "sasq_fakequant_fwd_pc_ckpt")
+
+
+def sasq_fakequant_bwd_pc_ckpt_workspace(rows: int, cols: int) -> int:
+    return int(_lib().sasq_fakequant_bwd_pc_ckpt_workspace(rows, cols))
+
+
+def sasq_fakequant_bwd_pc_ckpt(kept: torch.Tensor, dy: torch.Tensor, dx: Optional[torch.Tensor], ds: torch.Tensor, workspace: torch.Tensor,
+                               bits: int = 8) -> None:
+    _want(ds, torch.float32, "ds"); _want(kept, torch.int8, "kept")
+    rows, cols = dy.shape
+    if kept.shape != dy.shape or (dx is not None and (dx.dtype != dy.dtype or dx.shape != dy.shape)) or ds.numel() != cols:
+        raise ValueError("kept and dx must match dy, and ds must have one element per column")
+    _check(_lib().sasq_fakequant_bwd_pc_ckpt(_ptr(kept), _ptr(dy), _ptr(dx), _ptr(ds), rows, cols, bits, _dt(dy), _ptr(workspace),
+                                             workspace.numel() * workspace.element_size(), _stream()), "sasq_fakequant_bwd_pc_ckpt")
+
+
+def sasq_fakequant_fwd_ckpt_batch(items, bits: int = 8) -> None:
+    """items: sequence of (x, s, y, kept)."""
+    _ckpt_fwd("sasq_fakequant_fwd_ckpt_batch", items, bits, False)
+
+
+def sasq_fakequant_bwd_ckpt_batch_workspace(items) -> int:
+    """items as for sasq_fakequant_bwd_ckpt_batch (only the shapes are read)."""
+    return int(_lib().sasq_fakequant_bwd_ckpt_batch_workspace(_ckpt_items(items, True, False)[0], len(items)))
+
+
+def sasq_fakequant_bwd_ckpt_batch(items, workspace: torch.Tensor, bits: int = 8) -> None:
+    """items: sequence of (kept, dy, dx_or_None, ds)."""
+    _ckpt_bwd("sasq_fakequant_bwd_ckpt_batch", items, workspace, bits, False)
+
+
+def sasq_fakequant_fwd_pc_ckpt_batch(items, bits: int = 8) -> None:
+    """items: sequence of (x, s[cols], y, kept)."""
+    _ckpt_fwd("sasq_fakequant_fwd_pc_ckpt_batch", items, bits, True)
+
+
+def sasq_fakequant_bwd_pc_ckpt_batch_workspace(items) -> int:
+    """items as for sasq_fakequant_bwd_pc_ckpt_batch (only the shapes are read)."""
+    return int(_lib().sasq_fakequant_bwd_pc_ckpt_batch_workspace(_ckpt_items(items, True, True)[0], len(items)))
+
+
+def sasq_fakequant_bwd_pc_ckpt_batch(items, workspace: torch.Tensor, bits: int = 8) -> None:
+    """items: sequence of (kept, dy, dx_or_None, ds[cols])."""
+    _ckpt_bwd("sasq_fakequant_bwd_pc_ckpt_batch", items, workspace, bits, True)
 
 
 def sasq_scale_sgd_vec(s: torch.Tensor, ds: torch.Tensor, lr: float) -> None:

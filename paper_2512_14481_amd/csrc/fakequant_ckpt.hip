@@ -1,0 +1,560 @@
+// Fake quantization that keeps one byte an element for its backward, in place of the 16-bit x (sasq_fakequant_*_ckpt).
+//
+// The backward (Sec. 4.2, Eq. 4 and the chain rule) needs of x only whether it was clamped, and to which end, or else the rounding residual:
+//     dx = dy * m,   ds = sum dy * (m ? e : q),   e = q - x/s in [-1/2, 1/2]
+// The byte c is that residual in units of 1/252, or a mark: 127 above the range, -128 below it.  e is one fused product and difference (exact but for
+// its rounding to fp32), c the nearest whole number of the exact 252 e.  ds then is sum dy * t / 252 with t = c, or 252 q at the ends: each product of a
+// 16-bit dy and t is exact in fp32.  x itself in 8 bits would not do, as the residual is what 8 bits of x leave out.
+//
+// Bound by memory: forward x in, y and the byte out, 5 bytes an element; backward the byte and dy in, dx out, 5 bytes, where the form that keeps x has 6.
+#include "sasq_device.h"
+#include <type_traits>
+
+namespace sasq {
+
+constexpr int kCkThreads = 256, kCkWaves = kCkThreads / kWave, kCkUnroll = 4;
+constexpr float kCkSteps = 252.0f;
+constexpr int kCkHigh = 127, kCkLow = -128;
+constexpr int kCkCols = kWave * 8;               // columns of a block of the per-channel kernels
+constexpr int kCkMaxBatch = SASQ_MAX_BATCH;
+constexpr int kCkBlocks = 2048, kCkPartials = 512;
+
+struct CkItem {
+    const uint16_t* x;
+    const float* s;
+    uint16_t* out;
+    int8_t* kept;
+    const uint16_t* dy;
+    float* ds;
+    void* partial;                                // backward: of this tensor
+    int64_t rows, cols, n;
+    int64_t chunk_rows;                           // per channel: rows of a block,
+    int chunks;                                   // and blocks of a column block
+};
+struct CkBatch {
+    CkItem it[kCkMaxBatch];
+    int first[kCkMaxBatch + 1];
+    int count;
+};
+
+__device__ __forceinline__ int ck_item_of(const CkBatch& b, int block)
+{
+    int k = 0;
+#pragma unroll
+    for (int i = 1; i < kCkMaxBatch; ++i)
+        if (i < b.count && block >= b.first[i]) k = i;
+    return k;
+}
+
+// q * s and the byte, in the low bits of a float as pack_codes4 wants it.
+__device__ __forceinline__ float ck_fwd(float x, float inv_s, float s, float lo, float hi, float& byte)
+{
+    const float f = __builtin_fmaf(x, inv_s, kMagic);
+    const float c = __builtin_amdgcn_fmed3f(f, lo, hi);
+    const float q = c - kMagic;
+    const float e = __builtin_fmaf(-x, inv_s, q);
+    byte = __builtin_fmaf(e, kCkSteps, kMagic);
+    byte = f > c ? kMagic + (float)kCkHigh : byte;
+    byte = f < c ? kMagic + (float)kCkLow : byte;
+    return rounded_f32(q * s);                    // elements stored one by one would be multiplied and converted at once
+}
+
+template <int DT>
+__device__ __forceinline__ u32x4 ck_fwd_vec(const u32x4& in, const float (&inv_s)[8], const float (&s)[8], float lo, float hi, u32x2& kept)
+{
+    using S = Store16<DT>;
+    u32x4 out;
+    float b[8];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const float y0 = ck_fwd(S::lo(in[w]), inv_s[2 * w], s[2 * w], lo, hi, b[2 * w]);
+        const float y1 = ck_fwd(S::hi(in[w]), inv_s[2 * w + 1], s[2 * w + 1], lo, hi, b[2 * w + 1]);
+        out[w] = S::pack(y0, y1);
+    }
+    kept[0] = pack_codes4(b[0], b[1], b[2], b[3]);
+    kept[1] = pack_codes4(b[4], b[5], b[6], b[7]);
+    return out;
+}
+
+// 252 times what the byte stands for; m: inside the range.
+__device__ __forceinline__ float ck_value(int c, float lo252, float hi252, bool& m)
+{
+    const bool high = c == kCkHigh, low = c == kCkLow;
+    m = !high && !low;
+    return high ? hi252 : low ? lo252 : (float)c;
+}
+
+// dx and the eight terms of ds times 252.
+template <int DT>
+__device__ __forceinline__ u32x4 ck_bwd_vec(const u32x2& kept, const u32x4& g, float lo252, float hi252, float (&term)[8])
+{
+    using S = Store16<DT>;
+    u32x4 out;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        bool ma, mb;
+        const int c0 = (int)(kept[w >> 1] << (24 - 16 * (w & 1))) >> 24, c1 = (int)(kept[w >> 1] << (16 - 16 * (w & 1))) >> 24;
+        term[2 * w] = S::lo(g[w]) * ck_value(c0, lo252, hi252, ma);
+        term[2 * w + 1] = S::hi(g[w]) * ck_value(c1, lo252, hi252, mb);
+        out[w] = g[w] & ((ma ? 0x0000FFFFu : 0u) | (mb ? 0xFFFF0000u : 0u));
+    }
+    return out;
+}
+
+__device__ __forceinline__ float ck_low(int bits) { return -(float)(1 << (bits - 1)); }
+__device__ __forceinline__ float ck_high(int bits) { return (float)((1 << (bits - 1)) - 1); }
+
+// ---- one factor per tensor: a flat array, eight elements a lane and access ----
+template <int DT>
+__global__ __launch_bounds__(kCkThreads) void ck_fwd_kernel(const CkBatch b, int bits)
+{
+    using S = Store16<DT>;
+    const int k = ck_item_of(b, (int)blockIdx.x);
+    const CkItem& it = b.it[k];
+    const int64_t block = (int)blockIdx.x - b.first[k], blocks = b.first[k + 1] - b.first[k];
+    const float f = *it.s, lo = kMagic + ck_low(bits), hi = kMagic + ck_high(bits);
+    float s[8], inv_s[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { s[e] = f; inv_s[e] = 1.0f / f; }
+    const u32x4* x = reinterpret_cast<const u32x4*>(it.x);
+    u32x4* y = reinterpret_cast<u32x4*>(it.out);
+    u32x2* kept = reinterpret_cast<u32x2*>(it.kept);
+    const int64_t nvec = it.n / 8;
+    constexpr int64_t kChunk = (int64_t)kCkThreads * kCkUnroll;
+    for (int64_t base = block * kChunk; base < nvec; base += blocks * kChunk) {
+        u32x4 in[kCkUnroll];
+#pragma unroll
+        for (int u = 0; u < kCkUnroll; ++u) in[u] = x[min(base + u * kCkThreads + (int64_t)threadIdx.x, nvec - 1)];
+#pragma unroll
+        for (int u = 0; u < kCkUnroll; ++u) {
+            const int64_t i = base + u * kCkThreads + threadIdx.x;
+            u32x2 kp;
+            const u32x4 out = ck_fwd_vec<DT>(in[u], inv_s, s, lo, hi, kp);
+            if (i < nvec) {
+                __builtin_nontemporal_store(out, &y[i]);
+                __builtin_nontemporal_store(kp, &kept[i]);
+            }
+        }
+    }
+    if (block == blocks - 1 && threadIdx.x < (unsigned)(it.n - nvec * 8)) {
+        const int64_t i = nvec * 8 + threadIdx.x;
+        float byte;
+        const float v = ck_fwd(S::one(it.x[i]), inv_s[0], f, lo, hi, byte);
+        it.out[i] = S::enc(v);
+        it.kept[i] = (int8_t)(__float_as_int(byte) - kMagicBits);
+    }
+}
+
+template <int DT>
+__global__ __launch_bounds__(kCkThreads) void ck_bwd_kernel(const CkBatch b, int bits)
+{
+    using S = Store16<DT>;
+    const int k = ck_item_of(b, (int)blockIdx.x);
+    const CkItem& it = b.it[k];
+    const int64_t block = (int)blockIdx.x - b.first[k], blocks = b.first[k + 1] - b.first[k];
+    const float lo = ck_low(bits) * kCkSteps, hi = ck_high(bits) * kCkSteps;
+    const u32x2* kept = reinterpret_cast<const u32x2*>(it.kept);
+    const u32x4* dy = reinterpret_cast<const u32x4*>(it.dy);
+    u32x4* dx = reinterpret_cast<u32x4*>(it.out);
+    const int64_t nvec = it.n / 8;
+    constexpr int64_t kChunk = (int64_t)kCkThreads * kCkUnroll;
+    double acc = 0.0;                              // eight terms in fp32, everything above that in fp64
+    for (int64_t base = block * kChunk; base < nvec; base += blocks * kChunk) {
+        u32x2 kp[kCkUnroll];
+        u32x4 g[kCkUnroll];
+#pragma unroll
+        for (int u = 0; u < kCkUnroll; ++u) {
+            const int64_t i = min(base + u * kCkThreads + (int64_t)threadIdx.x, nvec - 1);
+            kp[u] = __builtin_nontemporal_load(&kept[i]);
+            g[u] = __builtin_nontemporal_load(&dy[i]);
+        }
+#pragma unroll
+        for (int u = 0; u < kCkUnroll; ++u) {
+            const int64_t i = base + u * kCkThreads + threadIdx.x;
+            float term[8], sum = 0.0f;
+            const u32x4 out = ck_bwd_vec<DT>(kp[u], g[u], lo, hi, term);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum += term[e];
+            if (i < nvec) {
+                acc += (double)sum;
+                if (dx) __builtin_nontemporal_store(out, &dx[i]);
+            }
+        }
+    }
+    if (block == blocks - 1 && threadIdx.x < (unsigned)(it.n - nvec * 8)) {
+        const int64_t i = nvec * 8 + threadIdx.x;
+        bool m;
+        acc += (double)(S::one(it.dy[i]) * ck_value(it.kept[i], lo, hi, m));
+        if (dx) it.out[i] = m ? it.dy[i] : (uint16_t)0;
+    }
+    __shared__ double part[kCkWaves];
+    const double w = wave_sum(acc);
+    if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = w;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double all = 0.0;
+        for (int i = 0; i < kCkWaves; ++i) all += part[i];
+        static_cast<double*>(it.partial)[block] = all;
+    }
+}
+
+// ds of a tensor from its blocks' sums, in a fixed order.
+__global__ __launch_bounds__(kCkThreads) void ck_join_kernel(const CkBatch b)
+{
+    const CkItem& it = b.it[blockIdx.x];
+    const int n = b.first[blockIdx.x + 1] - b.first[blockIdx.x];
+    const double* p = static_cast<const double*>(it.partial);
+    double acc = 0.0;
+    for (int i = threadIdx.x; i < n; i += kCkThreads) acc += p[i];
+    __shared__ double part[kCkWaves];
+    const double w = wave_sum(acc);
+    if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = w;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double all = 0.0;
+        for (int i = 0; i < kCkWaves; ++i) all += part[i];
+        *it.ds = (float)(all / (double)kCkSteps);
+    }
+}
+
+// ---- one factor per column ----
+// A block takes 512 columns of a run of rows, each of its waves every fourth of them.  VEC: a lane has eight columns next to each other and a row's
+// elements in one access; otherwise (rows that are no multiple of eight) every 64th column, an access each.
+template <bool VEC>
+__device__ __forceinline__ int64_t ck_col(int64_t col_block, int lane, int e) { return col_block * kCkCols + (VEC ? lane * 8 + e : e * kWave + lane); }
+
+template <int DT, bool VEC>
+__device__ __forceinline__ u32x4 ck_load_row(const uint16_t* at, int64_t col_block, int lane, int64_t cols)
+{
+    if (VEC) return *reinterpret_cast<const u32x4*>(at + ck_col<VEC>(col_block, lane, 0));
+    u32x4 v;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const int64_t c0 = ck_col<VEC>(col_block, lane, 2 * w), c1 = ck_col<VEC>(col_block, lane, 2 * w + 1);
+        v[w] = (uint32_t)at[min(c0, cols - 1)] | (uint32_t)at[min(c1, cols - 1)] << 16;
+    }
+    return v;
+}
+template <bool VEC>
+__device__ __forceinline__ u32x2 ck_load_kept(const int8_t* at, int64_t col_block, int lane, int64_t cols)
+{
+    if (VEC) return *reinterpret_cast<const u32x2*>(at + ck_col<VEC>(col_block, lane, 0));
+    u32x2 v = {0u, 0u};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e >> 2] |= (uint32_t)(uint8_t)at[min(ck_col<VEC>(col_block, lane, e), cols - 1)] << (8 * (e & 3));
+    return v;
+}
+template <bool VEC>
+__device__ __forceinline__ void ck_store_row(uint16_t* at, const u32x4& v, int64_t col_block, int lane, int64_t cols)
+{
+    if (VEC) {
+        __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(at + ck_col<VEC>(col_block, lane, 0)));
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (ck_col<VEC>(col_block, lane, e) < cols) at[ck_col<VEC>(col_block, lane, e)] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+}
+template <bool VEC>
+__device__ __forceinline__ void ck_store_kept(int8_t* at, const u32x2& v, int64_t col_block, int lane, int64_t cols)
+{
+    if (VEC) {
+        __builtin_nontemporal_store(v, reinterpret_cast<u32x2*>(at + ck_col<VEC>(col_block, lane, 0)));
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (ck_col<VEC>(col_block, lane, e) < cols) at[ck_col<VEC>(col_block, lane, e)] = (int8_t)(v[e >> 2] >> (8 * (e & 3)));
+}
+
+template <int DT, bool VEC>
+__device__ __forceinline__ void ck_fwd_pc_body(const CkItem& it, int block, int bits)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t cb = block / it.chunks, cols = it.cols;
+    const int64_t r0 = block % it.chunks * it.chunk_rows, r1 = min(it.rows, r0 + it.chunk_rows);
+    if (VEC && ck_col<VEC>(cb, lane, 0) >= cols) return;
+    const float lo = kMagic + ck_low(bits), hi = kMagic + ck_high(bits);
+    float s[8], inv_s[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        s[e] = it.s[min(ck_col<VEC>(cb, lane, e), cols - 1)];
+        inv_s[e] = 1.0f / s[e];
+    }
+    for (int64_t base = r0 + wave; base < r1; base += kCkWaves * kCkUnroll) {
+        u32x4 in[kCkUnroll];
+#pragma unroll
+        for (int u = 0; u < kCkUnroll; ++u) in[u] = ck_load_row<DT, VEC>(it.x + min(base + u * kCkWaves, r1 - 1) * cols, cb, lane, cols);
+#pragma unroll
+        for (int u = 0; u < kCkUnroll; ++u) {
+            const int64_t r = base + u * kCkWaves;
+            if (r >= r1) break;
+            u32x2 kp;
+            const u32x4 out = ck_fwd_vec<DT>(in[u], inv_s, s, lo, hi, kp);
+            ck_store_row<VEC>(it.out + r * cols, out, cb, lane, cols);
+            ck_store_kept<VEC>(it.kept + r * cols, kp, cb, lane, cols);
+        }
+    }
+}
+
+template <int DT>
+__global__ __launch_bounds__(kCkThreads) void ck_fwd_pc_kernel(const CkBatch b, int bits)
+{
+    const int k = ck_item_of(b, (int)blockIdx.x);
+    const CkItem& it = b.it[k];
+    const int block = (int)blockIdx.x - b.first[k];
+    if (it.cols % 8 == 0) ck_fwd_pc_body<DT, true>(it, block, bits);
+    else                  ck_fwd_pc_body<DT, false>(it, block, bits);
+}
+
+template <int DT, bool VEC>
+__device__ __forceinline__ void ck_bwd_pc_body(const CkItem& it, int block, int bits, float (&red)[kCkWaves][kCkCols])
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t cb = block / it.chunks, cols = it.cols;
+    const int64_t r0 = block % it.chunks * it.chunk_rows, r1 = min(it.rows, r0 + it.chunk_rows);
+    const float lo = ck_low(bits) * kCkSteps, hi = ck_high(bits) * kCkSteps;
+    double acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};      // four rows in fp32, everything above that in fp64
+    if (!VEC || ck_col<VEC>(cb, lane, 0) < cols) {
+        for (int64_t base = r0 + wave; base < r1; base += kCkWaves * kCkUnroll) {
+            u32x2 kp[kCkUnroll];
+            u32x4 g[kCkUnroll];
+#pragma unroll
+            for (int u = 0; u < kCkUnroll; ++u) {
+                const int64_t at = min(base + u * kCkWaves, r1 - 1) * cols;
+                kp[u] = ck_load_kept<VEC>(it.kept + at, cb, lane, cols);
+                g[u] = ck_load_row<DT, VEC>(it.dy + at, cb, lane, cols);
+            }
+            float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+            for (int u = 0; u < kCkUnroll; ++u) {
+                const int64_t r = base + u * kCkWaves;
+                float term[8];
+                const u32x4 out = ck_bwd_vec<DT>(kp[u], g[u], lo, hi, term);
+                if (r >= r1) break;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] += term[e];
+                if (it.out) ck_store_row<VEC>(it.out + r * cols, out, cb, lane, cols);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[e] += (double)sum[e];
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) red[wave][ck_col<VEC>(0, lane, e)] = (float)acc[e];
+    __syncthreads();
+    for (int c = threadIdx.x; c < kCkCols; c += kCkThreads) {
+        if (cb * kCkCols + c >= cols) continue;
+        double all = 0.0;
+#pragma unroll
+        for (int w = 0; w < kCkWaves; ++w) all += (double)red[w][c];
+        if (it.chunks == 1) it.ds[cb * kCkCols + c] = (float)(all / (double)kCkSteps);
+        else                static_cast<float*>(it.partial)[(int64_t)(block % it.chunks) * cols + cb * kCkCols + c] = (float)all;
+    }
+}
+
+template <int DT>
+__global__ __launch_bounds__(kCkThreads) void ck_bwd_pc_kernel(const CkBatch b, int bits)
+{
+    __shared__ float red[kCkWaves][kCkCols];
+    const int k = ck_item_of(b, (int)blockIdx.x);
+    const CkItem& it = b.it[k];
+    const int block = (int)blockIdx.x - b.first[k];
+    if (it.cols % 8 == 0) ck_bwd_pc_body<DT, true>(it, block, bits, red);
+    else                  ck_bwd_pc_body<DT, false>(it, block, bits, red);
+}
+
+__global__ __launch_bounds__(kCkThreads) void ck_join_pc_kernel(const CkBatch b)
+{
+    const CkItem& it = b.it[blockIdx.y];
+    if (it.chunks == 1) return;
+    for (int64_t c = (int64_t)blockIdx.x * kCkThreads + threadIdx.x; c < it.cols; c += (int64_t)gridDim.x * kCkThreads) {
+        double all = 0.0;
+        for (int i = 0; i < it.chunks; ++i) all += (double)static_cast<const float*>(it.partial)[(int64_t)i * it.cols + c];
+        it.ds[c] = (float)(all / (double)kCkSteps);
+    }
+}
+
+// ---- plan ----
+static int ck_blocks(int64_t n, int most)
+{
+    const int64_t need = (n / 8 + (int64_t)kCkThreads * kCkUnroll - 1) / ((int64_t)kCkThreads * kCkUnroll);
+    return (int)(need < 1 ? 1 : need < most ? need : most);
+}
+static int64_t ck_col_blocks(int64_t cols) { return (cols + kCkCols - 1) / kCkCols; }
+// Rows of a block: they follow from the tensor alone, so that a batch gives the bits of the single calls.
+static int64_t ck_chunk_rows(int64_t rows, int64_t cols)
+{
+    int64_t r = 16;
+    while (r < 64 && (rows + 2 * r - 1) / (2 * r) * ck_col_blocks(cols) >= 512) r *= 2;
+    while ((rows + r - 1) / r > 256) r *= 2;
+    return r;
+}
+constexpr int64_t kCkMaxElements = INT64_C(1) << 40, kCkMaxCols = INT64_C(1) << 24;
+constexpr int64_t kCkMaxBlocks = INT64_C(1) << 23;       // a launch holds fewer than 2^32 threads
+
+static size_t ck_partial_bytes(int64_t rows, int64_t cols, bool pc)
+{
+    if (!pc) return kCkPartials * sizeof(double);
+    const int64_t r = ck_chunk_rows(rows, cols), chunks = (rows + r - 1) / r;
+    return ((size_t)(chunks * cols) * sizeof(float) + 255) / 256 * 256;
+}
+
+static int ck_check(const sasq_ckpt_item* items, int count, bool pc, bool backward, int bits, int dt)
+{
+    if (!items) return SASQ_ERR_NULL;
+    if (count <= 0 || count > kCkMaxBatch) return SASQ_ERR_SHAPE;
+    if (bits < 2 || bits > 8) return SASQ_ERR_UNSUPPORTED;
+    if (dt != SASQ_F16 && dt != SASQ_BF16) return SASQ_ERR_UNSUPPORTED;
+    int64_t blocks = 0;
+    for (int i = 0; i < count; ++i) {
+        const sasq_ckpt_item& it = items[i];
+        if (!it.kept || (backward ? (!it.dy || !it.ds) : (!it.x || !it.s || !it.out))) return SASQ_ERR_NULL;
+        if (it.rows <= 0 || it.cols <= 0 || it.rows > kCkMaxElements / it.cols || (pc && it.cols > kCkMaxCols)) return SASQ_ERR_SHAPE;
+        if (!aligned16(it.kept) || !aligned16(it.out) || (backward ? !aligned16(it.dy) : !aligned16(it.x))) return SASQ_ERR_ALIGN;
+        if (pc) blocks += (it.rows + ck_chunk_rows(it.rows, it.cols) - 1) / ck_chunk_rows(it.rows, it.cols) * ck_col_blocks(it.cols);
+    }
+    return blocks > kCkMaxBlocks ? SASQ_ERR_SHAPE : SASQ_OK;
+}
+
+static void ck_plan(const sasq_ckpt_item* items, int count, bool pc, bool backward, char* workspace, CkBatch& b)
+{
+    b.count = count;
+    b.first[0] = 0;
+    size_t at = 0;
+    for (int i = 0; i < count; ++i) {
+        const sasq_ckpt_item& it = items[i];
+        CkItem& k = b.it[i];
+        k.x = static_cast<const uint16_t*>(it.x);
+        k.s = it.s;
+        k.out = static_cast<uint16_t*>(it.out);
+        k.kept = it.kept;
+        k.dy = static_cast<const uint16_t*>(it.dy);
+        k.ds = it.ds;
+        k.rows = it.rows; k.cols = it.cols; k.n = it.rows * it.cols;
+        k.partial = workspace + at;
+        int blocks;
+        if (pc) {
+            const int64_t r = ck_chunk_rows(it.rows, it.cols);
+            k.chunk_rows = r;
+            k.chunks = (int)((it.rows + r - 1) / r);
+            blocks = (int)(k.chunks * ck_col_blocks(it.cols));
+        } else {
+            blocks = ck_blocks(k.n, backward ? kCkPartials : kCkBlocks);
+        }
+        if (backward) at += ck_partial_bytes(it.rows, it.cols, pc);
+        b.first[i + 1] = b.first[i] + blocks;
+    }
+    for (int i = count; i < kCkMaxBatch; ++i) b.first[i + 1] = b.first[count];
+}
+
+static size_t ck_workspace(const sasq_ckpt_item* items, int count, bool pc)
+{
+    if (!items || count <= 0 || count > kCkMaxBatch) return 0;
+    size_t bytes = 0;
+    for (int i = 0; i < count; ++i) {
+        if (items[i].rows <= 0 || items[i].cols <= 0 || items[i].rows > kCkMaxElements / items[i].cols || (pc && items[i].cols > kCkMaxCols)) return 0;
+        bytes += ck_partial_bytes(items[i].rows, items[i].cols, pc);
+    }
+    return bytes;
+}
+
+static int ck_fwd(const sasq_ckpt_item* items, int count, bool pc, int bits, sasq_dtype dt, void* stream)
+{
+    const int rc = ck_check(items, count, pc, false, bits, (int)dt);
+    if (rc) return rc;
+    CkBatch b{};
+    ck_plan(items, count, pc, false, nullptr, b);
+    hipStream_t st = as_stream(stream);
+    const int grid = b.first[count];
+    if (pc) {
+        if (dt == SASQ_F16) ck_fwd_pc_kernel<SASQ_F16><<<grid, kCkThreads, 0, st>>>(b, bits);
+        else                ck_fwd_pc_kernel<SASQ_BF16><<<grid, kCkThreads, 0, st>>>(b, bits);
+    } else {
+        if (dt == SASQ_F16) ck_fwd_kernel<SASQ_F16><<<grid, kCkThreads, 0, st>>>(b, bits);
+        else                ck_fwd_kernel<SASQ_BF16><<<grid, kCkThreads, 0, st>>>(b, bits);
+    }
+    return hipGetLastError() == hipSuccess ? SASQ_OK : SASQ_ERR_LAUNCH;
+}
+
+static int ck_bwd(const sasq_ckpt_item* items, int count, bool pc, int bits, sasq_dtype dt, void* workspace, size_t workspace_bytes, void* stream)
+{
+    const int rc = ck_check(items, count, pc, true, bits, (int)dt);
+    if (rc) return rc;
+    if (!workspace || workspace_bytes < ck_workspace(items, count, pc)) return SASQ_ERR_WORKSPACE;
+    if (!aligned16(workspace)) return SASQ_ERR_ALIGN;
+    CkBatch b{};
+    ck_plan(items, count, pc, true, static_cast<char*>(workspace), b);
+    hipStream_t st = as_stream(stream);
+    const int grid = b.first[count];
+    if (pc) {
+        if (dt == SASQ_F16) ck_bwd_pc_kernel<SASQ_F16><<<grid, kCkThreads, 0, st>>>(b, bits);
+        else                ck_bwd_pc_kernel<SASQ_BF16><<<grid, kCkThreads, 0, st>>>(b, bits);
+        int64_t widest = 0;
+        for (int i = 0; i < count; ++i)
+            if (b.it[i].chunks > 1 && b.it[i].cols > widest) widest = b.it[i].cols;
+        const int64_t blocks = (widest + kCkThreads - 1) / kCkThreads;
+        if (blocks) ck_join_pc_kernel<<<dim3((unsigned)(blocks < 1024 ? blocks : 1024), (unsigned)count), kCkThreads, 0, st>>>(b);
+    } else {
+        if (dt == SASQ_F16) ck_bwd_kernel<SASQ_F16><<<grid, kCkThreads, 0, st>>>(b, bits);
+        else                ck_bwd_kernel<SASQ_BF16><<<grid, kCkThreads, 0, st>>>(b, bits);
+        ck_join_kernel<<<count, kCkThreads, 0, st>>>(b);
+    }
+    return hipGetLastError() == hipSuccess ? SASQ_OK : SASQ_ERR_LAUNCH;
+}
+
+}  // namespace sasq
+
+using namespace sasq;
+
+extern "C" int sasq_fakequant_fwd_ckpt_batch(const sasq_ckpt_item* items, int count, int bits, sasq_dtype dt, void* stream)
+{
+    return ck_fwd(items, count, false, bits, dt, stream);
+}
+extern "C" int sasq_fakequant_fwd_pc_ckpt_batch(const sasq_ckpt_item* items, int count, int bits, sasq_dtype dt, void* stream)
+{
+    return ck_fwd(items, count, true, bits, dt, stream);
+}
+extern "C" size_t sasq_fakequant_bwd_ckpt_batch_workspace(const sasq_ckpt_item* items, int count) { return ck_workspace(items, count, false); }
+extern "C" size_t sasq_fakequant_bwd_pc_ckpt_batch_workspace(const sasq_ckpt_item* items, int count) { return ck_workspace(items, count, true); }
+extern "C" int sasq_fakequant_bwd_ckpt_batch(const sasq_ckpt_item* items, int count, int bits, sasq_dtype dt, void* workspace, size_t workspace_bytes, void* stream)
+{
+    return ck_bwd(items, count, false, bits, dt, workspace, workspace_bytes, stream);
+}
+extern "C" int sasq_fakequant_bwd_pc_ckpt_batch(const sasq_ckpt_item* items, int count, int bits, sasq_dtype dt, void* workspace, size_t workspace_bytes, void* stream)
+{
+    return ck_bwd(items, count, true, bits, dt, workspace, workspace_bytes, stream);
+}
+
+extern "C" int sasq_fakequant_fwd_ckpt(const void* x, const float* s, void* y, int8_t* kept, int64_t rows, int64_t cols, int bits, sasq_dtype dt, void* stream)
+{
+    const sasq_ckpt_item it{x, s, y, kept, nullptr, nullptr, rows, cols};
+    return ck_fwd(&it, 1, false, bits, dt, stream);
+}
+extern "C" int sasq_fakequant_fwd_pc_ckpt(const void* x, const float* s, void* y, int8_t* kept, int64_t rows, int64_t cols, int bits, sasq_dtype dt, void* stream)
+{
+    const sasq_ckpt_item it{x, s, y, kept, nullptr, nullptr, rows, cols};
+    return ck_fwd(&it, 1, true, bits, dt, stream);
+}
+extern "C" size_t sasq_fakequant_bwd_ckpt_workspace(int64_t rows, int64_t cols)
+{
+    const sasq_ckpt_item it{nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, rows, cols};
+    return ck_workspace(&it, 1, false);
+}
+extern "C" size_t sasq_fakequant_bwd_pc_ckpt_workspace(int64_t rows, int64_t cols)
+{
+    const sasq_ckpt_item it{nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, rows, cols};
+    return ck_workspace(&it, 1, true);
+}
+extern "C" int sasq_fakequant_bwd_ckpt(const int8_t* kept, const void* dy, void* dx, float* ds, int64_t rows, int64_t cols, int bits, sasq_dtype dt,
+                                       void* workspace, size_t workspace_bytes, void* stream)
+{
+    const sasq_ckpt_item it{nullptr, nullptr, dx, const_cast<int8_t*>(kept), dy, ds, rows, cols};
+    return ck_bwd(&it, 1, false, bits, dt, workspace, workspace_bytes, stream);
+}
+extern "C" int sasq_fakequant_bwd_pc_ckpt(const int8_t* kept, const void* dy, void* dx, float* ds, int64_t rows, int64_t cols, int bits, sasq_dtype dt,
+                                          void* workspace, size_t workspace_bytes, void* stream)
+{
+    const sasq_ckpt_item it{nullptr, nullptr, dx, const_cast<int8_t*>(kept), dy, ds, rows, cols};
+    return ck_bwd(&it, 1, true, bits, dt, workspace, workspace_bytes, stream);
+}
