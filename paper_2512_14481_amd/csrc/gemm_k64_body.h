@@ -91,9 +91,8 @@ __device__ __forceinline__ void lds_load16(uint32_t lds_a, uint32_t lds_b, const
 // K tiles ahead.  us, halves | lines, operands from memory: f16 4096 x 11008 -> 4096 254 | 231, 4096 x 4096 -> 11008 273 | 258, bf16 255 | 231
 // and 268 | 258, 4096 x 4096 -> 4096 101 | 94, 1024 x 5120 -> 5120 79 | 66, 777 x 4096 -> 4096 36 | 36; weights in the caches, f16 241 | 234, 259 |
 // 258, bf16 235 | 227, 258 | 257, 95 | 93, 71 | 62, 32 | 29.
-// EXT: what a GEMM of its own brings along where it is more than a product of two dense operands (linear_ce_gemm.h): rows of X `x_pitch` bytes
-// apart and weight blocks `w_kt` K tiles a row of blocks, both of more than the K contracted, and what becomes of the sums (`finish`, in place
-// of the epilogue).
+// EXT: what a GEMM of its own brings along where it is more than a product of two dense operands (linear_ce_gemm.hip), with OP 1: X in 1 KB blocks
+// too, `x_kt` and `w_kt` blocks a row of blocks, of which K may be a part, and what becomes of the sums (`finish`, in place of the epilogue).
 struct NoExt { static constexpr bool kOn = false; };
 template <int DT, int WMODE, int BM, int BN, bool ROWS, int GROUPED = GR_NONE, int OP = 0, class EXT = NoExt>
 __device__ __forceinline__
@@ -103,7 +102,7 @@ void gemm_k64_body(const int8_t* __restrict__ xq, const uint8_t* __restrict__ wq
                    int32_t* __restrict__ acc_out, int M, int N, int K,
                    int tm, int tn, char* lds, int group_tiles = 0, const EXT& ext = EXT{})
 {
-    static_assert(!EXT::kOn || OP != 0, "extended GEMMs contract 16-bit floats");
+    static_assert(!EXT::kOn || OP == 1, "extended GEMMs contract 16-bit floats");
     static_assert(!GROUPED || (BM == 128 && !ROWS), "grouped factors: 128-row tiles");
     static_assert(OP == 0 || (WMODE == KW_I8B && !ROWS && !GROUPED), "float contraction: pre-arranged weight blocks, no factors");
     constexpr bool FLT = OP != 0, XL = OP == 2;
@@ -136,19 +135,20 @@ void gemm_k64_body(const int8_t* __restrict__ xq, const uint8_t* __restrict__ wq
     const int lrow = lane >> 2;
     const int lchunk = (lane & 3) ^ (((lane >> 3) & 3) ^ ((lane >> 5) & 1));
     const int last_rb = (M - 1) >> 4;
-    int XP = K, WKT = KT;
-    if constexpr (EXT::kOn) { XP = ext.x_pitch; WKT = ext.w_kt; }
-    const int8_t* xpanel = FLT ? xq + (int64_t)m0 * XP : xq + (int64_t)(m0 >> 4) * KT * 1024;
-    constexpr int kXTileStep = FLT ? kBK : 1024;
+    constexpr bool XROWS = FLT && !EXT::kOn;
+    int XKT = KT, WKT = KT;
+    if constexpr (EXT::kOn) { XKT = ext.x_kt; WKT = ext.w_kt; }
+    const int8_t* xpanel = XROWS ? xq + (int64_t)m0 * K : xq + (int64_t)(m0 >> 4) * XKT * 1024;
+    constexpr int kXTileStep = XROWS ? kBK : 1024;
     const int8_t* wpanel = reinterpret_cast<const int8_t*>(wq) + (WMODE == KW_I8B ? (int64_t)(n0 >> 4) * WKT * 1024
                                                                   : I4 ? (int64_t)(n0 >> 5) * KT * 1024 : (int64_t)n0 * K);
     constexpr int XO = XL ? 2 * XS : XS;
     uint32_t xoff[XO], woff[WSL];
 #pragma unroll
     for (int j = 0; j < XO; ++j)
-        xoff[j] = XL  ? (uint32_t)(min((4 * j + wave) * 8 + (lane >> 3), M - 1 - m0) * XP + (((lane & 7) ^ (lane >> 3)) << 4))
-                : FLT ? (uint32_t)(min((4 * j + wave) * 16 + lrow, M - 1 - m0) * XP + lchunk * 16)
-                      : (uint32_t)(min(4 * j + wave, last_rb - (m0 >> 4)) * KT * 1024 + lane * 16);
+        xoff[j] = XL  ? (uint32_t)(min((4 * j + wave) * 8 + (lane >> 3), M - 1 - m0) * K + (((lane & 7) ^ (lane >> 3)) << 4))
+                : XROWS ? (uint32_t)(min((4 * j + wave) * 16 + lrow, M - 1 - m0) * K + lchunk * 16)
+                        : (uint32_t)(min(4 * j + wave, last_rb - (m0 >> 4)) * XKT * 1024 + lane * 16);
 #pragma unroll
     for (int j = 0; j < WSL; ++j) {
         if (I4) woff[j] = (uint32_t)(min(4 * j + wave, ((N - 1) >> 5) - (n0 >> 5)) * KT * 1024 + lane * 16);   // blocks of 32 rows

@@ -50,11 +50,18 @@ struct CeArgs {
     float* u;                                   // [T] packed: u
     float* row_loss;                            // [T] packed: loss, for the mean
     RowStat* stats;                             // [columns of a piece / stat_cols][T]
-    uint16_t* xs;                               // [T][Hp] packed rows of x, zeros past H
-    uint16_t* a;                                // [T][piece]
+    uint16_t* xs;                               // packed rows of x, zeros past H, in the 1 KB blocks of the GEMMs' operands (block_at)
+    uint16_t* a;                                // a_v of a piece, rows and columns in the same blocks
     float* acc;                                 // [splits][T][Hp]
 };
 constexpr int stat_cols(int tile) { return tile == 2 ? 64 : 128; }     // half a tile's columns: what a wave has
+
+// Element (row, col) of an operand in 1 KB blocks of 16 rows x 32 columns, `kt` blocks a row of blocks; col a multiple of 8: a chunk of 16 bytes.
+__device__ __forceinline__ int64_t block_at(int64_t row, int col, int kt)
+{
+    const int r = (int)(row & 15), c = (col >> 3) & 3;
+    return ((row >> 4) * kt + (col >> 5)) * 512 + ((4 * r + (c ^ swz64(r))) << 3) + (col & 7);
+}
 
 void launch_ce_logits(const CeArgs& c, sasq_dtype dt, int64_t col0, int64_t cols, hipStream_t st);
 void launch_ce_grad(const CeArgs& c, sasq_dtype dt, int64_t col0, int64_t cols, hipStream_t st);

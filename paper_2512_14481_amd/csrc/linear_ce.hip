@@ -121,7 +121,6 @@ __global__ __launch_bounds__(256) void ce_stage_kernel(const uint16_t* __restric
     const int p = (int)blockIdx.x * 4 + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (p >= *count) return;
     const uint16_t* src = x + (int64_t)row[p] * stride;
-    uint16_t* dst = xs + (int64_t)p * Hp;
     for (int h = lane * 8; h < Hp; h += 512) {
         u32x4 o = {0u, 0u, 0u, 0u};
         if (VEC && h < H) {
@@ -133,7 +132,7 @@ __global__ __launch_bounds__(256) void ce_stage_kernel(const uint16_t* __restric
                 o[e] = lo | hi << 16;
             }
         }
-        *reinterpret_cast<u32x4*>(dst + h) = o;
+        *reinterpret_cast<u32x4*>(xs + block_at(p, h, Hp / 32)) = o;
     }
 }
 
@@ -201,7 +200,7 @@ __global__ __launch_bounds__(256) void ce_scale_kernel(uint16_t* __restrict__ a,
     const float m = run[p].m;
     for (int c = threadIdx.x * 8; c < cols; c += 256 * 8) {
         const float f = exp2f(stats[(int64_t)(c / stat_cols) * T + p].m - m);
-        u32x4* at = reinterpret_cast<u32x4*>(a + (int64_t)p * pitch + c);
+        u32x4* at = reinterpret_cast<u32x4*>(a + block_at(p, c, (int)pitch / 32));
         u32x4 v = *at;
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = S::pack(S::lo(v[e]) * f, S::hi(v[e]) * f);
@@ -227,8 +226,6 @@ __global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ ac
         uu = u[p];
         t = tgt[p];
     }
-    const int tr = t & 15;
-    const uint8_t* blocks = head + (int64_t)(t >> 4) * (Hp / 32) * 1024 + tr * 64;
     for (int h = threadIdx.x * 8; h < H; h += 256 * 8) {
         float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
         if (p >= 0) {
@@ -237,7 +234,7 @@ __global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ ac
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] += at[e];
             }
-            const u32x4 w = *reinterpret_cast<const u32x4*>(blocks + (int64_t)(h >> 5) * 1024 + ((((h >> 3) & 3) ^ swz64(tr)) << 4));
+            const u32x4 w = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(head) + block_at(t, h, Hp / 32));
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = g * __builtin_fmaf(cf, v[e], -uu * ((e & 1) ? S::hi(w[e >> 1]) : S::lo(w[e >> 1])));
         }
@@ -317,9 +314,10 @@ static size_t ce_plan(CeArgs& c, int64_t piece, char* base)
     part(c.u, T * 4);
     part(c.row_loss, T * 4);
     part(c.stats, (size_t)(c.piece / stat_cols(c.tile)) * T * 8);
-    part(c.xs, T * (size_t)c.Hp * 2);
+    const size_t T16 = (T + 15) / 16 * 16;
+    part(c.xs, T16 * (size_t)c.Hp * 2);
     if (c.grad) {
-        part(c.a, T * (size_t)c.piece * 2);
+        part(c.a, T16 * (size_t)c.piece * 2);
         part(c.acc, (size_t)c.splits * T * (size_t)c.Hp * 4);
     }
     return at;

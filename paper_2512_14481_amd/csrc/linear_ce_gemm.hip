@@ -14,100 +14,116 @@ __device__ __forceinline__ bool tile_of_counted(int tiles_m, int tiles_n, int& t
     return (int)(blockIdx.x >> 3) < per && tile_of_block((int)blockIdx.x, tiles_m, tiles_n, tm, tn);
 }
 
+// Lanes l and l ^ 16, or l ^ 32, with the results of both.
+__device__ __forceinline__ float max16(float v)
+{
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+__device__ __forceinline__ float max32(float v)
+{
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+__device__ __forceinline__ float add16(float v)
+{
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+}
+__device__ __forceinline__ float add32(float v)
+{
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+}
+
 // ---- logits: z of a tile, reduced and stored as a_v ----
 template <int DT, bool GRAD>
 struct LogitsExt {
     static constexpr bool kOn = true;
-    int x_pitch, w_kt;
+    int x_kt, w_kt;
     const int32_t* tgt;
     float* zt;
     RowStat* stats;
     int64_t T;                                  // rows of `stats`
     uint16_t* a;
-    int64_t a_pitch;
+    int a_kt;                                   // blocks a row of blocks
     int col0;                                   // first column of the piece
 
     // Lane (fq, frow) of a wave holds, for each of its MF rows b * 16 + frow, the columns 16 g + 4 fq + e: a row's columns lie in the four lanes
-    // of equal frow.
+    // of equal frow, which meet without LDS.  A 16-byte chunk of a_v is in two lanes; one exchange between neighbouring groups of sixteen
+    // lanes gives each a whole one, and a wave's store is a whole 1 KB block.
     template <int BM, int BN, class ACC>
-    __device__ __forceinline__ void finish(ACC& acc, int m0, int n0, int M, int N, char* lds) const
+    __device__ __forceinline__ void finish(ACC& acc, int m0, int n0, int M, int N, char*) const
     {
         using S = Store16<DT>;
-        constexpr int MF = BM / 32, NF = BN / 32, kStride = BN + 16;
+        constexpr int MF = BM / 32, NF = BN / 32;
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const int wm = wave & 1, wn = wave >> 1, frow = lane & 15, fq = lane >> 4;
         const int wn0 = n0 + wn * (BN / 2), wm0 = m0 + wm * (BM / 2);
-        const bool edge = wn0 + BN / 2 > N;                   // columns past the vocabulary
-        char* stage = lds + wave * 16 * kStride;
-        constexpr int kChunksPerRow = BN / 16, kRowsPerPass = 64 / kChunksPerRow, kPasses = 16 / kRowsPerPass;
-        const int crow = lane / kChunksPerRow, cchunk = lane % kChunksPerRow;
+        const bool edge = wn0 + BN / 2 > N;                    // columns past the vocabulary
+        RowStat* stat = stats + (int64_t)((wn0 - col0) / (BN / 2)) * T;
+        const int chunk = ((fq & 1) << 1) | (fq >> 1);         // of its row's four in a block
+        uint16_t* dst = a + ((int64_t)(wm0 >> 4) * a_kt + ((wn0 - col0) >> 5)) * 512 + ((4 * frow + (chunk ^ swz64(frow))) << 3);
 #pragma unroll
         for (int b = 0; b < MF; ++b) {
-            const int m = wm0 + b * 16 + frow;
             __builtin_amdgcn_sched_barrier(0);                 // a row of tiles at a time: all of them at once need more registers than there are
-            float zv[NF][4];
-#pragma unroll
-            for (int g = 0; g < NF; ++g)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) zv[g][e] = acc[g][b][e];
-            if (edge) {
-#pragma unroll
-                for (int g = 0; g < NF; ++g)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (wn0 + 16 * g + 4 * fq + e >= N) zv[g][e] = -__builtin_inff();
-            }
+            if (wm0 + b * 16 >= M) break;
+            const int m = wm0 + b * 16 + frow;
             const int t = tgt[min(m, M - 1)] - wn0;            // the target's place among the wave's columns
             const bool here = t >= 0 && t < BN / 2 && ((t >> 2) & 3) == fq;
-            if (__builtin_amdgcn_ballot_w64(here)) {
-                float z = 0.0f;
+            // Two copies of the rest: with the target or an edge among the columns, and without, where no element is looked at for them.
+            auto rows = [&](auto special) {
+                constexpr bool SPECIAL = decltype(special)::value;
+                float zv[NF][4];
 #pragma unroll
                 for (int g = 0; g < NF; ++g)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (here && t == 16 * g + 4 * fq + e) { z = zv[g][e]; zv[g][e] = -__builtin_inff(); }
-                if (here && m < M) zt[m] = z;
-            }
-            float top = zv[0][0];
+                    for (int e = 0; e < 4; ++e) zv[g][e] = acc[g][b][e];
+                if constexpr (SPECIAL) {
+                    float z = 0.0f;
 #pragma unroll
-            for (int g = 0; g < NF; ++g)
+                    for (int g = 0; g < NF; ++g)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) top = fmaxf(top, zv[g][e]);
-            top = fmaxf(top, __shfl_xor(top, 16, kWave));
-            top = fmaxf(top, __shfl_xor(top, 32, kWave));
-            // whole numbers, so that one M takes another's place by an exact factor
-            const float mm = top == -__builtin_inff() ? 0.0f : ceilf(top * kLog2e) - (float)kTopExp<DT>;
-            float sum = 0.0f;
-            u32x2 pk[NF];
-#pragma unroll
-            for (int g = 0; g < NF; ++g) {
-                float av[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float z = zv[g][e];
-                    av[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z, kLog2eLow, __builtin_fmaf(z, kLog2e, -mm)));
-                    sum += av[e];
+                        for (int e = 0; e < 4; ++e) {
+                            if (here && t == 16 * g + 4 * fq + e) { z = zv[g][e]; zv[g][e] = -__builtin_inff(); }
+                            if (edge && wn0 + 16 * g + 4 * fq + e >= N) zv[g][e] = -__builtin_inff();
+                        }
+                    if (here && m < M) zt[m] = z;
                 }
-                pk[g] = u32x2{S::pack(av[0], av[1]), S::pack(av[2], av[3])};
-            }
-            sum += __shfl_xor(sum, 16, kWave);
-            sum += __shfl_xor(sum, 32, kWave);
-            if (fq == 0 && m < M) stats[(int64_t)((wn0 - col0) / (BN / 2)) * T + m] = RowStat{mm, sum};
-            if constexpr (GRAD) {
-                // sixteen rows through the wave's own LDS, out in 128-bit stores; LDS serves a wave's requests in order
+                float top = zv[0][0];
 #pragma unroll
-                for (int g = 0; g < NF; ++g) *reinterpret_cast<u32x2*>(stage + frow * kStride + (16 * g + 4 * fq) * 2) = pk[g];
-                asm volatile("" ::: "memory");
-                u32x4 back[kPasses];
+                for (int g = 0; g < NF; ++g)
 #pragma unroll
-                for (int p = 0; p < kPasses; ++p) back[p] = *reinterpret_cast<const u32x4*>(stage + (p * kRowsPerPass + crow) * kStride + cchunk * 16);
-                asm volatile("" ::: "memory");
+                    for (int e = 0; e < 4; ++e) top = fmaxf(top, zv[g][e]);
+                top = max32(max16(top));
+                // whole numbers, so that one M takes another's place by an exact factor
+                float mm = ceilf(top * kLog2e) - (float)kTopExp<DT>;
+                if (SPECIAL) mm = top == -__builtin_inff() ? 0.0f : mm;
+                float sum = 0.0f;
+                u32x2 pk[NF];
 #pragma unroll
-                for (int p = 0; p < kPasses; ++p) {
-                    const int row = wm0 + b * 16 + p * kRowsPerPass + crow;
-                    if (row < M) *reinterpret_cast<u32x4*>(a + (int64_t)row * a_pitch + (wn0 - col0) + cchunk * 8) = back[p];
+                for (int g = 0; g < NF; ++g) {
+                    float av[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        av[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(zv[g][e], kLog2e, -mm));
+                        sum += av[e];
+                    }
+                    pk[g] = u32x2{S::pack(av[0], av[1]), S::pack(av[2], av[3])};
                 }
-            }
+                sum = add32(add16(sum));
+                if (fq == 0 && m < M) stat[m] = RowStat{mm, sum};
+                if constexpr (GRAD) {
+#pragma unroll
+                    for (int g = 0; g < NF; g += 2) {
+                        const auto lo = __builtin_amdgcn_permlane16_swap(pk[g][0], pk[g + 1][0], false, false);
+                        const auto hi = __builtin_amdgcn_permlane16_swap(pk[g][1], pk[g + 1][1], false, false);
+                        *reinterpret_cast<u32x4*>(dst + (int64_t)b * a_kt * 512 + (g >> 1) * 512) = u32x4{lo[0], hi[0], lo[1], hi[1]};
+                    }
+                }
+            };
+            if (edge || __builtin_amdgcn_ballot_w64(here)) rows(std::true_type{});
+            else                                           rows(std::false_type{});
         }
     }
 };
@@ -118,18 +134,18 @@ __attribute__((amdgpu_waves_per_eu(Tile<BM, BN>::kWavesPerSimd, Tile<BM, BN>::kW
 void ce_logits_kernel(const uint16_t* __restrict__ xs, const uint8_t* __restrict__ head, const int32_t* __restrict__ count, int V, int Hp,
                       int tiles_n, LogitsExt<DT, GRAD> ext)
 {
-    __shared__ __attribute__((aligned(1024))) char lds[lds_bytes_lines<BM, BN>()];
+    __shared__ __attribute__((aligned(1024))) char lds[kStages * Tile<BM, BN>::kStageBytes];
     const int M = *count;
     int tm, tn;
     if (!tile_of_counted((M + BM - 1) / BM, tiles_n, tm, tn)) return;
-    gemm_k64_body<DT, KW_I8B, BM, BN, false, GR_NONE, 2, LogitsExt<DT, GRAD>>(
+    gemm_k64_body<DT, KW_I8B, BM, BN, false, GR_NONE, 1, LogitsExt<DT, GRAD>>(
         reinterpret_cast<const int8_t*>(xs), head, nullptr, nullptr, nullptr, nullptr, nullptr, M, V, Hp * 2, tm, ext.col0 / BN + tn, lds, 0, ext);
 }
 
 // ---- gradient: running sums over v of a_v W_v ----
 struct SumsExt {
     static constexpr bool kOn = true;
-    int x_pitch, w_kt;
+    int x_kt, w_kt;
     float* acc;                                 // [T][Hp]
     const float* beta;                          // NULL: the first piece
     int Hp;
@@ -141,23 +157,31 @@ struct SumsExt {
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const int wm = wave & 1, wn = wave >> 1, frow = lane & 15, fq = lane >> 4;
         const int wn0 = n0 + wn * (BN / 2), wm0 = m0 + wm * (BM / 2);
+        // The next row of tiles' old sums are requested before this one's are needed.
+        f32x4 old[2][NF];
+        float f[2] = {0.0f, 0.0f};
+        auto fetch = [&](int b) {
+            const int m = min(wm0 + b * 16 + frow, M - 1);
+            f[b & 1] = beta[m];
+#pragma unroll
+            for (int g = 0; g < NF; ++g) old[b & 1][g] = *reinterpret_cast<const f32x4*>(acc + (int64_t)m * Hp + min(wn0 + 16 * g, Hp - 16) + 4 * fq);
+        };
+        if (beta) fetch(0);
 #pragma unroll
         for (int b = 0; b < MF; ++b) {
-            const int m = wm0 + b * 16 + frow;
             __builtin_amdgcn_sched_barrier(0);
-            if (m >= M) continue;
-            const float f = beta ? beta[m] : 0.0f;
+            const int m = wm0 + b * 16 + frow;
+            if (beta && b + 1 < MF) fetch(b + 1);
+            __builtin_amdgcn_sched_barrier(0);
             float* row = acc + (int64_t)m * Hp + wn0 + 4 * fq;
 #pragma unroll
             for (int g = 0; g < NF; ++g) {
-                if (wn0 + 16 * g >= Hp) break;
                 f32x4 v = sums[g][b];
                 if (beta) {
-                    const f32x4 old = *reinterpret_cast<const f32x4*>(row + 16 * g);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(old[e], f, v[e]);
+                    for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(old[b & 1][g][e], f[b & 1], v[e]);
                 }
-                *reinterpret_cast<f32x4*>(row + 16 * g) = v;
+                if (m < M && wn0 + 16 * g < Hp) *reinterpret_cast<f32x4*>(row + 16 * g) = v;
             }
         }
     }
@@ -170,7 +194,7 @@ __attribute__((amdgpu_waves_per_eu(Tile<BM, BN>::kWavesPerSimd, Tile<BM, BN>::kW
 void ce_grad_kernel(const uint16_t* __restrict__ a, const uint8_t* __restrict__ head_grad, const int32_t* __restrict__ count, int64_t T, int H, int Hp,
                     int cols64, int kt0, int tiles_n, int splits, SumsExt ext)
 {
-    __shared__ __attribute__((aligned(1024))) char lds[lds_bytes_lines<BM, BN>()];
+    __shared__ __attribute__((aligned(1024))) char lds[kStages * Tile<BM, BN>::kStageBytes];
     const int M = *count;
     int tm, tn;
     if (!tile_of_counted((M + BM - 1) / BM, tiles_n * splits, tm, tn)) return;
@@ -194,8 +218,8 @@ void ce_grad_kernel(const uint16_t* __restrict__ a, const uint8_t* __restrict__ 
         }
         return;
     }
-    gemm_k64_body<DT, KW_I8B, BM, BN, false, GR_NONE, 2, SumsExt>(
-        reinterpret_cast<const int8_t*>(a) + (int64_t)c0 * 128, head_grad + (int64_t)(kt0 + 2 * c0) * 1024, nullptr, nullptr, nullptr, nullptr, nullptr,
+    gemm_k64_body<DT, KW_I8B, BM, BN, false, GR_NONE, 1, SumsExt>(
+        reinterpret_cast<const int8_t*>(a) + (int64_t)c0 * 2048, head_grad + (int64_t)(kt0 + 2 * c0) * 1024, nullptr, nullptr, nullptr, nullptr, nullptr,
         M, H, (c1 - c0) * 128, tm, tn, lds, 0, ext);
 }
 
@@ -206,7 +230,7 @@ static void launch_logits(const CeArgs& c, int64_t col0, int64_t cols, hipStream
     const int grid = ((tiles_m * tiles_n + 7) / 8) * 8;
     auto go = [&](auto grad_tag) {
         constexpr bool GRAD = decltype(grad_tag)::value;
-        const LogitsExt<DT, GRAD> ext{c.Hp * 2, c.Hp / 32, c.tgt, c.zt, c.stats, c.T, c.a, c.piece, (int)col0};
+        const LogitsExt<DT, GRAD> ext{c.Hp / 32, c.Hp / 32, c.tgt, c.zt, c.stats, c.T, c.a, c.piece / 32, (int)col0};
         ce_logits_kernel<DT, BM, BN, GRAD><<<grid, kGemmThreads, 0, st>>>(c.xs, c.head, c.count, (int)c.V, c.Hp, tiles_n, ext);
     };
     if (c.grad) go(std::true_type{});
@@ -218,7 +242,7 @@ static void launch_grad(const CeArgs& c, int64_t col0, int64_t cols, hipStream_t
 {
     const int tiles_m = (int)((c.T + BM - 1) / BM), tiles_n = (int)((c.H + BN - 1) / BN);
     const int grid = ((tiles_m * tiles_n * c.splits + 7) / 8) * 8;
-    const SumsExt ext{c.piece * 2, c.Vp / 32, c.acc, col0 ? c.beta : nullptr, c.Hp};
+    const SumsExt ext{c.piece / 32, c.Vp / 32, c.acc, col0 ? c.beta : nullptr, c.Hp};
     ce_grad_kernel<DT, BM, BN><<<grid, kGemmThreads, 0, st>>>(c.a, c.head_grad, c.count, c.T, (int)c.H, c.Hp, (int)((cols + 63) / 64), (int)(col0 / 32),
                                                               tiles_n, c.splits, ext);
 }
