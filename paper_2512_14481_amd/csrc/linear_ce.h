@@ -56,6 +56,8 @@ struct CeArgs {
 };
 constexpr int stat_cols(int tile) { return tile == 2 ? 64 : 128; }     // half a tile's columns: what a wave has
 
+// Blocks from one row of blocks to the next, of `cols` columns (a multiple of 64): an odd number.
+__host__ __device__ constexpr int row_blocks(int64_t cols) { return (int)(cols / 32) | 1; }
 // Element (row, col) of an operand in 1 KB blocks of 16 rows x 32 columns, `kt` blocks a row of blocks; col a multiple of 8: a chunk of 16 bytes.
 __device__ __forceinline__ int64_t block_at(int64_t row, int col, int kt)
 {

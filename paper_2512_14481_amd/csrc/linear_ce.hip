@@ -132,7 +132,7 @@ __global__ __launch_bounds__(256) void ce_stage_kernel(const uint16_t* __restric
                 o[e] = lo | hi << 16;
             }
         }
-        *reinterpret_cast<u32x4*>(xs + block_at(p, h, Hp / 32)) = o;
+        *reinterpret_cast<u32x4*>(xs + block_at(p, h, row_blocks(Hp))) = o;
     }
 }
 
@@ -200,7 +200,7 @@ __global__ __launch_bounds__(256) void ce_scale_kernel(uint16_t* __restrict__ a,
     const float m = run[p].m;
     for (int c = threadIdx.x * 8; c < cols; c += 256 * 8) {
         const float f = exp2f(stats[(int64_t)(c / stat_cols) * T + p].m - m);
-        u32x4* at = reinterpret_cast<u32x4*>(a + block_at(p, c, (int)pitch / 32));
+        u32x4* at = reinterpret_cast<u32x4*>(a + block_at(p, c, row_blocks(pitch)));
         u32x4 v = *at;
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = S::pack(S::lo(v[e]) * f, S::hi(v[e]) * f);
@@ -234,7 +234,7 @@ __global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ ac
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] += at[e];
             }
-            const u32x4 w = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(head) + block_at(t, h, Hp / 32));
+            const u32x4 w = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(head) + block_at(t, h, row_blocks(Hp)));
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = g * __builtin_fmaf(cf, v[e], -uu * ((e & 1) ? S::hi(w[e >> 1]) : S::lo(w[e >> 1])));
         }
@@ -315,9 +315,9 @@ static size_t ce_plan(CeArgs& c, int64_t piece, char* base)
     part(c.row_loss, T * 4);
     part(c.stats, (size_t)(c.piece / stat_cols(c.tile)) * T * 8);
     const size_t T16 = (T + 15) / 16 * 16;
-    part(c.xs, T16 * (size_t)c.Hp * 2);
+    part(c.xs, T16 * row_blocks(c.Hp) * 64);
     if (c.grad) {
-        part(c.a, T16 * (size_t)c.piece * 2);
+        part(c.a, T16 * row_blocks(c.piece) * 64);
         part(c.acc, (size_t)c.splits * T * (size_t)c.Hp * 4);
     }
     return at;
@@ -368,8 +368,8 @@ using namespace sasq;
 extern "C" size_t sasq_head_bytes(int64_t V, int64_t H, sasq_head_form form)
 {
     if (V <= 0 || H <= 0 || V > kCeMaxVocab || H > kCeMaxHidden || up(H, 64) > kCeMaxProduct / V) return 0;
-    if (form == SASQ_HEAD_LOGITS) return (size_t)up(V, 16) * (size_t)up(H, 64) * 2;
-    if (form == SASQ_HEAD_GRAD) return (size_t)up(V, 64) * (size_t)up(H, 16) * 2;
+    if (form == SASQ_HEAD_LOGITS) return (size_t)up(V, 16) * row_blocks(up(H, 64)) * 64;
+    if (form == SASQ_HEAD_GRAD) return (size_t)up(H, 16) * row_blocks(up(V, 64)) * 64;
     return 0;
 }
 
@@ -385,11 +385,11 @@ extern "C" int sasq_prepare_head(const void* w, int64_t w_stride, void* head, in
     auto O = static_cast<u32x4*>(head);
     const bool vec = w_stride % 8 == 0;
     if (form == SASQ_HEAD_LOGITS) {
-        const int64_t kt = up(H, 64) / 32, chunks = up(V, 16) / 16 * kt * 64, blocks = (chunks + 255) / 256;
+        const int64_t kt = row_blocks(up(H, 64)), chunks = up(V, 16) / 16 * kt * 64, blocks = (chunks + 255) / 256;
         head_logits_kernel<<<(int)(blocks < 8192 ? blocks : 8192), 256, 0, st>>>(W, w_stride, O, V, H, kt, chunks, vec);
     } else {
         const int64_t tiles = up(V, 64) / 64 * (up(H, 64) / 64);
-        head_grad_kernel<<<(int)(tiles < 8192 ? tiles : 8192), 256, 0, st>>>(W, w_stride, O, V, H, up(H, 16) / 16, up(V, 64) / 32, tiles, vec);
+        head_grad_kernel<<<(int)(tiles < 8192 ? tiles : 8192), 256, 0, st>>>(W, w_stride, O, V, H, up(H, 16) / 16, row_blocks(up(V, 64)), tiles, vec);
     }
     return hipGetLastError() == hipSuccess ? SASQ_OK : SASQ_ERR_LAUNCH;
 }

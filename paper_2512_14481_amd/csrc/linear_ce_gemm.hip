@@ -230,7 +230,7 @@ static void launch_logits(const CeArgs& c, int64_t col0, int64_t cols, hipStream
     const int grid = ((tiles_m * tiles_n + 7) / 8) * 8;
     auto go = [&](auto grad_tag) {
         constexpr bool GRAD = decltype(grad_tag)::value;
-        const LogitsExt<DT, GRAD> ext{c.Hp / 32, c.Hp / 32, c.tgt, c.zt, c.stats, c.T, c.a, c.piece / 32, (int)col0};
+        const LogitsExt<DT, GRAD> ext{row_blocks(c.Hp), row_blocks(c.Hp), c.tgt, c.zt, c.stats, c.T, c.a, row_blocks(c.piece), (int)col0};
         ce_logits_kernel<DT, BM, BN, GRAD><<<grid, kGemmThreads, 0, st>>>(c.xs, c.head, c.count, (int)c.V, c.Hp, tiles_n, ext);
     };
     if (c.grad) go(std::true_type{});
@@ -242,7 +242,7 @@ static void launch_grad(const CeArgs& c, int64_t col0, int64_t cols, hipStream_t
 {
     const int tiles_m = (int)((c.T + BM - 1) / BM), tiles_n = (int)((c.H + BN - 1) / BN);
     const int grid = ((tiles_m * tiles_n * c.splits + 7) / 8) * 8;
-    const SumsExt ext{c.piece / 32, c.Vp / 32, c.acc, col0 ? c.beta : nullptr, c.Hp};
+    const SumsExt ext{row_blocks(c.piece), row_blocks(c.Vp), c.acc, col0 ? c.beta : nullptr, c.Hp};
     ce_grad_kernel<DT, BM, BN><<<grid, kGemmThreads, 0, st>>>(c.a, c.head_grad, c.count, c.T, (int)c.H, c.Hp, (int)((cols + 63) / 64), (int)(col0 / 32),
                                                               tiles_n, c.splits, ext);
 }
