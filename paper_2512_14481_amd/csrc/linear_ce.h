@@ -5,8 +5,10 @@
 //     loss = ln(1 + e^d)     lse = z_t + loss     u = 1 - p_t = 1 / (1 + e^-d)
 //     dx = g u (sum a_v W_v / S - W_t)
 // The target is kept out of the sums, so that nothing cancels in a row whose target is all but certain.  The vocabulary goes by in pieces:
-//     logits GEMM   z of a piece; each wave reduces its rows over its columns to (M, S), with M a whole number, and stores a_v in 16 bits
-//     join          M of the row so far: the running sums are scaled by 2^(M_old - M), and so (exactly) are the a_v of every wave's columns
+//     logits GEMM   z of a piece; each wave reduces its rows over its columns to (M, S) and stores a_v in 16 bits.  M is the row's so far, if
+//                   there is one and a_v can be held so, else a whole number from the wave's own columns
+//     join          M of the row so far, 2^(M_old - M) for its sums, and which rows have columns with another M
+//     scale         these rows' a_v, by powers of two: those of the first piece, which is made small, and few in others
 //     gradient GEMM the running sums over v of a_v W_v, fp32
 // and at last one kernel divides, subtracts W_t and rounds.  A pass costs the two products that the formulas have and no third; the logits
 // themselves are never stored.
@@ -19,8 +21,10 @@ namespace sasq {
 constexpr float kLog2e = 1.44269504088896340736f, kLog2eLow = 1.92596299112661746887e-8f;    // their sum is log2(e) to 49 bits
 constexpr float kLn2 = 0.693147180559945309417f;
 
-// 16-bit a_v are at most 2^kTopExp: fp16 has 2^-24 .. 2^15 to offer, bf16 the exponents of fp32.
-template <int DT> constexpr int kTopExp = DT == SASQ_F16 ? 15 : 0;
+// 16-bit a_v of a wave's own M are at most 2^kTopExp; those of the row's M so far may be 2^kRoom times as much.  fp16 has 2^-24 .. 2^15 to offer, bf16 the
+// exponents of fp32.
+template <int DT> constexpr int kTopExp = DT == SASQ_F16 ? 11 : 0;
+template <int DT> constexpr int kRoom = DT == SASQ_F16 ? 4 : 64;
 
 struct RowStat { float m, s; };                 // M (a whole number; -inf: no column yet) and S
 
@@ -28,8 +32,9 @@ struct CeArgs {
     // sizes
     int64_t T, V, H;
     int Hp, Vp;                                 // H and V in whole multiples of 64
-    int piece, splits;                          // columns of a piece, parts that its contraction is cut into
-    int tile, grad_tile;                        // 0: 256x256, 1: 128x256, 2: 128x128
+    int piece, first_piece;                     // columns of a piece, and of the first
+    int slots, max_splits;                      // parts that its contraction is cut into: as many as fill the slots of the chip (splits_of)
+    int tile, grad_tile;                        // 0: 256x256, 1: 128x256 (logits), 2: 128x128
     bool grad;
     // operands
     const void* x; int64_t x_stride;
@@ -46,14 +51,24 @@ struct CeArgs {
     float* zt;                                  // [T] packed: z_t
     RowStat* run;                               // [T] packed: M and S of the pieces so far
     float* beta;                                // [T] packed: 2^(M_old - M)
+    uint8_t* scale_rows;                        // [T / 16] packed: whether any of sixteen rows has columns with another M
+    uint32_t* ticket; double* part;             // of the mean: workgroups of the join that are done, their sums
     float* coef;                                // [T] packed: u / S
     float* u;                                   // [T] packed: u
-    float* row_loss;                            // [T] packed: loss, for the mean
     RowStat* stats;                             // [columns of a piece / stat_cols][T]
     uint16_t* xs;                               // packed rows of x, zeros past H, in the 1 KB blocks of the GEMMs' operands (block_at)
     uint16_t* a;                                // a_v of a piece, rows and columns in the same blocks
-    float* acc;                                 // [splits][T][Hp]
+    float* acc;                                 // [parts][counted rows][Hp]
 };
+// Parts of the contraction for so many counted rows.
+__host__ __device__ inline int splits_of(int64_t rows, int bm, int tiles_n, int slots, int max_splits)
+{
+    const int64_t tiles = (rows + bm - 1) / bm * tiles_n;
+    const int64_t s = tiles > 0 ? slots / tiles : 1;
+    return (int)(s < 1 ? 1 : s > max_splits ? max_splits : s);
+}
+constexpr int tile_rows(int tile) { return tile == 0 ? 256 : 128; }
+constexpr int tile_cols(int tile) { return tile == 2 ? 128 : 256; }
 constexpr int stat_cols(int tile) { return tile == 2 ? 64 : 128; }     // half a tile's columns: what a wave has
 
 // Blocks from one row of blocks to the next, of `cols` columns (a multiple of 64): an odd number.

@@ -78,7 +78,8 @@ __global__ __launch_bounds__(256) void head_grad_kernel(const uint16_t* __restri
 constexpr int kPackThreads = 1024;
 __global__ __launch_bounds__(kPackThreads) void ce_pack_kernel(const int32_t* __restrict__ targets, int T, int V, int32_t* __restrict__ count,
                                                               int32_t* __restrict__ pos, int32_t* __restrict__ row, int32_t* __restrict__ tgt,
-                                                              RowStat* __restrict__ run, float* __restrict__ loss, float* __restrict__ lse)
+                                                              RowStat* __restrict__ run, float* __restrict__ loss, float* __restrict__ lse, uint32_t* __restrict__ ticket,
+                                                              float* __restrict__ mean)
 {
     __shared__ int wave_count[kPackThreads / kWave];
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
@@ -110,7 +111,11 @@ __global__ __launch_bounds__(kPackThreads) void ce_pack_kernel(const int32_t* __
         }
         base += all;
     }
-    if (t == 0) *count = base;
+    if (t == 0) {
+        *count = base;
+        *ticket = 0;
+        if (mean && base == 0) *mean = 0.0f;
+    }
 }
 
 // A wave copies one counted row of x to its packed place, with zeros past H.
@@ -137,23 +142,38 @@ __global__ __launch_bounds__(256) void ce_stage_kernel(const uint16_t* __restric
 }
 
 // ---- between the products: M and S of each row so far ----
-// 16 rows a workgroup, 16 threads a row, each for every sixteenth group of columns.  The factors 2^(M_old - M) are exact.
-constexpr int kJoinRows = 16, kJoinLanes = 16;
-__global__ __launch_bounds__(256) void ce_join_kernel(const RowStat* __restrict__ stats, int groups, int64_t T, const int32_t* __restrict__ count,
-                                                     RowStat* __restrict__ run, float* __restrict__ beta, const float* __restrict__ zt,
-                                                     const int32_t* __restrict__ row, float* __restrict__ coef, float* __restrict__ u_out,
-                                                     float* __restrict__ row_loss, float* __restrict__ loss, float* __restrict__ lse, int last)
+// 16 rows a workgroup, 64 threads a row, each for every 64th group of columns, eight of them requested at a time.  All factors are exact powers of two.
+constexpr int kJoinRows = 16, kJoinLanes = 64, kJoinThreads = kJoinRows * kJoinLanes, kJoinAhead = 8;
+__global__ __launch_bounds__(kJoinThreads) void ce_join_kernel(const RowStat* __restrict__ stats, int groups, int64_t T, const int32_t* __restrict__ count,
+                                                              RowStat* __restrict__ run, float* __restrict__ beta, uint8_t* __restrict__ scale_rows,
+                                                              const float* __restrict__ zt, const int32_t* __restrict__ row, float* __restrict__ coef,
+                                                              float* __restrict__ u_out, float* __restrict__ loss, float* __restrict__ lse,
+                                                              float* __restrict__ mean, double* __restrict__ part_loss, uint32_t* __restrict__ ticket, int last)
 {
     __shared__ float part[kJoinLanes][kJoinRows];
+    __shared__ double row_loss[kJoinRows];
+    __shared__ bool is_last;
     const int r = threadIdx.x % kJoinRows, k = threadIdx.x / kJoinRows, p = (int)blockIdx.x * kJoinRows + r;
+    const RowStat* mine = stats + min((int64_t)p, T - 1);      // (rows past the counted ones hold anything)
+    const RowStat old = run[min((int64_t)p, T - 1)];
+    RowStat s[kJoinAhead];
+    auto fetch = [&](int g0) {
+#pragma unroll
+        for (int j = 0; j < kJoinAhead; ++j) {
+            const int g = g0 + j * kJoinLanes;
+            s[j] = mine[(int64_t)min(g, groups - 1) * T];
+            if (g >= groups) s[j].s = 0.0f;
+        }
+    };
+    float top = -__builtin_inff();
+    fetch(k);
     const int n = *count;
     if ((int)blockIdx.x * kJoinRows >= n) return;
-    const RowStat* mine = stats + min(p, n - 1);
-    const RowStat old = run[min(p, n - 1)];
-    float top = -__builtin_inff();
-    for (int g = k; g < groups; g += kJoinLanes) {
-        const RowStat s = mine[(int64_t)g * T];
-        if (s.s != 0.0f) top = fmaxf(top, s.m);
+    for (int g0 = k; g0 < groups; g0 += kJoinLanes * kJoinAhead) {
+        if (g0 != k) fetch(g0);
+#pragma unroll
+        for (int j = 0; j < kJoinAhead; ++j)
+            if (s[j].s != 0.0f) top = fmaxf(top, s[j].m);
     }
     part[k][r] = top;
     __syncthreads();
@@ -163,65 +183,130 @@ __global__ __launch_bounds__(256) void ce_join_kernel(const RowStat* __restrict_
     if (m == -__builtin_inff()) m = 0.0f;
     __syncthreads();
     float sum = 0.0f;
-    for (int g = k; g < groups; g += kJoinLanes) {
-        const RowStat s = mine[(int64_t)g * T];
-        if (s.s != 0.0f) sum += s.s * exp2f(s.m - m);
+    bool other = false;
+    for (int g0 = k; g0 < groups; g0 += kJoinLanes * kJoinAhead) {
+        if (groups > kJoinLanes * kJoinAhead) fetch(g0);
+#pragma unroll
+        for (int j = 0; j < kJoinAhead; ++j) {
+            if (s[j].s != 0.0f) sum += s[j].s * exp2f(s[j].m - m);
+            other = other || (s[j].s != 0.0f && s[j].m != m);
+        }
     }
     part[k][r] = sum;
-    __syncthreads();
-    if (k != 0 || p >= n) return;
-    const float f = old.s != 0.0f ? exp2f(old.m - m) : 0.0f;
-    float all = old.s * f;
+    const int any = __syncthreads_or(other && p < n);
+    if (scale_rows && threadIdx.x == 0) scale_rows[blockIdx.x] = any != 0;
+    if (k == 0 && p < n) {
+        const float f = old.s != 0.0f ? exp2f(old.m - m) : 0.0f;
+        float all = old.s * f;
 #pragma unroll
-    for (int j = 0; j < kJoinLanes; ++j) all += part[j][r];
-    run[p] = RowStat{m, all};
-    beta[p] = f;
-    if (!last) return;
-    // In fp64: a small loss is the exponential of a difference.
-    const double z = (double)zt[p];
-    const double d = all == 0.0f ? -(double)__builtin_inff() : ((double)m + log2((double)all)) * 0.69314718055994530942 - z;
-    const double l = d > 0.0 ? d + log1p(exp(-d)) : log1p(exp(d));
-    const double u = 1.0 / (1.0 + exp(-d));
-    loss[row[p]] = (float)l;
-    row_loss[p] = (float)l;
-    if (lse) lse[row[p]] = (float)(z + l);
-    u_out[p] = (float)u;
-    coef[p] = all == 0.0f ? 0.0f : (float)(u / (double)all);
+        for (int j = 0; j < kJoinLanes; ++j) all += part[j][r];
+        run[p] = RowStat{m, all};
+        beta[p] = f;
+        if (last) {
+            // In fp64: a small loss is the exponential of a difference.
+            const double z = (double)zt[p];
+            const double d = all == 0.0f ? -(double)__builtin_inff() : ((double)m + log2((double)all)) * 0.69314718055994530942 - z;
+            const double l = d > 0.0 ? d + log1p(exp(-d)) : log1p(exp(d));
+            const double u = 1.0 / (1.0 + exp(-d));
+            loss[row[p]] = (float)l;
+            if (lse) lse[row[p]] = (float)(z + l);
+            u_out[p] = (float)u;
+            coef[p] = all == 0.0f ? 0.0f : (float)(u / (double)all);
+            row_loss[r] = (double)(float)l;
+        }
+    } else if (k == 0) {
+        row_loss[r] = 0.0;
+    }
+    if (!last || !mean) return;
+    // the mean, where no kernel follows: every workgroup's sum is published, the last to arrive adds them in their order
+    __syncthreads();
+    const int blocks = (n + kJoinRows - 1) / kJoinRows;
+    if (threadIdx.x == 0) {
+        double all = 0.0;
+        for (int j = 0; j < kJoinRows; ++j) all += row_loss[j];
+        if (blocks == 1) {
+            *mean = (float)(all / (double)n);
+            is_last = false;
+        } else is_last = publish_then_ticket(&part_loss[blockIdx.x], all, ticket) == (uint32_t)blocks - 1;
+    }
+    __syncthreads();
+    if (!is_last) return;
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+    __shared__ double wave_part[kJoinThreads / kWave];
+    double all = 0.0;
+    for (int i = threadIdx.x; i < blocks; i += kJoinThreads) all += __hip_atomic_load(&part_loss[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    all = wave_sum(all);
+    if (threadIdx.x % kWave == 0) wave_part[threadIdx.x / kWave] = all;
+    __syncthreads();
+    if (threadIdx.x) return;
+    all = 0.0;
+    for (int j = 0; j < kJoinThreads / kWave; ++j) all += wave_part[j];
+    *mean = (float)(all / (double)n);
 }
 
-// a_v of a group of columns from its M to the row's, in place.
+// a_v of groups of columns with another M than their row's, in place: sixteen rows and 64 blocks a workgroup, a 1 KB block a wave and access.
+constexpr int kScaleBlocks = 64;
 template <int DT>
-__global__ __launch_bounds__(256) void ce_scale_kernel(uint16_t* __restrict__ a, int64_t pitch, int cols, int stat_cols, const RowStat* __restrict__ stats,
-                                                      const RowStat* __restrict__ run, int64_t T, const int32_t* __restrict__ count)
+__global__ __launch_bounds__(256) void ce_scale_kernel(uint16_t* __restrict__ a, int a_kt, int kt, int stat_blocks, const RowStat* __restrict__ stats,
+                                                      const RowStat* __restrict__ run, const uint8_t* __restrict__ scale_rows, int64_t T,
+                                                      const int32_t* __restrict__ count)
 {
     using S = Store16<DT>;
-    const int p = (int)blockIdx.x;
-    if (p >= *count) return;
+    const int n = *count, r16 = (int)blockIdx.x;
+    if (r16 * 16 >= n || !scale_rows[r16]) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int p = min(r16 * 16 + (lane >> 2), n - 1);
     const float m = run[p].m;
-    for (int c = threadIdx.x * 8; c < cols; c += 256 * 8) {
-        const float f = exp2f(stats[(int64_t)(c / stat_cols) * T + p].m - m);
-        u32x4* at = reinterpret_cast<u32x4*>(a + block_at(p, c, row_blocks(pitch)));
-        u32x4 v = *at;
+    const int k1 = min(kt, ((int)blockIdx.y + 1) * kScaleBlocks);
+    u32x4* at = reinterpret_cast<u32x4*>(a) + (int64_t)r16 * a_kt * 64 + lane;
+    constexpr int kAhead = 4;
+    for (int k = (int)blockIdx.y * kScaleBlocks + wave; k < k1; k += 4 * kAhead) {
+        u32x4 v[kAhead];
+        float f[kAhead];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = S::pack(S::lo(v[e]) * f, S::hi(v[e]) * f);
-        *at = v;
+        for (int j = 0; j < kAhead; ++j) {
+            const int kk = min(k + 4 * j, k1 - 1);
+            v[j] = at[(int64_t)kk * 64];
+            f[j] = stats[(int64_t)(kk / stat_blocks) * T + p].m;
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            if (k + 4 * j >= k1) break;
+            const float s = exp2f(f[j] - m);
+            u32x4 o;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = S::pack(S::lo(v[j][e]) * s, S::hi(v[j][e]) * s);
+            at[(int64_t)(k + 4 * j) * 64] = o;
+        }
     }
 }
 
 // ---- the end: dx of every row; left-out ones are 0 ----
 template <int DT, bool VEC>
-__global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ acc, int splits, int64_t T, const int32_t* __restrict__ count,
+__global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ acc, int bm, int tiles_n, int slots, int max_splits, const int32_t* __restrict__ count,
                                                    const int32_t* __restrict__ pos, const int32_t* __restrict__ tgt, const float* __restrict__ coef,
                                                    const float* __restrict__ u, const uint8_t* __restrict__ head, const float* __restrict__ row_weight,
-                                                   float scale, uint16_t* __restrict__ dx, int64_t stride, int H, int Hp)
+                                                   float scale, uint16_t* __restrict__ dx, int64_t stride, int H, int Hp, const float* __restrict__ loss,
+                                                   float* __restrict__ mean, int T)
 {
     using S = Store16<DT>;
     const int r = (int)blockIdx.x;
+    if (r == T) {                                 // a workgroup more: the mean, in fp64 and a fixed order
+        __shared__ double part[4];
+        double sum = 0.0;
+        for (int i = threadIdx.x; i < T; i += 256) sum += (double)loss[i];
+        sum = wave_sum(sum);
+        if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = sum;
+        __syncthreads();
+        if (threadIdx.x == 0) *mean = *count ? (float)((part[0] + part[1] + part[2] + part[3]) / (double)*count) : 0.0f;
+        return;
+    }
     const int p = pos[r];
     float g = 0.0f, cf = 0.0f, uu = 0.0f;
     int t = 0;
+    const int n = *count, splits = splits_of(n, bm, tiles_n, slots, max_splits);
     if (p >= 0) {
-        g = scale * (row_weight ? row_weight[r] : 1.0f / (float)*count);
+        g = scale * (row_weight ? row_weight[r] : 1.0f / (float)n);
         cf = coef[p];
         uu = u[p];
         t = tgt[p];
@@ -230,7 +315,7 @@ __global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ ac
         float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
         if (p >= 0) {
             for (int s = 0; s < splits; ++s) {
-                const float* at = acc + ((int64_t)s * T + p) * Hp + h;
+                const float* at = acc + ((int64_t)s * n + p) * Hp + h;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] += at[e];
             }
@@ -249,30 +334,25 @@ __global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ ac
     }
 }
 
-// Mean over the counted rows, fp64, in a fixed order.
-__global__ __launch_bounds__(1024) void ce_mean_kernel(const float* __restrict__ row_loss, const int32_t* __restrict__ count, float* __restrict__ mean)
-{
-    __shared__ double part[16];
-    const int n = *count;
-    double sum = 0.0;
-    for (int p = threadIdx.x; p < n; p += 1024) sum += (double)row_loss[p];
-    sum = wave_sum(sum);
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
-    __syncthreads();
-    if (threadIdx.x) return;
-    double all = 0.0;
-    for (int w = 0; w < 16; ++w) all += part[w];
-    *mean = n ? (float)(all / (double)n) : 0.0f;
-}
-
 // ---- plan ----
-// Columns of a piece: 128 MB of a_v, at least 256.
-static int64_t ce_piece(int64_t T, int64_t V)
+// Columns of a piece and of the first.  All of them while a_v takes 128 MB at most; without the gradient, while M and S of the waves take 256 MB.
+// Otherwise the first piece, all of whose a_v are read and written once more, has as many tiles of 256x256 as the chip has CUs, and the others a multiple
+// of them (a launch of 880 takes four rounds as one of 1024 does: 7B's logits 951 us in such pieces, 850 so), with 256 MB and about half of the
+// vocabulary at most.
+static void ce_pieces(int64_t T, int64_t V, int64_t piece, bool grad, int& cols, int& first)
 {
-    int64_t most = (INT64_C(1) << 26) / T / kPieceStep * kPieceStep;
-    if (most < kPieceStep) most = kPieceStep;
-    const int64_t pieces = (V + most - 1) / most;
-    return up((V + pieces - 1) / pieces, kPieceStep);
+    const int64_t all = up(V, kPieceStep), room = grad ? INT64_C(1) << 26 : INT64_C(1) << 32;
+    if (piece || T <= room / all) {
+        cols = first = (int)(piece && piece < all ? piece : all);
+        return;
+    }
+    const int64_t tiles_m = (T + 255) / 256, round = (tiles_m >= 256 ? 1 : 256 / tiles_m) * 256;
+    int64_t most = 2 * room / T;
+    if (most > (V + 1) / 2) most = (V + 1) / 2;
+    first = (int)(round < all ? round : all);
+    cols = (int)(most > round ? up(most, round) : round);
+    if (cols > all) cols = (int)all;
+    if (!grad) first = cols;
 }
 
 static int ce_tile(int64_t M, int64_t N)
@@ -283,27 +363,37 @@ static int ce_tile(int64_t M, int64_t N)
     const double c2 = 0.8 * (double)(t128 / 512) + (rest == 0 ? 0.0 : rest <= 256 ? 0.44 : 0.8);
     return c0 <= c1 && c0 <= c2 ? 0 : c1 < c2 ? 1 : 2;
 }
+// The gradient's tile: its contraction is cut until the chip is full, so what counts is the part of a tile that is used.
+static int ce_grad_tile(int64_t M, int64_t N)
+{
+    auto used = [&](int64_t bm, int64_t bn) { return (double)(M * N) / (double)(up(M, bm) * up(N, bn)); };
+    return 0.8 * used(128, 128) > used(256, 256) ? 2 : 0;
+}
 
 // Sizes and the workspace's parts, from `base` (0: only how long they are).
 static size_t ce_plan(CeArgs& c, int64_t piece, char* base)
 {
     c.Hp = (int)up(c.H, 64);
     c.Vp = (int)up(c.V, 64);
-    c.piece = (int)(piece ? (piece < up(c.V, kPieceStep) ? piece : up(c.V, kPieceStep)) : ce_piece(c.T, c.V));
+    ce_pieces(c.T, c.V, piece, c.grad, c.piece, c.first_piece);
     c.tile = ce_tile(c.T, c.piece);
-    c.grad_tile = ce_tile(c.T, c.H);
-    const int64_t bm = c.grad_tile == 0 ? 256 : 128, bn = c.grad_tile == 2 ? 128 : 256;
-    const int64_t tiles = ((c.T + bm - 1) / bm) * ((c.H + bn - 1) / bn), slots = c.grad_tile == 2 ? 512 : 256;
-    int64_t splits = slots / tiles;
-    if (splits > c.piece / 512) splits = c.piece / 512;
-    c.splits = (int)(splits < 1 ? 1 : splits);
+    c.grad_tile = ce_grad_tile(c.T, c.H);
+    const int bm = tile_rows(c.grad_tile), bn = tile_cols(c.grad_tile), sc = stat_cols(c.tile);
+    const int64_t tiles_n = (c.H + bn - 1) / bn;
+    c.slots = c.grad_tile == 2 ? 512 : 256;
+    c.max_splits = c.piece / 512 > 1 ? c.piece / 512 : 1;
+    // rows of sums, whatever number of rows counts: one part of all, or as many parts as there are slots for
+    int64_t sums = c.T, filled = c.slots / tiles_n * bm;
+    if (filled > c.T * c.max_splits) filled = c.T * c.max_splits;
+    if (sums < filled) sums = filled;
     size_t at = 0;
     auto part = [&](auto*& p, size_t bytes) {
         p = reinterpret_cast<std::remove_reference_t<decltype(p)>>(base + at);
         at += (bytes + 255) / 256 * 256;
     };
-    const size_t T = (size_t)c.T;
+    const size_t T = (size_t)c.T, T16 = (T + 15) / 16 * 16, groups = (size_t)(c.piece / sc);
     part(c.count, 4);
+    part(c.ticket, 4);
     part(c.pos, T * 4);
     part(c.row, T * 4);
     part(c.tgt, T * 4);
@@ -312,13 +402,13 @@ static size_t ce_plan(CeArgs& c, int64_t piece, char* base)
     part(c.beta, T * 4);
     part(c.coef, T * 4);
     part(c.u, T * 4);
-    part(c.row_loss, T * 4);
-    part(c.stats, (size_t)(c.piece / stat_cols(c.tile)) * T * 8);
-    const size_t T16 = (T + 15) / 16 * 16;
+    part(c.part, T16 / 16 * 8);
+    part(c.stats, groups * T * 8);
     part(c.xs, T16 * row_blocks(c.Hp) * 64);
     if (c.grad) {
+        part(c.scale_rows, T16 / 16);
         part(c.a, T16 * row_blocks(c.piece) * 64);
-        part(c.acc, (size_t)c.splits * T * (size_t)c.Hp * 4);
+        part(c.acc, (size_t)sums * (size_t)c.Hp * 4);
     }
     return at;
 }
@@ -333,32 +423,36 @@ template <int DT>
 static void ce_run(const CeArgs& c, sasq_dtype dt, hipStream_t st)
 {
     const int T = (int)c.T, H = (int)c.H;
-    ce_pack_kernel<<<1, kPackThreads, 0, st>>>(c.targets, T, (int)c.V, c.count, c.pos, c.row, c.tgt, c.run, c.loss, c.lse);
+    ce_pack_kernel<<<1, kPackThreads, 0, st>>>(c.targets, T, (int)c.V, c.count, c.pos, c.row, c.tgt, c.run, c.loss, c.lse, c.ticket, c.mean);
     if (c.x_stride % 8 == 0 && H % 8 == 0)
         ce_stage_kernel<true><<<(T + 3) / 4, 256, 0, st>>>(static_cast<const uint16_t*>(c.x), c.x_stride, c.xs, c.count, c.row, H, c.Hp);
     else
         ce_stage_kernel<false><<<(T + 3) / 4, 256, 0, st>>>(static_cast<const uint16_t*>(c.x), c.x_stride, c.xs, c.count, c.row, H, c.Hp);
     const int sc = stat_cols(c.tile), bn = 2 * sc;
-    for (int64_t col0 = 0; col0 < c.V; col0 += c.piece) {
-        const int64_t cols = c.V - col0 < c.piece ? c.V - col0 : c.piece;
+    for (int64_t col0 = 0; col0 < c.V;) {
+        const int64_t piece = col0 ? c.piece : c.first_piece, cols = c.V - col0 < piece ? c.V - col0 : piece;
         const int groups = (int)((cols + bn - 1) / bn) * 2;
         launch_ce_logits(c, dt, col0, cols, st);
-        ce_join_kernel<<<(T + kJoinRows - 1) / kJoinRows, 256, 0, st>>>(c.stats, groups, c.T, c.count, c.run, c.beta, c.zt, c.row, c.coef, c.u, c.row_loss,
-                                                                       c.loss, c.lse, col0 + cols >= c.V);
+        ce_join_kernel<<<(T + kJoinRows - 1) / kJoinRows, kJoinThreads, 0, st>>>(
+            c.stats, groups, c.T, c.count, c.run, c.beta, c.grad ? c.scale_rows : nullptr, c.zt, c.row, c.coef, c.u, c.loss, c.lse, c.grad ? nullptr : c.mean,
+            c.part, c.ticket, col0 + cols >= c.V);
         if (c.grad) {
-            ce_scale_kernel<DT><<<T, 256, 0, st>>>(c.a, c.piece, (int)up(cols, 64), sc, c.stats, c.run, c.T, c.count);
+            const int kt = (int)(up(cols, 64) / 32);
+            ce_scale_kernel<DT><<<dim3((T + 15) / 16, (kt + kScaleBlocks - 1) / kScaleBlocks), 256, 0, st>>>(c.a, row_blocks(c.piece), kt, sc / 32, c.stats, c.run,
+                                                                                                             c.scale_rows, c.T, c.count);
             launch_ce_grad(c, dt, col0, cols, st);
         }
+        col0 += cols;
     }
     if (c.grad) {
+        const int bm = tile_rows(c.grad_tile), tiles_n = (int)((c.H + tile_cols(c.grad_tile) - 1) / tile_cols(c.grad_tile));
         if (c.dx_stride % 8 == 0 && H % 8 == 0)
-            ce_dx_kernel<DT, true><<<T, 256, 0, st>>>(c.acc, c.splits, c.T, c.count, c.pos, c.tgt, c.coef, c.u, c.head, c.row_weight, c.scale,
-                                                      static_cast<uint16_t*>(c.dx), c.dx_stride, H, c.Hp);
+            ce_dx_kernel<DT, true><<<T + (c.mean ? 1 : 0), 256, 0, st>>>(c.acc, bm, tiles_n, c.slots, c.max_splits, c.count, c.pos, c.tgt, c.coef, c.u, c.head, c.row_weight, c.scale,
+                                                      static_cast<uint16_t*>(c.dx), c.dx_stride, H, c.Hp, c.loss, c.mean, T);
         else
-            ce_dx_kernel<DT, false><<<T, 256, 0, st>>>(c.acc, c.splits, c.T, c.count, c.pos, c.tgt, c.coef, c.u, c.head, c.row_weight, c.scale,
-                                                       static_cast<uint16_t*>(c.dx), c.dx_stride, H, c.Hp);
+            ce_dx_kernel<DT, false><<<T + (c.mean ? 1 : 0), 256, 0, st>>>(c.acc, bm, tiles_n, c.slots, c.max_splits, c.count, c.pos, c.tgt, c.coef, c.u, c.head, c.row_weight, c.scale,
+                                                       static_cast<uint16_t*>(c.dx), c.dx_stride, H, c.Hp, c.loss, c.mean, T);
     }
-    if (c.mean) ce_mean_kernel<<<1, 1024, 0, st>>>(c.row_loss, c.count, c.mean);
 }
 
 }  // namespace sasq

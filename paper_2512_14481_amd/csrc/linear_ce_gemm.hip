@@ -43,6 +43,7 @@ struct LogitsExt {
     int x_kt, w_kt;
     const int32_t* tgt;
     float* zt;
+    const RowStat* run;                         // of the pieces before, or NULL
     RowStat* stats;
     int64_t T;                                  // rows of `stats`
     uint16_t* a;
@@ -71,6 +72,7 @@ struct LogitsExt {
             const int m = wm0 + b * 16 + frow;
             const int t = tgt[min(m, M - 1)] - wn0;            // the target's place among the wave's columns
             const bool here = t >= 0 && t < BN / 2 && ((t >> 2) & 3) == fq;
+            const RowStat before = run ? run[min(m, M - 1)] : RowStat{0.0f, 0.0f};
             // Two copies of the rest: with the target or an edge among the columns, and without, where no element is looked at for them.
             auto rows = [&](auto special) {
                 constexpr bool SPECIAL = decltype(special)::value;
@@ -99,6 +101,7 @@ struct LogitsExt {
                 // whole numbers, so that one M takes another's place by an exact factor
                 float mm = ceilf(top * kLog2e) - (float)kTopExp<DT>;
                 if (SPECIAL) mm = top == -__builtin_inff() ? 0.0f : mm;
+                if (before.s != 0.0f && mm <= before.m + (float)kRoom<DT>) mm = before.m;
                 float sum = 0.0f;
                 u32x2 pk[NF];
 #pragma unroll
@@ -187,21 +190,22 @@ struct SumsExt {
     }
 };
 
-// The contraction over the piece's columns is cut into `splits` parts of whole 64 columns, each with running sums of its own.
+// The contraction over the piece's columns is cut into parts of whole 64 columns, each with running sums of its own.
 template <int DT, int BM, int BN>
 __global__ __launch_bounds__(kGemmThreads)
 __attribute__((amdgpu_waves_per_eu(Tile<BM, BN>::kWavesPerSimd, Tile<BM, BN>::kWavesPerSimd)))
-void ce_grad_kernel(const uint16_t* __restrict__ a, const uint8_t* __restrict__ head_grad, const int32_t* __restrict__ count, int64_t T, int H, int Hp,
-                    int cols64, int kt0, int tiles_n, int splits, SumsExt ext)
+void ce_grad_kernel(const uint16_t* __restrict__ a, const uint8_t* __restrict__ head_grad, const int32_t* __restrict__ count, int H, int Hp,
+                    int cols64, int kt0, int tiles_n, int slots, int max_splits, SumsExt ext)
 {
     __shared__ __attribute__((aligned(1024))) char lds[kStages * Tile<BM, BN>::kStageBytes];
     const int M = *count;
+    const int splits = splits_of(M, BM, tiles_n, slots, max_splits);
     int tm, tn;
     if (!tile_of_counted((M + BM - 1) / BM, tiles_n * splits, tm, tn)) return;
     const int part = tn / tiles_n;
     tn -= part * tiles_n;
     const int c0 = (int)((int64_t)cols64 * part / splits), c1 = (int)((int64_t)cols64 * (part + 1) / splits);
-    ext.acc += (int64_t)part * T * Hp;
+    ext.acc += (int64_t)part * M * Hp;
     if (c0 == c1) {                             // a last piece of fewer columns than parts
         for (int i = threadIdx.x; i < BM * (BN / 4); i += kGemmThreads) {
             const int m = tm * BM + i / (BN / 4), n = tn * BN + i % (BN / 4) * 4;
@@ -230,7 +234,7 @@ static void launch_logits(const CeArgs& c, int64_t col0, int64_t cols, hipStream
     const int grid = ((tiles_m * tiles_n + 7) / 8) * 8;
     auto go = [&](auto grad_tag) {
         constexpr bool GRAD = decltype(grad_tag)::value;
-        const LogitsExt<DT, GRAD> ext{row_blocks(c.Hp), row_blocks(c.Hp), c.tgt, c.zt, c.stats, c.T, c.a, row_blocks(c.piece), (int)col0};
+        const LogitsExt<DT, GRAD> ext{row_blocks(c.Hp), row_blocks(c.Hp), c.tgt, c.zt, GRAD && col0 ? c.run : nullptr, c.stats, c.T, c.a, row_blocks(c.piece), (int)col0};
         ce_logits_kernel<DT, BM, BN, GRAD><<<grid, kGemmThreads, 0, st>>>(c.xs, c.head, c.count, (int)c.V, c.Hp, tiles_n, ext);
     };
     if (c.grad) go(std::true_type{});
@@ -240,11 +244,13 @@ static void launch_logits(const CeArgs& c, int64_t col0, int64_t cols, hipStream
 template <int DT, int BM, int BN>
 static void launch_grad(const CeArgs& c, int64_t col0, int64_t cols, hipStream_t st)
 {
-    const int tiles_m = (int)((c.T + BM - 1) / BM), tiles_n = (int)((c.H + BN - 1) / BN);
-    const int grid = ((tiles_m * tiles_n * c.splits + 7) / 8) * 8;
+    const int tiles_n = (int)((c.H + BN - 1) / BN);
+    const int64_t tiles = (c.T + BM - 1) / BM * tiles_n;
+    // for any number of counted rows: as many tiles as there are slots, or one part
+    const int64_t most = tiles > c.slots ? tiles : tiles * c.max_splits < c.slots ? tiles * c.max_splits : c.slots;
     const SumsExt ext{row_blocks(c.piece), row_blocks(c.Vp), c.acc, col0 ? c.beta : nullptr, c.Hp};
-    ce_grad_kernel<DT, BM, BN><<<grid, kGemmThreads, 0, st>>>(c.a, c.head_grad, c.count, c.T, (int)c.H, c.Hp, (int)((cols + 63) / 64), (int)(col0 / 32),
-                                                              tiles_n, c.splits, ext);
+    ce_grad_kernel<DT, BM, BN><<<(unsigned)((most + 7) / 8 * 8), kGemmThreads, 0, st>>>(
+        c.a, c.head_grad, c.count, (int)c.H, c.Hp, (int)((cols + 63) / 64), (int)(col0 / 32), tiles_n, c.slots, c.max_splits, ext);
 }
 
 template <int DT, typename Go>
@@ -265,8 +271,12 @@ void launch_ce_logits(const CeArgs& c, sasq_dtype dt, int64_t col0, int64_t cols
 void launch_ce_grad(const CeArgs& c, sasq_dtype dt, int64_t col0, int64_t cols, hipStream_t st)
 {
     auto go = [&](auto d, auto bm, auto bn) { launch_grad<decltype(d)::value, decltype(bm)::value, decltype(bn)::value>(c, col0, cols, st); };
-    if (dt == SASQ_F16) by_tile<SASQ_F16>(c.grad_tile, go);
-    else                by_tile<SASQ_BF16>(c.grad_tile, go);
+    auto by_size = [&](auto d) {
+        if (c.grad_tile == 0) go(d, std::integral_constant<int, 256>{}, std::integral_constant<int, 256>{});
+        else                  go(d, std::integral_constant<int, 128>{}, std::integral_constant<int, 128>{});
+    };
+    if (dt == SASQ_F16) by_size(std::integral_constant<int, SASQ_F16>{});
+    else                by_size(std::integral_constant<int, SASQ_BF16>{});
 }
 
 }  // namespace sasq

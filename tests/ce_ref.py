@@ -6,7 +6,7 @@ terms' sizes; doubled for the matrix unit's own intermediate roundings):
   lse   2 ez (numerator and target) and the sum over V, its logarithm and the rounding of the result: (V + 8) 2^-24 + 2^-24 |lse|
   loss  d = lse_o - z_t is off by that; loss = ln(1 + e^d) by at most u times as much, and 2^-24 of itself
   dx    the average of W over the others is off by eps (exponentials in 16 bits, relative) + 2 (2 ez + 2^-20) + 2 V 2^-24 of sum q |W|, in fp16 also by
-        2^-24 2^-14 (V smallest steps, relative to the largest) max |W|; u by what d is off by; then one rounding, and the type's smallest step
+V 2^-34 max |W| (two roundings to the smallest step, 2^-24, beside a largest exponential of 2^10 at least); u by what d is off by; then one rounding, and the type's smallest step
 """
 from __future__ import annotations
 
@@ -55,7 +55,7 @@ class Head:
             eps = HALF[self.dtype]
             dx[rows] = g * u[:, None] * (q @ w - w[t])
             rel = (eps + 2 * (2 * ez + 2.0 ** -20) + 2 * V * u32)[:, None]
-            flush = V * 2.0 ** -38 * w.abs().max() if self.dtype == "f16" else 0.0
+            flush = V * 2.0 ** -34 * w.abs().max() if self.dtype == "f16" else 0.0
             e_dx[rows] = (g * u[:, None]).abs() * (rel * (q @ w.abs()) + flush + (2 * ed[:, None] + 8 * u32) * (q @ w - w[t]).abs()) * 1.01
             e_dx[rows] += eps * dx[rows].abs() * 1.01 + TINY[self.dtype]
         n = max(len(rows), 1)

@@ -49,7 +49,7 @@ def test_head():
     for change, rc in [(dict(w=None), NULL), (dict(head=None), NULL), (dict(form=2), UNSUPPORTED), (dict(dt=2), UNSUPPORTED), (dict(V=0), SHAPE), (dict(H=0), SHAPE),
                        (dict(stride=63), SHAPE), (dict(V=(1 << 23) + 1), SHAPE), (dict(w=P + 2), ALIGN), (dict(head=P + 8), ALIGN)]:
         assert prep(**change) == rc, change
-    assert B.sasq_head_bytes(100, 65, B.SASQ_HEAD_LOGITS) == 112 * 128 * 2 and B.sasq_head_bytes(100, 65, B.SASQ_HEAD_GRAD) == 128 * 80 * 2
+    assert B.sasq_head_bytes(100, 65, B.SASQ_HEAD_LOGITS) == 112 * 5 * 64 and B.sasq_head_bytes(100, 65, B.SASQ_HEAD_GRAD) == 80 * 5 * 64
     assert B.sasq_head_bytes(0, 64, 0) == B.sasq_head_bytes(64, 0, 0) == B.sasq_head_bytes(64, 64, 2) == 0
 
 
