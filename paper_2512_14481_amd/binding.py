@@ -82,6 +82,11 @@ _NATIVE = ("sasq_fakequant_fwd", "sasq_fakequant_bwd", "sasq_fakequant_fwd_batch
 # The same for serving: what it takes and refuses is in tests of its own.
 _NATIVE_SERVING = ("sasq_kv_append", "sasq_paged_attention")
 
+# And for the calls of a training step that keep a byte an element, and for its loss.
+_NATIVE_TRAINING = ("sasq_fakequant_fwd_ckpt", "sasq_fakequant_bwd_ckpt", "sasq_fakequant_fwd_pc_ckpt", "sasq_fakequant_bwd_pc_ckpt",
+                    "sasq_fakequant_fwd_ckpt_batch", "sasq_fakequant_bwd_ckpt_batch", "sasq_fakequant_fwd_pc_ckpt_batch",
+                    "sasq_fakequant_bwd_pc_ckpt_batch", "sasq_linear_ce")
+
 
 class _Unbound:
     """Stands for the native module until the library is loaded, or where it cannot be: takes no call."""
@@ -107,7 +112,7 @@ def _load_native(lib: ctypes.CDLL):
         if module.ABI != marshal_abi():
             raise ImportError(f"built for {module.ABI}, this is {marshal_abi()}")
         module.bind({name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value
-                     for name in _NATIVE + _NATIVE_SERVING + ("sasq_packed_weight_bytes", "sasq_bwd_weight_bytes")})
+                     for name in _NATIVE + _NATIVE_SERVING + _NATIVE_TRAINING + ("sasq_head_bytes", "sasq_packed_weight_bytes", "sasq_bwd_weight_bytes")})
     except (ImportError, OSError, AttributeError) as e:
         warnings.warn(f"{MARSHAL_PATH} is not used, calls go through ctypes ({e}); "
                       "build it with `python -m paper_2512_14481_amd.build`", RuntimeWarning, stacklevel=3)
@@ -203,6 +208,14 @@ def _ptr(t: Optional[torch.Tensor]):
     if not t.is_contiguous():
         raise ValueError("SASQ entry points take contiguous tensors")
     return ctypes.c_void_p(t.data_ptr())
+
+
+def _here(t: Optional[torch.Tensor]):
+    """_ptr of a tensor that has to be on the current device, whose stream the call goes to."""
+    p = _ptr(t)
+    if t is not None and t.device.index != torch.cuda.current_device():
+        raise ValueError("SASQ entry points take tensors of the current device")
+    return p
 
 
 def _stream():
@@ -410,10 +423,10 @@ def _ckpt_items(items, backward: bool, pc: bool):
     for i, it in enumerate(items):
         if backward:
             kept, like, out, f = it
-            arr[i].dy, arr[i].ds = _ptr(like).value, _ptr(f).value
+            arr[i].dy, arr[i].ds = _here(like).value, _here(f).value
         else:
             like, f, out, kept = it
-            arr[i].x, arr[i].s = _ptr(like).value, _ptr(f).value
+            arr[i].x, arr[i].s = _here(like).value, _here(f).value
         _want(kept, torch.int8, "kept"); _want(f, torch.float32, "ds" if backward else "s")
         if out is not None and (out.dtype != like.dtype or out.shape != like.shape):
             raise ValueError("dx must match dy" if backward else "y must match x")
@@ -426,28 +439,37 @@ def _ckpt_items(items, backward: bool, pc: bool):
             dt = _dt(like)
         elif _dt(like) != dt:
             raise TypeError("all tensors of a batch must have the same dtype")
-        arr[i].out, arr[i].kept = None if out is None else _ptr(out).value, _ptr(kept).value
+        arr[i].out, arr[i].kept = None if out is None else _here(out).value, _here(kept).value
         arr[i].rows, arr[i].cols = rows, cols
     return arr, dt
 
 
 def _ckpt_fwd(name: str, items, bits: int, pc: bool) -> None:
+    rc = getattr(_native, name)(items, bits)
+    if rc is not None:
+        return _check(rc, name)
     arr, dt = _ckpt_items(items, False, pc)
     _check(getattr(_lib(), name)(arr, len(items), bits, dt, _stream()), name)
 
 
 def _ckpt_bwd(name: str, items, workspace: torch.Tensor, bits: int, pc: bool) -> None:
+    rc = getattr(_native, name)(items, workspace, bits)
+    if rc is not None:
+        return _check(rc, name)
     arr, dt = _ckpt_items(items, True, pc)
-    _check(getattr(_lib(), name)(arr, len(items), bits, dt, _ptr(workspace), workspace.numel() * workspace.element_size(), _stream()), name)
+    _check(getattr(_lib(), name)(arr, len(items), bits, dt, _here(workspace), workspace.numel() * workspace.element_size(), _stream()), name)
 
 
 def sasq_fakequant_fwd_ckpt(x: torch.Tensor, s: torch.Tensor, y: torch.Tensor, kept: torch.Tensor, bits: int = 8) -> None:
     """kept: int8 of x's shape, written: what sasq_fakequant_bwd_ckpt needs of x."""
+    rc = _native.sasq_fakequant_fwd_ckpt(x, s, y, kept, bits)
+    if rc is not None:
+        return _check(rc, "sasq_fakequant_fwd_ckpt")
     _want(s, torch.float32, "s"); _want(kept, torch.int8, "kept")
     if y.dtype != x.dtype or y.shape != x.shape or kept.shape != x.shape or s.numel() != 1:
         raise ValueError("y and kept must match x, and s holds one element")
     rows, cols = x.shape[0], x.numel() // max(x.shape[0], 1)
-    _check(_lib().sasq_fakequant_fwd_ckpt(_ptr(x), _ptr(s), _ptr(y), _ptr(kept), rows, cols, bits, _dt(x), _stream()), "sasq_fakequant_fwd_ckpt")
+    _check(_lib().sasq_fakequant_fwd_ckpt(_here(x), _here(s), _here(y), _here(kept), rows, cols, bits, _dt(x), _stream()), "sasq_fakequant_fwd_ckpt")
 
 
 def sasq_fakequant_bwd_ckpt_workspace(rows: int, cols: int) -> int:
@@ -456,20 +478,26 @@ def sasq_fakequant_bwd_ckpt_workspace(rows: int, cols: int) -> int:
 
 def sasq_fakequant_bwd_ckpt(kept: torch.Tensor, dy: torch.Tensor, dx: Optional[torch.Tensor], ds: torch.Tensor, workspace: torch.Tensor,
                             bits: int = 8) -> None:
+    rc = _native.sasq_fakequant_bwd_ckpt(kept, dy, dx, ds, workspace, bits)
+    if rc is not None:
+        return _check(rc, "sasq_fakequant_bwd_ckpt")
     _want(ds, torch.float32, "ds"); _want(kept, torch.int8, "kept")
     if kept.shape != dy.shape or (dx is not None and (dx.dtype != dy.dtype or dx.shape != dy.shape)) or ds.numel() != 1:
         raise ValueError("kept and dx must match dy, and ds holds one element")
     rows, cols = dy.shape[0], dy.numel() // max(dy.shape[0], 1)
-    _check(_lib().sasq_fakequant_bwd_ckpt(_ptr(kept), _ptr(dy), _ptr(dx), _ptr(ds), rows, cols, bits, _dt(dy), _ptr(workspace),
+    _check(_lib().sasq_fakequant_bwd_ckpt(_here(kept), _here(dy), _here(dx), _here(ds), rows, cols, bits, _dt(dy), _here(workspace),
                                           workspace.numel() * workspace.element_size(), _stream()), "sasq_fakequant_bwd_ckpt")
 
 
 def sasq_fakequant_fwd_pc_ckpt(x: torch.Tensor, s: torch.Tensor, y: torch.Tensor, kept: torch.Tensor, bits: int = 8) -> None:
+    rc = _native.sasq_fakequant_fwd_pc_ckpt(x, s, y, kept, bits)
+    if rc is not None:
+        return _check(rc, "sasq_fakequant_fwd_pc_ckpt")
     _want(s, torch.float32, "s"); _want(kept, torch.int8, "kept")
     rows, cols = x.shape
     if y.dtype != x.dtype or y.shape != x.shape or kept.shape != x.shape or s.numel() != cols:
         raise ValueError("y and kept must match x, and s must have one element per column")
-    _check(_lib().sasq_fakequant_fwd_pc_ckpt(_ptr(x), _ptr(s), _ptr(y), _ptr(kept), rows, cols, bits, _dt(x), _stream()), "sasq_fakequant_fwd_pc_ckpt")
+    _check(_lib().sasq_fakequant_fwd_pc_ckpt(_here(x), _here(s), _here(y), _here(kept), rows, cols, bits, _dt(x), _stream()), "sasq_fakequant_fwd_pc_ckpt")
 
 
 def sasq_fakequant_bwd_pc_ckpt_workspace(rows: int, cols: int) -> int:
@@ -478,11 +506,14 @@ def sasq_fakequant_bwd_pc_ckpt_workspace(rows: int, cols: int) -> int:
 
 def sasq_fakequant_bwd_pc_ckpt(kept: torch.Tensor, dy: torch.Tensor, dx: Optional[torch.Tensor], ds: torch.Tensor, workspace: torch.Tensor,
                                bits: int = 8) -> None:
+    rc = _native.sasq_fakequant_bwd_pc_ckpt(kept, dy, dx, ds, workspace, bits)
+    if rc is not None:
+        return _check(rc, "sasq_fakequant_bwd_pc_ckpt")
     _want(ds, torch.float32, "ds"); _want(kept, torch.int8, "kept")
     rows, cols = dy.shape
     if kept.shape != dy.shape or (dx is not None and (dx.dtype != dy.dtype or dx.shape != dy.shape)) or ds.numel() != cols:
         raise ValueError("kept and dx must match dy, and ds must have one element per column")
-    _check(_lib().sasq_fakequant_bwd_pc_ckpt(_ptr(kept), _ptr(dy), _ptr(dx), _ptr(ds), rows, cols, bits, _dt(dy), _ptr(workspace),
+    _check(_lib().sasq_fakequant_bwd_pc_ckpt(_here(kept), _here(dy), _here(dx), _here(ds), rows, cols, bits, _dt(dy), _here(workspace),
                                              workspace.numel() * workspace.element_size(), _stream()), "sasq_fakequant_bwd_pc_ckpt")
 
 
@@ -748,6 +779,8 @@ def _row_stride(t: torch.Tensor, name: str) -> int:
         raise ValueError(f"{name} must be a matrix, got {tuple(t.shape)}")
     if not t.is_cuda:
         raise ValueError("SASQ entry points take device tensors")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError("SASQ entry points take tensors of the current device")
     if t.stride(1) != 1 and t.shape[1] > 1:
         raise ValueError(f"the elements of a row of {name} must be next to each other")
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
@@ -763,7 +796,7 @@ def sasq_prepare_head(w: torch.Tensor, head: torch.Tensor, form: int) -> None:
     V, H = w.shape
     if head.numel() * head.element_size() != sasq_head_bytes(V, H, form):
         raise ValueError("head must have sasq_head_bytes(V, H, form) bytes")
-    _check(_lib().sasq_prepare_head(_at(w), stride, _ptr(head), V, H, form, _dt(w), _stream()), "sasq_prepare_head")
+    _check(_lib().sasq_prepare_head(_at(w), stride, _here(head), V, H, form, _dt(w), _stream()), "sasq_prepare_head")
 
 
 def sasq_linear_ce_workspace(T: int, V: int, H: int, grad: bool, piece: int = 0) -> int:
@@ -776,6 +809,9 @@ def sasq_linear_ce(x: torch.Tensor, head: torch.Tensor, targets: torch.Tensor, l
                    piece: int = 0) -> None:
     """x, dx: [T, H], rows may be apart; targets: [T] int32; loss, lse, row_weight: [T] float32; mean: one float32.  head, head_grad: the
     layouts that sasq_prepare_head made of a [V, H] head (head_grad goes with dx)."""
+    rc = _native.sasq_linear_ce(x, head, targets, loss, V, workspace, lse, mean, dx, head_grad, row_weight, scale, piece)
+    if rc is not None:
+        return _check(rc, "sasq_linear_ce")
     x_stride, dx_stride = _row_stride(x, "x"), 0 if dx is None else _row_stride(dx, "dx")
     T, H = x.shape
     if dx is not None and (dx.shape != x.shape or dx.dtype != x.dtype):
@@ -793,8 +829,8 @@ def sasq_linear_ce(x: torch.Tensor, head: torch.Tensor, targets: torch.Tensor, l
         raise ValueError("head must have sasq_head_bytes(V, H, SASQ_HEAD_LOGITS) bytes")
     if head_grad is not None and head_grad.numel() * head_grad.element_size() != sasq_head_bytes(V, H, SASQ_HEAD_GRAD):
         raise ValueError("head_grad must have sasq_head_bytes(V, H, SASQ_HEAD_GRAD) bytes")
-    _check(_lib().sasq_linear_ce(_at(x), x_stride, _ptr(head), _ptr(head_grad), _ptr(targets), _ptr(row_weight), ctypes.c_float(scale), _ptr(loss),
-                                 _ptr(lse), _ptr(mean), _at(dx), dx_stride, T, V, H, piece, _dt(x), _ptr(workspace),
+    _check(_lib().sasq_linear_ce(_at(x), x_stride, _here(head), _here(head_grad), _here(targets), _here(row_weight), ctypes.c_float(scale), _here(loss),
+                                 _here(lse), _here(mean), _at(dx), dx_stride, T, V, H, piece, _dt(x), _here(workspace),
                                  workspace.numel() * workspace.element_size(), _stream()), "sasq_linear_ce")
 
 

@@ -18,6 +18,8 @@ constexpr int kCkHigh = 127, kCkLow = -128;
 constexpr int kCkCols = kWave * 8;               // columns of a block of the per-channel kernels
 constexpr int kCkMaxBatch = SASQ_MAX_BATCH;
 constexpr int kCkBlocks = 2048, kCkPartials = 512;
+constexpr int kCkSmallThreads = 1024, kCkSmallUnroll = 3;
+constexpr int64_t kCkSmall = (int64_t)kCkSmallThreads * kCkSmallUnroll * 8;
 
 struct CkItem {
     const uint16_t* x;
@@ -145,38 +147,42 @@ __global__ __launch_bounds__(kCkThreads) void ck_fwd_kernel(const CkBatch b, int
     }
 }
 
-template <int DT>
-__global__ __launch_bounds__(kCkThreads) void ck_bwd_kernel(const CkBatch b, int bits)
+// SMALL: a workgroup of 1024 threads takes a whole tensor, and its ds needs no join.  The products are exact in fp32 and added in fp64: sums over many
+// elements that nearly cancel keep their digits.
+template <int DT, bool SMALL>
+__global__ __launch_bounds__(SMALL ? kCkSmallThreads : kCkThreads) void ck_bwd_kernel(const CkBatch b, int bits)
 {
     using S = Store16<DT>;
-    const int k = ck_item_of(b, (int)blockIdx.x);
+    constexpr int kThreads = SMALL ? kCkSmallThreads : kCkThreads, kWaves = kThreads / kWave, kUnroll = SMALL ? kCkSmallUnroll : kCkUnroll;
+    const int k = SMALL ? (int)blockIdx.x : ck_item_of(b, (int)blockIdx.x);
     const CkItem& it = b.it[k];
-    const int64_t block = (int)blockIdx.x - b.first[k], blocks = b.first[k + 1] - b.first[k];
+    const int64_t block = SMALL ? 0 : (int)blockIdx.x - b.first[k], blocks = SMALL ? 1 : b.first[k + 1] - b.first[k];
     const float lo = ck_low(bits) * kCkSteps, hi = ck_high(bits) * kCkSteps;
     const u32x2* kept = reinterpret_cast<const u32x2*>(it.kept);
     const u32x4* dy = reinterpret_cast<const u32x4*>(it.dy);
     u32x4* dx = reinterpret_cast<u32x4*>(it.out);
     const int64_t nvec = it.n / 8;
-    constexpr int64_t kChunk = (int64_t)kCkThreads * kCkUnroll;
-    double acc = 0.0;                              // eight terms in fp32, everything above that in fp64
+    constexpr int64_t kChunk = (int64_t)kThreads * kUnroll;
+    double acc = 0.0;
     for (int64_t base = block * kChunk; base < nvec; base += blocks * kChunk) {
-        u32x2 kp[kCkUnroll];
-        u32x4 g[kCkUnroll];
+        u32x2 kp[kUnroll];
+        u32x4 g[kUnroll];
 #pragma unroll
-        for (int u = 0; u < kCkUnroll; ++u) {
-            const int64_t i = min(base + u * kCkThreads + (int64_t)threadIdx.x, nvec - 1);
+        for (int u = 0; u < kUnroll; ++u) {
+            const int64_t i = min(base + u * kThreads + (int64_t)threadIdx.x, nvec - 1);
             kp[u] = __builtin_nontemporal_load(&kept[i]);
             g[u] = __builtin_nontemporal_load(&dy[i]);
         }
 #pragma unroll
-        for (int u = 0; u < kCkUnroll; ++u) {
-            const int64_t i = base + u * kCkThreads + threadIdx.x;
-            float term[8], sum = 0.0f;
+        for (int u = 0; u < kUnroll; ++u) {
+            const int64_t i = base + u * kThreads + threadIdx.x;
+            float term[8];
+            double sum = 0.0;
             const u32x4 out = ck_bwd_vec<DT>(kp[u], g[u], lo, hi, term);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum += term[e];
+            for (int e = 0; e < 8; ++e) sum += (double)term[e];
             if (i < nvec) {
-                acc += (double)sum;
+                acc += sum;
                 if (dx) __builtin_nontemporal_store(out, &dx[i]);
             }
         }
@@ -184,17 +190,20 @@ __global__ __launch_bounds__(kCkThreads) void ck_bwd_kernel(const CkBatch b, int
     if (block == blocks - 1 && threadIdx.x < (unsigned)(it.n - nvec * 8)) {
         const int64_t i = nvec * 8 + threadIdx.x;
         bool m;
-        acc += (double)(S::one(it.dy[i]) * ck_value(it.kept[i], lo, hi, m));
-        if (dx) it.out[i] = m ? it.dy[i] : (uint16_t)0;
+        const uint16_t g = it.dy[i];
+        acc += (double)(S::one(g) * ck_value(it.kept[i], lo, hi, m));
+        if (dx) it.out[i] = m ? g : (uint16_t)0;
     }
-    __shared__ double part[kCkWaves];
+    __shared__ double part[kWaves];
     const double w = wave_sum(acc);
     if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = w;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        double all = 0.0;
-        for (int i = 0; i < kCkWaves; ++i) all += part[i];
-        static_cast<double*>(it.partial)[block] = all;
+    if (threadIdx.x < kWave) {
+        const double all = wave_sum(threadIdx.x < kWaves ? part[threadIdx.x] : 0.0);
+        if (threadIdx.x == 0) {
+            if (blocks == 1) *it.ds = (float)(all / (double)kCkSteps);
+            else             static_cast<double*>(it.partial)[block] = all;
+        }
     }
 }
 
@@ -203,6 +212,7 @@ __global__ __launch_bounds__(kCkThreads) void ck_join_kernel(const CkBatch b)
 {
     const CkItem& it = b.it[blockIdx.x];
     const int n = b.first[blockIdx.x + 1] - b.first[blockIdx.x];
+    if (n == 1) return;
     const double* p = static_cast<const double*>(it.partial);
     double acc = 0.0;
     for (int i = threadIdx.x; i < n; i += kCkThreads) acc += p[i];
@@ -297,14 +307,15 @@ __device__ __forceinline__ void ck_fwd_pc_body(const CkItem& it, int block, int 
     }
 }
 
-template <int DT>
+// ANY: some tensor of the launch has rows that are no multiple of eight (a kernel with both bodies needs more registers).
+template <int DT, bool ANY>
 __global__ __launch_bounds__(kCkThreads) void ck_fwd_pc_kernel(const CkBatch b, int bits)
 {
     const int k = ck_item_of(b, (int)blockIdx.x);
     const CkItem& it = b.it[k];
     const int block = (int)blockIdx.x - b.first[k];
-    if (it.cols % 8 == 0) ck_fwd_pc_body<DT, true>(it, block, bits);
-    else                  ck_fwd_pc_body<DT, false>(it, block, bits);
+    if (!ANY || it.cols % 8 == 0) ck_fwd_pc_body<DT, true>(it, block, bits);
+    else                          ck_fwd_pc_body<DT, false>(it, block, bits);
 }
 
 template <int DT, bool VEC>
@@ -353,26 +364,42 @@ __device__ __forceinline__ void ck_bwd_pc_body(const CkItem& it, int block, int 
     }
 }
 
-template <int DT>
+template <int DT, bool ANY>
 __global__ __launch_bounds__(kCkThreads) void ck_bwd_pc_kernel(const CkBatch b, int bits)
 {
     __shared__ float red[kCkWaves][kCkCols];
     const int k = ck_item_of(b, (int)blockIdx.x);
     const CkItem& it = b.it[k];
     const int block = (int)blockIdx.x - b.first[k];
-    if (it.cols % 8 == 0) ck_bwd_pc_body<DT, true>(it, block, bits, red);
-    else                  ck_bwd_pc_body<DT, false>(it, block, bits, red);
+    if (!ANY || it.cols % 8 == 0) ck_bwd_pc_body<DT, true>(it, block, bits, red);
+    else                          ck_bwd_pc_body<DT, false>(it, block, bits, red);
 }
 
+// 64 columns a workgroup, a quarter of the row blocks a wave, eight loads in flight; the order of the sum follows from the sizes.
+constexpr int kCkJoinAhead = 8;
 __global__ __launch_bounds__(kCkThreads) void ck_join_pc_kernel(const CkBatch b)
 {
+    __shared__ double part[kCkWaves][kWave];
     const CkItem& it = b.it[blockIdx.y];
-    if (it.chunks == 1) return;
-    for (int64_t c = (int64_t)blockIdx.x * kCkThreads + threadIdx.x; c < it.cols; c += (int64_t)gridDim.x * kCkThreads) {
-        double all = 0.0;
-        for (int i = 0; i < it.chunks; ++i) all += (double)static_cast<const float*>(it.partial)[(int64_t)i * it.cols + c];
-        it.ds[c] = (float)(all / (double)kCkSteps);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t c = (int64_t)blockIdx.x * kWave + lane;
+    if (it.chunks == 1 || (int64_t)blockIdx.x * kWave >= it.cols) return;
+    const float* p = static_cast<const float*>(it.partial) + min(c, it.cols - 1);
+    double all = 0.0;
+    for (int i0 = wave; i0 < it.chunks; i0 += kCkWaves * kCkJoinAhead) {
+        float v[kCkJoinAhead];
+#pragma unroll
+        for (int j = 0; j < kCkJoinAhead; ++j) v[j] = p[min(i0 + j * kCkWaves, it.chunks - 1) * it.cols];
+#pragma unroll
+        for (int j = 0; j < kCkJoinAhead; ++j) all += i0 + j * kCkWaves < it.chunks ? (double)v[j] : 0.0;
     }
+    part[wave][lane] = all;
+    __syncthreads();
+    if (wave || c >= it.cols) return;
+    all = 0.0;
+#pragma unroll
+    for (int w = 0; w < kCkWaves; ++w) all += part[w][lane];
+    it.ds[c] = (float)(all / (double)kCkSteps);
 }
 
 // ---- plan ----
@@ -385,6 +412,7 @@ static int64_t ck_col_blocks(int64_t cols) { return (cols + kCkCols - 1) / kCkCo
 // Rows of a block: they follow from the tensor alone, so that a batch gives the bits of the single calls.
 static int64_t ck_chunk_rows(int64_t rows, int64_t cols)
 {
+    if (rows <= 64) return 64;                      // one block of all: no join
     int64_t r = 16;
     while (r < 64 && (rows + 2 * r - 1) / (2 * r) * ck_col_blocks(cols) >= 512) r *= 2;
     while ((rows + r - 1) / r > 256) r *= 2;
@@ -459,6 +487,13 @@ static size_t ck_workspace(const sasq_ckpt_item* items, int count, bool pc)
     return bytes;
 }
 
+static bool ck_odd_rows(const CkBatch& b)
+{
+    for (int i = 0; i < b.count; ++i)
+        if (b.it[i].cols % 8) return true;
+    return false;
+}
+
 static int ck_fwd(const sasq_ckpt_item* items, int count, bool pc, int bits, sasq_dtype dt, void* stream)
 {
     const int rc = ck_check(items, count, pc, false, bits, (int)dt);
@@ -467,13 +502,14 @@ static int ck_fwd(const sasq_ckpt_item* items, int count, bool pc, int bits, sas
     ck_plan(items, count, pc, false, nullptr, b);
     hipStream_t st = as_stream(stream);
     const int grid = b.first[count];
-    if (pc) {
-        if (dt == SASQ_F16) ck_fwd_pc_kernel<SASQ_F16><<<grid, kCkThreads, 0, st>>>(b, bits);
-        else                ck_fwd_pc_kernel<SASQ_BF16><<<grid, kCkThreads, 0, st>>>(b, bits);
-    } else {
-        if (dt == SASQ_F16) ck_fwd_kernel<SASQ_F16><<<grid, kCkThreads, 0, st>>>(b, bits);
-        else                ck_fwd_kernel<SASQ_BF16><<<grid, kCkThreads, 0, st>>>(b, bits);
-    }
+    auto go = [&](auto dt_tag) {
+        constexpr int DT = decltype(dt_tag)::value;
+        if (!pc)                     ck_fwd_kernel<DT><<<grid, kCkThreads, 0, st>>>(b, bits);
+        else if (ck_odd_rows(b))     ck_fwd_pc_kernel<DT, true><<<grid, kCkThreads, 0, st>>>(b, bits);
+        else                         ck_fwd_pc_kernel<DT, false><<<grid, kCkThreads, 0, st>>>(b, bits);
+    };
+    if (dt == SASQ_F16) go(std::integral_constant<int, SASQ_F16>{});
+    else                go(std::integral_constant<int, SASQ_BF16>{});
     return hipGetLastError() == hipSuccess ? SASQ_OK : SASQ_ERR_LAUNCH;
 }
 
@@ -487,19 +523,24 @@ static int ck_bwd(const sasq_ckpt_item* items, int count, bool pc, int bits, sas
     ck_plan(items, count, pc, true, static_cast<char*>(workspace), b);
     hipStream_t st = as_stream(stream);
     const int grid = b.first[count];
-    if (pc) {
-        if (dt == SASQ_F16) ck_bwd_pc_kernel<SASQ_F16><<<grid, kCkThreads, 0, st>>>(b, bits);
-        else                ck_bwd_pc_kernel<SASQ_BF16><<<grid, kCkThreads, 0, st>>>(b, bits);
-        int64_t widest = 0;
-        for (int i = 0; i < count; ++i)
-            if (b.it[i].chunks > 1 && b.it[i].cols > widest) widest = b.it[i].cols;
-        const int64_t blocks = (widest + kCkThreads - 1) / kCkThreads;
-        if (blocks) ck_join_pc_kernel<<<dim3((unsigned)(blocks < 1024 ? blocks : 1024), (unsigned)count), kCkThreads, 0, st>>>(b);
-    } else {
-        if (dt == SASQ_F16) ck_bwd_kernel<SASQ_F16><<<grid, kCkThreads, 0, st>>>(b, bits);
-        else                ck_bwd_kernel<SASQ_BF16><<<grid, kCkThreads, 0, st>>>(b, bits);
-        ck_join_kernel<<<count, kCkThreads, 0, st>>>(b);
+    bool small = !pc, join = false;
+    int64_t widest = 0;
+    for (int i = 0; i < count; ++i) {
+        if (b.it[i].n > kCkSmall) small = false;
+        if (pc ? b.it[i].chunks > 1 : b.first[i + 1] - b.first[i] > 1) join = true;
+        if (b.it[i].cols > widest) widest = b.it[i].cols;
     }
+    auto go = [&](auto dt_tag) {
+        constexpr int DT = decltype(dt_tag)::value;
+        if (small)                   ck_bwd_kernel<DT, true><<<count, kCkSmallThreads, 0, st>>>(b, bits);
+        else if (!pc)                ck_bwd_kernel<DT, false><<<grid, kCkThreads, 0, st>>>(b, bits);
+        else if (ck_odd_rows(b))     ck_bwd_pc_kernel<DT, true><<<grid, kCkThreads, 0, st>>>(b, bits);
+        else                         ck_bwd_pc_kernel<DT, false><<<grid, kCkThreads, 0, st>>>(b, bits);
+    };
+    if (dt == SASQ_F16) go(std::integral_constant<int, SASQ_F16>{});
+    else                go(std::integral_constant<int, SASQ_BF16>{});
+    if (join && pc)          ck_join_pc_kernel<<<dim3((unsigned)((widest + kWave - 1) / kWave), (unsigned)count), kCkThreads, 0, st>>>(b);
+    else if (join && !small) ck_join_kernel<<<count, kCkThreads, 0, st>>>(b);
     return hipGetLastError() == hipSuccess ? SASQ_OK : SASQ_ERR_LAUNCH;
 }
 

@@ -9,6 +9,7 @@
 // checks in Python, which name the fault.  Nothing is kept from one call to the next but the entry points' addresses.
 #include <Python.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 
 #include "sasq.h"
@@ -37,6 +38,10 @@ struct Entry {
     decltype(&sasq_prepare_bwd_weight) prepare_bwd_weight;
     decltype(&sasq_kv_append) kv_append;
     decltype(&sasq_paged_attention) paged_attention;
+    decltype(&sasq_fakequant_fwd_ckpt_batch) ckpt_fwd[2];  // per tensor, per channel
+    decltype(&sasq_fakequant_bwd_ckpt_batch) ckpt_bwd[2];
+    decltype(&sasq_head_bytes) head_bytes;
+    decltype(&sasq_linear_ce) linear_ce;
 };
 Entry entry{};
 
@@ -486,6 +491,138 @@ int paged_attention(PyObject* const* a)
     });
 }
 
+// ---- what a scale-training step keeps and its loss: tensors have to be on the current device, whose stream the call goes to ----
+const at::Tensor& here(PyObject* o)
+{
+    const at::Tensor& t = tensor(o);
+    want(t.get_device() == c10::hip::current_device());
+    return t;
+}
+const at::Tensor& here(PyObject* o, at::ScalarType type)
+{
+    const at::Tensor& t = here(o);
+    want(t.scalar_type() == type);
+    return t;
+}
+
+// One item: a forward's (x, s, y, kept) or a backward's (kept, dy, dx_or_None, ds).
+sasq_ckpt_item ckpt_item(PyObject* const* a, bool backward, bool per_channel, sasq_dtype& dt)
+{
+    const at::Tensor &kept = here(a[backward ? 0 : 3], at::kChar), &like = here(a[backward ? 1 : 0]), &f = here(a[backward ? 3 : 1], at::kFloat);
+    const at::Tensor* out = a[2] == Py_None && backward ? nullptr : &here(a[2]);
+    if (out) same(*out, like);
+    want(kept.sizes() == like.sizes() && (!per_channel || like.dim() == 2));
+    dt = dtype_of(like);
+    sasq_ckpt_item it{};
+    it.cols = row_length(like);
+    it.rows = like.size(0);
+    want(f.numel() == (per_channel ? it.cols : 1));
+    it.out = pointer(out);
+    it.kept = pointer<int8_t>(kept);
+    if (backward) {
+        it.dy = pointer(like);
+        it.ds = pointer<float>(f);
+    } else {
+        it.x = pointer(like);
+        it.s = pointer<float>(f);
+    }
+    return it;
+}
+
+struct CkptItems {
+    sasq_ckpt_item item[SASQ_MAX_BATCH];
+    int count;
+    sasq_dtype dt;
+};
+CkptItems ckpt_items(PyObject* list, bool backward, bool per_channel)
+{
+    want(PyList_CheckExact(list) || PyTuple_CheckExact(list));
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(list);
+    want(n >= 1 && n <= SASQ_MAX_BATCH);
+    CkptItems c{};
+    c.count = static_cast<int>(n);
+    for (Py_ssize_t i = 0; i < n; ++i) {
+        PyObject* t = PySequence_Fast_GET_ITEM(list, i);
+        want(PyTuple_CheckExact(t) && PyTuple_GET_SIZE(t) == 4);
+        PyObject* a[4];
+        for (int k = 0; k < 4; ++k) a[k] = PyTuple_GET_ITEM(t, k);
+        sasq_dtype dt;
+        c.item[i] = ckpt_item(a, backward, per_channel, dt);
+        want(i == 0 || dt == c.dt);
+        c.dt = dt;
+    }
+    return c;
+}
+
+int ckpt_fwd(const CkptItems& c, bool per_channel, PyObject* bits_at)
+{
+    const int bits = small(bits_at);
+    return unlocked([&](void* st) { return entry.ckpt_fwd[per_channel](c.item, c.count, bits, c.dt, st); });
+}
+int ckpt_bwd(const CkptItems& c, bool per_channel, PyObject* workspace, PyObject* bits_at)
+{
+    const at::Tensor& ws = here(workspace);
+    const int bits = small(bits_at);
+    void* wp = pointer(ws);
+    const size_t wb = bytes(ws);
+    return unlocked([&](void* st) { return entry.ckpt_bwd[per_channel](c.item, c.count, bits, c.dt, wp, wb, st); });
+}
+template <bool PC> int ckpt_fwd_batch(PyObject* const* a) { return ckpt_fwd(ckpt_items(a[0], false, PC), PC, a[1]); }          // items, bits
+template <bool PC> int ckpt_bwd_batch(PyObject* const* a) { return ckpt_bwd(ckpt_items(a[0], true, PC), PC, a[1], a[2]); }     // items, workspace, bits
+template <bool PC> int ckpt_fwd_one(PyObject* const* a)                                                                        // x, s, y, kept, bits
+{
+    CkptItems c{};
+    c.item[0] = ckpt_item(a, false, PC, c.dt);
+    c.count = 1;
+    return ckpt_fwd(c, PC, a[4]);
+}
+template <bool PC> int ckpt_bwd_one(PyObject* const* a)                                                                        // kept, dy, dx_or_None, ds, workspace, bits
+{
+    CkptItems c{};
+    c.item[0] = ckpt_item(a, true, PC, c.dt);
+    c.count = 1;
+    return ckpt_bwd(c, PC, a[4], a[5]);
+}
+
+// A [rows, cols] operand whose rows may be apart, and their distance.
+const at::Tensor& matrix(PyObject* o, int64_t& stride)
+{
+    want(THPVariable_CheckExact(o));
+    const at::Tensor& t = THPVariable_Unpack(o);
+    want(t.is_cuda() && t.get_device() == c10::hip::current_device() && t.dim() == 2 && (t.stride(1) == 1 || t.size(1) == 1));
+    stride = t.size(0) > 1 ? t.stride(0) : t.size(1);
+    return t;
+}
+
+// x, head, targets, loss, V, workspace, lse_or_None, mean_or_None, dx_or_None, head_grad_or_None, row_weight_or_None, scale, piece
+int linear_ce(PyObject* const* a)
+{
+    int64_t x_stride = 0, dx_stride = 0;
+    const at::Tensor &x = matrix(a[0], x_stride), &head = here(a[1]), &targets = here(a[2], at::kInt), &ws = here(a[5]);
+    const int64_t T = x.size(0), H = x.size(1), V = integer(a[4]), piece = integer(a[12]);
+    const sasq_dtype dt = dtype_of(x);
+    auto floats_of = [&](PyObject* o, int64_t n) -> float* {
+        if (o == Py_None) return nullptr;
+        const at::Tensor& t = here(o, at::kFloat);
+        want(t.numel() == n);
+        return pointer<float>(t);
+    };
+    want(a[3] != Py_None && targets.numel() == T);
+    float *loss = floats_of(a[3], T), *lse = floats_of(a[6], T), *mean = floats_of(a[7], 1), *weight = floats_of(a[10], T);
+    const at::Tensor* dx = a[8] == Py_None ? nullptr : &matrix(a[8], dx_stride);
+    const at::Tensor* grad = a[9] == Py_None ? nullptr : &here(a[9]);
+    want(!dx || grad);
+    if (dx) same(*dx, x);
+    want(bytes(head) == entry.head_bytes(V, H, SASQ_HEAD_LOGITS) && (!grad || bytes(*grad) == entry.head_bytes(V, H, SASQ_HEAD_GRAD)));
+    const float scale = static_cast<float>(real(a[11]));
+    void *xp = x.data_ptr(), *hp = pointer(head), *gp = pointer(grad), *dp = dx ? dx->data_ptr() : nullptr, *wp = pointer(ws);
+    const int32_t* tp = pointer<int32_t>(targets);
+    const size_t wb = bytes(ws);
+    return unlocked([&](void* st) {
+        return entry.linear_ce(xp, x_stride, hp, gp, tp, weight, scale, loss, lse, mean, dp, dx_stride, T, V, H, piece, dt, wp, wb, st);
+    });
+}
+
 // bind({"sasq_...": address, ...}): the entry points of the library that the binding has loaded
 PyObject* bind(PyObject*, PyObject* table)
 {
@@ -506,7 +643,10 @@ PyObject* bind(PyObject*, PyObject* table)
         set("sasq_bwd_weight_bytes", e.bwd_weight_bytes) && set("sasq_linear_bwd_input", e.linear_bwd_input) &&
         set("sasq_absmax_scale", e.absmax_scale) && set("sasq_quantize_weight", e.quantize_weight) &&
         set("sasq_pack_weight", e.pack_weight) && set("sasq_prepare_bwd_weight", e.prepare_bwd_weight) &&
-        set("sasq_kv_append", e.kv_append) && set("sasq_paged_attention", e.paged_attention);
+        set("sasq_kv_append", e.kv_append) && set("sasq_paged_attention", e.paged_attention) &&
+        set("sasq_fakequant_fwd_ckpt_batch", e.ckpt_fwd[0]) && set("sasq_fakequant_fwd_pc_ckpt_batch", e.ckpt_fwd[1]) &&
+        set("sasq_fakequant_bwd_ckpt_batch", e.ckpt_bwd[0]) && set("sasq_fakequant_bwd_pc_ckpt_batch", e.ckpt_bwd[1]) &&
+        set("sasq_head_bytes", e.head_bytes) && set("sasq_linear_ce", e.linear_ce);
     if (!ok) return nullptr;
     entry = e;
     Py_RETURN_NONE;
@@ -535,6 +675,15 @@ PyMethodDef methods[] = {
     SASQ_METHOD("sasq_prepare_bwd_weight", prepare_bwd_weight, 7),
     SASQ_METHOD("sasq_kv_append", kv_append, 11),
     SASQ_METHOD("sasq_paged_attention", paged_attention, 8),
+    SASQ_METHOD("sasq_fakequant_fwd_ckpt", ckpt_fwd_one<false>, 5),
+    SASQ_METHOD("sasq_fakequant_fwd_pc_ckpt", ckpt_fwd_one<true>, 5),
+    SASQ_METHOD("sasq_fakequant_bwd_ckpt", ckpt_bwd_one<false>, 6),
+    SASQ_METHOD("sasq_fakequant_bwd_pc_ckpt", ckpt_bwd_one<true>, 6),
+    SASQ_METHOD("sasq_fakequant_fwd_ckpt_batch", ckpt_fwd_batch<false>, 2),
+    SASQ_METHOD("sasq_fakequant_fwd_pc_ckpt_batch", ckpt_fwd_batch<true>, 2),
+    SASQ_METHOD("sasq_fakequant_bwd_ckpt_batch", ckpt_bwd_batch<false>, 3),
+    SASQ_METHOD("sasq_fakequant_bwd_pc_ckpt_batch", ckpt_bwd_batch<true>, 3),
+    SASQ_METHOD("sasq_linear_ce", linear_ce, 13),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

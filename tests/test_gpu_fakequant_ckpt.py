@@ -1,7 +1,7 @@
 """Fake quantization with one byte an element kept for the backward: against the definition in 64 bits, and against the form that keeps x.
 
-Tolerance of ds: its products are exact in fp32, at most eight (per channel: four, and two roundings of partial sums) are added in fp32 and the rest in fp64,
-so it is off by at most 8 * 2^-24 of the sum of the terms' sizes, and by one rounding of its own.
+Tolerance of ds: its products are exact in fp32 and added in fp64, per channel four in fp32 first (and two roundings of partial sums), so it is off by at most
+8 * 2^-24 of the sum of the terms' sizes, and by one rounding of its own.
 """
 from __future__ import annotations
 
