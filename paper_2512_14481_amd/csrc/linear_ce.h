@@ -36,6 +36,7 @@ struct CeArgs {
     int slots, max_splits;                      // parts that its contraction is cut into: as many as fill the slots of the chip (splits_of)
     int tile, grad_tile;                        // 0: 256x256, 1: 128x256 (logits), 2: 128x128
     bool grad;
+    int few_parts;                              // few rows (linear_ce_few.hip): parts of the gradient's contraction, 0: the tiles
     // operands
     const void* x; int64_t x_stride;
     const uint8_t* head; const uint8_t* head_grad;
@@ -82,5 +83,10 @@ __device__ __forceinline__ int64_t block_at(int64_t row, int col, int kt)
 
 void launch_ce_logits(const CeArgs& c, sasq_dtype dt, int64_t col0, int64_t cols, hipStream_t st);
 void launch_ce_grad(const CeArgs& c, sasq_dtype dt, int64_t col0, int64_t cols, hipStream_t st);
+
+// At most kFewRows rows, the whole vocabulary in one piece (linear_ce_few.hip).  M and S are of kFewCols columns; rows are not packed.
+constexpr int kFewRows = 64, kFewCols = 64;
+void launch_ce_few_logits(const CeArgs& c, sasq_dtype dt, hipStream_t st);
+void launch_ce_few_grad(const CeArgs& c, sasq_dtype dt, hipStream_t st);
 
 }  // namespace sasq

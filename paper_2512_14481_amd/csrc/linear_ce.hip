@@ -78,7 +78,7 @@ __global__ __launch_bounds__(256) void head_grad_kernel(const uint16_t* __restri
 constexpr int kPackThreads = 1024;
 __global__ __launch_bounds__(kPackThreads) void ce_pack_kernel(const int32_t* __restrict__ targets, int T, int V, int32_t* __restrict__ count,
                                                               int32_t* __restrict__ pos, int32_t* __restrict__ row, int32_t* __restrict__ tgt,
-                                                              RowStat* __restrict__ run, float* __restrict__ loss, float* __restrict__ lse, uint32_t* __restrict__ ticket,
+                                                              float* __restrict__ loss, float* __restrict__ lse, uint32_t* __restrict__ ticket,
                                                               float* __restrict__ mean)
 {
     __shared__ int wave_count[kPackThreads / kWave];
@@ -103,7 +103,6 @@ __global__ __launch_bounds__(kPackThreads) void ce_pack_kernel(const int32_t* __
             pos[r] = p;
             row[p] = r;
             tgt[p] = v;
-            run[p] = RowStat{0.0f, 0.0f};
         } else if (r < T) {
             pos[r] = -1;
             loss[r] = 0.0f;
@@ -143,19 +142,22 @@ __global__ __launch_bounds__(256) void ce_stage_kernel(const uint16_t* __restric
 
 // ---- between the products: M and S of each row so far ----
 // 16 rows a workgroup, 64 threads a row, each for every 64th group of columns, eight of them requested at a time.  All factors are exact powers of two.
+// targets: rows are not packed, and some of the T may be left out; NULL: they are, and *count of them are there.
 constexpr int kJoinRows = 16, kJoinLanes = 64, kJoinThreads = kJoinRows * kJoinLanes, kJoinAhead = 8;
 __global__ __launch_bounds__(kJoinThreads) void ce_join_kernel(const RowStat* __restrict__ stats, int groups, int64_t T, const int32_t* __restrict__ count,
                                                               RowStat* __restrict__ run, float* __restrict__ beta, uint8_t* __restrict__ scale_rows,
                                                               const float* __restrict__ zt, const int32_t* __restrict__ row, float* __restrict__ coef,
                                                               float* __restrict__ u_out, float* __restrict__ loss, float* __restrict__ lse,
-                                                              float* __restrict__ mean, double* __restrict__ part_loss, uint32_t* __restrict__ ticket, int last)
+                                                              float* __restrict__ mean, double* __restrict__ part_loss, uint32_t* __restrict__ ticket,
+                                                              const int32_t* __restrict__ targets, int V, int first, int last)
 {
     __shared__ float part[kJoinLanes][kJoinRows];
     __shared__ double row_loss[kJoinRows];
     __shared__ bool is_last;
     const int r = threadIdx.x % kJoinRows, k = threadIdx.x / kJoinRows, p = (int)blockIdx.x * kJoinRows + r;
     const RowStat* mine = stats + min((int64_t)p, T - 1);      // (rows past the counted ones hold anything)
-    const RowStat old = run[min((int64_t)p, T - 1)];
+    const RowStat old = first ? RowStat{0.0f, 0.0f} : run[min((int64_t)p, T - 1)];
+    const int target = targets ? targets[min((int64_t)p, T - 1)] : 0;
     RowStat s[kJoinAhead];
     auto fetch = [&](int g0) {
 #pragma unroll
@@ -167,7 +169,7 @@ __global__ __launch_bounds__(kJoinThreads) void ce_join_kernel(const RowStat* __
     };
     float top = -__builtin_inff();
     fetch(k);
-    const int n = *count;
+    const int counted = *count, n = targets ? (int)T : counted;
     if ((int)blockIdx.x * kJoinRows >= n) return;
     for (int g0 = k; g0 < groups; g0 += kJoinLanes * kJoinAhead) {
         if (g0 != k) fetch(g0);
@@ -204,15 +206,17 @@ __global__ __launch_bounds__(kJoinThreads) void ce_join_kernel(const RowStat* __
         beta[p] = f;
         if (last) {
             // In fp64: a small loss is the exponential of a difference.
+            const bool counts = !targets || (target >= 0 && target < V);
             const double z = (double)zt[p];
             const double d = all == 0.0f ? -(double)__builtin_inff() : ((double)m + log2((double)all)) * 0.69314718055994530942 - z;
             const double l = d > 0.0 ? d + log1p(exp(-d)) : log1p(exp(d));
             const double u = 1.0 / (1.0 + exp(-d));
-            loss[row[p]] = (float)l;
-            if (lse) lse[row[p]] = (float)(z + l);
+            const int to = row ? row[p] : p;
+            loss[to] = counts ? (float)l : 0.0f;
+            if (lse) lse[to] = counts ? (float)(z + l) : 0.0f;
             u_out[p] = (float)u;
             coef[p] = all == 0.0f ? 0.0f : (float)(u / (double)all);
-            row_loss[r] = (double)(float)l;
+            row_loss[r] = counts ? (double)(float)l : 0.0;
         }
     } else if (k == 0) {
         row_loss[r] = 0.0;
@@ -225,7 +229,7 @@ __global__ __launch_bounds__(kJoinThreads) void ce_join_kernel(const RowStat* __
         double all = 0.0;
         for (int j = 0; j < kJoinRows; ++j) all += row_loss[j];
         if (blocks == 1) {
-            *mean = (float)(all / (double)n);
+            *mean = counted ? (float)(all / (double)counted) : 0.0f;
             is_last = false;
         } else is_last = publish_then_ticket(&part_loss[blockIdx.x], all, ticket) == (uint32_t)blocks - 1;
     }
@@ -241,7 +245,7 @@ __global__ __launch_bounds__(kJoinThreads) void ce_join_kernel(const RowStat* __
     if (threadIdx.x) return;
     all = 0.0;
     for (int j = 0; j < kJoinThreads / kWave; ++j) all += wave_part[j];
-    *mean = (float)(all / (double)n);
+    *mean = counted ? (float)(all / (double)counted) : 0.0f;
 }
 
 // a_v of groups of columns with another M than their row's, in place: sixteen rows and 64 blocks a workgroup, a 1 KB block a wave and access.
@@ -283,11 +287,11 @@ __global__ __launch_bounds__(256) void ce_scale_kernel(uint16_t* __restrict__ a,
 
 // ---- the end: dx of every row; left-out ones are 0 ----
 template <int DT, bool VEC>
-__global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ acc, int bm, int tiles_n, int slots, int max_splits, const int32_t* __restrict__ count,
+__global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ acc, int bm, int tiles_n, int slots, int max_splits, int few_parts, const int32_t* __restrict__ count,
                                                    const int32_t* __restrict__ pos, const int32_t* __restrict__ tgt, const float* __restrict__ coef,
                                                    const float* __restrict__ u, const uint8_t* __restrict__ head, const float* __restrict__ row_weight,
                                                    float scale, uint16_t* __restrict__ dx, int64_t stride, int H, int Hp, const float* __restrict__ loss,
-                                                   float* __restrict__ mean, int T)
+                                                   float* __restrict__ mean, int T, int V)
 {
     using S = Store16<DT>;
     const int r = (int)blockIdx.x;
@@ -301,21 +305,25 @@ __global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ ac
         if (threadIdx.x == 0) *mean = *count ? (float)((part[0] + part[1] + part[2] + part[3]) / (double)*count) : 0.0f;
         return;
     }
-    const int p = pos[r];
+    // few_parts: rows are not packed, and their targets tell which count
+    int p = few_parts ? r : pos[r];
     float g = 0.0f, cf = 0.0f, uu = 0.0f;
     int t = 0;
-    const int n = *count, splits = splits_of(n, bm, tiles_n, slots, max_splits);
+    const int n = *count, splits = few_parts ? few_parts : splits_of(n, bm, tiles_n, slots, max_splits), rows = few_parts ? T : n;
+    if (p >= 0) {
+        t = tgt[p];
+        if (few_parts && (t < 0 || t >= V)) p = -1;
+    }
     if (p >= 0) {
         g = scale * (row_weight ? row_weight[r] : 1.0f / (float)n);
         cf = coef[p];
         uu = u[p];
-        t = tgt[p];
     }
     for (int h = threadIdx.x * 8; h < H; h += 256 * 8) {
         float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
         if (p >= 0) {
             for (int s = 0; s < splits; ++s) {
-                const float* at = acc + ((int64_t)s * n + p) * Hp + h;
+                const float* at = acc + ((int64_t)s * rows + p) * Hp + h;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] += at[e];
             }
@@ -376,7 +384,14 @@ static size_t ce_plan(CeArgs& c, int64_t piece, char* base)
     c.Hp = (int)up(c.H, 64);
     c.Vp = (int)up(c.V, 64);
     ce_pieces(c.T, c.V, piece, c.grad, c.piece, c.first_piece);
-    c.tile = ce_tile(c.T, c.piece);
+    c.few_parts = 0;
+    if (c.T <= kFewRows && c.piece >= c.V) {
+        // as many workgroups as fill the chip twice, of 16 K steps a wave at least
+        int64_t parts = 1024 / ((c.Hp + kFewCols - 1) / kFewCols);
+        if (parts > c.Vp / 2048) parts = c.Vp / 2048;
+        c.few_parts = (int)(parts < 1 ? 1 : parts);
+    }
+    c.tile = c.few_parts ? 2 : ce_tile(c.T, c.piece);         // (few rows: M and S of 64 columns, as of such a tile's waves)
     c.grad_tile = ce_grad_tile(c.T, c.H);
     const int bm = tile_rows(c.grad_tile), bn = tile_cols(c.grad_tile), sc = stat_cols(c.tile);
     const int64_t tiles_n = (c.H + bn - 1) / bn;
@@ -386,12 +401,13 @@ static size_t ce_plan(CeArgs& c, int64_t piece, char* base)
     int64_t sums = c.T, filled = c.slots / tiles_n * bm;
     if (filled > c.T * c.max_splits) filled = c.T * c.max_splits;
     if (sums < filled) sums = filled;
+    if (c.few_parts) sums = c.T * c.few_parts;
     size_t at = 0;
     auto part = [&](auto*& p, size_t bytes) {
         p = reinterpret_cast<std::remove_reference_t<decltype(p)>>(base + at);
         at += (bytes + 255) / 256 * 256;
     };
-    const size_t T = (size_t)c.T, T16 = (T + 15) / 16 * 16, groups = (size_t)(c.piece / sc);
+    const size_t T = (size_t)c.T, T16 = c.few_parts && T > 32 ? 64 : (T + 15) / 16 * 16, groups = (size_t)(c.piece / sc);
     part(c.count, 4);
     part(c.ticket, 4);
     part(c.pos, T * 4);
@@ -420,10 +436,40 @@ static bool ce_sizes_ok(int64_t T, int64_t V, int64_t H, int64_t piece)
 }
 
 template <int DT>
+static void launch_dx(const CeArgs& c, hipStream_t st)
+{
+    const int T = (int)c.T, H = (int)c.H, bm = tile_rows(c.grad_tile), tiles_n = (int)((c.H + tile_cols(c.grad_tile) - 1) / tile_cols(c.grad_tile));
+    const bool vec = c.dx_stride % 8 == 0 && H % 8 == 0;
+    auto go = [&](auto v) {
+        ce_dx_kernel<DT, decltype(v)::value><<<T + (c.mean ? 1 : 0), 256, 0, st>>>(
+            c.acc, bm, tiles_n, c.slots, c.max_splits, c.few_parts, c.count, c.pos, c.few_parts ? c.targets : c.tgt, c.coef, c.u, c.head, c.row_weight, c.scale,
+            static_cast<uint16_t*>(c.dx), c.dx_stride, H, c.Hp, c.loss, c.mean, T, (int)c.V);
+    };
+    if (vec) go(std::true_type{});
+    else     go(std::false_type{});
+}
+
+static void launch_join(const CeArgs& c, int groups, bool first, bool last, hipStream_t st)
+{
+    ce_join_kernel<<<(unsigned)((c.T + kJoinRows - 1) / kJoinRows), kJoinThreads, 0, st>>>(
+        c.stats, groups, c.T, c.count, c.run, c.beta, c.grad && !c.few_parts ? c.scale_rows : nullptr, c.zt, c.few_parts ? nullptr : c.row, c.coef, c.u, c.loss,
+        c.lse, c.grad ? nullptr : c.mean, c.part, c.ticket, c.few_parts ? c.targets : nullptr, (int)c.V, first, last);
+}
+
+template <int DT>
 static void ce_run(const CeArgs& c, sasq_dtype dt, hipStream_t st)
 {
     const int T = (int)c.T, H = (int)c.H;
-    ce_pack_kernel<<<1, kPackThreads, 0, st>>>(c.targets, T, (int)c.V, c.count, c.pos, c.row, c.tgt, c.run, c.loss, c.lse, c.ticket, c.mean);
+    if (c.few_parts) {
+        launch_ce_few_logits(c, dt, st);
+        launch_join(c, (int)((c.V + kFewCols - 1) / kFewCols), true, true, st);
+        if (c.grad) {
+            launch_ce_few_grad(c, dt, st);
+            launch_dx<DT>(c, st);
+        }
+        return;
+    }
+    ce_pack_kernel<<<1, kPackThreads, 0, st>>>(c.targets, T, (int)c.V, c.count, c.pos, c.row, c.tgt, c.loss, c.lse, c.ticket, c.mean);
     if (c.x_stride % 8 == 0 && H % 8 == 0)
         ce_stage_kernel<true><<<(T + 3) / 4, 256, 0, st>>>(static_cast<const uint16_t*>(c.x), c.x_stride, c.xs, c.count, c.row, H, c.Hp);
     else
@@ -433,9 +479,7 @@ static void ce_run(const CeArgs& c, sasq_dtype dt, hipStream_t st)
         const int64_t piece = col0 ? c.piece : c.first_piece, cols = c.V - col0 < piece ? c.V - col0 : piece;
         const int groups = (int)((cols + bn - 1) / bn) * 2;
         launch_ce_logits(c, dt, col0, cols, st);
-        ce_join_kernel<<<(T + kJoinRows - 1) / kJoinRows, kJoinThreads, 0, st>>>(
-            c.stats, groups, c.T, c.count, c.run, c.beta, c.grad ? c.scale_rows : nullptr, c.zt, c.row, c.coef, c.u, c.loss, c.lse, c.grad ? nullptr : c.mean,
-            c.part, c.ticket, col0 + cols >= c.V);
+        launch_join(c, groups, col0 == 0, col0 + cols >= c.V, st);
         if (c.grad) {
             const int kt = (int)(up(cols, 64) / 32);
             ce_scale_kernel<DT><<<dim3((T + 15) / 16, (kt + kScaleBlocks - 1) / kScaleBlocks), 256, 0, st>>>(c.a, row_blocks(c.piece), kt, sc / 32, c.stats, c.run,
@@ -444,15 +488,7 @@ static void ce_run(const CeArgs& c, sasq_dtype dt, hipStream_t st)
         }
         col0 += cols;
     }
-    if (c.grad) {
-        const int bm = tile_rows(c.grad_tile), tiles_n = (int)((c.H + tile_cols(c.grad_tile) - 1) / tile_cols(c.grad_tile));
-        if (c.dx_stride % 8 == 0 && H % 8 == 0)
-            ce_dx_kernel<DT, true><<<T + (c.mean ? 1 : 0), 256, 0, st>>>(c.acc, bm, tiles_n, c.slots, c.max_splits, c.count, c.pos, c.tgt, c.coef, c.u, c.head, c.row_weight, c.scale,
-                                                      static_cast<uint16_t*>(c.dx), c.dx_stride, H, c.Hp, c.loss, c.mean, T);
-        else
-            ce_dx_kernel<DT, false><<<T + (c.mean ? 1 : 0), 256, 0, st>>>(c.acc, bm, tiles_n, c.slots, c.max_splits, c.count, c.pos, c.tgt, c.coef, c.u, c.head, c.row_weight, c.scale,
-                                                       static_cast<uint16_t*>(c.dx), c.dx_stride, H, c.Hp, c.loss, c.mean, T);
-    }
+    if (c.grad) launch_dx<DT>(c, st);
 }
 
 }  // namespace sasq
