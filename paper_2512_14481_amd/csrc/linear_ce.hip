@@ -151,7 +151,8 @@ __global__ __launch_bounds__(kJoinThreads) void ce_join_kernel(const RowStat* __
                                                               float* __restrict__ mean, double* __restrict__ part_loss, uint32_t* __restrict__ ticket,
                                                               const int32_t* __restrict__ targets, int V, int first, int last)
 {
-    __shared__ float part[kJoinLanes][kJoinRows];
+    constexpr int kWaves = kJoinThreads / kWave;
+    __shared__ float part[kWaves][kJoinRows];
     __shared__ double row_loss[kJoinRows];
     __shared__ bool is_last;
     const int r = threadIdx.x % kJoinRows, k = threadIdx.x / kJoinRows, p = (int)blockIdx.x * kJoinRows + r;
@@ -177,11 +178,17 @@ __global__ __launch_bounds__(kJoinThreads) void ce_join_kernel(const RowStat* __
         for (int j = 0; j < kJoinAhead; ++j)
             if (s[j].s != 0.0f) top = fmaxf(top, s[j].m);
     }
-    part[k][r] = top;
+    // a wave has four of a row's threads: they meet by shuffles, the waves in LDS
+    const int wave = threadIdx.x / kWave;
+    auto share = [&](float v) {
+        if (threadIdx.x % kWave < kJoinRows) part[wave][r] = v;
+    };
+    top = fmaxf(top, __shfl_xor(top, 16, kWave));
+    share(fmaxf(top, __shfl_xor(top, 32, kWave)));
     __syncthreads();
     float m = old.s != 0.0f ? old.m : -__builtin_inff();
 #pragma unroll
-    for (int j = 0; j < kJoinLanes; ++j) m = fmaxf(m, part[j][r]);
+    for (int j = 0; j < kWaves; ++j) m = fmaxf(m, part[j][r]);
     if (m == -__builtin_inff()) m = 0.0f;
     __syncthreads();
     float sum = 0.0f;
@@ -194,14 +201,15 @@ __global__ __launch_bounds__(kJoinThreads) void ce_join_kernel(const RowStat* __
             other = other || (s[j].s != 0.0f && s[j].m != m);
         }
     }
-    part[k][r] = sum;
+    sum += __shfl_xor(sum, 16, kWave);
+    share(sum + __shfl_xor(sum, 32, kWave));
     const int any = __syncthreads_or(other && p < n);
     if (scale_rows && threadIdx.x == 0) scale_rows[blockIdx.x] = any != 0;
     if (k == 0 && p < n) {
         const float f = old.s != 0.0f ? exp2f(old.m - m) : 0.0f;
         float all = old.s * f;
 #pragma unroll
-        for (int j = 0; j < kJoinLanes; ++j) all += part[j][r];
+        for (int j = 0; j < kWaves; ++j) all += part[j][r];
         run[p] = RowStat{m, all};
         beta[p] = f;
         if (last) {
@@ -386,9 +394,9 @@ static size_t ce_plan(CeArgs& c, int64_t piece, char* base)
     ce_pieces(c.T, c.V, piece, c.grad, c.piece, c.first_piece);
     c.few_parts = 0;
     if (c.T <= kFewRows && c.piece >= c.V) {
-        // as many workgroups as fill the chip twice, of 16 K steps a wave at least
-        int64_t parts = 1024 / ((c.Hp + kFewCols - 1) / kFewCols);
-        if (parts > c.Vp / 2048) parts = c.Vp / 2048;
+        // as many workgroups as fill the chip twice, of 64 columns a wave at least
+        int64_t parts = 512 / ((c.Hp + kFewCols - 1) / kFewCols);
+        if (parts > c.Vp / 512) parts = c.Vp / 512;
         c.few_parts = (int)(parts < 1 ? 1 : parts);
     }
     c.tile = c.few_parts ? 2 : ce_tile(c.T, c.piece);         // (few rows: M and S of 64 columns, as of such a tile's waves)

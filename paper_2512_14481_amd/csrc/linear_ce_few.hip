@@ -1,6 +1,6 @@
 // sasq_linear_ce for at most 64 rows (linear_ce.h): both products read the head once, from memory into registers, and are bound by that.
 //
-// A workgroup has 64 rows of a head's layout (64 vocabulary entries for the logits, 64 channels for the gradient) and its four waves a quarter of the
+// A workgroup has 64 rows of a head's layout (64 vocabulary entries for the logits, 64 channels for the gradient) and its eight waves an eighth of the
 // contraction each: a wave loads four 1 KB blocks at a time, which are four operands of v_mfma_f32_16x16x32 as they lie, and the rows of x (or their
 // exponentials) beside them from L2.  The waves' sums meet in LDS.  There are as many waves as fill the chip twice from 32000 entries on, each with 8 to 16 KB
 // requested ahead.  No rows are packed: left-out ones are computed along and dropped.
@@ -11,53 +11,72 @@
 
 namespace sasq {
 
-constexpr int kFewBlocks = kFewCols / 16, kFewPitch = kFewCols + 4, kFewStep = 2;
+constexpr int kFewBlocks = kFewCols / 16, kFewPitch = kFewCols + 4, kFewWaves = 8, kFewThreads = kFewWaves * kWave;
 
-// Sums over the K steps [k0, k1) of 32 of W (row blocks at `w`, `w_kt` KB apart, of which `there` are there: the last one stands in for others) times
-// 16 MB rows that `load` brings: lane (fq, frow) holds acc[nb][b][e], of row 16 b + frow and column 16 nb + 4 fq + e.
+// Sums of a wave's share of the K steps [k0, k1), of 32 each and an even number, of W (row blocks at `w`, `w_kt` KB apart, of which `there` are there: the
+// last one stands in for others) times 16 MB rows that `load` brings: lane (fq, frow) holds acc[nb][b][e], of row 16 b + frow and column 16 nb + 4 fq + e.
+// The waves take the steps in turn, so that what a workgroup reads at a time lies together.
 template <int DT, int MB, typename Load>
 __device__ __forceinline__ void few_product(const uint8_t* __restrict__ w, int64_t w_kt, int there, int k0, int k1, f32x4 (&acc)[kFewBlocks][MB], Load&& load)
 {
+    constexpr int kStep = MB == 1 ? 2 : 1;                     // K steps requested at once: what leaves room for the waves of two workgroups on a CU
+    constexpr int kTurn = kStep * kFewWaves;
 #pragma unroll
     for (int nb = 0; nb < kFewBlocks; ++nb)
 #pragma unroll
         for (int b = 0; b < MB; ++b) acc[nb][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     const int lane = threadIdx.x & 63, r = lane & 15, c = lane >> 4;
-    const uint8_t* at = w + ((4 * r + (c ^ swz64(r))) << 4);
-    i32x4 wf[2][kFewStep][kFewBlocks], xf[2][kFewStep][MB];
+    const uint32_t at = (uint32_t)(4 * r + (c ^ swz64(r))) << 4;
+    i32x4 wf[2][kStep][kFewBlocks], xf[2][kStep][MB];
     auto fetch = [&](int set, int k) {
 #pragma unroll
-        for (int s = 0; s < kFewStep; ++s) {
-            const int kk = min(k + s, k1 - 1);
+        for (int s = 0; s < kStep; ++s) {
 #pragma unroll
-            for (int nb = 0; nb < kFewBlocks; ++nb) wf[set][s][nb] = *reinterpret_cast<const i32x4*>(at + (min(nb, there - 1) * w_kt + kk) * 1024);
+            for (int nb = 0; nb < kFewBlocks; ++nb)
+                wf[set][s][nb] = __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(w + (min(nb, there - 1) * w_kt + k + s) * 1024 + at));
 #pragma unroll
-            for (int b = 0; b < MB; ++b) xf[set][s][b] = load(b, kk);
+            for (int b = 0; b < MB; ++b) xf[set][s][b] = load(b, k + s);
         }
     };
-    auto multiply = [&](int set, int k) {
+    auto multiply = [&](int set) {
 #pragma unroll
-        for (int s = 0; s < kFewStep; ++s) {
-            if (k + s >= k1) break;
+        for (int s = 0; s < kStep; ++s)
 #pragma unroll
             for (int nb = 0; nb < kFewBlocks; ++nb)
 #pragma unroll
                 for (int b = 0; b < MB; ++b) acc[nb][b] = Mfma16x16<DT>::mma(wf[set][s][nb], xf[set][s][b], acc[nb][b]);
-        }
     };
-    if (k0 >= k1) return;
-    fetch(0, k0);
-    for (int k = k0; k < k1; k += 2 * kFewStep) {
-        if (k + kFewStep < k1) fetch(1, k + kFewStep);
-        multiply(0, k);
-        if (k + 2 * kFewStep < k1) fetch(0, k + 2 * kFewStep);
-        if (k + kFewStep < k1) multiply(1, k + kFewStep);
+    int k = k0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * kStep;         // uniform: block addresses stay scalar
+    if (k < k1) fetch(0, k);
+    for (; k < k1; k += 2 * kTurn) {
+        if (k + kTurn < k1) fetch(1, k + kTurn);
+        multiply(0);
+        if (k + 2 * kTurn < k1) fetch(0, k + 2 * kTurn);
+        if (k + kTurn < k1) multiply(1);
     }
 }
 
-// The four waves' sums: thread t then has, of row 16 b + t / 16, the columns 4 (t % 16) .. + 3.
+template <int N>
+__device__ __forceinline__ float few_turn(float v) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x120 + N, 0xf, 0xf, true)); }
+// Over sixteen lanes next to each other, for all of them.
+__device__ __forceinline__ float few_max(float v)
+{
+    v = fmaxf(v, few_turn<8>(v));
+    v = fmaxf(v, few_turn<4>(v));
+    v = fmaxf(v, few_turn<2>(v));
+    return fmaxf(v, few_turn<1>(v));
+}
+__device__ __forceinline__ float few_sum(float v)
+{
+    v += few_turn<8>(v);
+    v += few_turn<4>(v);
+    v += few_turn<2>(v);
+    return v + few_turn<1>(v);
+}
+
+// The waves' sums: thread t of the first 256 then has, of row 16 b + t / 16, the columns 4 (t % 16) .. + 3.
 template <int MB>
-__device__ __forceinline__ void few_meet(const f32x4 (&acc)[kFewBlocks][MB], float (&lds)[4][16][kFewPitch], f32x4 (&out)[MB])
+__device__ __forceinline__ void few_meet(const f32x4 (&acc)[kFewBlocks][MB], float (&lds)[kFewWaves][16][kFewPitch], f32x4 (&out)[MB])
 {
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6, frow = lane & 15, fq = lane >> 4;
 #pragma unroll
@@ -68,19 +87,19 @@ __device__ __forceinline__ void few_meet(const f32x4 (&acc)[kFewBlocks][MB], flo
         __syncthreads();
         out[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int w = 0; w < 4; ++w) out[b] += *reinterpret_cast<const f32x4*>(&lds[w][t >> 4][4 * (t & 15)]);
+        for (int w = 0; w < kFewWaves; ++w) out[b] += *reinterpret_cast<const f32x4*>(&lds[w][(t >> 4) & 15][4 * (t & 15)]);
     }
 }
 
 template <int DT, int MB, bool VEC, bool GRAD>
-__global__ __launch_bounds__(256) void ce_few_logits_kernel(const uint16_t* __restrict__ x, int64_t stride, const uint8_t* __restrict__ head,
+__global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(MB == 4 ? 2 : 4))) void ce_few_logits_kernel(const uint16_t* __restrict__ x, int64_t stride, const uint8_t* __restrict__ head,
                                                            const int32_t* __restrict__ targets, int T, int V, int H, int Hp, RowStat* __restrict__ stats,
                                                            float* __restrict__ zt, uint16_t* __restrict__ a, int a_kt, int32_t* __restrict__ count,
                                                            uint32_t* __restrict__ ticket)
 {
     using S = Store16<DT>;
-    __shared__ __attribute__((aligned(16))) float lds[4][16][kFewPitch];
-    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, frow = lane & 15, fq = lane >> 4;
+    __shared__ __attribute__((aligned(16))) float lds[kFewWaves][16][kFewPitch];
+    const int t = threadIdx.x, lane = t & 63, frow = lane & 15, fq = lane >> 4;
     const int v0 = (int)blockIdx.x * kFewCols;
     if (blockIdx.x == 0 && t < 64) {                           // how many rows count, for the kernels behind this one
         const int v = t < T ? targets[t] : -1;
@@ -91,8 +110,10 @@ __global__ __launch_bounds__(256) void ce_few_logits_kernel(const uint16_t* __re
         }
     }
     const int64_t w_kt = row_blocks(Hp);
-    const int nk = Hp / 32;
     f32x4 acc[kFewBlocks][MB];
+    int tgt[MB];                                               // of the rows that this thread reduces at the end
+#pragma unroll
+    for (int b = 0; b < MB; ++b) tgt[b] = targets[min(16 * b + ((t >> 4) & 15), T - 1)];
     const uint16_t* row[MB];
 #pragma unroll
     for (int b = 0; b < MB; ++b) row[b] = x + (int64_t)min(16 * b + frow, T - 1) * stride;
@@ -111,14 +132,15 @@ __global__ __launch_bounds__(256) void ce_few_logits_kernel(const uint16_t* __re
         return __builtin_bit_cast(i32x4, o);
     };
     // columns past the vocabulary's end are dropped below
-    few_product<DT, MB>(head + (int64_t)(v0 >> 4) * w_kt * 1024, w_kt, ((V - 1) >> 4) - (v0 >> 4) + 1, nk * wave / 4, nk * (wave + 1) / 4, acc, load);
+    few_product<DT, MB>(head + (int64_t)(v0 >> 4) * w_kt * 1024, w_kt, ((V - 1) >> 4) - (v0 >> 4) + 1, 0, Hp / 32, acc, load);
     f32x4 z[MB];
     few_meet<MB>(acc, lds, z);
+    if (t >= 256) return;
     const int r16 = t >> 4, v = v0 + 4 * (t & 15);
 #pragma unroll
     for (int b = 0; b < MB; ++b) {
         const int m = 16 * b + r16;
-        const int target = targets[min(m, T - 1)];
+        const int target = tgt[b];
         float top = -__builtin_inff();
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -126,8 +148,7 @@ __global__ __launch_bounds__(256) void ce_few_logits_kernel(const uint16_t* __re
             if (v + e >= V || v + e == target) z[b][e] = -__builtin_inff();
             top = fmaxf(top, z[b][e]);
         }
-#pragma unroll
-        for (int o = 1; o < 16; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
+        top = few_max(top);
         const float mm = top == -__builtin_inff() ? 0.0f : ceilf(top * kLog2e) - (float)kTopExp<DT>;
         float av[4], sum = 0.0f;
 #pragma unroll
@@ -135,8 +156,7 @@ __global__ __launch_bounds__(256) void ce_few_logits_kernel(const uint16_t* __re
             av[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[b][e], kLog2e, -mm));
             sum += av[e];
         }
-#pragma unroll
-        for (int o = 1; o < 16; o <<= 1) sum += __shfl_xor(sum, o, kWave);
+        sum = few_sum(sum);
         if ((t & 15) == 0 && m < T) stats[(int64_t)blockIdx.x * T + m] = RowStat{mm, sum};
         if (GRAD) *reinterpret_cast<u32x2*>(a + block_at(m, v, a_kt)) = u32x2{S::pack(av[0], av[1]), S::pack(av[2], av[3])};
     }
@@ -144,16 +164,15 @@ __global__ __launch_bounds__(256) void ce_few_logits_kernel(const uint16_t* __re
 
 // The gradient's sums over a part of the vocabulary; exponentials are brought to their row's M on the way.
 template <int DT, int MB>
-__global__ __launch_bounds__(256) void ce_few_grad_kernel(const uint16_t* __restrict__ a, int a_kt, const uint8_t* __restrict__ head_grad, int T, int H, int Hp, int Vp,
+__global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(MB == 4 ? 2 : 4))) void ce_few_grad_kernel(const uint16_t* __restrict__ a, int a_kt, const uint8_t* __restrict__ head_grad, int T, int H, int Hp, int Vp,
                                                          const RowStat* __restrict__ stats, const RowStat* __restrict__ run, float* __restrict__ acc_out, int parts)
 {
     using S = Store16<DT>;
-    __shared__ __attribute__((aligned(16))) float lds[4][16][kFewPitch];
-    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, frow = lane & 15, fq = lane >> 4;
+    __shared__ __attribute__((aligned(16))) float lds[kFewWaves][16][kFewPitch];
+    const int t = threadIdx.x, lane = t & 63, frow = lane & 15, fq = lane >> 4;
     const int cols = (Hp + kFewCols - 1) / kFewCols, part = (int)blockIdx.x / cols, h0 = (int)blockIdx.x % cols * kFewCols;
     // K steps in pairs: 64 columns share M and S
     const int pairs = Vp / 64, p0 = (int)((int64_t)pairs * part / parts), p1 = (int)((int64_t)pairs * (part + 1) / parts);
-    const int k0 = 2 * (p0 + (p1 - p0) * wave / 4), k1 = 2 * (p0 + (p1 - p0) * (wave + 1) / 4);
     f32x4 acc[kFewBlocks][MB];
     float m[MB];
 #pragma unroll
@@ -168,9 +187,10 @@ __global__ __launch_bounds__(256) void ce_few_grad_kernel(const uint16_t* __rest
     };
     const int64_t w_kt = row_blocks(Vp);
     // sums of channels past the end are not used
-    few_product<DT, MB>(head_grad + (int64_t)(h0 >> 4) * w_kt * 1024, w_kt, ((H - 1) >> 4) - (h0 >> 4) + 1, k0, k1, acc, load);
+    few_product<DT, MB>(head_grad + (int64_t)(h0 >> 4) * w_kt * 1024, w_kt, ((H - 1) >> 4) - (h0 >> 4) + 1, 2 * p0, 2 * p1, acc, load);
     f32x4 out[MB];
     few_meet<MB>(acc, lds, out);
+    if (t >= 256) return;
 #pragma unroll
     for (int b = 0; b < MB; ++b) {
         const int row = 16 * b + (t >> 4), h = h0 + 4 * (t & 15);
@@ -183,7 +203,7 @@ void launch_ce_few_logits(const CeArgs& c, sasq_dtype dt, hipStream_t st)
     const int grid = (int)((c.V + kFewCols - 1) / kFewCols), mb = (int)((c.T + 15) / 16);
     const bool vec = c.x_stride % 8 == 0 && c.H % 8 == 0;
     auto go = [&](auto d, auto m, auto v, auto g) {
-        ce_few_logits_kernel<decltype(d)::value, decltype(m)::value, decltype(v)::value, decltype(g)::value><<<grid, 256, 0, st>>>(
+        ce_few_logits_kernel<decltype(d)::value, decltype(m)::value, decltype(v)::value, decltype(g)::value><<<grid, kFewThreads, 0, st>>>(
             static_cast<const uint16_t*>(c.x), c.x_stride, c.head, c.targets, (int)c.T, (int)c.V, (int)c.H, c.Hp, c.stats, c.zt, c.a, row_blocks(c.piece),
             c.count, c.ticket);
     };
@@ -202,7 +222,7 @@ void launch_ce_few_grad(const CeArgs& c, sasq_dtype dt, hipStream_t st)
 {
     const int mb = (int)((c.T + 15) / 16), grid = (c.Hp + kFewCols - 1) / kFewCols * c.few_parts;
     auto go = [&](auto d, auto m) {
-        ce_few_grad_kernel<decltype(d)::value, decltype(m)::value><<<grid, 256, 0, st>>>(c.a, row_blocks(c.piece), c.head_grad, (int)c.T, (int)c.H, c.Hp, c.Vp,
+        ce_few_grad_kernel<decltype(d)::value, decltype(m)::value><<<grid, kFewThreads, 0, st>>>(c.a, row_blocks(c.piece), c.head_grad, (int)c.T, (int)c.H, c.Hp, c.Vp,
                                                                                         c.stats, c.run, c.acc, c.few_parts);
     };
     auto by_rows = [&](auto d) {
