@@ -82,33 +82,50 @@ __global__ __launch_bounds__(kPackThreads) void ce_pack_kernel(const int32_t* __
                                                               float* __restrict__ mean)
 {
     __shared__ int wave_count[kPackThreads / kWave];
+    constexpr int kEach = 4;                                   // rows of a thread, next to each other
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     int base = 0;
-    for (int r0 = 0; r0 < T; r0 += kPackThreads) {
-        const int r = r0 + t;
-        const int v = r < T ? targets[r] : -1;
-        const bool counts = v >= 0 && v < V;
-        const uint64_t mask = __builtin_amdgcn_ballot_w64(counts);
-        if (lane == 0) wave_count[wave] = __popcll(mask);
+    for (int r0 = 0; r0 < T; r0 += kPackThreads * kEach) {
+        int v[kEach];
+        bool counts[kEach];
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const int r = r0 + t * kEach + j;
+            v[j] = r < T ? targets[r] : -1;
+        }
+        int below = 0, all = 0;                                // counted rows of the lanes before this one, and of the wave
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            counts[j] = v[j] >= 0 && v[j] < V;
+            const uint64_t mask = __builtin_amdgcn_ballot_w64(counts[j]);
+            below += __popcll(mask & ((UINT64_C(1) << lane) - 1));
+            all += __popcll(mask);
+        }
+        if (lane == 0) wave_count[wave] = all;
         __syncthreads();
-        int before = 0, all = 0;
+        int before = 0, round = 0;
 #pragma unroll
         for (int w = 0; w < kPackThreads / kWave; ++w) {
             before += w < wave ? wave_count[w] : 0;
-            all += wave_count[w];
+            round += wave_count[w];
         }
         __syncthreads();
-        if (counts) {
-            const int p = base + before + __popcll(mask & ((UINT64_C(1) << lane) - 1));
-            pos[r] = p;
-            row[p] = r;
-            tgt[p] = v;
-        } else if (r < T) {
-            pos[r] = -1;
-            loss[r] = 0.0f;
-            if (lse) lse[r] = 0.0f;
+        int p = base + before + below;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const int r = r0 + t * kEach + j;
+            if (counts[j]) {
+                pos[r] = p;
+                row[p] = r;
+                tgt[p] = v[j];
+                ++p;
+            } else if (r < T) {
+                pos[r] = -1;
+                loss[r] = 0.0f;
+                if (lse) lse[r] = 0.0f;
+            }
         }
-        base += all;
+        base += round;
     }
     if (t == 0) {
         *count = base;
@@ -159,6 +176,8 @@ __global__ __launch_bounds__(kJoinThreads) void ce_join_kernel(const RowStat* __
     const RowStat* mine = stats + min((int64_t)p, T - 1);      // (rows past the counted ones hold anything)
     const RowStat old = first ? RowStat{0.0f, 0.0f} : run[min((int64_t)p, T - 1)];
     const int target = targets ? targets[min((int64_t)p, T - 1)] : 0;
+    const float target_z = zt[min((int64_t)p, T - 1)];
+    const int to = row ? row[min((int64_t)p, T - 1)] : p;
     RowStat s[kJoinAhead];
     auto fetch = [&](int g0) {
 #pragma unroll
@@ -215,11 +234,10 @@ __global__ __launch_bounds__(kJoinThreads) void ce_join_kernel(const RowStat* __
         if (last) {
             // In fp64: a small loss is the exponential of a difference.
             const bool counts = !targets || (target >= 0 && target < V);
-            const double z = (double)zt[p];
+            const double z = (double)target_z;
             const double d = all == 0.0f ? -(double)__builtin_inff() : ((double)m + log2((double)all)) * 0.69314718055994530942 - z;
-            const double l = d > 0.0 ? d + log1p(exp(-d)) : log1p(exp(d));
-            const double u = 1.0 / (1.0 + exp(-d));
-            const int to = row ? row[p] : p;
+            const double ex = exp(-fabs(d)), over = 1.0 / (1.0 + ex);
+            const double l = fmax(d, 0.0) + log1p(ex), u = d > 0.0 ? over : ex * over;
             loss[to] = counts ? (float)l : 0.0f;
             if (lse) lse[to] = counts ? (float)(z + l) : 0.0f;
             u_out[p] = (float)u;
@@ -371,12 +389,18 @@ static void ce_pieces(int64_t T, int64_t V, int64_t piece, bool grad, int& cols,
     if (!grad) first = cols;
 }
 
-static int ce_tile(int64_t M, int64_t N)
+// The logits' tile, by the time of its rounds of 256 workgroups (of 128x128 tiles a CU holds two): what a tile takes to start and for its epilogue, and its K
+// tiles.  us, whole call without the gradient, 256x256 | 128x256 | 128x128, T x H -> V: 128 x 4096 -> 32000 103 | 93 | 75, 200 rows 109 | 90 | 98, 333
+// 121 | 139 | 125, 512 123 | 146 | 164, 2048 430 | 499 | 523, 711 x 5120 -> 32000 238 | 246 | 269, 333 x 1376 -> 100003 165 | 147 | 138, 1500 x 1024 ->
+// 50000 196 | 211 | 192, 3000 x 512 -> 8000 65 | 61 | 50.
+static int ce_tile(int64_t M, int64_t N, int64_t K)
 {
     auto tiles = [&](int64_t bm, int64_t bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
+    const double kt = (double)(K / 32);
     const int64_t t128 = tiles(128, 128), rest = t128 % 512;
-    const double c0 = (double)((tiles(256, 256) + 255) / 256), c1 = 0.68 * (double)((tiles(128, 256) + 255) / 256);
-    const double c2 = 0.8 * (double)(t128 / 512) + (rest == 0 ? 0.0 : rest <= 256 ? 0.44 : 0.8);
+    const double two = 1.5 + 0.55 * kt, one = 1.5 + 0.31 * kt;
+    const double c0 = (double)((tiles(256, 256) + 255) / 256) * (8.5 + 0.77 * kt), c1 = (double)((tiles(128, 256) + 255) / 256) * (6.0 + 0.53 * kt);
+    const double c2 = (double)(t128 / 512) * two + (rest == 0 ? 0.0 : rest <= 256 ? one : two);
     return c0 <= c1 && c0 <= c2 ? 0 : c1 < c2 ? 1 : 2;
 }
 // The gradient's tile: its contraction is cut until the chip is full, so what counts is the part of a tile that is used.
@@ -399,7 +423,7 @@ static size_t ce_plan(CeArgs& c, int64_t piece, char* base)
         if (parts > c.Vp / 512) parts = c.Vp / 512;
         c.few_parts = (int)(parts < 1 ? 1 : parts);
     }
-    c.tile = c.few_parts ? 2 : ce_tile(c.T, c.piece);         // (few rows: M and S of 64 columns, as of such a tile's waves)
+    c.tile = c.few_parts ? 2 : ce_tile(c.T, c.piece, c.Hp);         // (few rows: M and S of 64 columns, as of such a tile's waves)
     c.grad_tile = ce_grad_tile(c.T, c.H);
     const int bm = tile_rows(c.grad_tile), bn = tile_cols(c.grad_tile), sc = stat_cols(c.tile);
     const int64_t tiles_n = (c.H + bn - 1) / bn;
