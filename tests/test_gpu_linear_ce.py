@@ -205,6 +205,107 @@ def test_captured_and_replayed():
             assert torch.equal(got, want[k]), k
 
 
+@pytest.mark.parametrize("T,V,H,piece", [(30, 700, 64, 0), (30, 700, 64, 256), (200, 700, 64, 0), (200, 900, 64, 512)])
+def test_no_row_counts(T, V, H, piece):
+    """All rows left out, in each form, and then a call whose rows count on the same workspace."""
+    p = Head(T, V, H, "f16", seed=40)
+    hw = heads(p.w)
+    ws = B.new_workspace(max(B.sasq_linear_ce_workspace(T, V, H, g, piece) for g in (False, True)))
+    ws.fill_(0xFF)
+    t = torch.full((T,), -1, dtype=torch.int32, device="cuda")
+    for targets in (t, p.t.cuda(), t):
+        for dx in (None, torch.full((T, H), 5.0, dtype=torch.float16, device="cuda")):
+            loss, lse, mean = (torch.full((n,), 5.0, device="cuda") for n in (T, T, 1))
+            B.sasq_linear_ce(p.x.cuda(), hw[0], targets, loss, V, ws, lse=lse, mean=mean, dx=dx, head_grad=hw[1], piece=piece)
+            out = {"loss": loss, "lse": lse, "mean": mean, "dx": dx}
+            if targets is t:
+                assert all(v is None or not v.any() for v in out.values())
+            else:
+                check(out, p.reference())
+
+
+def test_two_graphs_on_one_workspace():
+    """Graphs of two sizes that share a workspace, replayed in turn."""
+    a, b = Head(20, 700, 64, "f16", seed=41), Head(150, 700, 64, "f16", seed=42)
+    b.w = a.w
+    hw = heads(a.w)
+    ws = B.new_workspace(max(B.sasq_linear_ce_workspace(n, 700, 64, True) for n in (20, 150)))
+    graphs = []
+    for p in (a, b):
+        x, t, loss, mean, dx = p.x.cuda(), p.t.cuda(), torch.empty(p.T, device="cuda"), torch.empty(1, device="cuda"), torch.empty(p.T, 64, dtype=torch.float16, device="cuda")
+        run = lambda x=x, t=t, loss=loss, mean=mean, dx=dx: B.sasq_linear_ce(x, hw[0], t, loss, 700, ws, mean=mean, dx=dx, head_grad=hw[1])
+        run()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            run()
+        graphs.append((g, {"loss": loss, "mean": mean, "dx": dx}, p.reference(), x))
+    for _ in range(3):
+        for g, out, ref, _x in graphs:
+            for v in out.values():
+                v.fill_(math.nan)
+            g.replay()
+            torch.cuda.synchronize()
+            check(out, ref)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_a_row_that_is_not_finite(dtype):
+    """A NaN or an infinity in a counted row's x stays in that row (and in the mean)."""
+    for T in (20, 90):
+        p = Head(T, 600, 64, dtype, seed=43)
+        ref = p.reference(row_weight=torch.ones(T))
+        x = p.x.clone()
+        x[3, 5], x[11, 0] = math.nan, math.inf
+        p.x = x
+        out = call(p, row_weight=torch.ones(T))
+        ok = torch.ones(T, dtype=torch.bool)
+        ok[3] = ok[11] = False
+        assert not torch.isfinite(out["loss"][3]) and not torch.isfinite(out["mean"]).any()
+        for k in ("loss", "lse", "dx"):
+            v, (want, tol) = out[k].cpu().double(), ref[k]
+            assert ((v - want).abs() <= tol)[ok].all(), k
+
+
+@pytest.mark.parametrize("T,V", [(40, 300), (130, 300)])
+def test_equal_logits_and_one_column(T, V):
+    """Zero heads: all logits equal, loss ln V; a vocabulary of one entry: loss 0 and no gradient."""
+    p = Head(T, V, 64, "bf16", seed=44)
+    p.w = torch.zeros_like(p.w)
+    check(call(p), p.reference())
+    q = Head(T, 1, 64, "bf16", seed=45)
+    out = call(q)
+    assert not out["loss"].any() and not out["dx"].any()
+
+
+def test_a_long_vocabulary_and_row():
+    """Offsets past 2^31 bytes in the head's layouts: entries and channels at the far end are those of a small head that holds them alone."""
+    V, H, T = 300000, 4096, 3                                     # 2.4 GB a layout
+    g = torch.Generator(device="cuda").manual_seed(1)
+    w = torch.zeros((V, H), dtype=torch.bfloat16, device="cuda")
+    part = torch.randn((1000, H), generator=g, device="cuda").mul_(1 / 64).to(torch.bfloat16)
+    w[-1000:] = part
+    hl, hg = (torch.empty(B.sasq_head_bytes(V, H, f), dtype=torch.uint8, device="cuda") for f in (0, 1))
+    B.sasq_prepare_head(w, hl, 0)
+    B.sasq_prepare_head(w, hg, 1)
+    del w
+    x = torch.randn((T, H), generator=g, device="cuda").to(torch.bfloat16)
+    t = torch.tensor([V - 1, V - 1000, V - 7], dtype=torch.int32, device="cuda")
+    loss, dx = torch.empty(T, device="cuda"), torch.empty_like(x)
+    z = x.double() @ part.double().t()
+    at = (t.long() - (V - 1000))[:, None]
+    lse = torch.logsumexp(torch.cat((z, torch.full((T, 1), math.log(V - 1000), dtype=torch.float64, device="cuda")), 1), 1, keepdim=True)
+    want = (lse - z.gather(1, at))[:, 0]
+    p = (z - lse).exp()
+    grad = (p.scatter_add(1, at, torch.full_like(at, -1.0, dtype=torch.float64)) @ part.double()) / T
+    for piece in (0, 131072):
+        B.sasq_linear_ce(x, hl, t, loss, V, B.new_workspace(B.sasq_linear_ce_workspace(T, V, H, True, piece)), dx=dx, head_grad=hg, piece=piece)
+        # fp32 sums of 300000 terms, of which 299000 are equal: 2^-24 of the sum a term at most, and 2 H 2^-24 sum |x w| of the logits, 100 for these
+        assert ((loss.double() - want).abs() <= 2 * 2 * H * 2.0 ** -24 * 100 + V * 2.0 ** -24).all()
+        bound = 2.0 ** -8 * grad.abs() + 2.0 ** -8 * (p @ part.double().abs()) / T * 2 + 0.07 * (grad.abs() + (p @ part.double().abs()) / T)
+        assert ((dx.double() - grad).abs() <= bound + 1e-9).all()
+
+
 def test_other_stream():
     p = Head(128, 3000, 256, "f16", seed=30)
     want = call(p)
