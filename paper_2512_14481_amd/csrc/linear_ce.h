@@ -34,7 +34,7 @@ struct CeArgs {
     int Hp, Vp;                                 // H and V in whole multiples of 64
     int piece, first_piece;                     // columns of a piece, and of the first
     int slots, max_splits;                      // parts that its contraction is cut into: as many as fill the slots of the chip (splits_of)
-    int tile, grad_tile;                        // 0: 256x256, 1: 128x256 (logits), 2: 128x128
+    int tile, grad_tile;                        // 0: 256x256, 2: 128x128
     bool grad;
     int few_parts;                              // few rows (linear_ce_few.hip): parts of the gradient's contraction, 0: the tiles
     // operands
@@ -69,7 +69,7 @@ __host__ __device__ inline int splits_of(int64_t rows, int bm, int tiles_n, int 
     return (int)(s < 1 ? 1 : s > max_splits ? max_splits : s);
 }
 constexpr int tile_rows(int tile) { return tile == 0 ? 256 : 128; }
-constexpr int tile_cols(int tile) { return tile == 2 ? 128 : 256; }
+constexpr int tile_cols(int tile) { return tile_rows(tile); }
 constexpr int stat_cols(int tile) { return tile == 2 ? 64 : 128; }     // half a tile's columns: what a wave has
 
 // Blocks from one row of blocks to the next, of `cols` columns (a multiple of 64): an odd number.

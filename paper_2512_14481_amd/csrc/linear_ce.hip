@@ -390,18 +390,18 @@ static void ce_pieces(int64_t T, int64_t V, int64_t piece, bool grad, int& cols,
 }
 
 // The logits' tile, by the time of its rounds of 256 workgroups (of 128x128 tiles a CU holds two): what a tile takes to start and for its epilogue, and its K
-// tiles.  us, whole call without the gradient, 256x256 | 128x256 | 128x128, T x H -> V: 128 x 4096 -> 32000 103 | 93 | 75, 200 rows 109 | 90 | 98, 333
-// 121 | 139 | 125, 512 123 | 146 | 164, 2048 430 | 499 | 523, 711 x 5120 -> 32000 238 | 246 | 269, 333 x 1376 -> 100003 165 | 147 | 138, 1500 x 1024 ->
-// 50000 196 | 211 | 192, 3000 x 512 -> 8000 65 | 61 | 50.
+// tiles.  us, whole call without the gradient, 256x256 | 128x128, T x H -> V (a last round of few as halves): 128 x 4096 -> 32000 93 | 75, 200 rows 90 | 98,
+// 333 121 | 125, 512 123 | 164, 2048 430 | 523, 711 x 5120 -> 32000 210 | 269, 333 x 1376 -> 100003 165 | 138, 1500 x 1024 -> 50000 196 | 192, 3000 x
+// 512 -> 8000 65 | 50.  Tiles of 128x256 throughout were in front nowhere but where halves are them.
 static int ce_tile(int64_t M, int64_t N, int64_t K)
 {
     auto tiles = [&](int64_t bm, int64_t bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
     const double kt = (double)(K / 32);
-    const int64_t t128 = tiles(128, 128), rest = t128 % 512;
+    const int64_t t256 = tiles(256, 256), tail = t256 % 256, t128 = tiles(128, 128), rest = t128 % 512;
     const double two = 1.5 + 0.55 * kt, one = 1.5 + 0.31 * kt;
-    const double c0 = (double)((tiles(256, 256) + 255) / 256) * (8.5 + 0.77 * kt), c1 = (double)((tiles(128, 256) + 255) / 256) * (6.0 + 0.53 * kt);
+    const double c0 = ((double)(t256 / 256) + (tail == 0 ? 0.0 : tail <= 128 ? 0.65 : 1.0)) * (8.5 + 0.77 * kt);
     const double c2 = (double)(t128 / 512) * two + (rest == 0 ? 0.0 : rest <= 256 ? one : two);
-    return c0 <= c1 && c0 <= c2 ? 0 : c1 < c2 ? 1 : 2;
+    return c0 <= c2 ? 0 : 2;
 }
 // The gradient's tile: its contraction is cut until the chip is full, so what counts is the part of a tile that is used.
 static int ce_grad_tile(int64_t M, int64_t N)

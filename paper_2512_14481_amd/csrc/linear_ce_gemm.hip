@@ -131,6 +131,18 @@ struct LogitsExt {
     }
 };
 
+// The tile of number `logical` in the order of tile_of_block.
+__device__ __forceinline__ void tile_at(int logical, int tiles_m, int tiles_n, int& tm, int& tn)
+{
+    constexpr int PN = 4;
+    const int panel = logical / (tiles_m * PN), in = logical - panel * tiles_m * PN, width = min(PN, tiles_n - panel * PN);
+    tm = in / width;
+    tn = panel * PN + in % width;
+}
+
+// Tiles of 256x256 come in rounds of 256 workgroups; a last round of at most 128 goes as twice as many tiles of 128 rows, which take 0.65 of a round.
+constexpr int kHalvesTo = 128;
+
 template <int DT, int BM, int BN, bool GRAD>
 __global__ __launch_bounds__(kGemmThreads)
 __attribute__((amdgpu_waves_per_eu(Tile<BM, BN>::kWavesPerSimd, Tile<BM, BN>::kWavesPerSimd)))
@@ -138,9 +150,28 @@ void ce_logits_kernel(const uint16_t* __restrict__ xs, const uint8_t* __restrict
                       int tiles_n, LogitsExt<DT, GRAD> ext)
 {
     __shared__ __attribute__((aligned(1024))) char lds[kStages * Tile<BM, BN>::kStageBytes];
-    const int M = *count;
+    const int M = *count, tiles_m = (M + BM - 1) / BM;
     int tm, tn;
-    if (!tile_of_counted((M + BM - 1) / BM, tiles_n, tm, tn)) return;
+    if constexpr (BM == 256) {
+        const int total = tiles_m * tiles_n, tail = total % 256, whole = total - tail;
+        if (tail && tail <= kHalvesTo) {
+            const int id = (int)blockIdx.x - whole, per = ((id < 0 ? whole : 2 * tail) + 7) >> 3, at = id < 0 ? (int)blockIdx.x : id;
+            const int logical = (at & 7) * per + (at >> 3);
+            if (at >> 3 >= per || (id >= 0 && logical >= 2 * tail)) return;
+            tile_at(id < 0 ? logical : whole + logical / 2, tiles_m, tiles_n, tm, tn);
+            if (id >= 0) {
+                tm = 2 * tm + (logical & 1);
+                if (tm * 128 < M)
+                    gemm_k64_body<DT, KW_I8B, 128, BN, false, GR_NONE, 1, LogitsExt<DT, GRAD>>(
+                        reinterpret_cast<const int8_t*>(xs), head, nullptr, nullptr, nullptr, nullptr, nullptr, M, V, Hp * 2, tm, ext.col0 / BN + tn, lds, 0, ext);
+                return;
+            }
+        } else if (!tile_of_counted(tiles_m, tiles_n, tm, tn)) {
+            return;
+        }
+    } else if (!tile_of_counted(tiles_m, tiles_n, tm, tn)) {
+        return;
+    }
     gemm_k64_body<DT, KW_I8B, BM, BN, false, GR_NONE, 1, LogitsExt<DT, GRAD>>(
         reinterpret_cast<const int8_t*>(xs), head, nullptr, nullptr, nullptr, nullptr, nullptr, M, V, Hp * 2, tm, ext.col0 / BN + tn, lds, 0, ext);
 }
@@ -231,7 +262,7 @@ template <int DT, int BM, int BN>
 static void launch_logits(const CeArgs& c, int64_t col0, int64_t cols, hipStream_t st)
 {
     const int tiles_m = (int)((c.T + BM - 1) / BM), tiles_n = (int)((cols + BN - 1) / BN);
-    const int grid = ((tiles_m * tiles_n + 7) / 8) * 8;
+    const int grid = ((tiles_m * tiles_n + 7) / 8) * 8 + (BM == 256 ? kHalvesTo + 8 : 0);
     auto go = [&](auto grad_tag) {
         constexpr bool GRAD = decltype(grad_tag)::value;
         const LogitsExt<DT, GRAD> ext{row_blocks(c.Hp), row_blocks(c.Hp), c.tgt, c.zt, GRAD && col0 ? c.run : nullptr, c.stats, c.T, c.a, row_blocks(c.piece), (int)col0};
@@ -253,30 +284,25 @@ static void launch_grad(const CeArgs& c, int64_t col0, int64_t cols, hipStream_t
         c.a, c.head_grad, c.count, (int)c.H, c.Hp, (int)((cols + 63) / 64), (int)(col0 / 32), tiles_n, c.slots, c.max_splits, ext);
 }
 
-template <int DT, typename Go>
-static void by_tile(int tile, Go&& go)
+template <typename Go>
+static void by_type_and_tile(sasq_dtype dt, int tile, Go&& go)
 {
-    if (tile == 0)      go(std::integral_constant<int, DT>{}, std::integral_constant<int, 256>{}, std::integral_constant<int, 256>{});
-    else if (tile == 1) go(std::integral_constant<int, DT>{}, std::integral_constant<int, 128>{}, std::integral_constant<int, 256>{});
-    else                go(std::integral_constant<int, DT>{}, std::integral_constant<int, 128>{}, std::integral_constant<int, 128>{});
+    auto by_tile = [&](auto d) {
+        if (tile == 0) go(d, std::integral_constant<int, 256>{});
+        else           go(d, std::integral_constant<int, 128>{});
+    };
+    if (dt == SASQ_F16) by_tile(std::integral_constant<int, SASQ_F16>{});
+    else                by_tile(std::integral_constant<int, SASQ_BF16>{});
 }
 
 void launch_ce_logits(const CeArgs& c, sasq_dtype dt, int64_t col0, int64_t cols, hipStream_t st)
 {
-    auto go = [&](auto d, auto bm, auto bn) { launch_logits<decltype(d)::value, decltype(bm)::value, decltype(bn)::value>(c, col0, cols, st); };
-    if (dt == SASQ_F16) by_tile<SASQ_F16>(c.tile, go);
-    else                by_tile<SASQ_BF16>(c.tile, go);
+    by_type_and_tile(dt, c.tile, [&](auto d, auto b) { launch_logits<decltype(d)::value, decltype(b)::value, decltype(b)::value>(c, col0, cols, st); });
 }
 
 void launch_ce_grad(const CeArgs& c, sasq_dtype dt, int64_t col0, int64_t cols, hipStream_t st)
 {
-    auto go = [&](auto d, auto bm, auto bn) { launch_grad<decltype(d)::value, decltype(bm)::value, decltype(bn)::value>(c, col0, cols, st); };
-    auto by_size = [&](auto d) {
-        if (c.grad_tile == 0) go(d, std::integral_constant<int, 256>{}, std::integral_constant<int, 256>{});
-        else                  go(d, std::integral_constant<int, 128>{}, std::integral_constant<int, 128>{});
-    };
-    if (dt == SASQ_F16) by_size(std::integral_constant<int, SASQ_F16>{});
-    else                by_size(std::integral_constant<int, SASQ_BF16>{});
+    by_type_and_tile(dt, c.grad_tile, [&](auto d, auto b) { launch_grad<decltype(d)::value, decltype(b)::value, decltype(b)::value>(c, col0, cols, st); });
 }
 
 }  // namespace sasq

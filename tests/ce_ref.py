@@ -30,14 +30,14 @@ class Head:
         out = torch.rand(T, generator=g) < left_out
         self.t = torch.where(out, torch.where(torch.arange(T) % 2 == 0, -100, V + 3), t).to(torch.int32)
 
-    def reference(self, row_weight=None, scale=1.0):
+    def reference(self, row_weight=None, scale=1.0, device="cpu"):
         """{name: (values, tolerance)}, in 64 bits."""
-        x, w, T, V, H = self.x.double(), self.w.double(), self.T, self.V, self.H
-        rows = ((self.t >= 0) & (self.t < V)).nonzero()[:, 0]
-        zero = lambda *s: torch.zeros(s, dtype=torch.float64)
+        x, w, T, V, H = self.x.to(device).double(), self.w.to(device).double(), self.T, self.V, self.H
+        rows = ((self.t.to(device) >= 0) & (self.t.to(device) < V)).nonzero()[:, 0]
+        zero = lambda *s: torch.zeros(s, dtype=torch.float64, device=device)
         loss, lse, dx, e_loss, e_lse, e_dx = zero(T), zero(T), zero(T, H), zero(T), zero(T), zero(T, H)
         if len(rows):
-            t, xr, i = self.t[rows].long(), x[rows], torch.arange(len(rows))
+            t, xr, i = self.t.to(device)[rows].long(), x[rows], torch.arange(len(rows), device=device)
             z, u32 = xr @ w.t(), 2.0 ** -24
             ez = 2 * H * u32 * (xr.abs() @ w.abs().t()).amax(1)
             zt = z[i, t]
@@ -51,7 +51,7 @@ class Head:
             e_loss[rows] = u * ed * 1.01 + u32 * loss[rows] + 1e-30
             e_lse[rows] = ed + u32 * lse[rows].abs()
             q = torch.softmax(z, 1).nan_to_num(0.0)
-            g = scale * (torch.full((T,), 1.0 / len(rows), dtype=torch.float64) if row_weight is None else row_weight.double())[rows, None]
+            g = scale * (torch.full((T,), 1.0 / len(rows), dtype=torch.float64, device=device) if row_weight is None else row_weight.to(device).double())[rows, None]
             eps = HALF[self.dtype]
             dx[rows] = g * u[:, None] * (q @ w - w[t])
             rel = (eps + 2 * (2 * ez + 2.0 ** -20) + 2 * V * u32)[:, None]
@@ -68,7 +68,7 @@ def check(got, ref, names=None):
         if value is None:
             continue
         want, tol = ref[name]
-        v = value.detach().cpu().double().view(want.shape)
+        v = value.detach().to(want.device).double().view(want.shape)
         off = (v - want).abs()
         bad = ~(off <= tol)
         assert not bad.any(), (name, int(bad.sum()), "of", bad.numel(), "first", bad.nonzero()[0].tolist(), v[bad][:3].tolist(), want[bad][:3].tolist(),

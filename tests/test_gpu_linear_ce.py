@@ -50,6 +50,14 @@ def test_sizes(T, V, H, dtype):
     check(call(p, scale=scale), p.reference(scale=scale))
 
 
+@pytest.mark.parametrize("dtype,left_out,grad", [("f16", 0.0, True), ("bf16", 0.55, True), ("f16", 0.2, False)])
+@pytest.mark.parametrize("T,V,H", [(520, 9000, 4096), (1100, 16001, 4096), (2100, 9000, 2048), (129, 33000, 1024), (3000, 24000, 320)])
+def test_large_tiles(T, V, H, dtype, left_out, grad):
+    """256x256 tiles, whole rounds and last rounds as halves, by the rows that count; contractions cut into parts; several pieces (the definition on the device)."""
+    p = Head(T, V, H, dtype, seed=T, left_out=left_out)
+    check(call(p, grad=grad, scale=256.0), p.reference(scale=256.0, device="cuda"))
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("T,V,H", [(1, 1, 1), (16, 1000, 256), (300, 5000, 640)])
 def test_without_gradient(T, V, H, dtype):
