@@ -458,12 +458,12 @@ int sasq_linear_bwd_input(const void* dy, const void* wt, void* dx, float* acc_o
  *   targets    [T] device int32;  row_weight  [T] device fp32 or NULL;  scale: a factor on the gradient (loss scaling), 1 otherwise
  *   loss       [T] device fp32, written;  lse  [T] device fp32 or NULL, written;  mean  device fp32 scalar or NULL, written
  *   dx         [T, H] device 16-bit `dt`, rows dx_stride apart, written, or NULL: no gradient; may be x itself (with its stride)
- *   T, V       at most 2^23;  H at most 2^20;  any sizes, multiples of 64 of H cost nothing extra
+ *   T at most 2^23, V 2^22, H 2^20;  any sizes, multiples of 64 of H cost nothing extra
  *   piece      columns of the vocabulary at a time, a multiple of 256, or 0: the library's choice (256 MB of the workspace)
  *   workspace  >= sasq_linear_ce_workspace(T, V, H, dx != NULL, piece) bytes, 16-byte aligned; needs no initialisation
  * Sums are fp32, those over a row's losses fp64; the exponentials that the gradient contracts with W are rounded to 16 bits, relative to the
  * largest of their row but for the target's, which is kept apart: rows whose target is all but certain lose nothing.  Results do not change from
- * run to run.  Logits must be finite.
+ * run to run.  Logits must be finite and less than 2^24 in size.
  *
  * sasq_prepare_head lays W [V, H] (16-bit, rows w_stride elements apart) out for the two products, once for a head: 1 KB blocks of 16 rows x 32
  * columns as in sasq_prepare_bwd_weight, rows v and columns h (SASQ_HEAD_LOGITS), or rows h and columns v (SASQ_HEAD_GRAD), the columns padded to

@@ -18,8 +18,8 @@
 
 namespace sasq {
 
-constexpr float kLog2e = 1.44269504088896340736f, kLog2eLow = 1.92596299112661746887e-8f;    // their sum is log2(e) to 49 bits
-constexpr float kLn2 = 0.693147180559945309417f;
+// (off by 2^-26 of itself: of a logit z, its exponential is off by 2^-26 |z|, less than the product that z is)
+constexpr float kLog2e = 1.44269504088896340736f;
 
 // 16-bit a_v of a wave's own M are at most 2^kTopExp; those of the row's M so far may be 2^kRoom times as much.  fp16 has 2^-24 .. 2^15 to offer, bf16 the
 // exponents of fp32.

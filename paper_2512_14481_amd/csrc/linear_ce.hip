@@ -6,8 +6,8 @@
 
 namespace sasq {
 
-constexpr int64_t kCeMaxTokens = INT64_C(1) << 23, kCeMaxVocab = INT64_C(1) << 23, kCeMaxHidden = INT64_C(1) << 20;
-constexpr int64_t kCeMaxProduct = INT64_C(1) << 37;                 // elements of x and of the head
+constexpr int64_t kCeMaxTokens = INT64_C(1) << 23, kCeMaxVocab = INT64_C(1) << 22, kCeMaxHidden = INT64_C(1) << 20;
+constexpr int64_t kCeMaxProduct = INT64_C(1) << 37;                 // elements of x, of the head, and of a piece of the logits
 constexpr int kPieceStep = 256;
 
 static int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
@@ -302,7 +302,7 @@ __global__ __launch_bounds__(256) void ce_scale_kernel(uint16_t* __restrict__ a,
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
             if (k + 4 * j >= k1) break;
-            const float s = exp2f(f[j] - m);
+            const float s = exp2f(fminf(f[j] - m, 0.0f));      // (a group of nothing but the target has no M, and zeros)
             u32x4 o;
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[e] = S::pack(S::lo(v[j][e]) * s, S::hi(v[j][e]) * s);
@@ -464,7 +464,7 @@ static size_t ce_plan(CeArgs& c, int64_t piece, char* base)
 static bool ce_sizes_ok(int64_t T, int64_t V, int64_t H, int64_t piece)
 {
     return T > 0 && V > 0 && H > 0 && T <= kCeMaxTokens && V <= kCeMaxVocab && H <= kCeMaxHidden && up(H, 64) <= kCeMaxProduct / T &&
-           up(H, 64) <= kCeMaxProduct / V && piece >= 0 && piece % kPieceStep == 0;
+           up(H, 64) <= kCeMaxProduct / V && piece >= 0 && piece % kPieceStep == 0 && (piece < V ? piece : V) <= kCeMaxProduct / T;
 }
 
 template <int DT>

@@ -179,7 +179,7 @@ __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(MB 
     for (int b = 0; b < MB; ++b) m[b] = run[min(16 * b + frow, T - 1)].m;
     auto load = [&](int b, int k) {
         const u32x4 v = *reinterpret_cast<const u32x4*>(a + block_at(16 * b + frow, k * 32 + 8 * fq, a_kt));
-        const float f = exp2f(stats[(int64_t)(k >> 1) * T + min(16 * b + frow, T - 1)].m - m[b]);
+        const float f = exp2f(fminf(stats[(int64_t)(k >> 1) * T + min(16 * b + frow, T - 1)].m - m[b], 0.0f));     // (a group of nothing but the target has no M)
         u32x4 o;
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] = S::pack(S::lo(v[e]) * f, S::hi(v[e]) * f);

@@ -59,7 +59,7 @@ def test_large_tiles(T, V, H, dtype, left_out, grad):
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
-@pytest.mark.parametrize("T,V,H", [(1, 1, 1), (16, 1000, 256), (300, 5000, 640)])
+@pytest.mark.parametrize("T,V,H", [(1, 1, 1), (16, 1000, 256), (50, 700, 64), (300, 5000, 640)])
 def test_without_gradient(T, V, H, dtype):
     p = Head(T, V, H, dtype, seed=3, left_out=0.2)
     check(call(p, grad=False), p.reference())
@@ -273,6 +273,17 @@ def test_a_row_that_is_not_finite(dtype):
         for k in ("loss", "lse", "dx"):
             v, (want, tol) = out[k].cpu().double(), ref[k]
             assert ((v - want).abs() <= tol)[ok].all(), k
+
+
+@pytest.mark.parametrize("T,V,piece", [(20, 65, 0), (20, 257, 256), (100, 257, 0), (100, 129, 0)])
+def test_low_logits_and_a_group_of_the_target_alone(T, V, piece):
+    """All logits about -150, and the target alone behind the last whole group of columns: it is in no sum, and its group has no maximum of its own."""
+    p = Head(T, V, 64, "bf16", seed=46, sure=0.0)
+    p.w = (p.w.float() - 150.0 / 64).to(torch.bfloat16)
+    p.x = (1.0 + 0.05 * p.x.float()).to(torch.bfloat16)
+    p.t[::2] = V - 1
+    assert p.reference()["lse"][0].max() < -100
+    check(call(p, piece=piece), p.reference())
 
 
 @pytest.mark.parametrize("T,V", [(40, 300), (130, 300)])
