@@ -37,6 +37,7 @@ struct CeArgs {
     int tile, grad_tile;                        // 0: 256x256, 2: 128x128
     bool grad;
     int few_parts;                              // few rows (linear_ce_few.hip): parts of the gradient's contraction, 0: the tiles
+    bool few_own_join;                          // and so few groups of columns that the gradient's kernels join them by themselves
     // operands
     const void* x; int64_t x_stride;
     const uint8_t* head; const uint8_t* head_grad;
@@ -85,7 +86,8 @@ void launch_ce_logits(const CeArgs& c, sasq_dtype dt, int64_t col0, int64_t cols
 void launch_ce_grad(const CeArgs& c, sasq_dtype dt, int64_t col0, int64_t cols, hipStream_t st);
 
 // At most kFewRows rows, the whole vocabulary in one piece (linear_ce_few.hip).  M and S are of kFewCols columns; rows are not packed.
-constexpr int kFewRows = 64, kFewCols = 64;
+// kFewOwnJoin: up to so many M and S in all, every workgroup of the gradient reads them and the join is no kernel of its own (64 x 256 -> 1000 22.8 -> 18.8 us).
+constexpr int kFewRows = 64, kFewCols = 64, kFewOwnJoin = 4096;
 void launch_ce_few_logits(const CeArgs& c, sasq_dtype dt, hipStream_t st);
 void launch_ce_few_grad(const CeArgs& c, sasq_dtype dt, hipStream_t st);
 

@@ -158,9 +158,23 @@ __global__ __launch_bounds__(256) void ce_stage_kernel(const uint16_t* __restric
 }
 
 // ---- between the products: M and S of each row so far ----
-// 16 rows a workgroup, 64 threads a row, each for every 64th group of columns, eight of them requested at a time.  All factors are exact powers of two.
+// ROWS rows a workgroup, 1024 / ROWS threads a row, eight groups of columns requested at a time by each.  16 rows, whose M and S are whole cache lines, or 4
+// where a row has many groups (333 x 1376 -> 100003, 1564 groups, 16 | 4 rows: 15.0 | 10.8 us).  All factors are exact powers of two.
 // targets: rows are not packed, and some of the T may be left out; NULL: they are, and *count of them are there.
-constexpr int kJoinRows = 16, kJoinLanes = 64, kJoinThreads = kJoinRows * kJoinLanes, kJoinAhead = 8;
+constexpr int kJoinThreads = 1024, kJoinAhead = 8, kJoinManyGroups = 512;
+
+struct RowEnd { float loss, lse, u, coef; };
+// What M and S over the others and z of the target make of a row, in fp64: a small loss is the exponential of a difference.
+__device__ __forceinline__ RowEnd row_end(float m, float s, float zt)
+{
+    const double z = (double)zt;
+    const double d = s == 0.0f ? -(double)__builtin_inff() : ((double)m + log2((double)s)) * 0.69314718055994530942 - z;
+    const double ex = exp(-fabs(d)), over = 1.0 / (1.0 + ex);
+    const double l = fmax(d, 0.0) + log1p(ex), u = d > 0.0 ? over : ex * over;
+    return RowEnd{(float)l, (float)(z + l), (float)u, s == 0.0f ? 0.0f : (float)(u / (double)s)};
+}
+
+template <int ROWS>
 __global__ __launch_bounds__(kJoinThreads) void ce_join_kernel(const RowStat* __restrict__ stats, int groups, int64_t T, const int32_t* __restrict__ count,
                                                               RowStat* __restrict__ run, float* __restrict__ beta, uint8_t* __restrict__ scale_rows,
                                                               const float* __restrict__ zt, const int32_t* __restrict__ row, float* __restrict__ coef,
@@ -168,7 +182,7 @@ __global__ __launch_bounds__(kJoinThreads) void ce_join_kernel(const RowStat* __
                                                               float* __restrict__ mean, double* __restrict__ part_loss, uint32_t* __restrict__ ticket,
                                                               const int32_t* __restrict__ targets, int V, int first, int last)
 {
-    constexpr int kWaves = kJoinThreads / kWave;
+    constexpr int kJoinRows = ROWS, kJoinLanes = kJoinThreads / ROWS, kWaves = kJoinThreads / kWave;
     __shared__ float part[kWaves][kJoinRows];
     __shared__ double row_loss[kJoinRows];
     __shared__ bool is_last;
@@ -197,13 +211,14 @@ __global__ __launch_bounds__(kJoinThreads) void ce_join_kernel(const RowStat* __
         for (int j = 0; j < kJoinAhead; ++j)
             if (s[j].s != 0.0f) top = fmaxf(top, s[j].m);
     }
-    // a wave has four of a row's threads: they meet by shuffles, the waves in LDS
+    // a row's threads in a wave meet by shuffles, the waves in LDS
     const int wave = threadIdx.x / kWave;
     auto share = [&](float v) {
         if (threadIdx.x % kWave < kJoinRows) part[wave][r] = v;
     };
-    top = fmaxf(top, __shfl_xor(top, 16, kWave));
-    share(fmaxf(top, __shfl_xor(top, 32, kWave)));
+#pragma unroll
+    for (int o = ROWS; o < kWave; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
+    share(top);
     __syncthreads();
     float m = old.s != 0.0f ? old.m : -__builtin_inff();
 #pragma unroll
@@ -220,8 +235,9 @@ __global__ __launch_bounds__(kJoinThreads) void ce_join_kernel(const RowStat* __
             other = other || (s[j].s != 0.0f && s[j].m != m);
         }
     }
-    sum += __shfl_xor(sum, 16, kWave);
-    share(sum + __shfl_xor(sum, 32, kWave));
+#pragma unroll
+    for (int o = ROWS; o < kWave; o <<= 1) sum += __shfl_xor(sum, o, kWave);
+    share(sum);
     const int any = __syncthreads_or(other && p < n);
     if (scale_rows && threadIdx.x == 0) scale_rows[blockIdx.x] = any != 0;
     if (k == 0 && p < n) {
@@ -232,17 +248,13 @@ __global__ __launch_bounds__(kJoinThreads) void ce_join_kernel(const RowStat* __
         run[p] = RowStat{m, all};
         beta[p] = f;
         if (last) {
-            // In fp64: a small loss is the exponential of a difference.
             const bool counts = !targets || (target >= 0 && target < V);
-            const double z = (double)target_z;
-            const double d = all == 0.0f ? -(double)__builtin_inff() : ((double)m + log2((double)all)) * 0.69314718055994530942 - z;
-            const double ex = exp(-fabs(d)), over = 1.0 / (1.0 + ex);
-            const double l = fmax(d, 0.0) + log1p(ex), u = d > 0.0 ? over : ex * over;
-            loss[to] = counts ? (float)l : 0.0f;
-            if (lse) lse[to] = counts ? (float)(z + l) : 0.0f;
-            u_out[p] = (float)u;
-            coef[p] = all == 0.0f ? 0.0f : (float)(u / (double)all);
-            row_loss[r] = counts ? (double)(float)l : 0.0;
+            const RowEnd end = row_end(m, all, target_z);
+            loss[to] = counts ? end.loss : 0.0f;
+            if (lse) lse[to] = counts ? end.lse : 0.0f;
+            u_out[p] = end.u;
+            coef[p] = end.coef;
+            row_loss[r] = counts ? (double)end.loss : 0.0;
         }
     } else if (k == 0) {
         row_loss[r] = 0.0;
@@ -278,12 +290,15 @@ __global__ __launch_bounds__(kJoinThreads) void ce_join_kernel(const RowStat* __
 constexpr int kScaleBlocks = 64;
 template <int DT>
 __global__ __launch_bounds__(256) void ce_scale_kernel(uint16_t* __restrict__ a, int a_kt, int kt, int stat_blocks, const RowStat* __restrict__ stats,
-                                                      const RowStat* __restrict__ run, const uint8_t* __restrict__ scale_rows, int64_t T,
+                                                      const RowStat* __restrict__ run, const uint8_t* __restrict__ scale_rows, int flags, int64_t T,
                                                       const int32_t* __restrict__ count)
 {
     using S = Store16<DT>;
     const int n = *count, r16 = (int)blockIdx.x;
-    if (r16 * 16 >= n || !scale_rows[r16]) return;
+    if (r16 * 16 >= n) return;
+    int any = 0;                                              // `flags` of the join's workgroups tell for sixteen rows
+    for (int f = r16 * flags; f < (r16 + 1) * flags && f * (16 / flags) < n; ++f) any |= scale_rows[f];
+    if (!any) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int p = min(r16 * 16 + (lane >> 2), n - 1);
     const float m = run[p].m;
@@ -311,20 +326,62 @@ __global__ __launch_bounds__(256) void ce_scale_kernel(uint16_t* __restrict__ a,
     }
 }
 
+// M, S and what follows of row r from the groups of columns of a single piece, by `each` threads of a wave next to each other (a power of two), of which this is
+// number i.
+__device__ __forceinline__ RowEnd few_row_end(const RowStat* __restrict__ stats, int groups, int T, int r, float zt, int i, int each)
+{
+    constexpr int kAhead = 4;
+    RowStat s[kAhead];
+    auto fetch = [&](int g0) {
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            s[j] = stats[(int64_t)min(g0 + j * each, groups - 1) * T + r];
+            if (g0 + j * each >= groups) s[j].s = 0.0f;
+        }
+    };
+    float m = -__builtin_inff(), sum = 0.0f;
+    for (int g0 = i; g0 < groups; g0 += each * kAhead) {
+        fetch(g0);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+            if (s[j].s != 0.0f) m = fmaxf(m, s[j].m);
+    }
+    for (int o = 1; o < each; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, kWave));
+    if (m == -__builtin_inff()) m = 0.0f;
+    for (int g0 = i; g0 < groups; g0 += each * kAhead) {
+        if (groups > each * kAhead) fetch(g0);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+            if (s[j].s != 0.0f) sum += s[j].s * exp2f(s[j].m - m);
+    }
+    for (int o = 1; o < each; o <<= 1) sum += __shfl_xor(sum, o, kWave);
+    return row_end(m, sum, zt);
+}
+
 // ---- the end: dx of every row; left-out ones are 0 ----
-template <int DT, bool VEC>
+// JOIN: few rows of few groups of columns, which no other kernel has joined: a workgroup does so for its row, the one more for all.
+template <int DT, bool VEC, bool JOIN>
 __global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ acc, int bm, int tiles_n, int slots, int max_splits, int few_parts, const int32_t* __restrict__ count,
                                                    const int32_t* __restrict__ pos, const int32_t* __restrict__ tgt, const float* __restrict__ coef,
                                                    const float* __restrict__ u, const uint8_t* __restrict__ head, const float* __restrict__ row_weight,
                                                    float scale, uint16_t* __restrict__ dx, int64_t stride, int H, int Hp, const float* __restrict__ loss,
-                                                   float* __restrict__ mean, int T, int V)
+                                                   float* __restrict__ mean, int T, int V, const RowStat* __restrict__ stats, int groups,
+                                                   const float* __restrict__ zt, float* __restrict__ loss_out, float* __restrict__ lse)
 {
     using S = Store16<DT>;
     const int r = (int)blockIdx.x;
     if (r == T) {                                 // a workgroup more: the mean, in fp64 and a fixed order
         __shared__ double part[4];
         double sum = 0.0;
-        for (int i = threadIdx.x; i < T; i += 256) sum += (double)loss[i];
+        if constexpr (JOIN) {
+            // (few rows: as many threads for each as there are)
+            const int each = T <= 4 ? 64 : T <= 8 ? 32 : T <= 16 ? 16 : T <= 32 ? 8 : 4, i = (int)threadIdx.x / each;
+            const int t = tgt[min(i, T - 1)];
+            const RowEnd end = few_row_end(stats, groups, T, min(i, T - 1), zt[min(i, T - 1)], (int)threadIdx.x % each, each);
+            if (i < T && t >= 0 && t < V && threadIdx.x % each == 0) sum = (double)end.loss;
+        } else {
+            for (int i = threadIdx.x; i < T; i += 256) sum += (double)loss[i];
+        }
         sum = wave_sum(sum);
         if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = sum;
         __syncthreads();
@@ -340,8 +397,16 @@ __global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ ac
         t = tgt[p];
         if (few_parts && (t < 0 || t >= V)) p = -1;
     }
-    if (p >= 0) {
-        g = scale * (row_weight ? row_weight[r] : 1.0f / (float)n);
+    if (p >= 0) g = scale * (row_weight ? row_weight[r] : 1.0f / (float)n);
+    if constexpr (JOIN) {
+        const RowEnd end = few_row_end(stats, groups, T, r, zt[r], (int)threadIdx.x % kWave, kWave);
+        if (threadIdx.x == 0) {
+            loss_out[r] = p >= 0 ? end.loss : 0.0f;
+            if (lse) lse[r] = p >= 0 ? end.lse : 0.0f;
+        }
+        cf = end.coef;
+        uu = end.u;
+    } else if (p >= 0) {
         cf = coef[p];
         uu = u[p];
     }
@@ -410,6 +475,8 @@ static int ce_grad_tile(int64_t M, int64_t N)
     return 0.8 * used(128, 128) > used(256, 256) ? 2 : 0;
 }
 
+static int ce_few_groups(const CeArgs& c) { return (int)((c.V + kFewCols - 1) / kFewCols); }
+
 // Sizes and the workspace's parts, from `base` (0: only how long they are).
 static size_t ce_plan(CeArgs& c, int64_t piece, char* base)
 {
@@ -417,11 +484,13 @@ static size_t ce_plan(CeArgs& c, int64_t piece, char* base)
     c.Vp = (int)up(c.V, 64);
     ce_pieces(c.T, c.V, piece, c.grad, c.piece, c.first_piece);
     c.few_parts = 0;
+    c.few_own_join = false;
     if (c.T <= kFewRows && c.piece >= c.V) {
         // as many workgroups as fill the chip twice, of 64 columns a wave at least
         int64_t parts = 512 / ((c.Hp + kFewCols - 1) / kFewCols);
         if (parts > c.Vp / 512) parts = c.Vp / 512;
         c.few_parts = (int)(parts < 1 ? 1 : parts);
+        c.few_own_join = c.grad && c.T * ce_few_groups(c) <= kFewOwnJoin;
     }
     c.tile = c.few_parts ? 2 : ce_tile(c.T, c.piece, c.Hp);         // (few rows: M and S of 64 columns, as of such a tile's waves)
     c.grad_tile = ce_grad_tile(c.T, c.H);
@@ -450,11 +519,11 @@ static size_t ce_plan(CeArgs& c, int64_t piece, char* base)
     part(c.beta, T * 4);
     part(c.coef, T * 4);
     part(c.u, T * 4);
-    part(c.part, T16 / 16 * 8);
+    part(c.part, (T + 3) / 4 * 8);
     part(c.stats, groups * T * 8);
     part(c.xs, T16 * row_blocks(c.Hp) * 64);
     if (c.grad) {
-        part(c.scale_rows, T16 / 16);
+        part(c.scale_rows, (T + 3) / 4);
         part(c.a, T16 * row_blocks(c.piece) * 64);
         part(c.acc, (size_t)sums * (size_t)c.Hp * 4);
     }
@@ -472,20 +541,31 @@ static void launch_dx(const CeArgs& c, hipStream_t st)
 {
     const int T = (int)c.T, H = (int)c.H, bm = tile_rows(c.grad_tile), tiles_n = (int)((c.H + tile_cols(c.grad_tile) - 1) / tile_cols(c.grad_tile));
     const bool vec = c.dx_stride % 8 == 0 && H % 8 == 0;
-    auto go = [&](auto v) {
-        ce_dx_kernel<DT, decltype(v)::value><<<T + (c.mean ? 1 : 0), 256, 0, st>>>(
+    auto go = [&](auto v, auto join) {
+        ce_dx_kernel<DT, decltype(v)::value, decltype(join)::value><<<T + (c.mean ? 1 : 0), 256, 0, st>>>(
             c.acc, bm, tiles_n, c.slots, c.max_splits, c.few_parts, c.count, c.pos, c.few_parts ? c.targets : c.tgt, c.coef, c.u, c.head, c.row_weight, c.scale,
-            static_cast<uint16_t*>(c.dx), c.dx_stride, H, c.Hp, c.loss, c.mean, T, (int)c.V);
+            static_cast<uint16_t*>(c.dx), c.dx_stride, H, c.Hp, c.loss, c.mean, T, (int)c.V, c.stats, ce_few_groups(c), c.zt, c.loss, c.lse);
     };
-    if (vec) go(std::true_type{});
-    else     go(std::false_type{});
+    auto by_join = [&](auto v) {
+        if (c.few_own_join) go(v, std::true_type{});
+        else                go(v, std::false_type{});
+    };
+    if (vec) by_join(std::true_type{});
+    else     by_join(std::false_type{});
 }
+
+static int join_rows(int groups) { return groups > kJoinManyGroups ? 4 : 16; }
 
 static void launch_join(const CeArgs& c, int groups, bool first, bool last, hipStream_t st)
 {
-    ce_join_kernel<<<(unsigned)((c.T + kJoinRows - 1) / kJoinRows), kJoinThreads, 0, st>>>(
-        c.stats, groups, c.T, c.count, c.run, c.beta, c.grad && !c.few_parts ? c.scale_rows : nullptr, c.zt, c.few_parts ? nullptr : c.row, c.coef, c.u, c.loss,
-        c.lse, c.grad ? nullptr : c.mean, c.part, c.ticket, c.few_parts ? c.targets : nullptr, (int)c.V, first, last);
+    auto go = [&](auto rows) {
+        constexpr int ROWS = decltype(rows)::value;
+        ce_join_kernel<ROWS><<<(unsigned)((c.T + ROWS - 1) / ROWS), kJoinThreads, 0, st>>>(
+            c.stats, groups, c.T, c.count, c.run, c.beta, c.grad && !c.few_parts ? c.scale_rows : nullptr, c.zt, c.few_parts ? nullptr : c.row, c.coef, c.u, c.loss,
+            c.lse, c.grad ? nullptr : c.mean, c.part, c.ticket, c.few_parts ? c.targets : nullptr, (int)c.V, first, last);
+    };
+    if (join_rows(groups) == 4) go(std::integral_constant<int, 4>{});
+    else                        go(std::integral_constant<int, 16>{});
 }
 
 template <int DT>
@@ -494,7 +574,7 @@ static void ce_run(const CeArgs& c, sasq_dtype dt, hipStream_t st)
     const int T = (int)c.T, H = (int)c.H;
     if (c.few_parts) {
         launch_ce_few_logits(c, dt, st);
-        launch_join(c, (int)((c.V + kFewCols - 1) / kFewCols), true, true, st);
+        if (!c.few_own_join) launch_join(c, ce_few_groups(c), true, true, st);
         if (c.grad) {
             launch_ce_few_grad(c, dt, st);
             launch_dx<DT>(c, st);
@@ -515,7 +595,7 @@ static void ce_run(const CeArgs& c, sasq_dtype dt, hipStream_t st)
         if (c.grad) {
             const int kt = (int)(up(cols, 64) / 32);
             ce_scale_kernel<DT><<<dim3((T + 15) / 16, (kt + kScaleBlocks - 1) / kScaleBlocks), 256, 0, st>>>(c.a, row_blocks(c.piece), kt, sc / 32, c.stats, c.run,
-                                                                                                             c.scale_rows, c.T, c.count);
+                                                                                                             c.scale_rows, 16 / join_rows(groups), c.T, c.count);
             launch_ce_grad(c, dt, col0, cols, st);
         }
         col0 += cols;

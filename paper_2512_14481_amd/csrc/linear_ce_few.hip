@@ -8,6 +8,7 @@
 #include "gemm_tile.h"
 #include "gemm_k64_body.h"
 #include "linear_ce.h"
+#include <limits.h>
 
 namespace sasq {
 
@@ -163,7 +164,7 @@ __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(MB 
 }
 
 // The gradient's sums over a part of the vocabulary; exponentials are brought to their row's M on the way.
-template <int DT, int MB>
+template <int DT, int MB, bool JOIN>
 __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(MB == 4 ? 2 : 4))) void ce_few_grad_kernel(const uint16_t* __restrict__ a, int a_kt, const uint8_t* __restrict__ head_grad, int T, int H, int Hp, int Vp,
                                                          const RowStat* __restrict__ stats, const RowStat* __restrict__ run, float* __restrict__ acc_out, int parts)
 {
@@ -175,8 +176,25 @@ __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(MB 
     const int pairs = Vp / 64, p0 = (int)((int64_t)pairs * part / parts), p1 = (int)((int64_t)pairs * (part + 1) / parts);
     f32x4 acc[kFewBlocks][MB];
     float m[MB];
+    if constexpr (JOIN) {                                      // the rows' M, whole numbers, from their groups' (no kernel has joined them)
+        __shared__ int top[64];
+        if (t < 64) top[t] = INT_MIN;
+        __syncthreads();
+        const int all = (Vp / kFewCols) * T;
+        for (int i = t; i < all; i += kFewThreads) {
+            const RowStat s = stats[i];
+            if (s.s != 0.0f) atomicMax(&top[i % T], (int)s.m);
+        }
+        __syncthreads();
 #pragma unroll
-    for (int b = 0; b < MB; ++b) m[b] = run[min(16 * b + frow, T - 1)].m;
+        for (int b = 0; b < MB; ++b) {
+            const int at = top[min(16 * b + frow, T - 1)];
+            m[b] = at == INT_MIN ? 0.0f : (float)at;
+        }
+    } else {
+#pragma unroll
+        for (int b = 0; b < MB; ++b) m[b] = run[min(16 * b + frow, T - 1)].m;
+    }
     auto load = [&](int b, int k) {
         const u32x4 v = *reinterpret_cast<const u32x4*>(a + block_at(16 * b + frow, k * 32 + 8 * fq, a_kt));
         const float f = exp2f(fminf(stats[(int64_t)(k >> 1) * T + min(16 * b + frow, T - 1)].m - m[b], 0.0f));     // (a group of nothing but the target has no M)
@@ -222,7 +240,11 @@ void launch_ce_few_grad(const CeArgs& c, sasq_dtype dt, hipStream_t st)
 {
     const int mb = (int)((c.T + 15) / 16), grid = (c.Hp + kFewCols - 1) / kFewCols * c.few_parts;
     auto go = [&](auto d, auto m) {
-        ce_few_grad_kernel<decltype(d)::value, decltype(m)::value><<<grid, kFewThreads, 0, st>>>(c.a, row_blocks(c.piece), c.head_grad, (int)c.T, (int)c.H, c.Hp, c.Vp,
+        if (c.few_own_join)
+            ce_few_grad_kernel<decltype(d)::value, decltype(m)::value, true><<<grid, kFewThreads, 0, st>>>(
+                c.a, row_blocks(c.piece), c.head_grad, (int)c.T, (int)c.H, c.Hp, c.Vp, c.stats, c.run, c.acc, c.few_parts);
+        else
+            ce_few_grad_kernel<decltype(d)::value, decltype(m)::value, false><<<grid, kFewThreads, 0, st>>>(c.a, row_blocks(c.piece), c.head_grad, (int)c.T, (int)c.H, c.Hp, c.Vp,
                                                                                         c.stats, c.run, c.acc, c.few_parts);
     };
     auto by_rows = [&](auto d) {
