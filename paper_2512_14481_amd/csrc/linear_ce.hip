@@ -136,13 +136,9 @@ __global__ __launch_bounds__(kPackThreads) void ce_pack_kernel(const int32_t* __
 
 // A wave copies one counted row of x to its packed place, with zeros past H.
 template <bool VEC>
-__global__ __launch_bounds__(256) void ce_stage_kernel(const uint16_t* __restrict__ x, int64_t stride, uint16_t* __restrict__ xs, const int32_t* __restrict__ count,
-                                                      const int32_t* __restrict__ row, int H, int Hp)
+__device__ __forceinline__ void ce_stage_row(const uint16_t* __restrict__ src, uint16_t* __restrict__ xs, int p, int H, int Hp)
 {
-    const int p = (int)blockIdx.x * 4 + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (p >= *count) return;
-    const uint16_t* src = x + (int64_t)row[p] * stride;
-    for (int h = lane * 8; h < Hp; h += 512) {
+    for (int h = (int)(threadIdx.x & 63) * 8; h < Hp; h += 512) {
         u32x4 o = {0u, 0u, 0u, 0u};
         if (VEC && h < H) {
             o = *reinterpret_cast<const u32x4*>(src + h);
@@ -155,6 +151,65 @@ __global__ __launch_bounds__(256) void ce_stage_kernel(const uint16_t* __restric
         }
         *reinterpret_cast<u32x4*>(xs + block_at(p, h, row_blocks(Hp))) = o;
     }
+}
+template <bool VEC>
+__global__ __launch_bounds__(256) void ce_stage_kernel(const uint16_t* __restrict__ x, int64_t stride, uint16_t* __restrict__ xs, const int32_t* __restrict__ count,
+                                                      const int32_t* __restrict__ row, int H, int Hp)
+{
+    const int p = (int)blockIdx.x * 4 + (int)(threadIdx.x >> 6);
+    if (p < *count) ce_stage_row<VEC>(x + (int64_t)row[p] * stride, xs, p, H, Hp);
+}
+
+// Both at once: a workgroup counts the rows before its four by itself, up to kPackedTo rows (a launch and its wait less, 4 us; the counting takes T^2 / 2 bytes
+// of L2 reads, 32 MB at most).
+constexpr int kPackedTo = 8192;
+template <bool VEC>
+__global__ __launch_bounds__(256) void ce_pack_stage_kernel(const uint16_t* __restrict__ x, int64_t stride, uint16_t* __restrict__ xs,
+                                                           const int32_t* __restrict__ targets, int T, int V, int32_t* __restrict__ count,
+                                                           int32_t* __restrict__ pos, int32_t* __restrict__ row, int32_t* __restrict__ tgt,
+                                                           float* __restrict__ loss, float* __restrict__ lse, uint32_t* __restrict__ ticket,
+                                                           float* __restrict__ mean, int H, int Hp)
+{
+    constexpr int kAhead = 8;
+    __shared__ int wave_count[4];
+    const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), r0 = (int)blockIdx.x * 4;
+    int mine[4], before = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) mine[j] = r0 + j < T ? targets[r0 + j] : -1;
+    for (int i = t; i - t < r0; i += 256 * kAhead) {
+        int v[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) v[j] = targets[min(i + 256 * j, T - 1)];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) before += __popcll(__builtin_amdgcn_ballot_w64(i + 256 * j < r0 && v[j] >= 0 && v[j] < V));
+    }
+    if ((t & 63) == 0) wave_count[wave] = before;
+    __syncthreads();
+    int p = wave_count[0] + wave_count[1] + wave_count[2] + wave_count[3], own = -1, target = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const bool counts = mine[j] >= 0 && mine[j] < V;
+        if (j == wave && counts) { own = p; target = mine[j]; }
+        p += counts;
+    }
+    const int r = r0 + wave;
+    if (t == 0 && r0 + 4 >= T) {                               // the last four rows
+        *count = p;
+        *ticket = 0;
+        if (mean && p == 0) *mean = 0.0f;
+    }
+    if (r >= T) return;
+    if ((t & 63) == 0) {
+        pos[r] = own;
+        if (own >= 0) {
+            row[own] = r;
+            tgt[own] = target;
+        } else {
+            loss[r] = 0.0f;
+            if (lse) lse[r] = 0.0f;
+        }
+    }
+    if (own >= 0) ce_stage_row<VEC>(x + (int64_t)r * stride, xs, own, H, Hp);
 }
 
 // ---- between the products: M and S of each row so far ----
@@ -462,9 +517,13 @@ static int ce_tile(int64_t M, int64_t N, int64_t K)
 {
     auto tiles = [&](int64_t bm, int64_t bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
     const double kt = (double)(K / 32);
-    const int64_t t256 = tiles(256, 256), tail = t256 % 256, t128 = tiles(128, 128), rest = t128 % 512;
+    const int64_t halves = M % 256 > 0 && M % 256 <= 128 ? tiles(1 << 30, 256) : 0, t256 = tiles(256, 256) - halves, tail = t256 % 256;
+    const int64_t t128 = tiles(128, 128), rest = t128 % 512;
     const double two = 1.5 + 0.55 * kt, one = 1.5 + 0.31 * kt;
-    const double c0 = ((double)(t256 / 256) + (tail == 0 ? 0.0 : tail <= 128 ? 0.65 : 1.0)) * (8.5 + 0.77 * kt);
+    const double last = tail == 0 ? 0.0 : tail <= 128 ? 0.65 : 1.0;
+    double rounds = (double)(t256 / 256) + last;
+    if (halves) rounds = fmax(t256 ? 1.0 : 0.65, ((double)t256 + 0.65 * (double)halves) / 256.0 + 0.2);
+    const double c0 = rounds * (8.5 + 0.77 * kt);
     const double c2 = (double)(t128 / 512) * two + (rest == 0 ? 0.0 : rest <= 256 ? one : two);
     return c0 <= c2 ? 0 : 2;
 }
@@ -581,11 +640,19 @@ static void ce_run(const CeArgs& c, sasq_dtype dt, hipStream_t st)
         }
         return;
     }
-    ce_pack_kernel<<<1, kPackThreads, 0, st>>>(c.targets, T, (int)c.V, c.count, c.pos, c.row, c.tgt, c.loss, c.lse, c.ticket, c.mean);
-    if (c.x_stride % 8 == 0 && H % 8 == 0)
-        ce_stage_kernel<true><<<(T + 3) / 4, 256, 0, st>>>(static_cast<const uint16_t*>(c.x), c.x_stride, c.xs, c.count, c.row, H, c.Hp);
-    else
-        ce_stage_kernel<false><<<(T + 3) / 4, 256, 0, st>>>(static_cast<const uint16_t*>(c.x), c.x_stride, c.xs, c.count, c.row, H, c.Hp);
+    auto stage = [&](auto v) {
+        constexpr bool VEC = decltype(v)::value;
+        const auto x = static_cast<const uint16_t*>(c.x);
+        if (T <= kPackedTo) {
+            ce_pack_stage_kernel<VEC><<<(T + 3) / 4, 256, 0, st>>>(x, c.x_stride, c.xs, c.targets, T, (int)c.V, c.count, c.pos, c.row, c.tgt, c.loss, c.lse, c.ticket,
+                                                                   c.mean, H, c.Hp);
+            return;
+        }
+        ce_pack_kernel<<<1, kPackThreads, 0, st>>>(c.targets, T, (int)c.V, c.count, c.pos, c.row, c.tgt, c.loss, c.lse, c.ticket, c.mean);
+        ce_stage_kernel<VEC><<<(T + 3) / 4, 256, 0, st>>>(x, c.x_stride, c.xs, c.count, c.row, H, c.Hp);
+    };
+    if (c.x_stride % 8 == 0 && H % 8 == 0) stage(std::true_type{});
+    else                                   stage(std::false_type{});
     const int sc = stat_cols(c.tile), bn = 2 * sc;
     for (int64_t col0 = 0; col0 < c.V;) {
         const int64_t piece = col0 ? c.piece : c.first_piece, cols = c.V - col0 < piece ? c.V - col0 : piece;

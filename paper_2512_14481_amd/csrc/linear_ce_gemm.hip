@@ -140,7 +140,8 @@ __device__ __forceinline__ void tile_at(int logical, int tiles_m, int tiles_n, i
     tn = panel * PN + in % width;
 }
 
-// Tiles of 256x256 come in rounds of 256 workgroups; a last round of at most 128 goes as twice as many tiles of 128 rows, which take 0.65 of a round.
+// Tiles of 256x256 come in rounds of 256 workgroups; a last round of at most 128 goes as twice as many tiles of 128 rows, which take 0.65 of a round, and so does
+// a last row of tiles of at most 128 rows.
 constexpr int kHalvesTo = 128;
 
 template <int DT, int BM, int BN, bool GRAD>
@@ -153,20 +154,16 @@ void ce_logits_kernel(const uint16_t* __restrict__ xs, const uint8_t* __restrict
     const int M = *count, tiles_m = (M + BM - 1) / BM;
     int tm, tn;
     if constexpr (BM == 256) {
-        const int total = tiles_m * tiles_n, tail = total % 256, whole = total - tail;
-        if (tail && tail <= kHalvesTo) {
-            const int id = (int)blockIdx.x - whole, per = ((id < 0 ? whole : 2 * tail) + 7) >> 3, at = id < 0 ? (int)blockIdx.x : id;
-            const int logical = (at & 7) * per + (at >> 3);
-            if (at >> 3 >= per || (id >= 0 && logical >= 2 * tail)) return;
-            tile_at(id < 0 ? logical : whole + logical / 2, tiles_m, tiles_n, tm, tn);
-            if (id >= 0) {
-                tm = 2 * tm + (logical & 1);
-                if (tm * 128 < M)
-                    gemm_k64_body<DT, KW_I8B, 128, BN, false, GR_NONE, 1, LogitsExt<DT, GRAD>>(
-                        reinterpret_cast<const int8_t*>(xs), head, nullptr, nullptr, nullptr, nullptr, nullptr, M, V, Hp * 2, tm, ext.col0 / BN + tn, lds, 0, ext);
-                return;
-            }
-        } else if (!tile_of_counted(tiles_m, tiles_n, tm, tn)) {
+        const int total = tiles_m * tiles_n, last = total % 256, tail = last <= kHalvesTo ? last : 0, whole = total - tail;
+        const int id = tail ? (int)blockIdx.x - whole : -1, per = ((id < 0 ? whole : 2 * tail) + 7) >> 3, at = id < 0 ? (int)blockIdx.x : id;
+        const int logical = (at & 7) * per + (at >> 3);
+        if (at >> 3 >= per || logical >= (id < 0 ? whole : 2 * tail)) return;
+        tile_at(id < 0 ? logical : whole + logical / 2, tiles_m, tiles_n, tm, tn);
+        int half = 2 * tm + (id < 0 ? 0 : logical & 1);
+        if (id >= 0 || M - tm * 256 <= 128) {
+            if (half * 128 < M)
+                gemm_k64_body<DT, KW_I8B, 128, BN, false, GR_NONE, 1, LogitsExt<DT, GRAD>>(
+                    reinterpret_cast<const int8_t*>(xs), head, nullptr, nullptr, nullptr, nullptr, nullptr, M, V, Hp * 2, half, ext.col0 / BN + tn, lds, 0, ext);
             return;
         }
     } else if (!tile_of_counted(tiles_m, tiles_n, tm, tn)) {
