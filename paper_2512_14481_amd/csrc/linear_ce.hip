@@ -138,18 +138,26 @@ __global__ __launch_bounds__(kPackThreads) void ce_pack_kernel(const int32_t* __
 template <bool VEC>
 __device__ __forceinline__ void ce_stage_row(const uint16_t* __restrict__ src, uint16_t* __restrict__ xs, int p, int H, int Hp)
 {
-    for (int h = (int)(threadIdx.x & 63) * 8; h < Hp; h += 512) {
-        u32x4 o = {0u, 0u, 0u, 0u};
-        if (VEC && h < H) {
-            o = *reinterpret_cast<const u32x4*>(src + h);
-        } else {
+    constexpr int kAhead = 4;
+    for (int h0 = (int)(threadIdx.x & 63) * 8; h0 < Hp; h0 += 512 * kAhead) {
+        u32x4 o[kAhead];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t lo = h + 2 * e < H ? src[h + 2 * e] : 0u, hi = h + 2 * e + 1 < H ? src[h + 2 * e + 1] : 0u;
-                o[e] = lo | hi << 16;
+        for (int j = 0; j < kAhead; ++j) {
+            const int h = h0 + 512 * j;
+            o[j] = u32x4{0u, 0u, 0u, 0u};
+            if (VEC) {
+                if (h < H) o[j] = *reinterpret_cast<const u32x4*>(src + h);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t lo = h + 2 * e < H ? src[h + 2 * e] : 0u, hi = h + 2 * e + 1 < H ? src[h + 2 * e + 1] : 0u;
+                    o[j][e] = lo | hi << 16;
+                }
             }
         }
-        *reinterpret_cast<u32x4*>(xs + block_at(p, h, row_blocks(Hp))) = o;
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+            if (h0 + 512 * j < Hp) *reinterpret_cast<u32x4*>(xs + block_at(p, h0 + 512 * j, row_blocks(Hp))) = o[j];
     }
 }
 template <bool VEC>
@@ -341,12 +349,11 @@ __global__ __launch_bounds__(kJoinThreads) void ce_join_kernel(const RowStat* __
     *mean = counted ? (float)(all / (double)counted) : 0.0f;
 }
 
-// a_v of groups of columns with another M than their row's, in place: sixteen rows and 64 blocks a workgroup, a 1 KB block a wave and access.
-constexpr int kScaleBlocks = 64;
+// a_v of groups of columns with another M than their row's, in place: sixteen rows and `each` blocks a workgroup, a 1 KB block a wave and access.
 template <int DT>
 __global__ __launch_bounds__(256) void ce_scale_kernel(uint16_t* __restrict__ a, int a_kt, int kt, int stat_blocks, const RowStat* __restrict__ stats,
                                                       const RowStat* __restrict__ run, const uint8_t* __restrict__ scale_rows, int flags, int64_t T,
-                                                      const int32_t* __restrict__ count)
+                                                      const int32_t* __restrict__ count, int each)
 {
     using S = Store16<DT>;
     const int n = *count, r16 = (int)blockIdx.x;
@@ -357,10 +364,10 @@ __global__ __launch_bounds__(256) void ce_scale_kernel(uint16_t* __restrict__ a,
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int p = min(r16 * 16 + (lane >> 2), n - 1);
     const float m = run[p].m;
-    const int k1 = min(kt, ((int)blockIdx.y + 1) * kScaleBlocks);
+    const int k1 = min(kt, ((int)blockIdx.y + 1) * each);
     u32x4* at = reinterpret_cast<u32x4*>(a) + (int64_t)r16 * a_kt * 64 + lane;
     constexpr int kAhead = 4;
-    for (int k = (int)blockIdx.y * kScaleBlocks + wave; k < k1; k += 4 * kAhead) {
+    for (int k = (int)blockIdx.y * each + wave; k < k1; k += 4 * kAhead) {
         u32x4 v[kAhead];
         float f[kAhead];
 #pragma unroll
@@ -413,7 +420,8 @@ __device__ __forceinline__ RowEnd few_row_end(const RowStat* __restrict__ stats,
     return row_end(m, sum, zt);
 }
 
-// ---- the end: dx of every row; left-out ones are 0 ----
+// ---- the end: dx of every row, kDxCols channels a workgroup; left-out ones are 0 ----
+constexpr int kDxCols = 256 * 8;
 // JOIN: few rows of few groups of columns, which no other kernel has joined: a workgroup does so for its row, the one more for all.
 template <int DT, bool VEC, bool JOIN>
 __global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ acc, int bm, int tiles_n, int slots, int max_splits, int few_parts, const int32_t* __restrict__ count,
@@ -424,8 +432,9 @@ __global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ ac
                                                    const float* __restrict__ zt, float* __restrict__ loss_out, float* __restrict__ lse)
 {
     using S = Store16<DT>;
-    const int r = (int)blockIdx.x;
+    const int r = (int)blockIdx.x, h = (int)blockIdx.y * kDxCols + (int)threadIdx.x * 8;
     if (r == T) {                                 // a workgroup more: the mean, in fp64 and a fixed order
+        if (blockIdx.y) return;
         __shared__ double part[4];
         double sum = 0.0;
         if constexpr (JOIN) {
@@ -455,7 +464,7 @@ __global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ ac
     if (p >= 0) g = scale * (row_weight ? row_weight[r] : 1.0f / (float)n);
     if constexpr (JOIN) {
         const RowEnd end = few_row_end(stats, groups, T, r, zt[r], (int)threadIdx.x % kWave, kWave);
-        if (threadIdx.x == 0) {
+        if (h == 0) {
             loss_out[r] = p >= 0 ? end.loss : 0.0f;
             if (lse) lse[r] = p >= 0 ? end.lse : 0.0f;
         }
@@ -465,26 +474,36 @@ __global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ ac
         cf = coef[p];
         uu = u[p];
     }
-    for (int h = threadIdx.x * 8; h < H; h += 256 * 8) {
-        float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (p >= 0) {
-            for (int s = 0; s < splits; ++s) {
-                const float* at = acc + ((int64_t)s * rows + p) * Hp + h;
+    if (h >= H) return;
+    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (p >= 0) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(head) + block_at(t, h, row_blocks(Hp)));
+        constexpr int kAhead = 4;
+        for (int s = 0; s < splits; s += kAhead) {
+            f32x4 at[kAhead][2];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] += at[e];
+            for (int j = 0; j < kAhead; ++j) {
+                const f32x4* from = reinterpret_cast<const f32x4*>(acc + ((int64_t)min(s + j, splits - 1) * rows + p) * Hp + h);
+                at[j][0] = from[0];
+                at[j][1] = from[1];
             }
-            const u32x4 w = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(head) + block_at(t, h, row_blocks(Hp)));
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = g * __builtin_fmaf(cf, v[e], -uu * ((e & 1) ? S::hi(w[e >> 1]) : S::lo(w[e >> 1])));
-        }
-        uint16_t* dst = dx + (int64_t)r * stride + h;
-        if (VEC) {
-            *reinterpret_cast<u32x4*>(dst) = u32x4{S::pack(v[0], v[1]), S::pack(v[2], v[3]), S::pack(v[4], v[5]), S::pack(v[6], v[7])};
-        } else {
+            for (int j = 0; j < kAhead; ++j) {
+                if (s + j >= splits) break;
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (h + e < H) dst[e] = S::enc(v[e]);
+                for (int e = 0; e < 8; ++e) v[e] += at[j][e >> 2][e & 3];
+            }
         }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = g * __builtin_fmaf(cf, v[e], -uu * ((e & 1) ? S::hi(w[e >> 1]) : S::lo(w[e >> 1])));
+    }
+    uint16_t* dst = dx + (int64_t)r * stride + h;
+    if (VEC) {
+        *reinterpret_cast<u32x4*>(dst) = u32x4{S::pack(v[0], v[1]), S::pack(v[2], v[3]), S::pack(v[4], v[5]), S::pack(v[6], v[7])};
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (h + e < H) dst[e] = S::enc(v[e]);
     }
 }
 
@@ -534,7 +553,18 @@ static int ce_grad_tile(int64_t M, int64_t N)
     return 0.8 * used(128, 128) > used(256, 256) ? 2 : 0;
 }
 
-static int ce_few_groups(const CeArgs& c) { return (int)((c.V + kFewCols - 1) / kFewCols); }
+// Columns of a workgroup of few rows' logits: fewer where 64 would leave CUs without one, and where a row or four cost nothing beside the head; each workgroup
+// reads all of x, so more rows want more columns.  us, whole call without the gradient, 64 | 32 | 16 columns, T x H -> V: 1 x 4096 -> 2000 17.8 | 13.6 | 12.9,
+// -> 8000 20.7 | 18.1 | 19.4, -> 32000 51.4 | 47.3 | 45.7 (with the gradient 97 | 94 | 96); 16 x 4096 -> 2000 20.7 | 17.2 | 14.9, -> 8000 23.6 | 19.6 | 22.3,
+// -> 32000 52.8 | 54.3 | 64.9; 64 x 4096 -> 2000 36.0 | 31.5 | 29.9, -> 8000 38.4 | 33.4 | 47.7, -> 32000 72 | 96 | 154; 1 x 1024 -> 128000 45.6 | 49.8 | 52.5.
+static int ce_few_cols(const CeArgs& c)
+{
+    if (c.H < 2048) return kFewCols;
+    if (c.Vp / 16 <= 256) return 16;
+    if (c.Vp / 32 <= 256) return 32;
+    return c.T <= 4 && c.H >= 4096 ? c.grad ? 32 : 16 : kFewCols;
+}
+static int ce_few_groups(const CeArgs& c) { return c.Vp / c.few_cols; }
 
 // Sizes and the workspace's parts, from `base` (0: only how long they are).
 static size_t ce_plan(CeArgs& c, int64_t piece, char* base)
@@ -544,11 +574,13 @@ static size_t ce_plan(CeArgs& c, int64_t piece, char* base)
     ce_pieces(c.T, c.V, piece, c.grad, c.piece, c.first_piece);
     c.few_parts = 0;
     c.few_own_join = false;
+    c.few_cols = kFewCols;
     if (c.T <= kFewRows && c.piece >= c.V) {
         // as many workgroups as fill the chip twice, of 64 columns a wave at least
         int64_t parts = 512 / ((c.Hp + kFewCols - 1) / kFewCols);
         if (parts > c.Vp / 512) parts = c.Vp / 512;
         c.few_parts = (int)(parts < 1 ? 1 : parts);
+        c.few_cols = ce_few_cols(c);
         c.few_own_join = c.grad && c.T * ce_few_groups(c) <= kFewOwnJoin;
     }
     c.tile = c.few_parts ? 2 : ce_tile(c.T, c.piece, c.Hp);         // (few rows: M and S of 64 columns, as of such a tile's waves)
@@ -567,7 +599,7 @@ static size_t ce_plan(CeArgs& c, int64_t piece, char* base)
         p = reinterpret_cast<std::remove_reference_t<decltype(p)>>(base + at);
         at += (bytes + 255) / 256 * 256;
     };
-    const size_t T = (size_t)c.T, T16 = c.few_parts && T > 32 ? 64 : (T + 15) / 16 * 16, groups = (size_t)(c.piece / sc);
+    const size_t T = (size_t)c.T, T16 = c.few_parts && T > 32 ? 64 : (T + 15) / 16 * 16, groups = (size_t)(c.few_parts ? ce_few_groups(c) : c.piece / sc);
     part(c.count, 4);
     part(c.ticket, 4);
     part(c.pos, T * 4);
@@ -598,10 +630,10 @@ static bool ce_sizes_ok(int64_t T, int64_t V, int64_t H, int64_t piece)
 template <int DT>
 static void launch_dx(const CeArgs& c, hipStream_t st)
 {
-    const int T = (int)c.T, H = (int)c.H, bm = tile_rows(c.grad_tile), tiles_n = (int)((c.H + tile_cols(c.grad_tile) - 1) / tile_cols(c.grad_tile));
+    const int T = (int)c.T, H = (int)c.H, chunks = (H + kDxCols - 1) / kDxCols, bm = tile_rows(c.grad_tile), tiles_n = (int)((c.H + tile_cols(c.grad_tile) - 1) / tile_cols(c.grad_tile));
     const bool vec = c.dx_stride % 8 == 0 && H % 8 == 0;
     auto go = [&](auto v, auto join) {
-        ce_dx_kernel<DT, decltype(v)::value, decltype(join)::value><<<T + (c.mean ? 1 : 0), 256, 0, st>>>(
+        ce_dx_kernel<DT, decltype(v)::value, decltype(join)::value><<<dim3(T + (c.mean ? 1 : 0), chunks), 256, 0, st>>>(
             c.acc, bm, tiles_n, c.slots, c.max_splits, c.few_parts, c.count, c.pos, c.few_parts ? c.targets : c.tgt, c.coef, c.u, c.head, c.row_weight, c.scale,
             static_cast<uint16_t*>(c.dx), c.dx_stride, H, c.Hp, c.loss, c.mean, T, (int)c.V, c.stats, ce_few_groups(c), c.zt, c.loss, c.lse);
     };
@@ -661,8 +693,9 @@ static void ce_run(const CeArgs& c, sasq_dtype dt, hipStream_t st)
         launch_join(c, groups, col0 == 0, col0 + cols >= c.V, st);
         if (c.grad) {
             const int kt = (int)(up(cols, 64) / 32);
-            ce_scale_kernel<DT><<<dim3((T + 15) / 16, (kt + kScaleBlocks - 1) / kScaleBlocks), 256, 0, st>>>(c.a, row_blocks(c.piece), kt, sc / 32, c.stats, c.run,
-                                                                                                             c.scale_rows, 16 / join_rows(groups), c.T, c.count);
+            const int rows16 = (T + 15) / 16, each = kt * rows16 < 64 * 1024 ? 16 : 64;
+            ce_scale_kernel<DT><<<dim3(rows16, (kt + each - 1) / each), 256, 0, st>>>(c.a, row_blocks(c.piece), kt, sc / 32, c.stats, c.run, c.scale_rows,
+                                                                                      16 / join_rows(groups), c.T, c.count, each);
             launch_ce_grad(c, dt, col0, cols, st);
         }
         col0 += cols;

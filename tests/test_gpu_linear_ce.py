@@ -58,6 +58,28 @@ def test_large_tiles(T, V, H, dtype, left_out, grad):
     check(call(p, grad=grad, scale=256.0), p.reference(scale=256.0, device="cuda"))
 
 
+@pytest.mark.parametrize("dtype,left_out,grad", [("f16", 0.0, True), ("bf16", 0.3, True), ("f16", 0.3, False)])
+@pytest.mark.parametrize("T,V,H", [(1, 300, 4097), (2, 4096, 2050), (3, 8300, 4096), (16, 8192, 2049), (17, 300, 2048), (20, 4097, 2100), (33, 2049, 2113), (64, 4096, 2056),
+                                   (64, 8191, 2050), (64, 8200, 2048)])
+def test_few_rows_of_long_ones(T, V, H, dtype, left_out, grad):
+    """At most 64 rows, long enough that the logits' workgroups take 16, 32 or 64 columns by the vocabulary's size."""
+    p = Head(T, V, H, dtype, seed=T + V, left_out=left_out)
+    check(call(p, grad=grad, scale=32.0), p.reference(scale=32.0, device="cuda"))
+
+
+@pytest.mark.parametrize("T,V,H", [(4093, 300, 64), (8191, 300, 64), (8193, 300, 64), (9001, 130, 100), (20000, 65, 72)])
+def test_many_rows_packed(T, V, H):
+    """The rows that count are packed by the kernel that stages them, or, where they are many, by one of its own."""
+    p = Head(T, V, H, "bf16", seed=T, left_out=0.4)
+    check(call(p, scale=64.0), p.reference(scale=64.0, device="cuda"))
+
+
+@pytest.mark.parametrize("T,V,H", [(384, 30000, 1024), (640, 9000, 2048), (257, 33000, 520), (1281, 16000, 512)])
+def test_a_last_row_of_tiles_that_is_half_full(T, V, H):
+    p = Head(T, V, H, "f16", seed=T)
+    check(call(p, scale=64.0), p.reference(scale=64.0, device="cuda"))
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("T,V,H", [(1, 1, 1), (16, 1000, 256), (50, 700, 64), (300, 5000, 640)])
 def test_without_gradient(T, V, H, dtype):
