@@ -285,25 +285,35 @@ __device__ __forceinline__ void ck_fwd_pc_body(const CkItem& it, int block, int 
     const int64_t r0 = block % it.chunks * it.chunk_rows, r1 = min(it.rows, r0 + it.chunk_rows);
     if (VEC && ck_col<VEC>(cb, lane, 0) >= cols) return;
     const float lo = kMagic + ck_low(bits), hi = kMagic + ck_high(bits);
+    u32x4 in[2][kCkUnroll];
+    auto fetch = [&](int set, int64_t base) {
+#pragma unroll
+        for (int u = 0; u < kCkUnroll; ++u) in[set][u] = ck_load_row<DT, VEC>(it.x + min(base + u * kCkWaves, r1 - 1) * cols, cb, lane, cols);
+    };
+    fetch(0, r0 + wave);
     float s[8], inv_s[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         s[e] = it.s[min(ck_col<VEC>(cb, lane, e), cols - 1)];
         inv_s[e] = 1.0f / s[e];
     }
-    for (int64_t base = r0 + wave; base < r1; base += kCkWaves * kCkUnroll) {
-        u32x4 in[kCkUnroll];
-#pragma unroll
-        for (int u = 0; u < kCkUnroll; ++u) in[u] = ck_load_row<DT, VEC>(it.x + min(base + u * kCkWaves, r1 - 1) * cols, cb, lane, cols);
+    auto rows = [&](int set, int64_t base) {
 #pragma unroll
         for (int u = 0; u < kCkUnroll; ++u) {
             const int64_t r = base + u * kCkWaves;
             if (r >= r1) break;
             u32x2 kp;
-            const u32x4 out = ck_fwd_vec<DT>(in[u], inv_s, s, lo, hi, kp);
+            const u32x4 out = ck_fwd_vec<DT>(in[set][u], inv_s, s, lo, hi, kp);
             ck_store_row<VEC>(it.out + r * cols, out, cb, lane, cols);
             ck_store_kept<VEC>(it.kept + r * cols, kp, cb, lane, cols);
         }
+    };
+    constexpr int kStep = kCkWaves * kCkUnroll;
+    for (int64_t base = r0 + wave; base < r1; base += 2 * kStep) {
+        if (base + kStep < r1) fetch(1, base + kStep);
+        rows(0, base);
+        if (base + 2 * kStep < r1) fetch(0, base + 2 * kStep);
+        if (base + kStep < r1) rows(1, base + kStep);
     }
 }
 
