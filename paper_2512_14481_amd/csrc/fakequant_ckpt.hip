@@ -281,8 +281,8 @@ template <int DT, bool VEC>
 __device__ __forceinline__ void ck_fwd_pc_body(const CkItem& it, int block, int bits)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t cb = block / it.chunks, cols = it.cols;
-    const int64_t r0 = block % it.chunks * it.chunk_rows, r1 = min(it.rows, r0 + it.chunk_rows);
+    const int64_t cols = it.cols, across = (cols + kCkCols - 1) / kCkCols, cb = block % across, chunk = block / across;
+    const int64_t r0 = chunk * it.chunk_rows, r1 = min(it.rows, r0 + it.chunk_rows);
     if (VEC && ck_col<VEC>(cb, lane, 0) >= cols) return;
     const float lo = kMagic + ck_low(bits), hi = kMagic + ck_high(bits);
     u32x4 in[2][kCkUnroll];
@@ -332,8 +332,8 @@ template <int DT, bool VEC>
 __device__ __forceinline__ void ck_bwd_pc_body(const CkItem& it, int block, int bits, float (&red)[kCkWaves][kCkCols])
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t cb = block / it.chunks, cols = it.cols;
-    const int64_t r0 = block % it.chunks * it.chunk_rows, r1 = min(it.rows, r0 + it.chunk_rows);
+    const int64_t cols = it.cols, across = (cols + kCkCols - 1) / kCkCols, cb = block % across, chunk = block / across;
+    const int64_t r0 = chunk * it.chunk_rows, r1 = min(it.rows, r0 + it.chunk_rows);
     const float lo = ck_low(bits) * kCkSteps, hi = ck_high(bits) * kCkSteps;
     double acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};      // four rows in fp32, everything above that in fp64
     if (!VEC || ck_col<VEC>(cb, lane, 0) < cols) {
@@ -370,7 +370,7 @@ __device__ __forceinline__ void ck_bwd_pc_body(const CkItem& it, int block, int 
 #pragma unroll
         for (int w = 0; w < kCkWaves; ++w) all += (double)red[w][c];
         if (it.chunks == 1) it.ds[cb * kCkCols + c] = (float)(all / (double)kCkSteps);
-        else                static_cast<float*>(it.partial)[(int64_t)(block % it.chunks) * cols + cb * kCkCols + c] = (float)all;
+        else                static_cast<float*>(it.partial)[chunk * cols + cb * kCkCols + c] = (float)all;
     }
 }
 
