@@ -233,10 +233,13 @@ __global__ __launch_bounds__(kCkThreads) void ck_join_kernel(const CkBatch b)
 template <bool VEC>
 __device__ __forceinline__ int64_t ck_col(int64_t col_block, int lane, int e) { return col_block * kCkCols + (VEC ? lane * 8 + e : e * kWave + lane); }
 
-template <int DT, bool VEC>
+template <int DT, bool VEC, bool ONCE>
 __device__ __forceinline__ u32x4 ck_load_row(const uint16_t* at, int64_t col_block, int lane, int64_t cols)
 {
-    if (VEC) return *reinterpret_cast<const u32x4*>(at + ck_col<VEC>(col_block, lane, 0));
+    if (VEC) {
+        const auto from = reinterpret_cast<const u32x4*>(at + ck_col<VEC>(col_block, lane, 0));
+        return ONCE ? __builtin_nontemporal_load(from) : *from;
+    }
     u32x4 v;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
@@ -248,7 +251,7 @@ __device__ __forceinline__ u32x4 ck_load_row(const uint16_t* at, int64_t col_blo
 template <bool VEC>
 __device__ __forceinline__ u32x2 ck_load_kept(const int8_t* at, int64_t col_block, int lane, int64_t cols)
 {
-    if (VEC) return *reinterpret_cast<const u32x2*>(at + ck_col<VEC>(col_block, lane, 0));
+    if (VEC) return __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(at + ck_col<VEC>(col_block, lane, 0)));
     u32x2 v = {0u, 0u};
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e >> 2] |= (uint32_t)(uint8_t)at[min(ck_col<VEC>(col_block, lane, e), cols - 1)] << (8 * (e & 3));
@@ -288,7 +291,7 @@ __device__ __forceinline__ void ck_fwd_pc_body(const CkItem& it, int block, int 
     u32x4 in[2][kCkUnroll];
     auto fetch = [&](int set, int64_t base) {
 #pragma unroll
-        for (int u = 0; u < kCkUnroll; ++u) in[set][u] = ck_load_row<DT, VEC>(it.x + min(base + u * kCkWaves, r1 - 1) * cols, cb, lane, cols);
+        for (int u = 0; u < kCkUnroll; ++u) in[set][u] = ck_load_row<DT, VEC, false>(it.x + min(base + u * kCkWaves, r1 - 1) * cols, cb, lane, cols);
     };
     fetch(0, r0 + wave);
     float s[8], inv_s[8];
@@ -344,7 +347,7 @@ __device__ __forceinline__ void ck_bwd_pc_body(const CkItem& it, int block, int 
             for (int u = 0; u < kCkUnroll; ++u) {
                 const int64_t at = min(base + u * kCkWaves, r1 - 1) * cols;
                 kp[u] = ck_load_kept<VEC>(it.kept + at, cb, lane, cols);
-                g[u] = ck_load_row<DT, VEC>(it.dy + at, cb, lane, cols);
+                g[u] = ck_load_row<DT, VEC, true>(it.dy + at, cb, lane, cols);
             }
             float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
