@@ -6,7 +6,8 @@ terms' sizes; doubled for the matrix unit's own intermediate roundings):
   lse   2 ez (numerator and target) and the sum over V, its logarithm and the rounding of the result: (V + 8) 2^-24 + 2^-24 |lse|
   loss  d = lse_o - z_t is off by that; loss = ln(1 + e^d) by at most u times as much, and 2^-24 of itself
   dx    the average of W over the others is off by eps (exponentials in 16 bits, relative) + 2 (2 ez + 2^-20) + 2 V 2^-24 of sum q |W|, in fp16 also by
-V 2^-34 max |W| (two roundings to the smallest step, 2^-24, beside a largest exponential of 2^10 at least); u by what d is off by; then one rounding, and the type's smallest step
+        V 2^-34 max |W| (two roundings to the smallest step, 2^-24, beside a largest exponential of 2^10 at least);
+        u by what d is off by; then one rounding, and the type's smallest step
 """
 from __future__ import annotations
 
