@@ -86,10 +86,10 @@ __device__ __forceinline__ int64_t block_at(int64_t row, int col, int kt)
 void launch_ce_logits(const CeArgs& c, sasq_dtype dt, int64_t col0, int64_t cols, hipStream_t st);
 void launch_ce_grad(const CeArgs& c, sasq_dtype dt, int64_t col0, int64_t cols, hipStream_t st);
 
-// At most kFewRows rows, the whole vocabulary in one piece (linear_ce_few.hip).  M and S are of few_cols columns (16, 32 or 64); rows are not packed.
+// At most kFewRows rows, or kFewMost where the head is small (ce_few), the whole vocabulary in one piece (linear_ce_few.hip).  M and S are of few_cols columns (16, 32 or 64); rows are not packed.
 // kFewOwnJoin: up to so many M and S in all, every workgroup of the gradient reads them and the join is no kernel of its own (64 x 256 -> 1000 22.8 -> 18.8 us).
 // kFewCols: most columns of a workgroup of the logits, and channels of one of the gradient.
-constexpr int kFewRows = 64, kFewCols = 64, kFewOwnJoin = 4096;
+constexpr int kFewMost = 2048, kFewRows = 64, kFewCols = 64, kFewOwnJoin = 4096;
 void launch_ce_few_logits(const CeArgs& c, sasq_dtype dt, hipStream_t st);
 void launch_ce_few_grad(const CeArgs& c, sasq_dtype dt, hipStream_t st);
 

@@ -557,6 +557,17 @@ static int ce_grad_tile(int64_t M, int64_t N)
     return 0.8 * used(128, 128) > used(256, 256) ? 2 : 0;
 }
 
+// Whether the kernels of few rows do the call: up to 64 rows, and where all of it is so small that it is launches that count (four in place of six, and none of
+// their workgroups waits for another's), 64 rows a workgroup.  us, whole call with the gradient, tiles | these, T x H -> V: 100 x 100 -> 600 32.0 | 21.4, 1000 x 512
+// -> 1000 48 | 26, 500 x 512 -> 4000 51 | 41, 500 x 4096 -> 500 69 | 43, 200 x 1024 -> 4000 51 | 37; but 300 x 4096 -> 1000 55 | 62, 100 x 512 -> 16000 44 | 49,
+// 512 x 128 -> 8000 39.7 | 40.6; rows that are not whole 16 bytes, 400 x 300 -> 700 34.7 | 30.5 but 700 x 700 -> 2000 54 | 62.
+static bool ce_few(const CeArgs& c)
+{
+    if (c.piece < c.V) return false;
+    if (c.T <= kFewRows) return true;
+    return c.T <= kFewMost && c.V <= 8192 && up(c.T, kFewRows) / kFewRows * (c.Vp / kFewCols) <= 512 && c.T * c.V * c.H <= (c.H % 8 ? INT64_C(1) << 27 : INT64_C(1) << 30);
+}
+
 // Columns of a workgroup of few rows' logits: fewer where 64 would leave CUs without one, and where a row or four cost nothing beside the head; each workgroup
 // reads all of x, so more rows want more columns.  us, whole call without the gradient, 64 | 32 | 16 columns, T x H -> V: 1 x 4096 -> 2000 17.8 | 13.6 | 12.9,
 // -> 8000 20.7 | 18.1 | 19.4, -> 32000 51.4 | 47.3 | 45.7 (with the gradient 97 | 94 | 96); 16 x 4096 -> 2000 20.7 | 17.2 | 14.9, -> 8000 23.6 | 19.6 | 22.3,
@@ -579,15 +590,15 @@ static size_t ce_plan(CeArgs& c, int64_t piece, char* base)
     c.few_parts = 0;
     c.few_own_join = false;
     c.few_cols = kFewCols;
-    if (c.T <= kFewRows && c.piece >= c.V) {
+    if (ce_few(c)) {
         // as many workgroups as fill the chip twice, of 64 columns a wave at least
-        int64_t parts = 512 / ((c.Hp + kFewCols - 1) / kFewCols);
+        int64_t parts = 512 / ((c.Hp + kFewCols - 1) / kFewCols * ((c.T + kFewRows - 1) / kFewRows));
         if (parts > c.Vp / 512) parts = c.Vp / 512;
         c.few_parts = (int)(parts < 1 ? 1 : parts);
         c.few_cols = ce_few_cols(c);
-        c.few_own_join = c.grad && c.T * ce_few_groups(c) <= kFewOwnJoin;
+        c.few_own_join = c.grad && c.T <= kFewRows && c.T * ce_few_groups(c) <= kFewOwnJoin;
     }
-    c.tile = c.few_parts ? 2 : ce_tile(c.T, c.piece, c.Hp);         // (few rows: M and S of 64 columns, as of such a tile's waves)
+    c.tile = ce_tile(c.T, c.piece, c.Hp);
     c.grad_tile = ce_grad_tile(c.T, c.H);
     const int bm = tile_rows(c.grad_tile), bn = tile_cols(c.grad_tile), sc = stat_cols(c.tile);
     const int64_t tiles_n = (c.H + bn - 1) / bn;
@@ -603,7 +614,7 @@ static size_t ce_plan(CeArgs& c, int64_t piece, char* base)
         p = reinterpret_cast<std::remove_reference_t<decltype(p)>>(base + at);
         at += (bytes + 255) / 256 * 256;
     };
-    const size_t T = (size_t)c.T, T16 = c.few_parts && T > 32 ? 64 : (T + 15) / 16 * 16, groups = (size_t)(c.few_parts ? ce_few_groups(c) : c.piece / sc);
+    const size_t T = (size_t)c.T, T16 = c.few_parts && T > 32 ? (T + 63) / 64 * 64 : (T + 15) / 16 * 16, groups = (size_t)(c.few_parts ? ce_few_groups(c) : c.piece / sc);
     part(c.count, 4);
     part(c.ticket, 4);
     part(c.pos, T * 4);

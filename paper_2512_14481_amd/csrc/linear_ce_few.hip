@@ -113,11 +113,19 @@ __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(NB 
     __shared__ __attribute__((aligned(16))) FewLds<NB, MB> lds;
     const int t = threadIdx.x, lane = t & 63, frow = lane & 15, fq = lane >> 4;
     const int v0 = (int)blockIdx.x * 16 * NB;
-    if (blockIdx.x == 0 && t < 64) {                           // how many rows count, for the kernels behind this one
-        const int v = t < T ? targets[t] : -1;
-        const uint64_t mask = __builtin_amdgcn_ballot_w64(v >= 0 && v < V);
+    const int r0 = (int)blockIdx.y * kFewRows;
+    if (blockIdx.x + blockIdx.y == 0 && t < 64) {              // how many rows count, for the kernels behind this one
+        constexpr int kAhead = 8;
+        int all = 0;
+        for (int i0 = t; i0 - t < T; i0 += 64 * kAhead) {
+            int v[kAhead];
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) v[j] = targets[min(i0 + 64 * j, T - 1)];
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) all += __popcll(__builtin_amdgcn_ballot_w64(i0 + 64 * j < T && v[j] >= 0 && v[j] < V));
+        }
         if (t == 0) {
-            *count = __popcll(mask);
+            *count = all;
             *ticket = 0;
         }
     }
@@ -125,10 +133,10 @@ __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(NB 
     f32x4 acc[NB][MB];
     int tgt[Meet::kPasses];                                    // of the rows that this thread reduces at the end
 #pragma unroll
-    for (int q = 0; q < Meet::kPasses; ++q) tgt[q] = targets[min(Meet::row(q), T - 1)];
+    for (int q = 0; q < Meet::kPasses; ++q) tgt[q] = targets[min(r0 + Meet::row(q), T - 1)];
     const uint16_t* row[MB];
 #pragma unroll
-    for (int b = 0; b < MB; ++b) row[b] = x + (int64_t)min(16 * b + frow, T - 1) * stride;
+    for (int b = 0; b < MB; ++b) row[b] = x + (int64_t)min(r0 + 16 * b + frow, T - 1) * stride;
     auto load = [&](int b, int k) {
         const int h = k * 32 + 8 * fq;
         u32x4 o = {0u, 0u, 0u, 0u};
@@ -152,7 +160,7 @@ __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(NB 
     const int v = v0 + Meet::col();
 #pragma unroll
     for (int q = 0; q < Meet::kPasses; ++q) {
-        const int m = Meet::row(q);
+        const int m = r0 + Meet::row(q);
         const int target = tgt[q];
         float top = -__builtin_inff();
 #pragma unroll
@@ -186,6 +194,7 @@ __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(MB 
     __shared__ __attribute__((aligned(16))) FewLds<NB, MB> lds;
     const int t = threadIdx.x, lane = t & 63, frow = lane & 15, fq = lane >> 4;
     const int cols = (Hp + kFewCols - 1) / kFewCols, part = (int)blockIdx.x / cols, h0 = (int)blockIdx.x % cols * kFewCols;
+    const int r0 = (int)blockIdx.y * kFewRows;
     // in pairs of K steps
     const int pairs = Vp / 64, p0 = (int)((int64_t)pairs * part / parts), p1 = (int)((int64_t)pairs * (part + 1) / parts);
     f32x4 acc[NB][MB];
@@ -207,11 +216,11 @@ __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(MB 
         }
     } else {
 #pragma unroll
-        for (int b = 0; b < MB; ++b) m[b] = run[min(16 * b + frow, T - 1)].m;
+        for (int b = 0; b < MB; ++b) m[b] = run[min(r0 + 16 * b + frow, T - 1)].m;
     }
     auto load = [&](int b, int k) {
-        const u32x4 v = *reinterpret_cast<const u32x4*>(a + block_at(16 * b + frow, k * 32 + 8 * fq, a_kt));
-        const float f = exp2f(fminf(stats[(int64_t)((k * 32 + 8 * fq) >> stat_shift) * T + min(16 * b + frow, T - 1)].m - m[b], 0.0f));     // (a group of nothing but the target has no M)
+        const u32x4 v = *reinterpret_cast<const u32x4*>(a + block_at(r0 + 16 * b + frow, k * 32 + 8 * fq, a_kt));
+        const float f = exp2f(fminf(stats[(int64_t)((k * 32 + 8 * fq) >> stat_shift) * T + min(r0 + 16 * b + frow, T - 1)].m - m[b], 0.0f));     // (a group of nothing but the target has no M)
         u32x4 o;
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] = S::pack(S::lo(v[e]) * f, S::hi(v[e]) * f);
@@ -225,14 +234,15 @@ __global__ __launch_bounds__(kFewThreads) __attribute__((amdgpu_waves_per_eu(MB 
     if (t >= Meet::kUsed) return;
 #pragma unroll
     for (int q = 0; q < Meet::kPasses; ++q) {
-        const int row = Meet::row(q), h = h0 + Meet::col();
+        const int row = r0 + Meet::row(q), h = h0 + Meet::col();
         if (row < T) *reinterpret_cast<f32x4*>(acc_out + ((int64_t)part * T + row) * Hp + h) = out[q];
     }
 }
 
 void launch_ce_few_logits(const CeArgs& c, sasq_dtype dt, hipStream_t st)
 {
-    const int grid = c.Vp / c.few_cols, mb = (int)((c.T + 15) / 16);
+    const dim3 grid(c.Vp / c.few_cols, (unsigned)((c.T + kFewRows - 1) / kFewRows));
+    const int mb = (int)((c.T + 15) / 16);
     const bool vec = c.x_stride % 8 == 0 && c.H % 8 == 0;
     auto launch = [&](auto d, auto nb, auto m, auto v, auto g) {
         ce_few_logits_kernel<decltype(d)::value, decltype(nb)::value, decltype(m)::value, decltype(v)::value, decltype(g)::value><<<grid, kFewThreads, 0, st>>>(
@@ -257,7 +267,8 @@ void launch_ce_few_logits(const CeArgs& c, sasq_dtype dt, hipStream_t st)
 
 void launch_ce_few_grad(const CeArgs& c, sasq_dtype dt, hipStream_t st)
 {
-    const int mb = (int)((c.T + 15) / 16), grid = (c.Hp + kFewCols - 1) / kFewCols * c.few_parts, stat_shift = c.few_cols == 16 ? 4 : c.few_cols == 32 ? 5 : 6;
+    const dim3 grid((c.Hp + kFewCols - 1) / kFewCols * c.few_parts, (unsigned)((c.T + kFewRows - 1) / kFewRows));
+    const int mb = (int)((c.T + 15) / 16), stat_shift = c.few_cols == 16 ? 4 : c.few_cols == 32 ? 5 : 6;
     auto go = [&](auto d, auto m) {
         if (c.few_own_join)
             ce_few_grad_kernel<decltype(d)::value, decltype(m)::value, true><<<grid, kFewThreads, 0, st>>>(

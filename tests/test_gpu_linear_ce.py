@@ -67,6 +67,14 @@ def test_few_rows_of_long_ones(T, V, H, dtype, left_out, grad):
     check(call(p, grad=grad, scale=32.0), p.reference(scale=32.0, device="cuda"))
 
 
+@pytest.mark.parametrize("dtype,left_out,grad", [("f16", 0.0, True), ("bf16", 0.4, True), ("f16", 0.4, False)])
+@pytest.mark.parametrize("T,V,H", [(65, 600, 104), (100, 8192, 512), (128, 8200, 64), (193, 1000, 2048), (500, 513, 2056), (1000, 700, 256), (2048, 65, 72), (2049, 65, 72)])
+def test_many_rows_of_small_heads(T, V, H, dtype, left_out, grad):
+    """Up to 2048 rows go by 64 a workgroup where the head is small; limits of that."""
+    p = Head(T, V, H, dtype, seed=T + V, left_out=left_out)
+    check(call(p, grad=grad, scale=32.0), p.reference(scale=32.0, device="cuda"))
+
+
 @pytest.mark.parametrize("T,V,H", [(4093, 300, 64), (8191, 300, 64), (8193, 300, 64), (9001, 130, 100), (20000, 65, 72)])
 def test_many_rows_packed(T, V, H):
     """The rows that count are packed by the kernel that stages them, or, where they are many, by one of its own."""
