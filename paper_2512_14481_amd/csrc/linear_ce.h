@@ -33,7 +33,7 @@ struct CeArgs {
     int64_t T, V, H;
     int Hp, Vp;                                 // H and V in whole multiples of 64
     int piece, first_piece;                     // columns of a piece, and of the first
-    int slots, max_splits;                      // parts that its contraction is cut into: as many as fill the slots of the chip (splits_of)
+    int slots, max_splits;                      // parts that its contraction is cut into: as many as fill the slots of the chip (grad_parts)
     int tile, grad_tile;                        // 0: 256x256, 2: 128x128
     bool grad;
     int few_parts;                              // few rows (linear_ce_few.hip): parts of the gradient's contraction, 0: the tiles
@@ -63,12 +63,23 @@ struct CeArgs {
     uint16_t* a;                                // a_v of a piece, rows and columns in the same blocks
     float* acc;                                 // [parts][counted rows][Hp]
 };
-// Parts of the contraction for so many counted rows.
-__host__ __device__ inline int splits_of(int64_t rows, int bm, int tiles_n, int slots, int max_splits)
+// Parts of the gradient's contraction for so many counted rows: as many as fill the slots of the chip.  A last row of 256x256 tiles of at most 128 rows is of
+// halves, which take 0.65 of the time, and has fewer and longer parts.
+struct GradParts {
+    int tiles;                                  // rows of whole tiles, with `full` parts each
+    int full, half;                             // half: parts of the halves behind them, 0: there are none
+    __host__ __device__ int of_row(int64_t row, int bm) const { return row < (int64_t)tiles * bm ? full : half; }
+};
+__host__ __device__ inline GradParts grad_parts(int64_t rows, int bm, int tiles_n, int slots, int max_splits)
 {
-    const int64_t tiles = (rows + bm - 1) / bm * tiles_n;
-    const int64_t s = tiles > 0 ? slots / tiles : 1;
-    return (int)(s < 1 ? 1 : s > max_splits ? max_splits : s);
+    const int rest = (int)(rows % bm);
+    const bool halves = bm == 256 && rest > 0 && rest <= 128;
+    const int64_t tiles = rows / bm + (rest > 0 && !halves);
+    auto clamp = [&](int64_t s, int64_t most) { return (int)(s > most ? most : s < 1 ? 1 : s); };
+    GradParts p{(int)tiles, 0, 0};
+    if (tiles) p.full = clamp(100 * (int64_t)slots / (tiles_n * (100 * tiles + (halves ? 65 : 0))), max_splits);
+    if (halves) p.half = clamp((slots - tiles * p.full * tiles_n) / tiles_n, tiles ? p.full : max_splits);
+    return p;
 }
 constexpr int tile_rows(int tile) { return tile == 0 ? 256 : 128; }
 constexpr int tile_cols(int tile) { return tile_rows(tile); }

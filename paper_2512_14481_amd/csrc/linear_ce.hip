@@ -460,7 +460,7 @@ __global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ ac
     int p = few_parts ? r : pos[r];
     float g = 0.0f, cf = 0.0f, uu = 0.0f;
     int t = 0;
-    const int n = *count, splits = few_parts ? few_parts : splits_of(n, bm, tiles_n, slots, max_splits), rows = few_parts ? T : n;
+    const int n = *count, splits = few_parts ? few_parts : grad_parts(n, bm, tiles_n, slots, max_splits).of_row(p, bm), rows = few_parts ? T : n;
     if (p >= 0) {
         t = tgt[p];
         if (few_parts && (t < 0 || t >= V)) p = -1;
@@ -553,8 +553,10 @@ static int ce_tile(int64_t M, int64_t N, int64_t K)
 // The gradient's tile: its contraction is cut until the chip is full, so what counts is the part of a tile that is used.
 static int ce_grad_tile(int64_t M, int64_t N)
 {
-    auto used = [&](int64_t bm, int64_t bn) { return (double)(M * N) / (double)(up(M, bm) * up(N, bn)); };
-    return 0.8 * used(128, 128) > used(256, 256) ? 2 : 0;
+    const int64_t rest = M % 256;
+    const double rows = (double)(M / 256) + (rest == 0 ? 0.0 : rest <= 128 ? 0.65 : 1.0);
+    const double used256 = (double)(M * N) / (rows * 256.0 * (double)up(N, 256)), used128 = (double)(M * N) / (double)(up(M, 128) * up(N, 128));
+    return 0.8 * used128 > used256 ? 2 : 0;
 }
 
 // Whether the kernels of few rows do the call: up to 64 rows, and where all of it is so small that it is launches that count (four in place of six, and none of

@@ -223,20 +223,11 @@ struct SumsExt {
     }
 };
 
-// The contraction over the piece's columns is cut into parts of whole 64 columns, each with running sums of its own.
+// Part `part` of `splits` of the contraction over the piece's columns, whole 64 columns each, with running sums of its own.
 template <int DT, int BM, int BN>
-__global__ __launch_bounds__(kGemmThreads)
-__attribute__((amdgpu_waves_per_eu(Tile<BM, BN>::kWavesPerSimd, Tile<BM, BN>::kWavesPerSimd)))
-void ce_grad_kernel(const uint16_t* __restrict__ a, const uint8_t* __restrict__ head_grad, const int32_t* __restrict__ count, int H, int Hp,
-                    int cols64, int kt0, int tiles_n, int slots, int max_splits, SumsExt ext)
+__device__ __forceinline__ void grad_part(const uint16_t* a, const uint8_t* head_grad, int M, int H, int Hp, int cols64, int kt0, int part, int splits, int tm, int tn,
+                                          char* lds, SumsExt ext)
 {
-    __shared__ __attribute__((aligned(1024))) char lds[kStages * Tile<BM, BN>::kStageBytes];
-    const int M = *count;
-    const int splits = splits_of(M, BM, tiles_n, slots, max_splits);
-    int tm, tn;
-    if (!tile_of_counted((M + BM - 1) / BM, tiles_n * splits, tm, tn)) return;
-    const int part = tn / tiles_n;
-    tn -= part * tiles_n;
     const int c0 = (int)((int64_t)cols64 * part / splits), c1 = (int)((int64_t)cols64 * (part + 1) / splits);
     ext.acc += (int64_t)part * M * Hp;
     if (c0 == c1) {                             // a last piece of fewer columns than parts
@@ -261,6 +252,31 @@ void ce_grad_kernel(const uint16_t* __restrict__ a, const uint8_t* __restrict__ 
 }
 
 template <int DT, int BM, int BN>
+__global__ __launch_bounds__(kGemmThreads)
+__attribute__((amdgpu_waves_per_eu(Tile<BM, BN>::kWavesPerSimd, Tile<BM, BN>::kWavesPerSimd)))
+void ce_grad_kernel(const uint16_t* __restrict__ a, const uint8_t* __restrict__ head_grad, const int32_t* __restrict__ count, int H, int Hp,
+                    int cols64, int kt0, int tiles_n, int slots, int max_splits, SumsExt ext)
+{
+    __shared__ __attribute__((aligned(1024))) char lds[kStages * Tile<BM, BN>::kStageBytes];
+    const int M = *count;
+    const GradParts parts = grad_parts(M, BM, tiles_n, slots, max_splits);
+    const int whole = (parts.tiles * tiles_n * parts.full + 7) & ~7;
+    int tm, tn;
+    if ((int)blockIdx.x < whole) {
+        if (!tile_of_block((int)blockIdx.x, parts.tiles, tiles_n * parts.full, tm, tn)) return;
+        const int part = tn / tiles_n;
+        grad_part<DT, BM, BN>(a, head_grad, M, H, Hp, cols64, kt0, part, parts.full, tm, tn - part * tiles_n, lds, ext);
+        return;
+    }
+    if constexpr (BM == 256) {
+        const int id = (int)blockIdx.x - whole;
+        if (id >= ((tiles_n * parts.half + 7) & ~7) || !tile_of_block(id, 1, tiles_n * parts.half, tm, tn)) return;
+        const int part = tn / tiles_n;
+        grad_part<DT, 128, BN>(a, head_grad, M, H, Hp, cols64, kt0, part, parts.half, 2 * parts.tiles, tn - part * tiles_n, lds, ext);
+    }
+}
+
+template <int DT, int BM, int BN>
 static void launch_logits(const CeArgs& c, int64_t col0, int64_t cols, hipStream_t st)
 {
     const int tiles_m = (int)((c.T + BM - 1) / BM), tiles_n = (int)((cols + BN - 1) / BN);
@@ -278,11 +294,11 @@ template <int DT, int BM, int BN>
 static void launch_grad(const CeArgs& c, int64_t col0, int64_t cols, hipStream_t st)
 {
     const int tiles_n = (int)((c.H + BN - 1) / BN);
-    const int64_t tiles = (c.T + BM - 1) / BM * tiles_n;
-    // for any number of counted rows: as many tiles as there are slots, or one part
-    const int64_t most = tiles > c.slots ? tiles : tiles * c.max_splits < c.slots ? tiles * c.max_splits : c.slots;
+    const int64_t tiles = (c.T + BM - 1) / BM * tiles_n, all = tiles * c.max_splits;
+    // for any number of counted rows: a part a tile, or as many as there are slots, and a row of halves and what rounds up to whole eights
+    const int64_t most = (tiles > c.slots ? tiles : all < c.slots ? all : c.slots) + tiles_n + 16;
     const SumsExt ext{row_blocks(c.piece), row_blocks(c.Vp), c.acc, col0 ? c.beta : nullptr, c.Hp};
-    ce_grad_kernel<DT, BM, BN><<<(unsigned)((most + 7) / 8 * 8), kGemmThreads, 0, st>>>(
+    ce_grad_kernel<DT, BM, BN><<<(unsigned)most, kGemmThreads, 0, st>>>(
         c.a, c.head_grad, c.count, (int)c.H, c.Hp, (int)((cols + 63) / 64), (int)(col0 / 32), tiles_n, c.slots, c.max_splits, ext);
 }
 
