@@ -351,7 +351,7 @@ __global__ __launch_bounds__(kJoinThreads) void ce_join_kernel(const RowStat* __
 }
 
 // a_v of groups of columns with another M than their row's, in place: sixteen rows and `each` blocks a workgroup, a 1 KB block a wave and access.
-// Bytes: 333 x 100003, all of them, 134 MB in 28 us, 4.8 TB/s; where no row has to be touched 4.6 us, a launch and its wait.  Doing it on the fragments in the
+// Bytes: 333 x 100003, all of them, 134 MB in 24 us, 5.5 TB/s (64 blocks a workgroup 28); where no row has to be touched 4.6 us, a launch and its wait.  Doing it on the fragments in the
 // gradient GEMM instead costs that kernel more: 256x256 tiles 386 -> 448 us (their registers move), 128x128 123 -> 130.
 template <int DT>
 __global__ __launch_bounds__(256) void ce_scale_kernel(uint16_t* __restrict__ a, int a_kt, int kt, int stat_blocks, const RowStat* __restrict__ stats,
@@ -710,7 +710,7 @@ static void ce_run(const CeArgs& c, sasq_dtype dt, hipStream_t st)
         launch_join(c, groups, col0 == 0, col0 + cols >= c.V, st);
         if (c.grad) {
             const int kt = (int)(up(cols, 64) / 32);
-            const int rows16 = (T + 15) / 16, each = kt * rows16 < 64 * 1024 ? 16 : 64;
+            const int rows16 = (T + 15) / 16, each = col0 ? 64 : 16;          // (of later pieces few rows have any: larger workgroups leave sooner)
             ce_scale_kernel<DT><<<dim3(rows16, (kt + each - 1) / each), 256, 0, st>>>(c.a, row_blocks(c.piece), kt, sc / 32, c.stats, c.run, c.scale_rows,
                                                                                       16 / join_rows(groups), c.T, c.count, each);
             launch_ce_grad(c, dt, col0, cols, st);
