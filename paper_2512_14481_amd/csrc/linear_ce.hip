@@ -550,11 +550,13 @@ static int ce_tile(int64_t M, int64_t N, int64_t K)
     const double c2 = (double)(t128 / 512) * two + (rest == 0 ? 0.0 : rest <= 256 ? one : two);
     return c0 <= c2 ? 0 : 2;
 }
-// The gradient's tile: its contraction is cut until the chip is full, so what counts is the part of a tile that is used.
+// The gradient's tile: its contraction is cut until the chip is full, so what counts is the part of a tile that is used, with 0.65 of a tile for a half in
+// rows of 2048 and more; in short ones parts of 256x256 tiles are many, and their sums cost what the halves save.  us, whole call, 128x128 | 256x256 and halves,
+// T x H -> V: 333 x 1376 -> 100003 287 | 295, 300 x 1000 -> 60000 165 | 175, 350 x 2048 -> 100003 406 | 395, 384 x 4096 -> 20000 186 | 180.
 static int ce_grad_tile(int64_t M, int64_t N)
 {
     const int64_t rest = M % 256;
-    const double rows = (double)(M / 256) + (rest == 0 ? 0.0 : rest <= 128 ? 0.65 : 1.0);
+    const double rows = (double)(M / 256) + (rest == 0 ? 0.0 : rest <= 128 && N >= 2048 ? 0.65 : 1.0);
     const double used256 = (double)(M * N) / (rows * 256.0 * (double)up(N, 256)), used128 = (double)(M * N) / (double)(up(M, 128) * up(N, 128));
     return 0.8 * used128 > used256 ? 2 : 0;
 }
