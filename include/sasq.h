@@ -451,7 +451,7 @@ int sasq_linear_bwd_input(const void* dy, const void* wt, void* dx, float* acc_o
  *     dx[i] = scale * g[i] * (sum_v p[v] W[v] - W[t])                  p[v] = exp(z[v] - lse[i])
  * with g[i] = row_weight[i], or 1 / counted rows (the gradient of the mean) where row_weight is NULL.  The logits are not stored: the vocabulary
  * goes by in pieces, and both products of a piece are done before the next.  The head is frozen and has no gradient.
- * A row whose target lies outside [0, V) is left out: loss = lse = 0, dx = 0, whatever its x holds, and no product is done for it.  No counted
+ * A row whose target lies outside [0, V) is left out: loss = lse = 0, dx = 0, whatever its x holds; but for small calls no product is done for it.  No counted
  * row: *mean = 0.
  *   x          [T, H] device 16-bit `dt`, rows x_stride elements apart
  *   head       W as sasq_prepare_head laid it out with SASQ_HEAD_LOGITS;  head_grad: with SASQ_HEAD_GRAD, or NULL without dx

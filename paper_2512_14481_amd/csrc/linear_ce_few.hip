@@ -1,4 +1,4 @@
-// sasq_linear_ce for at most 64 rows (linear_ce.h): both products read the head once, from memory into registers, and are bound by that.
+// sasq_linear_ce for at most 64 rows, or more of a small head, 64 at a time (linear_ce.h): both products read the head once, from memory into registers, and are bound by that.
 //
 // A workgroup has 16 to 64 rows of a head's layout (vocabulary entries for the logits, channels for the gradient) and its eight waves an eighth of the
 // contraction each: a wave loads 1 KB blocks, which are operands of v_mfma_f32_16x16x32 as they lie, and the rows of x (or their exponentials) beside them

@@ -75,6 +75,66 @@ def test_many_rows_of_small_heads(T, V, H, dtype, left_out, grad):
     check(call(p, grad=grad, scale=32.0), p.reference(scale=32.0, device="cuda"))
 
 
+@pytest.mark.parametrize("dtype,left_out,grad", [("f16", 0.0, True), ("bf16", 0.4, True), ("f16", 0.4, False)])
+@pytest.mark.parametrize("T,V,H", [(130, 8209, 65), (300, 8193, 333), (70, 9001, 1), (2100, 513, 65), (65, 8193, 8), (257, 8449, 2049)])
+def test_tiles_of_odd_sizes(T, V, H, dtype, left_out, grad):
+    p = Head(T, V, H, dtype, seed=T + H, left_out=left_out)
+    check(call(p, grad=grad, scale=32.0), p.reference(scale=32.0, device="cuda"))
+
+
+@pytest.mark.parametrize("T,V", [(300, 700), (300, 8300)])
+def test_many_rows_apart_weighted_and_in_place(T, V):
+    """Strides, weights, a scale, the gradient in place of x: 64 rows a workgroup, and tiles."""
+    p = Head(T, V, 72, "bf16", seed=1, left_out=0.2)
+    rw = torch.randn(T, generator=torch.Generator().manual_seed(8))
+    ref = p.reference(row_weight=rw, scale=-3.0, device="cuda")
+    hw = heads(p.w)
+    for pad in (8, 3):
+        x = torch.full((T, 72 + pad), 7.0, dtype=DT["bf16"], device="cuda")
+        x[:, :72] = p.x.cuda()
+        check(call(p, hw=hw, x=x[:, :72], row_weight=rw, scale=-3.0), ref)
+        check(call(p, hw=hw, x=x[:, :72], dx=x[:, :72], row_weight=rw, scale=-3.0), ref)
+        assert (x[:, 72:] == 7.0).all()
+
+
+@pytest.mark.parametrize("T,V", [(130, 700), (150, 8300)])
+def test_many_rows_captured(T, V):
+    """Replayed with other rows left out, as many as none: what eager calls give."""
+    a, b, c = (Head(T, V, 96, "f16", seed=20 + i, left_out=o) for i, o in enumerate((0.3, 0.9, 1.0)))
+    hl, hg = heads(a.w)
+    x, t = a.x.cuda(), a.t.cuda()
+    ws = B.new_workspace(B.sasq_linear_ce_workspace(T, V, 96, True))
+    loss, lse, mean, dx = torch.empty(T, device="cuda"), torch.empty(T, device="cuda"), torch.empty(1, device="cuda"), torch.empty_like(x)
+    run = lambda: B.sasq_linear_ce(x, hl, t, loss, V, ws, lse=lse, mean=mean, dx=dx, head_grad=hg)
+    run()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        run()
+    for p in (b, a, c, b, a):
+        x.copy_(p.x.cuda())
+        t.copy_(p.t.cuda())
+        g.replay()
+        torch.cuda.synchronize()
+        want = call(p, hw=(hl, hg))
+        for got, k in ((loss, "loss"), (lse, "lse"), (mean, "mean"), (dx, "dx")):
+            assert torch.equal(got, want[k]), k
+
+
+@pytest.mark.parametrize("T,V", [(300, 8300), (300, 600)])
+def test_many_rows_of_which_one_is_not_finite(T, V):
+    p = Head(T, V, 64, "f16", seed=43)
+    ref = p.reference(row_weight=torch.ones(T))
+    p.x = p.x.clone()
+    p.x[3, 5], p.x[257, 0] = math.nan, math.inf
+    out = call(p, row_weight=torch.ones(T))
+    ok = torch.ones(T, dtype=torch.bool)
+    ok[3] = ok[257] = False
+    for k in ("loss", "lse", "dx"):
+        v, (want, tol) = out[k].cpu().double(), ref[k]
+        assert ((v - want).abs() <= tol)[ok].all() and not torch.isfinite(v[~ok]).all(), k
+
+
 @pytest.mark.parametrize("T,V,H", [(4093, 300, 64), (8191, 300, 64), (8193, 300, 64), (9001, 130, 100), (20000, 65, 72)])
 def test_many_rows_packed(T, V, H):
     """The rows that count are packed by the kernel that stages them, or, where they are many, by one of its own."""
