@@ -33,6 +33,9 @@
  *   - Workspaces come from sasq_workspace_init(): a workspace is caller-owned device memory
  *     that must have been passed ONCE to sasq_workspace_init before its first use, may be reused
  *     by any number of later calls, and must not be used by two calls that can overlap in time.
+ *     Its first 1024 bytes are control words that the reductions (sasq_absmax_scale, sasq_fakequant_bwd and its
+ *     per-channel and batch forms) find zero and leave zero.  The linears and sasq_paged_attention may write over all
+ *     of theirs: give them a workspace of their own, or initialise it again before a reduction uses it.
  *   - Graph capture: an entry point only launches kernels on the caller's stream (no allocation,
  *     no copy, no memset, no synchronisation), so calls may be recorded into a HIP graph and
  *     replayed; items arrays and other host arguments are read before the call returns.
@@ -229,7 +232,7 @@ int sasq_fakequant_bwd_pc_batch(const sasq_fq_item* items, int count, int bits, 
  *   kept       [rows, cols] device int8, 16-byte aligned, written by the forward, read by the backward
  *   s, ds      device fp32: a scalar, or (pc) [cols];  ds is overwritten, its terms are summed in an order that follows from the sizes
  *   bits       2..8, the same in both directions;  cols (pc): any up to 2^24, multiples of 8 are fast
- *   workspace (backward)  >= the matching query's bytes, 16-byte aligned; needs no initialisation
+ *   workspace (backward)  >= the matching query's bytes, 16-byte aligned; needs no initialisation, and its control words stay as they are
  * The batch forms do up to SASQ_MAX_BATCH tensors in one launch, with the results of the single calls (pc: bit for bit; ds of a whole tensor may
  * differ in the last bits).  items: HOST array, read before the call returns; items must not overlap each other's outputs.
  */
@@ -460,7 +463,8 @@ int sasq_linear_bwd_input(const void* dy, const void* wt, void* dx, float* acc_o
  *   dx         [T, H] device 16-bit `dt`, rows dx_stride apart, written, or NULL: no gradient; may be x itself (with its stride)
  *   T at most 2^23, V 2^22, H 2^20;  any sizes, multiples of 64 of H cost nothing extra
  *   piece      columns of the vocabulary at a time, a multiple of 256, or 0: the library's choice (256 MB of the workspace)
- *   workspace  >= sasq_linear_ce_workspace(T, V, H, dx != NULL, piece) bytes, 16-byte aligned; needs no initialisation
+ *   workspace  >= sasq_linear_ce_workspace(T, V, H, dx != NULL, piece) bytes, 16-byte aligned; needs no initialisation, and its control words stay
+ *              as they are
  * Sums are fp32, those over a row's losses fp64; the exponentials that the gradient contracts with W are rounded to 16 bits, relative to the
  * largest of their row but for the target's, which is kept apart: rows whose target is all but certain lose nothing.  Results do not change from
  * run to run.  Logits must be finite and less than 2^24 in size.

@@ -468,7 +468,7 @@ static void ck_plan(const sasq_ckpt_item* items, int count, bool pc, bool backwa
 {
     b.count = count;
     b.first[0] = 0;
-    size_t at = 0;
+    size_t at = kWsHeaderBytes;                      // the tickets of other calls on this workspace stay as they are
     for (int i = 0; i < count; ++i) {
         const sasq_ckpt_item& it = items[i];
         CkItem& k = b.it[i];
@@ -498,7 +498,7 @@ static void ck_plan(const sasq_ckpt_item* items, int count, bool pc, bool backwa
 static size_t ck_workspace(const sasq_ckpt_item* items, int count, bool pc)
 {
     if (!items || count <= 0 || count > kCkMaxBatch) return 0;
-    size_t bytes = 0;
+    size_t bytes = kWsHeaderBytes;
     for (int i = 0; i < count; ++i) {
         if (items[i].rows <= 0 || items[i].cols <= 0 || items[i].rows > kCkMaxElements / items[i].cols || (pc && items[i].cols > kCkMaxCols)) return 0;
         bytes += ck_partial_bytes(items[i].rows, items[i].cols, pc, count);

@@ -613,7 +613,7 @@ static size_t ce_plan(CeArgs& c, int64_t piece, char* base)
     if (filled > c.T * c.max_splits) filled = c.T * c.max_splits;
     if (sums < filled) sums = filled;
     if (c.few_parts) sums = c.T * c.few_parts;
-    size_t at = 0;
+    size_t at = kWsHeaderBytes;                                        // the tickets of other calls on this workspace stay as they are
     auto part = [&](auto*& p, size_t bytes) {
         p = reinterpret_cast<std::remove_reference_t<decltype(p)>>(base + at);
         at += (bytes + 255) / 256 * 256;
