@@ -467,7 +467,7 @@ int sasq_linear_bwd_input(const void* dy, const void* wt, void* dx, float* acc_o
  *              as they are
  * Sums are fp32, those over a row's losses fp64; the exponentials that the gradient contracts with W are rounded to 16 bits, relative to the
  * largest of their row but for the target's, which is kept apart: rows whose target is all but certain lose nothing.  Results do not change from
- * run to run.  Logits must be finite and less than 2^24 in size.
+ * run to run.  Logits must be finite and less than 2^24 in size, and so must bf16 entries of the head be less than 2^96.
  *
  * sasq_prepare_head lays W [V, H] (16-bit, rows w_stride elements apart) out for the two products, once for a head: 1 KB blocks of 16 rows x 32
  * columns as in sasq_prepare_bwd_weight, rows v and columns h (SASQ_HEAD_LOGITS), or rows h and columns v (SASQ_HEAD_GRAD), the columns padded to

@@ -21,10 +21,11 @@ namespace sasq {
 // (off by 2^-26 of itself: of a logit z, its exponential is off by 2^-26 |z|, less than the product that z is)
 constexpr float kLog2e = 1.44269504088896340736f;
 
-// 16-bit a_v of a wave's own M are at most 2^kTopExp; those of the row's M so far may be 2^kRoom times as much.  fp16 has 2^-24 .. 2^15 to offer, bf16 the
-// exponents of fp32.
+// 16-bit a_v of a wave's own M are at most 2^kTopExp; those of the row's M so far may be 2^kRoom times as much.  fp16 has 2^-24 .. 2^15 to offer.  bf16 has the
+// exponents of fp32, but the fp32 sums of a_v W_v have to hold them too: 2^22 terms of at most 2^8 max |W| stay below 2^128 for entries below 2^98 (room for 2^64
+// in its place left 2^42).  5.5 nats are what a row's largest logit may grow by from piece to piece before its columns are multiplied once more.
 template <int DT> constexpr int kTopExp = DT == SASQ_F16 ? 11 : 0;
-template <int DT> constexpr int kRoom = DT == SASQ_F16 ? 4 : 64;
+template <int DT> constexpr int kRoom = DT == SASQ_F16 ? 4 : 8;
 
 struct RowStat { float m, s; };                 // M (a whole number; -inf: no column yet) and S
 
