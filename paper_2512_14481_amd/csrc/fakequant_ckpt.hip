@@ -3,8 +3,9 @@
 // The backward (Sec. 4.2, Eq. 4 and the chain rule) needs of x only whether it was clamped, and to which end, or else the rounding residual:
 //     dx = dy * m,   ds = sum dy * (m ? e : q),   e = q - x/s in [-1/2, 1/2]
 // The byte c is that residual in units of 1/252, or a mark: 127 above the range, -128 below it.  e is one fused product and difference (exact but for
-// its rounding to fp32), c the nearest whole number of the exact 252 e.  ds then is sum dy * t / 252 with t = c, or 252 q at the ends: each product of a
-// 16-bit dy and t is exact in fp32.  x itself in 8 bits would not do, as the residual is what 8 bits of x leave out.
+// its rounding to fp32), c the nearest whole number of the exact 252 e.  ds then is sum dy * t / 252 with t = c, or 252 q at the ends.  The product of a 16-bit
+// dy and t (7 bits, 13 at the ends) is exact in fp32; bf16 has fp32's exponents, and there t goes by 2^-18, so that neither a product nor the sum of four
+// passes fp32 (what falls below its normal numbers loses 2^-139 of ds at most).  x itself in 8 bits would not do, as the residual is what 8 bits of x leave out.
 //
 // Bound by memory: forward x in, y and the byte out, 5 bytes an element; backward the byte and dy in, dx out, 5 bytes, where the form that keeps x has 6.
 #include "sasq_device.h"
@@ -14,6 +15,7 @@ namespace sasq {
 
 constexpr int kCkThreads = 256, kCkWaves = kCkThreads / kWave, kCkUnroll = 4;
 constexpr float kCkSteps = 252.0f;
+template <int DT> constexpr float kCkUnit = DT == SASQ_BF16 ? 0x1p-18f : 1.0f;       // terms of ds are kCkSteps * kCkUnit times as large
 constexpr int kCkHigh = 127, kCkLow = -128;
 constexpr int kCkCols = kWave * 8;               // columns of a block of the per-channel kernels
 constexpr int kCkMaxBatch = SASQ_MAX_BATCH;
@@ -78,15 +80,16 @@ __device__ __forceinline__ u32x4 ck_fwd_vec(const u32x4& in, const float (&inv_s
     return out;
 }
 
-// 252 times what the byte stands for; m: inside the range.
+// 252 units times what the byte stands for; m: inside the range.
+template <int DT>
 __device__ __forceinline__ float ck_value(int c, float lo252, float hi252, bool& m)
 {
     const bool high = c == kCkHigh, low = c == kCkLow;
     m = !high && !low;
-    return high ? hi252 : low ? lo252 : (float)c;
+    return high ? hi252 : low ? lo252 : (float)c * kCkUnit<DT>;
 }
 
-// dx and the eight terms of ds times 252.
+// dx and the eight terms of ds times 252 units.
 template <int DT>
 __device__ __forceinline__ u32x4 ck_bwd_vec(const u32x2& kept, const u32x4& g, float lo252, float hi252, float (&term)[8])
 {
@@ -96,8 +99,8 @@ __device__ __forceinline__ u32x4 ck_bwd_vec(const u32x2& kept, const u32x4& g, f
     for (int w = 0; w < 4; ++w) {
         bool ma, mb;
         const int c0 = (int)(kept[w >> 1] << (24 - 16 * (w & 1))) >> 24, c1 = (int)(kept[w >> 1] << (16 - 16 * (w & 1))) >> 24;
-        term[2 * w] = S::lo(g[w]) * ck_value(c0, lo252, hi252, ma);
-        term[2 * w + 1] = S::hi(g[w]) * ck_value(c1, lo252, hi252, mb);
+        term[2 * w] = S::lo(g[w]) * ck_value<DT>(c0, lo252, hi252, ma);
+        term[2 * w + 1] = S::hi(g[w]) * ck_value<DT>(c1, lo252, hi252, mb);
         out[w] = g[w] & ((ma ? 0x0000FFFFu : 0u) | (mb ? 0xFFFF0000u : 0u));
     }
     return out;
@@ -158,7 +161,8 @@ __global__ __launch_bounds__(SMALL ? kCkSmallThreads : kCkThreads) void ck_bwd_k
     const int k = SMALL ? (int)blockIdx.x : ck_item_of(b, (int)blockIdx.x);
     const CkItem& it = b.it[k];
     const int64_t block = SMALL ? 0 : (int)blockIdx.x - b.first[k], blocks = SMALL ? 1 : b.first[k + 1] - b.first[k];
-    const float lo = ck_low(bits) * kCkSteps, hi = ck_high(bits) * kCkSteps;
+    constexpr float kPer = kCkSteps * kCkUnit<DT>;
+    const float lo = ck_low(bits) * kPer, hi = ck_high(bits) * kPer;
     const u32x2* kept = reinterpret_cast<const u32x2*>(it.kept);
     const u32x4* dy = reinterpret_cast<const u32x4*>(it.dy);
     u32x4* dx = reinterpret_cast<u32x4*>(it.out);
@@ -192,7 +196,7 @@ __global__ __launch_bounds__(SMALL ? kCkSmallThreads : kCkThreads) void ck_bwd_k
         const int64_t i = nvec * 8 + threadIdx.x;
         bool m;
         const uint16_t g = it.dy[i];
-        acc += (double)(S::one(g) * ck_value(it.kept[i], lo, hi, m));
+        acc += (double)(S::one(g) * ck_value<DT>(it.kept[i], lo, hi, m));
         if (dx) it.out[i] = m ? g : (uint16_t)0;
     }
     __shared__ double part[kWaves];
@@ -202,13 +206,14 @@ __global__ __launch_bounds__(SMALL ? kCkSmallThreads : kCkThreads) void ck_bwd_k
     if (threadIdx.x < kWave) {
         const double all = wave_sum(threadIdx.x < kWaves ? part[threadIdx.x] : 0.0);
         if (threadIdx.x == 0) {
-            if (blocks == 1) *it.ds = (float)(all / (double)kCkSteps);
+            if (blocks == 1) *it.ds = (float)(all / (double)kPer);
             else             static_cast<double*>(it.partial)[block] = all;
         }
     }
 }
 
 // ds of a tensor from its blocks' sums, in a fixed order.
+template <int DT>
 __global__ __launch_bounds__(kCkThreads) void ck_join_kernel(const CkBatch b)
 {
     const CkItem& it = b.it[blockIdx.x];
@@ -224,7 +229,7 @@ __global__ __launch_bounds__(kCkThreads) void ck_join_kernel(const CkBatch b)
     if (threadIdx.x == 0) {
         double all = 0.0;
         for (int i = 0; i < kCkWaves; ++i) all += part[i];
-        *it.ds = (float)(all / (double)kCkSteps);
+        *it.ds = (float)(all / (double)(kCkSteps * kCkUnit<DT>));
     }
 }
 
@@ -340,7 +345,8 @@ __device__ __forceinline__ void ck_bwd_pc_body(const CkItem& it, int block, int 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t cols = it.cols, across = (cols + kCkCols - 1) / kCkCols, cb = block % across, chunk = block / across;
     const int64_t r0 = chunk * it.chunk_rows, r1 = min(it.rows, r0 + it.chunk_rows);
-    const float lo = ck_low(bits) * kCkSteps, hi = ck_high(bits) * kCkSteps;
+    constexpr float kPer = kCkSteps * kCkUnit<DT>;
+    const float lo = ck_low(bits) * kPer, hi = ck_high(bits) * kPer;
     double acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};      // four rows in fp32, everything above that in fp64
     if (!VEC || ck_col<VEC>(cb, lane, 0) < cols) {
         for (int64_t base = r0 + wave; base < r1; base += kCkWaves * kCkUnroll) {
@@ -375,7 +381,7 @@ __device__ __forceinline__ void ck_bwd_pc_body(const CkItem& it, int block, int 
         double all = 0.0;
 #pragma unroll
         for (int w = 0; w < kCkWaves; ++w) all += (double)red[w][c];
-        if (it.chunks == 1) it.ds[cb * kCkCols + c] = (float)(all / (double)kCkSteps);
+        if (it.chunks == 1) it.ds[cb * kCkCols + c] = (float)(all / (double)kPer);
         else                static_cast<float*>(it.partial)[chunk * cols + cb * kCkCols + c] = (float)all;
     }
 }
@@ -393,6 +399,7 @@ __global__ __launch_bounds__(kCkThreads) void ck_bwd_pc_kernel(const CkBatch b, 
 
 // 64 columns a workgroup, a quarter of the row blocks a wave, eight loads in flight; the order of the sum follows from the sizes.
 constexpr int kCkJoinAhead = 8;
+template <int DT>
 __global__ __launch_bounds__(kCkThreads) void ck_join_pc_kernel(const CkBatch b)
 {
     __shared__ double part[kCkWaves][kWave];
@@ -415,7 +422,7 @@ __global__ __launch_bounds__(kCkThreads) void ck_join_pc_kernel(const CkBatch b)
     all = 0.0;
 #pragma unroll
     for (int w = 0; w < kCkWaves; ++w) all += part[w][lane];
-    it.ds[c] = (float)(all / (double)kCkSteps);
+    it.ds[c] = (float)(all / (double)(kCkSteps * kCkUnit<DT>));
 }
 
 // ---- plan ----
@@ -555,11 +562,11 @@ static int ck_bwd(const sasq_ckpt_item* items, int count, bool pc, int bits, sas
         else if (!pc)                ck_bwd_kernel<DT, false><<<grid, kCkThreads, 0, st>>>(b, bits);
         else if (ck_odd_rows(b))     ck_bwd_pc_kernel<DT, true><<<grid, kCkThreads, 0, st>>>(b, bits);
         else                         ck_bwd_pc_kernel<DT, false><<<grid, kCkThreads, 0, st>>>(b, bits);
+        if (join && pc)              ck_join_pc_kernel<DT><<<dim3((unsigned)((widest + kWave - 1) / kWave), (unsigned)count), kCkThreads, 0, st>>>(b);
+        else if (join && !small)     ck_join_kernel<DT><<<count, kCkThreads, 0, st>>>(b);
     };
     if (dt == SASQ_F16) go(std::integral_constant<int, SASQ_F16>{});
     else                go(std::integral_constant<int, SASQ_BF16>{});
-    if (join && pc)          ck_join_pc_kernel<<<dim3((unsigned)((widest + kWave - 1) / kWave), (unsigned)count), kCkThreads, 0, st>>>(b);
-    else if (join && !small) ck_join_kernel<<<count, kCkThreads, 0, st>>>(b);
     return hipGetLastError() == hipSuccess ? SASQ_OK : SASQ_ERR_LAUNCH;
 }
 
