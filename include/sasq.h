@@ -462,9 +462,13 @@ int sasq_linear_bwd_input(const void* dy, const void* wt, void* dx, float* acc_o
  *   loss       [T] device fp32, written;  lse  [T] device fp32 or NULL, written;  mean  device fp32 scalar or NULL, written
  *   dx         [T, H] device 16-bit `dt`, rows dx_stride apart, written, or NULL: no gradient; may be x itself (with its stride)
  *   T at most 2^23, V 2^22, H 2^20;  any sizes, multiples of 64 of H cost nothing extra
- *   piece      columns of the vocabulary at a time, a multiple of 256, or 0: the library's choice (256 MB of the workspace)
+ *   piece      columns of the vocabulary at a time, a multiple of 256, or 0: the library's choice
  *   workspace  >= sasq_linear_ce_workspace(T, V, H, dx != NULL, piece) bytes, 16-byte aligned; needs no initialisation, and its control words stay
  *              as they are
+ *              It holds the counted rows of x, two numbers for every 64 columns of a piece and row (1 GB at most where the library chooses), and with
+ *              the gradient a 16-bit exponential for every column of a piece (about 0.3 GB, or 512 bytes a row where that is more) and the running
+ *              sums, fp32 [rows, H] of T rows or of as many as fill the chip.  The query does not fall where T grows: a workspace for the longest
+ *              batch serves shorter ones (of equal V, H, grad and piece).
  * Sums are fp32, those over a row's losses fp64; the exponentials that the gradient contracts with W are rounded to 16 bits, relative to the
  * largest of their row but for the target's, which is kept apart: rows whose target is all but certain lose nothing.  Results do not change from
  * run to run.  Logits must be finite and less than 2^24 in size, and so must bf16 entries of the head be less than 2^96.

@@ -512,13 +512,14 @@ __global__ __launch_bounds__(256) void ce_dx_kernel(const float* __restrict__ ac
 }
 
 // ---- plan ----
-// Columns of a piece and of the first.  All of them while a_v takes 128 MB at most; without the gradient, while M and S of the waves take 256 MB.
-// Otherwise the first piece, all of whose a_v are read and written once more, has as many tiles of 256x256 as the chip has CUs, and the others a multiple
-// of them (a launch of 880 takes four rounds as one of 1024 does: 7B's logits 951 us in such pieces, 850 so), with 256 MB and about half of the
-// vocabulary at most.
+// Columns of a piece and of the first.  All of them while a_v takes 128 MB at most; without the gradient, while M and S of the waves take 256 MB (512 in
+// groups of 64 columns).  Otherwise the first piece, all of whose a_v are read and written once more, has as many tiles of 256x256 as the chip has CUs, and the others a multiple
+// of them (a launch of 880 takes four rounds as one of 1024 does: 7B's logits 951 us in such pieces, 850 so), with 256 MB (512, 1024) and about half of the
+// vocabulary, but for the rounding to whole rounds, and 256 columns at least.
+constexpr int64_t kRoomGrad = INT64_C(1) << 26, kRoomAlone = INT64_C(1) << 32;      // rows times columns of a single piece
 static void ce_pieces(int64_t T, int64_t V, int64_t piece, bool grad, int& cols, int& first)
 {
-    const int64_t all = up(V, kPieceStep), room = grad ? INT64_C(1) << 26 : INT64_C(1) << 32;
+    const int64_t all = up(V, kPieceStep), room = grad ? kRoomGrad : kRoomAlone;
     if (piece || T <= room / all) {
         cols = first = (int)(piece && piece < all ? piece : all);
         return;
@@ -585,6 +586,43 @@ static int ce_few_cols(const CeArgs& c)
 }
 static int ce_few_groups(const CeArgs& c) { return c.Vp / c.few_cols; }
 
+// Sizes of the parts that do not simply grow with the number of rows: for T rows what any number up to T needs, so that a program may size its workspace for its
+// longest batch.  Each is a bound that grows with T, over both kinds of kernels and of tiles.
+struct CeRoom { int64_t rows, a, stats, sums; };                    // rows staged, bytes of a_v, number of M and S, rows of running sums
+static CeRoom ce_room(const CeArgs& c, int64_t piece)
+{
+    const int64_t T = c.T, all = piece && piece < up(c.V, kPieceStep) ? piece : up(c.V, kPieceStep), room = c.grad ? kRoomGrad : kRoomAlone;
+    CeRoom r;
+    r.rows = T > 32 ? up(T, 64) : up(T, 16);
+    int64_t cells = T * all;
+    r.a = r.rows * row_blocks(all) * 64;
+    if (!piece) {
+        // ce_pieces: one piece of T * cols <= room, or T * cols <= 2 room + T * round, where T * round is 2^16 a tile's rows or 256 T at most; T > room / all there.
+        // a_v has up to 63 rows more (15 in several pieces), and a block a row of blocks.
+        const int64_t rounds = 256 * (T + 63) > (INT64_C(5) << 22) ? 256 * (T + 63) : INT64_C(5) << 22, most = 4 * room + 128 * all + 2 * rounds + 64 * (T + 63);
+        if (r.a > most) r.a = most;
+        if (cells > 2 * room + rounds) cells = 2 * room + rounds;
+    }
+    r.stats = (cells + 63) / 64;
+    if (c.piece >= c.V) {
+        CeArgs few = c;
+        auto groups = [&](int64_t rows) { few.T = rows; return (int64_t)(c.Vp / ce_few_cols(few)); };
+        const int64_t to = c.V <= 8192 ? kFewMost : kFewRows, four = groups(4) * (T < 4 ? T : 4), more = groups(kFewRows) * (T < to ? T : to);
+        if (r.stats < four) r.stats = four;
+        if (r.stats < more) r.stats = more;
+    }
+    // one part of all, or as many parts as there are slots for
+    r.sums = 64 * (512 / (c.Hp / 64));
+    for (const int tile : {0, 2}) {
+        const int64_t filled = (tile == 2 ? 512 : 256) / ((c.H + tile_cols(tile) - 1) / tile_cols(tile)) * tile_rows(tile);
+        if (r.sums < filled) r.sums = filled;
+    }
+    const int64_t splits = all / 512 > 1 ? all / 512 : 1;
+    if (r.sums > T * splits) r.sums = T * splits;
+    if (r.sums < T) r.sums = T;
+    return r;
+}
+
 // Sizes and the workspace's parts, from `base` (0: only how long they are).
 static size_t ce_plan(CeArgs& c, int64_t piece, char* base)
 {
@@ -604,21 +642,15 @@ static size_t ce_plan(CeArgs& c, int64_t piece, char* base)
     }
     c.tile = ce_tile(c.T, c.piece, c.Hp);
     c.grad_tile = ce_grad_tile(c.T, c.H);
-    const int bm = tile_rows(c.grad_tile), bn = tile_cols(c.grad_tile), sc = stat_cols(c.tile);
-    const int64_t tiles_n = (c.H + bn - 1) / bn;
     c.slots = c.grad_tile == 2 ? 512 : 256;
     c.max_splits = c.piece / 512 > 1 ? c.piece / 512 : 1;
-    // rows of sums, whatever number of rows counts: one part of all, or as many parts as there are slots for
-    int64_t sums = c.T, filled = c.slots / tiles_n * bm;
-    if (filled > c.T * c.max_splits) filled = c.T * c.max_splits;
-    if (sums < filled) sums = filled;
-    if (c.few_parts) sums = c.T * c.few_parts;
+    const CeRoom room = ce_room(c, piece);
     size_t at = kWsHeaderBytes;                                        // the tickets of other calls on this workspace stay as they are
     auto part = [&](auto*& p, size_t bytes) {
         p = reinterpret_cast<std::remove_reference_t<decltype(p)>>(base + at);
         at += (bytes + 255) / 256 * 256;
     };
-    const size_t T = (size_t)c.T, T16 = c.few_parts && T > 32 ? (T + 63) / 64 * 64 : (T + 15) / 16 * 16, groups = (size_t)(c.few_parts ? ce_few_groups(c) : c.piece / sc);
+    const size_t T = (size_t)c.T;
     part(c.count, 4);
     part(c.ticket, 4);
     part(c.pos, T * 4);
@@ -630,12 +662,12 @@ static size_t ce_plan(CeArgs& c, int64_t piece, char* base)
     part(c.coef, T * 4);
     part(c.u, T * 4);
     part(c.part, (T + 3) / 4 * 8);
-    part(c.stats, groups * T * 8);
-    part(c.xs, T16 * row_blocks(c.Hp) * 64);
+    part(c.stats, (size_t)room.stats * 8);
+    part(c.xs, (size_t)room.rows * row_blocks(c.Hp) * 64);
     if (c.grad) {
         part(c.scale_rows, (T + 3) / 4);
-        part(c.a, T16 * row_blocks(c.piece) * 64);
-        part(c.acc, (size_t)sums * (size_t)c.Hp * 4);
+        part(c.a, (size_t)room.a);
+        part(c.acc, (size_t)room.sums * (size_t)c.Hp * 4);
     }
     return at;
 }

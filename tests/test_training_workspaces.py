@@ -19,3 +19,30 @@ def test_control_words_are_not_part_of_what_is_written(rows, cols):
         up = lambda n: -(-n // 256) * 256
         least = 2 * 256 + 7 * up(4 * rows) + up(8 * rows) + up(-(-rows // 4) * 8) + up(-(-rows // 16) * 16 * (-(-cols // 64) * 2 | 1) * 64)
         assert B.sasq_linear_ce_workspace(rows, 1000, cols, grad) >= HEADER + least
+
+
+@pytest.mark.parametrize("V,H", [(32000, 4096), (128256, 4096), (100003, 1376), (1000, 256), (513, 2056), (8192, 512), (8200, 64), (1, 1), (4000000, 64), (300000, 8192), (700, 100000)])
+@pytest.mark.parametrize("grad", [False, True])
+@pytest.mark.parametrize("piece", [0, 256, 4096, 1 << 22])
+def test_the_longest_batch_is_enough_for_shorter_ones(V, H, grad, piece):
+    """A program sizes its workspace once: what a number of rows needs, no smaller number needs more."""
+    need, before = B._lib().sasq_linear_ce_workspace, 0
+    lengths = [*range(1, 5000), *range(5000, 20000, 37), *range(20000, 140000, 997), *(1 << k for k in range(18, 24))]
+    for T in lengths:
+        n = need(T, V, H, grad, piece)
+        if n == 0:
+            assert T * min(piece or 1, V) > 1 << 36 or T * H > 1 << 36        # refused for its size
+            continue
+        assert n >= before, (T, n, before)
+        before = n
+
+
+def test_what_a_long_batch_needs():
+    """No more than the exponentials of a piece, 0.3 GB or 512 bytes a row, with a gradient; the running sums; x once more; M and S."""
+    need = B._lib().sasq_linear_ce_workspace
+    for T, V, H in ((4096, 32000, 4096), (8192, 32000, 8192), (8192, 128256, 8192), (1 << 17, 32000, 1024), (1 << 20, 32000, 64), (1777, 32000, 5120)):
+        Hp = -(-H // 64) * 64
+        rest = 2 * T * (Hp + 32) + max(T, 8192 * 1024 // Hp + 256) * Hp * 4 + 64 * T + (1 << 20)
+        stats = ((1 << 27) + (5 << 22) + 256 * (T + 63)) / 8                   # 8 bytes for 64 columns and row of a piece: twice 2^26, and a round of tiles more
+        assert need(T, V, H, 1, 0) <= max(0.33e9, 600 * T) * 1.07 + stats + rest, (T, V, H)
+        assert need(T, V, H, 0, 0) <= min(T * V / 8 * 1.01, 1.1e9) + rest
