@@ -232,7 +232,8 @@ int sasq_fakequant_bwd_pc_batch(const sasq_fq_item* items, int count, int bits, 
  *   kept       [rows, cols] device int8, 16-byte aligned, written by the forward, read by the backward
  *   s, ds      device fp32: a scalar, or (pc) [cols];  ds is overwritten, its terms are summed in an order that follows from the sizes
  *   bits       2..8, the same in both directions;  cols (pc): any up to 2^24, multiples of 8 are fast
- *   workspace (backward)  >= the matching query's bytes, 16-byte aligned; needs no initialisation, and its control words stay as they are
+ *   workspace (backward)  >= the matching query's bytes, 16-byte aligned; needs no initialisation, and its control words stay as they are.  The
+ *              query does not fall where tensors, rows or columns are added: a workspace for the largest batch serves smaller ones
  * The batch forms do up to SASQ_MAX_BATCH tensors in one launch, with the results of the single calls (pc: bit for bit; ds of a whole tensor may
  * differ in the last bits).  items: HOST array, read before the call returns; items must not overlap each other's outputs.
  */
@@ -471,7 +472,7 @@ int sasq_linear_bwd_input(const void* dy, const void* wt, void* dx, float* acc_o
  *              batch serves shorter ones (of equal V, H, grad and piece).
  * Sums are fp32, those over a row's losses fp64; the exponentials that the gradient contracts with W are rounded to 16 bits, relative to the
  * largest of their row but for the target's, which is kept apart: rows whose target is all but certain lose nothing.  Results do not change from
- * run to run.  Logits must be finite and less than 2^24 in size, and so must bf16 entries of the head be less than 2^96.
+ * run to run.  Logits must be finite and less than 2^24 in size, entries of a bf16 head less than 2^96.
  *
  * sasq_prepare_head lays W [V, H] (16-bit, rows w_stride elements apart) out for the two products, once for a head: 1 KB blocks of 16 rows x 32
  * columns as in sasq_prepare_bwd_weight, rows v and columns h (SASQ_HEAD_LOGITS), or rows h and columns v (SASQ_HEAD_GRAD), the columns padded to

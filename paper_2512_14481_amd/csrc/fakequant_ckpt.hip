@@ -441,17 +441,24 @@ static int64_t ck_chunk_rows(int64_t rows, int64_t cols)
     while ((rows + r - 1) / r > 256) r *= 2;
     return r;
 }
+// Most row blocks of a tensor of at most so many rows and any columns: ck_chunk_rows has 16 rows in a block at least, and 256 blocks at most.
+static int64_t ck_most_chunks(int64_t rows)
+{
+    if (rows <= 64) return 1;
+    const int64_t n = (rows + 15) / 16;
+    return n < 256 ? n : 256;
+}
 constexpr int64_t kCkMaxElements = INT64_C(1) << 40, kCkMaxCols = INT64_C(1) << 24;
 constexpr int64_t kCkMaxBlocks = INT64_C(1) << 23;       // a launch holds fewer than 2^32 threads
 
 // Workgroups of a tensor in the backward, a power of two: three tensors of an 8192-row 70B MLP 327 us with 512 each, 344 with 682, 337 with 1024, 370 with 256; one of
 // 8192 x 8192 66.8 with 512, 63.3 with 2048.
 static int ck_partials(int count) { return count == 1 ? 2048 : count == 2 ? 1024 : 512; }
+// What a tensor's partial sums take; in a batch of so many.  A workspace serves fewer tensors, rows and columns too.
 static size_t ck_partial_bytes(int64_t rows, int64_t cols, bool pc, int count)
 {
-    if (!pc) return ((size_t)ck_partials(count) * sizeof(double) + 255) / 256 * 256;
-    const int64_t r = ck_chunk_rows(rows, cols), chunks = (rows + r - 1) / r;
-    return ((size_t)(chunks * cols) * sizeof(float) + 255) / 256 * 256;
+    if (!pc) return (size_t)ck_partials(count) * sizeof(double);
+    return ((size_t)(ck_most_chunks(rows) * cols) * sizeof(float) + 255) / 256 * 256;
 }
 
 static int ck_check(const sasq_ckpt_item* items, int count, bool pc, bool backward, int bits, int dt)
@@ -510,7 +517,8 @@ static size_t ck_workspace(const sasq_ckpt_item* items, int count, bool pc)
         if (items[i].rows <= 0 || items[i].cols <= 0 || items[i].rows > kCkMaxElements / items[i].cols || (pc && items[i].cols > kCkMaxCols)) return 0;
         bytes += ck_partial_bytes(items[i].rows, items[i].cols, pc, count);
     }
-    return bytes;
+    const size_t one = kWsHeaderBytes + ck_partial_bytes(1, 1, false, 1);       // (one tensor has as many workgroups as four have)
+    return pc || bytes > one ? bytes : one;
 }
 
 static bool ck_odd_rows(const CkBatch& b)

@@ -46,3 +46,26 @@ def test_what_a_long_batch_needs():
         stats = ((1 << 27) + (5 << 22) + 256 * (T + 63)) / 8                   # 8 bytes for 64 columns and row of a piece: twice 2^26, and a round of tiles more
         assert need(T, V, H, 1, 0) <= 0.35e9 + 600 * T + stats + rest, (T, V, H)
         assert need(T, V, H, 0, 0) <= min(T * V / 8 * 1.01, 1.1e9) + rest
+
+
+def batch(*shapes):
+    arr = (B._CkptItem * len(shapes))()
+    for it, (rows, cols) in zip(arr, shapes):
+        it.rows, it.cols = rows, cols
+    return arr
+
+
+@pytest.mark.parametrize("pc", ["", "_pc"])
+def test_the_largest_batch_of_tensors_is_enough_for_smaller_ones(pc):
+    """Fewer tensors, fewer rows, fewer columns: none needs more."""
+    need = getattr(B._lib(), f"sasq_fakequant_bwd{pc}_ckpt_batch_workspace")
+    for shape in ((64, 256), (700, 1000), (8192, 8192), (1777, 13824)):
+        sizes = [need(batch(*[shape] * n), n) for n in range(1, 9)]
+        assert sizes[0] > HEADER and sizes == sorted(sizes), (shape, sizes)
+    rows = [*range(1, 600), *range(600, 70000, 61), *(1 << k for k in range(17, 25))]
+    for cols in (8, 1000, 4096, 40000):
+        sizes = [need(batch((r, cols)), 1) for r in rows]
+        assert sizes == sorted(sizes), cols
+    for r in (64, 1000, 5000):
+        sizes = [need(batch((r, c)), 1) for c in range(8, 40000, 56)]
+        assert sizes == sorted(sizes), r
