@@ -551,13 +551,15 @@ static int ce_tile(int64_t M, int64_t N, int64_t K)
     const double c2 = (double)(t128 / 512) * two + (rest == 0 ? 0.0 : rest <= 256 ? one : two);
     return c0 <= c2 ? 0 : 2;
 }
-// The gradient's tile: its contraction is cut until the chip is full, so what counts is the part of a tile that is used, with 0.65 of a tile for a half in
-// rows of 2048 and more; in short ones parts of 256x256 tiles are many, and their sums cost what the halves save.  us, whole call, 128x128 | 256x256 and halves,
-// T x H -> V: 333 x 1376 -> 100003 287 | 295, 300 x 1000 -> 60000 165 | 175, 350 x 2048 -> 100003 406 | 395, 384 x 4096 -> 20000 186 | 180.
-static int ce_grad_tile(int64_t M, int64_t N)
+// The gradient's tile: its contraction is cut until the chip is full, so what counts is the part of a tile that is used, with 0.65 of a tile for a half where
+// rows are of 2048 and more and the piece has more than 8192 columns.  In short rows parts of 256x256 tiles are many, and their sums cost what the halves save; of
+// short pieces there are too few parts to fill the chip with such tiles.  us, whole call, 128x128 | 256x256 and halves, T x H -> V: 333 x 1376 -> 100003 289 | 291,
+// 300 x 1000 -> 60000 163 | 169, 350 x 2048 -> 100003 389 | 377, 384 x 4096 -> 20000 184 | 179; 300 x 4096 -> 1000 55 | 70, -> 2000 62 | 73, -> 4000 68 | 78,
+// -> 8000 97 | 102.
+int ce_grad_tile(int64_t M, int64_t N, int64_t columns)
 {
     const int64_t rest = M % 256;
-    const double rows = (double)(M / 256) + (rest == 0 ? 0.0 : rest <= 128 && N >= 2048 ? 0.65 : 1.0);
+    const double rows = (double)(M / 256) + (rest == 0 ? 0.0 : rest <= 128 && N >= 2048 && columns > 8192 ? 0.65 : 1.0);
     const double used256 = (double)(M * N) / (rows * 256.0 * (double)up(N, 256)), used128 = (double)(M * N) / (double)(up(M, 128) * up(N, 128));
     return 0.8 * used128 > used256 ? 2 : 0;
 }
@@ -641,7 +643,7 @@ static size_t ce_plan(CeArgs& c, int64_t piece, char* base)
         c.few_own_join = c.grad && c.T <= kFewRows && c.T * ce_few_groups(c) <= kFewOwnJoin;
     }
     c.tile = ce_tile(c.T, c.piece, c.Hp);
-    c.grad_tile = ce_grad_tile(c.T, c.H);
+    c.grad_tile = ce_grad_tile(c.T, c.H, c.piece);
     c.slots = c.grad_tile == 2 ? 512 : 256;
     c.max_splits = c.piece / 512 > 1 ? c.piece / 512 : 1;
     const CeRoom room = ce_room(c, piece);
