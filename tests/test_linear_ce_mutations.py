@@ -1,4 +1,5 @@
-"""What the narrow bounds of tests/ce_sharp.py can see, on the host: results of a mistaken kernel, made from the definition in 64 bits, are outside of them at every size."""
+"""What the narrow bounds of tests/ce_sharp.py can see, on the host: results of a mistaken kernel, made from the definition in 64 bits, are outside of them at every size.
+A row's bounds do not depend on the others, so 260 of a size's rows are enough here."""
 from __future__ import annotations
 
 import math
@@ -10,18 +11,16 @@ from tests.ce_ref import DT, check
 from tests.ce_sharp import PIECES, SIZES, Sharp
 
 
-def rejected(ref, **got):
-    values = {k: ref[k][0].clone() for k in ("loss", "lse", "dx")}
-    for k, (rows, v) in got.items():
-        values[k][rows] = v
+def rejected(ref, row, **got):
+    """Whether a row of results lies outside."""
     try:
-        check(values, ref)
+        check(got, {k: (ref[k][0][row], ref[k][1][row]) for k in got})
     except AssertionError:
         return True
     return False
 
 
-ALL = sorted({s[:3] for s in SIZES} | {p[:3] for p in PIECES}, key=lambda s: s[0] * s[1] * s[2])
+ALL = sorted({(min(s[0], 260), *s[1:3]) for s in SIZES + PIECES}, key=lambda s: s[0] * s[1] * s[2])
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
@@ -39,8 +38,10 @@ def test_a_mistake_is_outside_the_bounds(T, V, H, dtype):
         dd = d[i] + math.log1p(-min(float(lost), 1 - 1e-15))
         return torch.nn.functional.softplus(dd, threshold=1e9)
 
-    def dx_of(i, factor, sums=1.0):                            # columns' exponentials times `factor`, in the gradient; its S times `sums`
-        return torch.sigmoid(d[i]) / n * ((q[i] * factor) @ w / sums - w[t[i]])
+    mean = q @ w
+
+    def dx_of(i, cols, factor, sums=1.0):                      # some columns' exponentials times `factor`, in the gradient; its S times `sums`
+        return torch.sigmoid(d[i]) / n * ((mean[i] + (factor - 1.0) * (q[i, cols] @ w[cols])) / sums - w[t[i]])
 
     for width in (16, 64, 128):
         groups = -(-V // width)
@@ -52,29 +53,25 @@ def test_a_mistake_is_outside_the_bounds(T, V, H, dtype):
             i = int(row[c])
             cols = slice(c * width, min(V, (c + 1) * width))
             lost = loss_of(i, share[i, c])
-            seen += rejected(ref, loss=(rows[i], lost), lse=(rows[i], zt[i] + lost))
+            seen += rejected(ref, rows[i], loss=lost, lse=zt[i] + lost)
             for factor, sums in ((0.0, 1 - float(share[i, c])), (0.0, 1.0), (2.0, 1.0), (0.25, 1.0)):
-                f = torch.ones(V, dtype=torch.float64)
-                f[cols] = factor
-                if rejected(ref, dx=(rows[i], dx_of(i, f, max(sums, 1e-15)))):
-                    seen_dx += 1
+                seen_dx += rejected(ref, rows[i], dx=dx_of(i, cols, factor, max(sums, 1e-15)))
         # a group without a column that any row leans on is seen by no bound; where there are rows for all of them, all are seen
         assert seen >= 0.9 * len(chosen) if T >= 16 else seen >= min(len(chosen), 2), (width, seen, len(chosen))
         least = 0.75 if T * 4 >= groups else 0.5 * T / groups
         assert seen_dx >= max(1, least * 4 * len(chosen)), (width, seen_dx, 4 * len(chosen))
     # a part of the contraction that is left out, or added twice; a pass of scaling that misses the first tenth
+    def heaviest(cols):                                        # the row that leans on them most
+        return int((q[:, cols].sum(1) * torch.sigmoid(d)).argmax())
+
     for parts in (2, 4, 8):
         for part in range(parts):
-            f = torch.ones(V, dtype=torch.float64)
-            f[V * part // parts:V * (part + 1) // parts] = 0.0
-            if f.all():
-                continue
-            i = int(((q * (1 - f)).sum(1) * torch.sigmoid(d)).argmax())
-            assert rejected(ref, dx=(rows[i], dx_of(i, f))) and rejected(ref, dx=(rows[i], dx_of(i, 2 - f))), (parts, part)
-    f = torch.ones(V, dtype=torch.float64)
-    f[:max(1, V // 10)] = 0.25
-    i = int(((q * (1 - f)).sum(1) * torch.sigmoid(d)).argmax())
-    assert rejected(ref, dx=(rows[i], dx_of(i, f)))
+            cols = slice(V * part // parts, V * (part + 1) // parts)
+            i = heaviest(cols)
+            assert all(rejected(ref, rows[i], dx=dx_of(i, cols, factor)) for factor in (0.0, 2.0)), (parts, part)
+    cols = slice(0, max(1, V // 10))
+    i = heaviest(cols)
+    assert rejected(ref, rows[i], dx=dx_of(i, cols, 0.25))
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
