@@ -466,7 +466,7 @@ int sasq_linear_bwd_input(const void* dy, const void* wt, void* dx, float* acc_o
  *   piece      columns of the vocabulary at a time, a multiple of 256, or 0: the library's choice
  *   workspace  >= sasq_linear_ce_workspace(T, V, H, dx != NULL, piece) bytes, 16-byte aligned; needs no initialisation, and its control words stay
  *              as they are
- *              It holds the counted rows of x, two numbers for every 64 columns of a piece and row (1 GB at most where the library chooses), and with
+ *              It holds the counted rows of x, two numbers for every 64 columns of a piece and row (1.4 GB at most where the library chooses), and with
  *              the gradient a 16-bit exponential for every column of a piece (0.35 GB and 600 bytes a row at most where the library chooses) and the running
  *              sums, fp32 [rows, H] of T rows or of as many as fill the chip.  The query does not fall where T grows: a workspace for the longest
  *              batch serves shorter ones (of equal V, H, grad and piece).

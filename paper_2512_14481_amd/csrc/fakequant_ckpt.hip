@@ -237,7 +237,8 @@ __global__ __launch_bounds__(kCkThreads) void ck_join_kernel(const CkBatch b)
 // Bytes: a 13B layer's seven, forward 56.7 us, 343 MB, 6.1 TB/s, backward 75.5 us, 404 MB, 5.4.  Blocks next to each other take columns next to each other (rows
 // below each other 153 us for both, so 149), and what the backward reads, once, passes the caches by (145).
 // A block takes 512 columns of a run of rows, each of its waves every fourth of them.  VEC: a lane has eight columns next to each other and a row's
-// elements in one access; otherwise (rows that are no multiple of eight) every 64th column, an access each.
+// elements in one access; otherwise (rows that are no multiple of eight) every 64th column, an access of 2 bytes or 1 each: 4096 x 4097 forward 44 us, backward 26,
+// where 4104 columns take 21 and 25 (4096 15 and 21), 1777 x 13825 45 and 32 where 13824 take 22 and 26.
 template <bool VEC>
 __device__ __forceinline__ int64_t ck_col(int64_t col_block, int lane, int e) { return col_block * kCkCols + (VEC ? lane * 8 + e : e * kWave + lane); }
 
@@ -347,7 +348,7 @@ __device__ __forceinline__ void ck_bwd_pc_body(const CkItem& it, int block, int 
     const int64_t r0 = chunk * it.chunk_rows, r1 = min(it.rows, r0 + it.chunk_rows);
     constexpr float kPer = kCkSteps * kCkUnit<DT>;
     const float lo = ck_low(bits) * kPer, hi = ck_high(bits) * kPer;
-    double acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};      // four rows in fp32, everything above that in fp64
+    double acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};      // four rows in fp32; a wave's sum and a block's are rounded to fp32 on their way, all else is added in fp64
     if (!VEC || ck_col<VEC>(cb, lane, 0) < cols) {
         for (int64_t base = r0 + wave; base < r1; base += kCkWaves * kCkUnroll) {
             u32x2 kp[kCkUnroll];
@@ -451,8 +452,10 @@ static int64_t ck_most_chunks(int64_t rows)
 constexpr int64_t kCkMaxElements = INT64_C(1) << 40, kCkMaxCols = INT64_C(1) << 24;
 constexpr int64_t kCkMaxBlocks = INT64_C(1) << 23;       // a launch holds fewer than 2^32 threads
 
-// Workgroups of a tensor in the backward, a power of two: three tensors of an 8192-row 70B MLP 327 us with 512 each, 344 with 682, 337 with 1024, 370 with 256; one of
-// 8192 x 8192 66.8 with 512, 63.3 with 2048.
+// Workgroups of a tensor in the backward, a power of two, by the number of tensors (what a small one does not fill it does not launch): one of 8192 x 8192 66.8 us
+// with 512, 63.3 with 2048; three of an 8192-row 70B MLP 327 with 512 each, 344 with 682, 337 with 1024, 370 with 256.  Of others the choice is within 3 % of the best:
+// 512 | 1024 | 2048 for two of 8192 x 8192 117.0 | 118.3 | 117.6, two of 2048 x 4096 18.5 | 19.0 | 18.8; 256 | 512 | 1024 for four of 2048 x 4096 33.0 | 31.7 | 32.1,
+// five 39.6 | 40.2 | 38.8, seven 53.9 | 53.6 | 52.0, eight 60.0 | 59.1 | 58.5.
 static int ck_partials(int count) { return count == 1 ? 2048 : count == 2 ? 1024 : 512; }
 // What a tensor's partial sums take; in a batch of so many.  A workspace serves fewer tensors, rows and columns too.
 static size_t ck_partial_bytes(int64_t rows, int64_t cols, bool pc, int count)

@@ -13,6 +13,7 @@ constexpr int kPieceStep = 256;
 static int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 
 // ---- the head's two layouts: 1 KB blocks of 16 rows x 32 columns, chunks swizzled as in every operand of the GEMMs ----
+// Once a head, bound by bytes: 32000 x 4096, 524 MB in and out, 96 us (5.5 TB/s) for the logits, 111 us (4.8) turned for the gradient.
 __device__ __forceinline__ uint16_t head_at(const uint16_t* w, int64_t stride, int64_t v, int64_t h, int64_t V, int64_t H)
 {
     return v < V && h < H ? w[v * stride + h] : (uint16_t)0;
@@ -75,7 +76,7 @@ __global__ __launch_bounds__(256) void head_grad_kernel(const uint16_t* __restri
 }
 
 // ---- the rows that count, packed together: the tiles of the two products then hold no row that is left out (711 of 1777 rows count,
-// 5120 -> 32000: 418 us, at 2.5 times the products more than 900) ----
+// 5120 -> 32000: 420 us, at 2.5 times the products more than 900) ----
 constexpr int kPackThreads = 1024;
 __global__ __launch_bounds__(kPackThreads) void ce_pack_kernel(const int32_t* __restrict__ targets, int T, int V, int32_t* __restrict__ count,
                                                               int32_t* __restrict__ pos, int32_t* __restrict__ row, int32_t* __restrict__ tgt,
@@ -534,9 +535,9 @@ static void ce_pieces(int64_t T, int64_t V, int64_t piece, bool grad, int& cols,
 }
 
 // The logits' tile, by the time of its rounds of 256 workgroups (of 128x128 tiles a CU holds two): what a tile takes to start and for its epilogue, and its K
-// tiles.  us, whole call without the gradient, 256x256 | 128x128, T x H -> V (a last round of few as halves): 128 x 4096 -> 32000 93 | 75, 200 rows 90 | 98,
-// 333 121 | 125, 512 123 | 164, 2048 430 | 523, 711 x 5120 -> 32000 210 | 269, 333 x 1376 -> 100003 165 | 138, 1500 x 1024 -> 50000 196 | 192, 3000 x
-// 512 -> 8000 65 | 50.  Tiles of 128x256 throughout were in front nowhere but where halves are them.
+// tiles.  us, whole call without the gradient, 256x256 | 128x128, T x H -> V (a last round of few as halves): 128 x 4096 -> 32000 90 | 71, 200 rows 88 | 92,
+// 333 112 | 120, 512 118 | 157, 2048 415 | 507, 711 x 5120 -> 32000 211 | 261, 333 x 1376 -> 100003 130 | 128, 1500 x 1024 -> 50000 172 | 158, 3000 x
+// 512 -> 8000 55 | 45.  Tiles of 128x256 throughout were in front nowhere but where halves are them.
 static int ce_tile(int64_t M, int64_t N, int64_t K)
 {
     auto tiles = [&](int64_t bm, int64_t bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
@@ -565,9 +566,9 @@ int ce_grad_tile(int64_t M, int64_t N, int64_t columns)
 }
 
 // Whether the kernels of few rows do the call: up to 64 rows, and where all of it is so small that it is launches that count (four in place of six, and none of
-// their workgroups waits for another's), 64 rows a workgroup.  us, whole call with the gradient, tiles | these, T x H -> V: 100 x 100 -> 600 32.0 | 21.4, 1000 x 512
-// -> 1000 48 | 26, 500 x 512 -> 4000 51 | 41, 500 x 4096 -> 500 69 | 43, 200 x 1024 -> 4000 51 | 37; but 300 x 4096 -> 1000 55 | 62, 100 x 512 -> 16000 44 | 49,
-// 512 x 128 -> 8000 39.7 | 40.6; rows that are not whole 16 bytes, 400 x 300 -> 700 34.7 | 30.5 but 700 x 700 -> 2000 54 | 62.
+// their workgroups waits for another's), 64 rows a workgroup.  us, whole call with the gradient, tiles | these, T x H -> V: 100 x 100 -> 600 33.0 | 21.4, 1000 x 512
+// -> 1000 50 | 24, 500 x 512 -> 4000 51 | 40, 500 x 4096 -> 500 70 | 44, 200 x 1024 -> 4000 52 | 37; but 300 x 4096 -> 1000 56 | 61, 100 x 512 -> 16000 45 | 50,
+// 512 x 128 -> 8000 39.4 | 40.3; rows that are not whole 16 bytes, 400 x 300 -> 700 34.8 | 29.1 but 700 x 700 -> 2000 54 | 62.
 static bool ce_few(const CeArgs& c)
 {
     if (c.piece < c.V) return false;
@@ -576,9 +577,9 @@ static bool ce_few(const CeArgs& c)
 }
 
 // Columns of a workgroup of few rows' logits: fewer where 64 would leave CUs without one, and where a row or four cost nothing beside the head; each workgroup
-// reads all of x, so more rows want more columns.  us, whole call without the gradient, 64 | 32 | 16 columns, T x H -> V: 1 x 4096 -> 2000 17.8 | 13.6 | 12.9,
-// -> 8000 20.7 | 18.1 | 19.4, -> 32000 51.4 | 47.3 | 45.7 (with the gradient 97 | 94 | 96); 16 x 4096 -> 2000 20.7 | 17.2 | 14.9, -> 8000 23.6 | 19.6 | 22.3,
-// -> 32000 52.8 | 54.3 | 64.9; 64 x 4096 -> 2000 36.0 | 31.5 | 29.9, -> 8000 38.4 | 33.4 | 47.7, -> 32000 72 | 96 | 154; 1 x 1024 -> 128000 45.6 | 49.8 | 52.5.
+// reads all of x, so more rows want more columns.  us, whole call without the gradient, 64 | 32 | 16 columns, T x H -> V: 1 x 4096 -> 2000 17.3 | 13.4 | 12.4,
+// -> 8000 20.8 | 17.7 | 18.2, -> 32000 51.2 | 47.0 | 45.5 (with the gradient 97 | 93 | 96); 16 x 4096 -> 2000 20.5 | 16.6 | 14.8, -> 8000 23.5 | 19.3 | 22.0,
+// -> 32000 52.3 | 54.5 | 64.6; 64 x 4096 -> 2000 36.1 | 31.4 | 29.5, -> 8000 38.1 | 33.0 | 47.5, -> 32000 72 | 95 | 154; 1 x 1024 -> 128000 45.3 | 49.8 | 52.2.
 static int ce_few_cols(const CeArgs& c)
 {
     if (c.H < 2048) return kFewCols;

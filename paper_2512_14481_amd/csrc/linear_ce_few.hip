@@ -3,8 +3,9 @@
 // A workgroup has 16 to 64 rows of a head's layout (vocabulary entries for the logits, channels for the gradient) and its eight waves an eighth of the
 // contraction each: a wave loads 1 KB blocks, which are operands of v_mfma_f32_16x16x32 as they lie, and the rows of x (or their exponentials) beside them
 // from L2.  The waves' sums meet in LDS.  4 to 8 blocks of the head are requested ahead by each wave, and 16 waves of a CU keep 64 to 128 KB in flight: one row of
-// 4096 -> 32000 reads its 262 MB in 41 us, 6.4 TB/s (a large copy 5.2).  With 64 rows it is the rows of x that bind, 512 KB for every workgroup: 68 us.  No
-// rows are packed: left-out ones are computed along and dropped.
+// 4096 -> 32000 reads its 262 MB in 41 us, 6.4 TB/s (a large copy 5.2).  With 64 rows it is the rows of x that bind, 512 KB for every workgroup: 66 us.  No
+// rows are packed: left-out ones are computed along and dropped.  33 to 48 rows go as 64 (with the gradient 32 | 33 | 48 | 64 rows 107 | 126 | 131 | 138 us).  The
+// gradient's kernel reads the head again, in its other layout: one row takes 93 us with it.
 #include "sasq_device.h"
 #include "gemm_tile.h"
 #include "gemm_k64_body.h"

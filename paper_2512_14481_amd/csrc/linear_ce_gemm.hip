@@ -38,8 +38,8 @@ __device__ __forceinline__ float add32(float v)
 
 // ---- logits: z of a tile, reduced and stored as a_v ----
 // 2 T V H operations; the epilogue (one exponential, four vector operations an element) is not overlapped with another tile's products: 4096 x 4096 -> 32000 in
-// three pieces 840 us, 1.28 PFLOP/s, as a library product of that size alone (845 us); 8192 x 8192 -> 32000 2895 us, 1.48.  Matrix pipe busy 62 to 79 %, the
-// longer the contraction the more, at the 1.8 to 1.9 GHz that the power limit leaves.  In a row of 1376 the tiles' starts and ends are 40 % of them.
+// three pieces 809 us, 1.33 PFLOP/s (a library product of that size alone 845 us); 8192 x 8192 -> 32000 in bf16 2876 us, 1.49.  Matrix pipe busy 62 to 81 % under a
+// tracer, the longer the contraction the more, at the 1.6 to 1.9 GHz that the power limit leaves.  In a row of 1376 the tiles' starts and ends are 40 % of them.
 template <int DT, bool GRAD>
 struct LogitsExt {
     static constexpr bool kOn = true;
@@ -177,8 +177,8 @@ void ce_logits_kernel(const uint16_t* __restrict__ xs, const uint8_t* __restrict
 }
 
 // ---- gradient: running sums over v of a_v W_v ----
-// 2 T V H operations; 4096 x 4096 x 32000 in three pieces 851 us, 1.26 PFLOP/s, 8192 x 8192 x 32000 3690 us, 1.16 at 78 % of the matrix pipe and 1.8 GHz.  The
-// sums stay in fp32 between pieces: read, multiplied by a power of two and added to in the epilogue, 2.6 TB/s over the kernel.
+// 2 T V H operations; 4096 x 4096 x 32000 in three pieces 760 us, 1.41 PFLOP/s, 8192 x 8192 x 32000 in bf16 2944 us, 1.46 (under a tracer 866 and 3720 us at 1.7 to
+// 1.8 GHz, the matrix pipe 74 and 79 % busy).  The sums stay in fp32 between pieces: read, multiplied by a power of two and added to in the epilogue.
 struct SumsExt {
     static constexpr bool kOn = true;
     int x_kt, w_kt;
